@@ -119,6 +119,44 @@ int slw_set_layer_weights(slw_ctx* ctx, int32_t layer, const slw_layer_weights* 
  * Resets the block manager (all sequences are forgotten).
  */
 int slw_kv_init(slw_ctx* ctx, void* k_pool, void* v_pool, int32_t num_blocks);
+/*
+ * The cache in 8 bits: attach caller-owned pools of e4m3 codes (OCP 8-bit
+ * floats, 4 exponent and 3 mantissa bits, largest 448) with one fp32 scale for
+ * each block of 16 tokens and kv head of K, and one of V:
+ *   k_pool   [n_layers][num_blocks][Hkv][hd/64][16][64]
+ *            code of (token t of the block, dim d) at (d/64)*1024 + t*64 + d%64
+ *            within the (layer, block, head) page of 16*hd bytes;
+ *   v_pool   [n_layers][num_blocks][Hkv][hd][16], code of (t, d) at d*16 + t;
+ *   k_scale, v_scale  fp32 [n_layers][num_blocks][Hkv], 4-byte aligned, powers
+ *            of two 2^e with -100 <= e <= 120; a cached value is code * scale.
+ * Half the memory and half the bytes that decode attention reads.  Every call
+ * that takes a context works on either cache: the iterations append K/V with
+ * the rule below and attend to the values the codes stand for, in the
+ * arithmetic of the bf16 cache (bf16 products, fp32 sums).
+ *   Appending tokens t0 .. t0+n-1 of a block takes e = max(-100, the least e
+ * with |x| <= 448 * 2^e for every new finite x), or the block's e where that
+ * is larger and t0 > 0; a new code is x * 2^-e rounded to nearest even (values
+ * that are not finite become NaN; at e = 120 codes stop at 240, whose value is
+ * the largest finite), and where e grew, the codes of tokens before t0 are
+ * rounded to it, which changes only those that become subnormal.  Tokens of
+ * the block past the last appended one lose their value when e grows.
+ * Resets the block manager, as slw_kv_init does; either call detaches the
+ * other's pools.
+ */
+int slw_kv_init_8bit(slw_ctx* ctx, void* k_pool, void* v_pool, void* k_scale, void* v_scale,
+                     int32_t num_blocks);
+/*
+ * Sliding-window attention with sinks, for either cache: in the layers flagged
+ * in `layers` (host [n_layers], nonzero = windowed; NULL = every layer) a row
+ * at position p attends to keys t <= p with t > p - window or t < sinks; the
+ * other layers attend to every t <= p.  window 0 (the state after slw_create)
+ * turns windows off.  0 <= sinks <= max_pos, sinks only with a window.  Keys
+ * outside are neither read nor waited for (in steps of 64), whatever the pools
+ * hold there, but their blocks stay the sequence's.
+ * Workspace sizes depend on the pools attached and the windows set: ask again
+ * after either call.
+ */
+int slw_set_window(slw_ctx* ctx, int32_t window, int32_t sinks, const uint8_t* layers);
 /* Number of free blocks. */
 int slw_kv_free_blocks(slw_ctx* ctx, int32_t* n_free);
 
@@ -220,6 +258,45 @@ int slw_mixed_iteration(slw_ctx* ctx, const slw_batch* batch, const void* x_in, 
  */
 #define SLW_STATIC_WS_BYTES ((size_t)128 << 20)
 int slw_mixed_iteration_static(slw_ctx* ctx, const slw_batch* batch, const void* x_in, void* x_out, void* stream);
+
+/*
+ * The cache operators on their own, for blocks other than the iteration's: a
+ * batch is handed over once, then every layer appends its K/V rows and attends.
+ *
+ * slw_attn_begin reserves KV room as slw_mixed_iteration does (all or nothing;
+ * a failed call returns the blocks), uploads the batch's metadata into `ws`
+ * (device, 16-byte aligned, ws_bytes >= slw_attn_workspace_size(ctx, C, B); a
+ * first kernel on `stream` copies it from a pinned staging ring) and returns a
+ * plan (host memory, freed by slw_attn_end).  It is not for streams under
+ * capture (SLW_EINVAL).  C == 0 and B == 0 together gives a plan whose calls do
+ * nothing.
+ *   The plan stays usable, any number of times, while its sequences live, `ws`
+ * is left alone and neither pools nor windows are set anew (then SLW_EINVAL).
+ * Its calls are asynchronous, allocate nothing and may be captured into
+ * graphs; calls of one plan share `ws`, so they run in one stream's order, or in
+ * an order the caller sees to.
+ *
+ * slw_attn_append writes the batch's K/V rows (chunk rows first, then decodes)
+ * of one layer into the cache: k and v device bf16 [C + B][Hkv * hd], row
+ * stride ld elements, k already rotated.  Only the rows' own slots change,
+ * and in the 8-bit cache the scales and older tokens of their blocks.
+ * slw_attn_attend computes one layer's attention of the batch's query rows
+ * over the cache, which must hold the batch's own tokens by then: q device
+ * bf16 [C + B][Hq * hd] with row stride ld, out device bf16 [C + B][Hq * hd]
+ * contiguous, not overlapping q.
+ *   Rows are 16-byte aligned and strides multiples of 8 elements, else
+ * SLW_EINVAL.  A masked key stays out of a row whatever its slot holds in
+ * every layer of an 8-bit or windowed cache.
+ */
+typedef struct slw_attn slw_attn;
+int slw_attn_workspace_size(slw_ctx* ctx, int32_t max_C, int32_t max_B, size_t* bytes);
+int slw_attn_begin(slw_ctx* ctx, const slw_batch* batch, void* ws, size_t ws_bytes, void* stream,
+                   slw_attn** plan);
+int slw_attn_append(slw_ctx* ctx, const slw_attn* plan, int32_t layer, const void* k, const void* v,
+                    int64_t ld, void* stream);
+int slw_attn_attend(slw_ctx* ctx, const slw_attn* plan, int32_t layer, const void* q, int64_t ld,
+                    void* out, void* stream);
+int slw_attn_end(slw_attn* plan);
 
 /* Slot of every row of the last slw_mixed_iteration (host int32, chunk rows first). */
 int slw_last_slots(slw_ctx* ctx, int32_t* out, int32_t cap, int32_t* n);
@@ -420,6 +497,15 @@ int slw_gemm_plan(int32_t m, int32_t n, int32_t k, int32_t out[6]);
  */
 int slw_attention_plan(const slw_model_cfg* cfg, int32_t B, const int32_t* context_lens, int32_t n_prefill,
                        const int32_t* prefix_lens, const int32_t* chunk_lens, int64_t out[12]);
+
+/*
+ * The same for windowed layers (slw_set_window's window and sinks; window 0:
+ * as above): keys and tiles counted are those left by the window, without the
+ * 64-key tiles between the sinks and the window.
+ */
+int slw_attention_plan_window(const slw_model_cfg* cfg, int32_t window, int32_t sinks, int32_t B,
+                              const int32_t* context_lens, int32_t n_prefill, const int32_t* prefix_lens,
+                              const int32_t* chunk_lens, int64_t out[12]);
 
 /* ------------------------------------------------------------------------ */
 /* Controller (Eq. 1 solved by bisection as Alg. 1 does; margin of Sec. 3.3) */

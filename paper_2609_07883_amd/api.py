@@ -37,7 +37,8 @@ EXPORTS = (
     "slw_serve", "slw_cost_table_analytic", "slw_build_cost_table_ctx", "slw_cost_table_from_samples_ctx",
     "slw_cost_table_prefixes", "slw_cost_table_lookup_ctx", "slw_select_chunk_ctx",
     "slw_mixed_iteration_static", "slw_flush_cache", "slw_fill_normal", "slw_gemm_plan",
-    "slw_attention_plan",
+    "slw_attention_plan", "slw_attention_plan_window", "slw_kv_init_8bit", "slw_set_window",
+    "slw_attn_workspace_size", "slw_attn_begin", "slw_attn_append", "slw_attn_attend", "slw_attn_end",
 )
 STATIC_WS_BYTES = 128 << 20
 STAGES = ("rmsnorm_attn", "rope_table", "qkv_gemm", "chunk_attn", "decode_attn", "attn_merge",
@@ -134,6 +135,13 @@ def lib() -> C.CDLL:
         "slw_destroy": ([vp], C.c_int),
         "slw_set_layer_weights": ([vp, i32, P(LayerWeightsC)], C.c_int),
         "slw_kv_init": ([vp, vp, vp, i32], C.c_int),
+        "slw_kv_init_8bit": ([vp, vp, vp, vp, vp, i32], C.c_int),
+        "slw_set_window": ([vp, i32, i32, P(C.c_uint8)], C.c_int),
+        "slw_attn_workspace_size": ([vp, i32, i32, P(sz)], C.c_int),
+        "slw_attn_begin": ([vp, P(BatchC), vp, sz, vp, P(vp)], C.c_int),
+        "slw_attn_append": ([vp, vp, i32, vp, vp, i64, vp], C.c_int),
+        "slw_attn_attend": ([vp, vp, i32, vp, i64, vp, vp], C.c_int),
+        "slw_attn_end": ([vp], C.c_int),
         "slw_kv_free_blocks": ([vp, P(i32)], C.c_int),
         "slw_seq_create": ([vp, i64], C.c_int),
         "slw_seq_free": ([vp, i64], C.c_int),
@@ -146,6 +154,7 @@ def lib() -> C.CDLL:
         "slw_fill_normal": ([vp, sz, C.c_uint64, C.c_float, C.c_float, vp], C.c_int),
         "slw_gemm_plan": ([i32, i32, i32, P(i32)], C.c_int),
         "slw_attention_plan": ([P(ModelCfg), i32, P(i32), i32, P(i32), P(i32), P(i64)], C.c_int),
+        "slw_attention_plan_window": ([P(ModelCfg), i32, i32, i32, P(i32), i32, P(i32), P(i32), P(i64)], C.c_int),
         "slw_last_slots": ([vp, P(i32), i32, P(i32)], C.c_int),
         "slw_workspace_view": ([vp, i32, i32, i32, P(sz), P(sz)], C.c_int),
         "slw_build_cost_table": ([vp, P(i32), i32, P(i32), i32, P(ProfileOpts), P(vp)], C.c_int),
@@ -338,19 +347,25 @@ ATTENTION_PLAN_FIELDS = ("decode_items", "decode_slots", "decode_max_keys", "dec
                          "chunk_max_tiles", "chunk_min_tiles", "chunk_tiles", "chunk_two_phase")
 
 
-def attention_plan(shape, context_lens, prefills=()) -> dict:
+def attention_plan(shape, context_lens, prefills=(), window: int = 0, sinks: int = 0) -> dict:
     """The attention work lists an iteration would build (host only).
 
     shape: a model shape (synth.ModelShape); context_lens: cached tokens of
-    each decode; prefills: (prefix_len, chunk_len) per prompt."""
+    each decode; prefills: (prefix_len, chunk_len) per prompt; window and
+    sinks: those of a windowed layer."""
     cfg = ModelCfg(shape.n_layers, shape.d_model, shape.n_q_heads, shape.n_kv_heads, shape.head_dim,
                    shape.ffn_dim, shape.rms_eps, shape.rope_theta, 16, shape.max_pos)
     cl = _i32(context_lens)
     pp = _i32([p for p, _ in prefills])
     pc = _i32([c for _, c in prefills])
     out = np.zeros(12, np.int64)
-    _check(lib().slw_attention_plan(C.byref(cfg), len(cl), _ptr(cl, C.c_int32), len(pp), _ptr(pp, C.c_int32),
-                                    _ptr(pc, C.c_int32), _ptr(out, C.c_int64)))
+    if window or sinks:
+        _check(lib().slw_attention_plan_window(C.byref(cfg), int(window), int(sinks), len(cl), _ptr(cl, C.c_int32),
+                                               len(pp), _ptr(pp, C.c_int32), _ptr(pc, C.c_int32),
+                                               _ptr(out, C.c_int64)))
+    else:
+        _check(lib().slw_attention_plan(C.byref(cfg), len(cl), _ptr(cl, C.c_int32), len(pp), _ptr(pp, C.c_int32),
+                                        _ptr(pc, C.c_int32), _ptr(out, C.c_int64)))
     return dict(zip(ATTENTION_PLAN_FIELDS, (int(v) for v in out)))
 
 
@@ -474,6 +489,27 @@ class Batch:
         return c[0]
 
 
+class AttnPlan:
+    """Owns a slw_attn* (a batch handed to the cache operators); keeps its context alive."""
+
+    def __init__(self, ctx: "Context", handle: int):
+        self._ctx = ctx
+        self._h = C.c_void_p(handle)
+
+    def __del__(self):
+        if getattr(self, "_h", None) and self._h.value and _lib is not None:
+            _lib.slw_attn_end(self._h)
+            self._h = None
+
+    def append(self, layer: int, k: int, v: int, ld: int, stream: int = 0):
+        """Enqueue the append of the batch's K/V rows (row stride ld elements) to one layer's cache."""
+        _check(lib().slw_attn_append(self._ctx._h, self._h, layer, k or None, v or None, ld, stream or None))
+
+    def attend(self, layer: int, q: int, ld: int, out: int, stream: int = 0):
+        """Enqueue one layer's attention of the batch's query rows (row stride ld elements)."""
+        _check(lib().slw_attn_attend(self._ctx._h, self._h, layer, q or None, ld, out or None, stream or None))
+
+
 class Context:
     """Owns a slw_ctx*.  Pointers passed in stay owned by the caller."""
 
@@ -509,6 +545,20 @@ class Context:
 
     def kv_init(self, k_pool: int, v_pool: int, num_blocks: int):
         _check(lib().slw_kv_init(self._h, C.c_void_p(k_pool), C.c_void_p(v_pool), num_blocks))
+
+    def kv_init_8bit(self, k_pool: int, v_pool: int, k_scale: int, v_scale: int, num_blocks: int):
+        """Attach pools of e4m3 codes with fp32 scales per (block, kv head)."""
+        _check(lib().slw_kv_init_8bit(self._h, C.c_void_p(k_pool), C.c_void_p(v_pool), C.c_void_p(k_scale),
+                                      C.c_void_p(v_scale), num_blocks))
+
+    def set_window(self, window: int, sinks: int = 0, layers=None):
+        """Sliding window and sinks of the layers flagged in `layers` (None: all); window 0: off."""
+        flags = None
+        if layers is not None:
+            if len(layers) != self.cfg.n_layers:
+                raise ValueError(f"{len(layers)} layer flags for {self.cfg.n_layers} layers")
+            flags = (C.c_uint8 * self.cfg.n_layers)(*(1 if f else 0 for f in layers))
+        _check(lib().slw_set_window(self._h, int(window), int(sinks), flags))
 
     def free_blocks(self) -> int:
         n = C.c_int32()
@@ -550,6 +600,19 @@ class Context:
     def mixed_iteration_static(self, batch: Batch, x_in: int, x_out: int, stream: int = 0):
         """The iteration on the library's static workspace (no allocation of any kind)."""
         _check(lib().slw_mixed_iteration_static(self._h, C.byref(batch.c_struct()), x_in, x_out, stream or None))
+
+    # the cache operators on their own
+    def attn_workspace_size(self, max_c: int, max_b: int) -> int:
+        b = C.c_size_t()
+        _check(lib().slw_attn_workspace_size(self._h, max_c, max_b, C.byref(b)))
+        return b.value
+
+    def attn_begin(self, batch: Batch, ws: int, ws_bytes: int, stream: int = 0) -> AttnPlan:
+        """Hand a batch to the cache operators: reserves its KV room and enqueues its metadata's upload into ws."""
+        h = C.c_void_p()
+        _check(lib().slw_attn_begin(self._h, C.byref(batch.c_struct()), ws or None, ws_bytes, stream or None,
+                                    C.byref(h)))
+        return AttnPlan(self, h.value)
 
     def set_stage_timing(self, depth: int):
         """Record per-stage HIP events for the last `depth` iterations (0: off)."""

@@ -1,0 +1,256 @@
+// Work lists of the two attentions of one iteration (host code, no GPU).
+#include "attn_plan.h"
+
+#include <algorithm>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace slw {
+
+namespace {
+
+// Decode attention runs one wave per work-group, two per SIMD (its register
+// use allows no more): kDecodeWaves of them fill a 256-CU part once.  Their
+// keys are cut into equal runs (at least kDecodeMinKeys each), so that every
+// wave of the launch finishes at about the same time.
+constexpr int kDecodeWaves = 2048;
+constexpr int kDecodeMinKeys = 128;
+// Chunk attention runs one work-group per CU (its register use allows no
+// more), so a launch of kChunkSlots work-groups with equal work finishes in
+// one round on a 256-CU part.  A work-group takes at least kChunkMinTiles
+// 64-key tiles, which keeps its fixed costs (Q load, partial write) small.
+constexpr int kChunkSlots = 256;
+constexpr int kChunkMinTiles = 4;
+// Whole query tiles per work-group when the largest group's load is within
+// 11/10 of an equal share.
+constexpr int64_t kChunkWholeSlackNum = 11, kChunkWholeSlackDen = 10;
+// Work items of at least kTwoPhaseTiles + kTwoPhaseTilesPer64 (positions of a
+// query tile, at least 64, / 64) 64-key tiles on average run the two-phase
+// chunk kernel at head dim 128.  Its fill and extra phases are paid per item,
+// and every wave computes all tiles of the item, which wastes a few more where
+// a query tile holds many positions (few heads a group).  Below the line it
+// loses; at head dim 64 it nearly always did (half the products under the same
+// softmax).  One-phase / two-phase us at n tiles per item:
+//   8B layer (4 heads a group): 1: 11.2 / 13.3, 2 (77 rows at 50): 18.6 / 23.5,
+//   3.5: 28.6 / 34.1, 9.5: 33.1 / 34.9, 17.5: 48.1 / 47.8, 20.2: 63.9 / 64.7,
+//   25.5: 61.8 / 62.6, 27.2: 81.4 / 79.6, 33.5: 76.8 / 75.8, 73: 292 / 272;
+//   2 heads: 28: 77.4 / 80.2, 35: 77.7 / 76.7, 50: 107 / 101;
+//   1 head: 31: 73.6 / 77.0, 36: 81.3 / 85.4, 51: 109.5 / 109.4, 84: 310 / 293;
+//   head dim 64: 1 head, 59: 102 / 108; 8 heads, 72: 108 / 110; 16 heads, 464: 1130 / 1152.
+constexpr int64_t kTwoPhaseTiles = 21, kTwoPhaseTilesPer64 = 5;
+
+}  // namespace
+
+int decode_slot_cap(const slw_model_cfg& c) { return std::max(1, kDecodeWaves / c.n_kv_heads); }
+// A run crosses at most one decode boundary more than it has runs: items <= slots + B - 1.
+int decode_work_cap(const slw_model_cfg& c, int B) { return decode_slot_cap(c) + B + 1; }
+
+// Query tiles of the chunk rows: each prefill's rows are tiled on their own,
+// so up to SLW_MAX_PREFILLS - 1 tiles more than one prefill of C rows needs.
+int chunk_tiles(const slw_model_cfg& c, int C) {
+    if (C <= 0) return 0;
+    return static_cast<int>(ceil_div(C, chunk_tile_positions(c.n_q_heads / c.n_kv_heads))) +
+           std::min(C, static_cast<int>(SLW_MAX_PREFILLS)) - 1;
+}
+int chunk_slot_cap(const slw_model_cfg& c) { return std::max(1, kChunkSlots / c.n_kv_heads); }
+int chunk_item_cap(const slw_model_cfg& c, int C) {
+    return C > 0 ? chunk_tiles(c, C) + chunk_slot_cap(c) : 0;
+}
+
+int32_t window_skip(const Window& w, int32_t first_pos) {
+    if (w.window <= 0) return 0;
+    const int64_t lo = static_cast<int64_t>(first_pos) - w.window + 1;  // first key of the window
+    const int64_t skip = lo / 64 * 64 - sink_end(w);
+    return lo > 0 && skip > 0 ? static_cast<int32_t>(skip) : 0;
+}
+
+// Query tiles of the chunk rows: each prefill's rows cut into tiles of
+// chunk_tile_positions(group) positions (a tile never mixes sequences).
+// Tile q: first chunk row, rows, first position and, when wanted, the offset
+// of its sequence's block table (bt_of_prefill[i] for prefill i).
+void query_tiles(const slw_model_cfg& c, const std::vector<Prefill>& pre, std::vector<int32_t>& row0,
+                 std::vector<int32_t>& rows, std::vector<int32_t>& pos0, std::vector<int32_t>* bt,
+                 const std::vector<int32_t>& bt_of_prefill) {
+    const int pwg = chunk_tile_positions(c.n_q_heads / c.n_kv_heads);
+    row0.clear();
+    rows.clear();
+    pos0.clear();
+    if (bt) bt->clear();
+    for (size_t i = 0; i < pre.size(); ++i)
+        for (int j = 0; j < pre[i].c; j += pwg) {
+            row0.push_back(pre[i].row0 + j);
+            rows.push_back(std::min(pwg, pre[i].c - j));
+            pos0.push_back(pre[i].prefix + j);
+            if (bt) bt->push_back(bt_of_prefill[i]);
+        }
+}
+
+// Decode attention work.  The keys of all decodes (decode b attends to
+// context_lens[b] + 1 of them, or those left by the window), laid end to end with each decode's range
+// padded to a multiple of 64, are cut into equal runs (multiples of 64 keys,
+// so that every item starts on a page pair; at least kDecodeMinKeys each, at
+// most decode_slot_cap(c) runs), one per wave of each kv head; a run that
+// crosses decodes becomes one item per decode it touches, and padding alone
+// makes no item.  Items come out in decode order, so each decode's items are
+// contiguous for the merge.
+int plan_decode(const slw_model_cfg& c, const Window& w, int B, const int32_t* context_lens, DecodePlan& p) {
+    p.b.clear();
+    p.kb.clear();
+    p.ke.clear();
+    p.off.assign(B + 1, 0);
+    p.slot_off.assign(1, 0);
+    p.skip.resize(std::max(B, 0));
+    if (B <= 0) return SLW_OK;
+    for (int b = 0; b < B; ++b) p.skip[b] = window_skip(w, context_lens[b]);
+    auto keys = [&](int b) { return context_lens[b] + 1 - p.skip[b]; };  // virtual
+    int64_t padded = 0;
+    for (int b = 0; b < B; ++b) padded += ceil_div(keys(b), 64) * 64;
+    const int64_t want = std::min<int64_t>(decode_slot_cap(c), std::max<int64_t>(1, padded / kDecodeMinKeys));
+    const int64_t per = ceil_div(ceil_div(padded, want), 64) * 64;
+    const int n_slots = static_cast<int>(ceil_div(padded, per));
+    p.slot_off.clear();
+    int b = 0;
+    int64_t start_b = 0;  // first key of decode b in the padded layout
+    for (int sl = 0; sl < n_slots; ++sl) {
+        p.slot_off.push_back(static_cast<int32_t>(p.b.size()));
+        int64_t r0 = sl * per;
+        const int64_t r1 = std::min(padded, r0 + per);
+        while (r0 < r1) {
+            const int32_t len = keys(b);
+            const int64_t span = ceil_div(len, 64) * 64;
+            if (r0 >= start_b + span) {  // past decode b
+                start_b += span;
+                p.off[++b] = static_cast<int32_t>(p.b.size());
+                continue;
+            }
+            const int64_t k0 = r0 - start_b, k1 = std::min<int64_t>(r1 - start_b, span);
+            if (k0 < len) {
+                p.b.push_back(b);
+                p.kb.push_back(static_cast<int32_t>(k0));
+                p.ke.push_back(static_cast<int32_t>(std::min<int64_t>(k1, len)));
+            }
+            r0 = start_b + k1;
+        }
+    }
+    p.slot_off.push_back(static_cast<int32_t>(p.b.size()));
+    while (b < B) p.off[++b] = static_cast<int32_t>(p.b.size());
+    if (static_cast<int>(p.b.size()) > decode_work_cap(c, B) || n_slots > decode_slot_cap(c))
+        return fail(SLW_EINVAL, "internal: decode work %zu / slots %d above cap", p.b.size(), n_slots);
+    for (int d = 0; d < B; ++d) {  // the items of each decode tile its keys
+        int64_t at = 0;
+        for (int i = p.off[d]; i < p.off[d + 1]; ++i) {
+            if (p.b[i] != d || p.kb[i] != at || p.ke[i] <= at) return fail(SLW_EINVAL, "internal: decode plan");
+            at = p.ke[i];
+        }
+        if (at != keys(d)) return fail(SLW_EINVAL, "internal: decode plan");
+    }
+    return SLW_OK;
+}
+
+// Chunk attention work over query tiles q (first position qt_pos0[q],
+// qt_rows[q] rows, keys 0 .. qt_pos0[q] + qt_rows[q] - 1, or those left by the
+// window).  Whole query tiles
+// where they balance: the tiles, longest first, each go to the least loaded
+// of `want` work-groups (LPT); when the largest load stays within
+// kChunkWholeSlack of an equal share, no tile is split and nothing is merged
+// (long prompts: many tiles of similar length).  Otherwise (fewer tiles than
+// work-groups, or tiles of very different lengths, as at the start of a
+// prompt) the 64-key tiles of every query tile, laid end to end, are cut into
+// equal runs, one per work-group of each kv head; a run that crosses query
+// tiles becomes one item per query tile it touches.  Items stay in query-tile
+// order; slot_items lists each work-group's items.
+int plan_chunk(const slw_model_cfg& c, const Window& w, int C, const std::vector<int32_t>& qt_pos0,
+               const std::vector<int32_t>& qt_rows, ChunkPlan& p) {
+    const int n_qt = static_cast<int>(qt_pos0.size());
+    p.items.clear();
+    p.slot_off.clear();
+    p.slot_items.clear();
+    p.whole = false;
+    p.qt_skip.resize(n_qt);
+    for (int q = 0; q < n_qt; ++q) p.qt_skip[q] = window_skip(w, qt_pos0[q]);
+    auto key_end = [&](int q) { return static_cast<int64_t>(qt_pos0[q]) + qt_rows[q] - p.qt_skip[q]; };  // virtual
+    std::vector<int64_t> tile_end(n_qt + 1, 0);
+    for (int q = 0; q < n_qt; ++q) tile_end[q + 1] = tile_end[q] + ceil_div(key_end(q), 64);
+    const int64_t total_tiles = tile_end[n_qt];
+    std::vector<int32_t>& it = p.items;
+    int n_slots = 0;
+    if (n_qt > 0) {
+        const int64_t want = std::min<int64_t>(chunk_slot_cap(c), std::max<int64_t>(1, total_tiles / kChunkMinTiles));
+        const int64_t per = ceil_div(total_tiles, want);
+        if (n_qt >= want) {
+            std::vector<int32_t> order(n_qt);
+            for (int q = 0; q < n_qt; ++q) order[q] = q;
+            auto len = [&](int q) { return tile_end[q + 1] - tile_end[q]; };
+            std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return len(x) > len(y); });
+            std::vector<int64_t> load(want, 0);
+            std::vector<int32_t> owner(n_qt);
+            for (int q : order) {
+                const int g = static_cast<int>(std::min_element(load.begin(), load.end()) - load.begin());
+                load[g] += len(q);
+                owner[q] = g;
+            }
+            const int64_t mx = *std::max_element(load.begin(), load.end());
+            if (mx * kChunkWholeSlackDen <= per * kChunkWholeSlackNum) {
+                p.whole = true;
+                n_slots = static_cast<int>(want);
+                for (int q = 0; q < n_qt; ++q) {
+                    it.push_back(q);
+                    it.push_back(0);
+                    it.push_back(static_cast<int32_t>(key_end(q)));
+                }
+                p.slot_off.assign(n_slots + 1, 0);
+                for (int q = 0; q < n_qt; ++q) ++p.slot_off[owner[q] + 1];
+                for (int g = 0; g < n_slots; ++g) p.slot_off[g + 1] += p.slot_off[g];
+                p.slot_items.resize(n_qt);
+                std::vector<int32_t> fill(p.slot_off.begin(), p.slot_off.end() - 1);
+                for (int q = 0; q < n_qt; ++q) p.slot_items[fill[owner[q]]++] = q;
+            }
+        }
+        if (!p.whole) {
+            n_slots = static_cast<int>(ceil_div(total_tiles, per));
+            p.slot_off.resize(n_slots + 1);
+            int q = 0;
+            for (int sl = 0; sl < n_slots; ++sl) {
+                p.slot_off[sl] = static_cast<int32_t>(it.size() / 3);
+                int64_t t0 = sl * per;
+                const int64_t t1 = std::min(total_tiles, t0 + per);
+                while (t0 < t1) {
+                    while (tile_end[q + 1] <= t0) ++q;
+                    const int64_t seg_end = std::min(t1, tile_end[q + 1]);
+                    it.push_back(q);
+                    it.push_back(static_cast<int32_t>((t0 - tile_end[q]) * 64));
+                    it.push_back(static_cast<int32_t>(std::min(key_end(q), (seg_end - tile_end[q]) * 64)));
+                    t0 = seg_end;
+                }
+            }
+            p.slot_off[n_slots] = static_cast<int32_t>(it.size() / 3);
+            p.slot_items.resize(it.size() / 3);
+            for (size_t i = 0; i < p.slot_items.size(); ++i) p.slot_items[i] = static_cast<int32_t>(i);
+        }
+    } else {
+        p.slot_off.assign(1, 0);
+    }
+    const int n_items = static_cast<int>(it.size() / 3);
+    const int64_t blocks64 = std::max(1, chunk_tile_positions(c.n_q_heads / c.n_kv_heads) / 64);
+    p.two_phase = c.head_dim == 128 && n_items > 0 &&
+                  total_tiles >= (kTwoPhaseTiles + kTwoPhaseTilesPer64 * blocks64) * n_items;
+    p.qt_off.assign(n_qt + 1, 0);
+    for (int q = 0, i = 0; q <= n_qt; ++q) {
+        while (i < n_items && it[3 * i] < q) ++i;
+        p.qt_off[q] = i;
+    }
+    if (n_items > chunk_item_cap(c, C) || n_slots > chunk_slot_cap(c))
+        return fail(SLW_EINVAL, "internal: chunk items %d / slots %d above cap", n_items, n_slots);
+    for (int q = 0; q < n_qt; ++q) {  // the items of each query tile tile its key range
+        int64_t at = 0;
+        for (int i = p.qt_off[q]; i < p.qt_off[q + 1]; ++i) {
+            if (it[3 * i + 1] != at || it[3 * i + 2] <= at) return fail(SLW_EINVAL, "internal: chunk plan");
+            at = it[3 * i + 2];
+        }
+        if (at != key_end(q)) return fail(SLW_EINVAL, "internal: chunk plan");
+    }
+    return SLW_OK;
+}
+
+}  // namespace slw

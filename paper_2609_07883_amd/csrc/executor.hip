@@ -8,6 +8,7 @@
 // append in its epilogue), chunk and decode attention, output GEMM into an
 // fp32 residual, RMSNorm, gate/up GEMM (SiLU*mul epilogue), down GEMM.
 #include <algorithm>
+#include <atomic>
 #include <chrono>
 #include <cstring>
 #include <limits>
@@ -17,6 +18,7 @@
 #include <unordered_set>
 #include <vector>
 
+#include "attn_plan.h"
 #include "common.h"
 #include "cost_table.h"
 #include "kernels.h"
@@ -27,35 +29,6 @@ using namespace slw;
 namespace {
 
 constexpr int kRing = 4;                 // pinned staging buffers in flight
-// Decode attention runs one wave per work-group, two per SIMD (its register
-// use allows no more): kDecodeWaves of them fill a 256-CU part once.  Their
-// keys are cut into equal runs (at least kDecodeMinKeys each), so that every
-// wave of the launch finishes at about the same time.
-constexpr int kDecodeWaves = 2048;
-constexpr int kDecodeMinKeys = 128;
-// Chunk attention runs one work-group per CU (its register use allows no
-// more), so a launch of kChunkSlots work-groups with equal work finishes in
-// one round on a 256-CU part.  A work-group takes at least kChunkMinTiles
-// 64-key tiles, which keeps its fixed costs (Q load, partial write) small.
-constexpr int kChunkSlots = 256;
-constexpr int kChunkMinTiles = 4;
-// Whole query tiles per work-group when the largest group's load is within
-// 11/10 of an equal share.
-constexpr int64_t kChunkWholeSlackNum = 11, kChunkWholeSlackDen = 10;
-// Work items of at least kTwoPhaseTiles + kTwoPhaseTilesPer64 (positions of a
-// query tile, at least 64, / 64) 64-key tiles on average run the two-phase
-// chunk kernel at head dim 128.  Its fill and extra phases are paid per item,
-// and every wave computes all tiles of the item, which wastes a few more where
-// a query tile holds many positions (few heads a group).  Below the line it
-// loses; at head dim 64 it nearly always did (half the products under the same
-// softmax).  One-phase / two-phase us at n tiles per item:
-//   8B layer (4 heads a group): 1: 11.2 / 13.3, 2 (77 rows at 50): 18.6 / 23.5,
-//   3.5: 28.6 / 34.1, 9.5: 33.1 / 34.9, 17.5: 48.1 / 47.8, 20.2: 63.9 / 64.7,
-//   25.5: 61.8 / 62.6, 27.2: 81.4 / 79.6, 33.5: 76.8 / 75.8, 73: 292 / 272;
-//   2 heads: 28: 77.4 / 80.2, 35: 77.7 / 76.7, 50: 107 / 101;
-//   1 head: 31: 73.6 / 77.0, 36: 81.3 / 85.4, 51: 109.5 / 109.4, 84: 310 / 293;
-//   head dim 64: 1 head, 59: 102 / 108; 8 heads, 72: 108 / 110; 16 heads, 464: 1130 / 1152.
-constexpr int64_t kTwoPhaseTiles = 21, kTwoPhaseTilesPer64 = 5;
 constexpr size_t kAlign = 256;
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
@@ -66,31 +39,7 @@ size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
         if (e_ != hipSuccess) return fail(SLW_EHIP, "%s: %s", #expr, hipGetErrorString(e_)); \
     } while (0)
 
-// One prefill of an iteration: `c` chunk rows from row `row0` on, at positions
-// prefix .. prefix + c - 1 of sequence `seq`.
-struct Prefill {
-    int64_t seq;
-    int32_t prefix;
-    int32_t c;
-    int32_t row0;
-};
-
 }  // namespace
-
-// Work lists of the two attentions of one iteration (host build areas).
-struct DecodePlan {
-    std::vector<int32_t> b, kb, ke;  // items: decode, first key (a multiple of 64), key past the last
-    std::vector<int32_t> off;        // [B + 1] first item of each decode
-    std::vector<int32_t> slot_off;   // [slots + 1] first item of each wave slot
-};
-struct ChunkPlan {
-    std::vector<int32_t> items;       // [3 n]: query tile, first key, key past the last
-    std::vector<int32_t> slot_off;    // [slots + 1] first entry of each work-group in slot_items
-    std::vector<int32_t> slot_items;  // [n] the items of each work-group in turn
-    std::vector<int32_t> qt_off;      // [n_qt + 1] first item of each query tile
-    bool whole = false;               // whole query tiles per work-group
-    bool two_phase = false;           // the two-phase kernel
-};
 
 struct slw_ctx {
     slw_model_cfg cfg{};
@@ -98,13 +47,19 @@ struct slw_ctx {
     std::vector<char> have_w;
     void* k_pool = nullptr;
     void* v_pool = nullptr;
+    float* k_scale = nullptr;   // e4m3 pools: their scales (null: bf16 pools)
+    float* v_scale = nullptr;
     KvManager kv;
     bool kv_ready = false;
+    uint64_t kv_id = 0;         // changes with every attachment of pools, and differs between contexts
+    Window win;                 // attention window of the layers flagged in `windowed`
+    std::vector<char> windowed;
+    bool any_windowed = false, any_full = true;
     std::vector<int32_t> last_slots;
     std::vector<int32_t> slots_build;  // slots of the iteration being built
     std::vector<Prefill> prefills;     // the iteration's prefills in row order
     std::vector<int32_t> meta;  // host build area
-    DecodePlan dplan;           // the iteration's attention work (host build areas)
+    DecodePlan dplan;           // attention work of one class of layers (host build areas)
     ChunkPlan cplan;
 
     // HIP resources, created on first device use
@@ -138,40 +93,61 @@ namespace {
 
 int qkv_width(const slw_model_cfg& c) { return (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim; }
 int max_blocks(const slw_model_cfg& c) { return static_cast<int>(ceil_div(c.max_pos, 16)); }
-int decode_slot_cap(const slw_model_cfg& c) { return std::max(1, kDecodeWaves / c.n_kv_heads); }
-// A run crosses at most one decode boundary more than it has runs: items <= slots + B - 1.
-int decode_work_cap(const slw_model_cfg& c, int B) { return decode_slot_cap(c) + B + 1; }
-
-// Query tiles of the chunk rows: each prefill's rows are tiled on their own,
-// so up to SLW_MAX_PREFILLS - 1 tiles more than one prefill of C rows needs.
-int chunk_tiles(const slw_model_cfg& c, int C) {
-    if (C <= 0) return 0;
-    return static_cast<int>(ceil_div(C, chunk_tile_positions(c.n_q_heads / c.n_kv_heads))) +
-           std::min(C, static_cast<int>(SLW_MAX_PREFILLS)) - 1;
-}
-int chunk_slot_cap(const slw_model_cfg& c) { return std::max(1, kChunkSlots / c.n_kv_heads); }
-int chunk_item_cap(const slw_model_cfg& c, int C) {
-    return C > 0 ? chunk_tiles(c, C) + chunk_slot_cap(c) : 0;
+// Blocks a batch of C chunk rows and B decodes appends to: each prompt may
+// begin and end inside a block.
+size_t append_cap(int C, int B) {
+    const size_t np = std::min(C, static_cast<int>(SLW_MAX_PREFILLS));
+    return std::min<size_t>(C, C / 16 + 2 * np) + B;
 }
 
-size_t meta_ints(const slw_model_cfg& c, int C, int B) {
-    const int M = C + B;
+// Metadata of the two attentions and the append (32-bit words): block tables,
+// query tiles, blocks to append to, and the work lists of each class of
+// layers (full attention, windowed).
+size_t attn_meta_ints(const slw_ctx& ctx, int C, int B) {
+    const slw_model_cfg& c = ctx.cfg;
     const size_t mb = static_cast<size_t>(max_blocks(c));
     const size_t np = C > 0 ? static_cast<size_t>(std::min(C, static_cast<int>(SLW_MAX_PREFILLS))) : 0;
-    return 2 * static_cast<size_t>(M) + B + (B + 1) + static_cast<size_t>(B) * mb + np * mb +
-           3 * static_cast<size_t>(decode_work_cap(c, B)) + (B + 1) + decode_slot_cap(c) + 1 +
-           4 * static_cast<size_t>(chunk_item_cap(c, C)) +
-           5 * static_cast<size_t>(chunk_tiles(c, C)) + 1 + chunk_slot_cap(c) + 1;
+    const size_t per_class = 3 * static_cast<size_t>(decode_work_cap(c, B)) + (B + 1) + decode_slot_cap(c) + 1 + B +
+                             4 * static_cast<size_t>(chunk_item_cap(c, C)) + 2 * static_cast<size_t>(chunk_tiles(c, C)) + 1 +
+                             chunk_slot_cap(c) + 1;
+    return B + (B + 1) + static_cast<size_t>(B) * mb + np * mb + 4 * static_cast<size_t>(chunk_tiles(c, C)) +
+           4 * append_cap(C, B) + per_class * (ctx.any_full + ctx.any_windowed);
+}
+
+size_t meta_ints(const slw_ctx& ctx, int C, int B) {
+    return 2 * (static_cast<size_t>(C) + B) + attn_meta_ints(ctx, C, B);
+}
+
+// Partial sums of the two attentions, after `off`.
+struct PartLayout {
+    size_t part_o, part_ml, cpart_o, cpart_ml, end;
+};
+PartLayout part_layout(const slw_model_cfg& c, int C, int B, size_t off) {
+    PartLayout P{};
+    auto take = [&](size_t bytes) {
+        size_t at = off;
+        off += align_up(bytes);
+        return at;
+    };
+    const int W = decode_work_cap(c, B);
+    P.part_o = take(B > 0 ? static_cast<size_t>(W) * c.n_q_heads * c.head_dim * 4 : 0);
+    P.part_ml = take(B > 0 ? static_cast<size_t>(W) * c.n_q_heads * 2 * 4 : 0);
+    const size_t crows = static_cast<size_t>(chunk_item_cap(c, C)) * c.n_kv_heads * 256;
+    P.cpart_o = take(crows * c.head_dim * 4);
+    P.cpart_ml = take(crows * 2 * 4);
+    P.end = off;
+    return P;
 }
 
 struct Layout {
-    size_t xn, qkv, attn, h, act, rope, meta, part_o, part_ml, cpart_o, cpart_ml, gemm_part, end_fixed;
+    size_t xn, qkv, attn, h, act, rope, new_k, new_v, meta, gemm_part, end_fixed;
+    PartLayout part;
     size_t gemm_part_bytes;  // from gemm_part on; set where the workspace is known
 };
 
-Layout layout(const slw_model_cfg& c, int C, int B) {
+Layout layout(const slw_ctx& ctx, int C, int B) {
+    const slw_model_cfg& c = ctx.cfg;
     const size_t M = static_cast<size_t>(C) + B;
-    const int W = decode_work_cap(c, B);
     Layout L{};
     size_t off = 0;
     auto take = [&](size_t bytes) {
@@ -185,12 +161,14 @@ Layout layout(const slw_model_cfg& c, int C, int B) {
     L.h = take(M * c.d_model * 4);  // fp32 residual stream inside the layer
     L.act = take(M * c.ffn_dim * 2);
     L.rope = take(M * (c.head_dim / 2) * 8);
-    L.meta = take(meta_ints(c, C, B) * 4);
-    L.part_o = take(B > 0 ? static_cast<size_t>(W) * c.n_q_heads * c.head_dim * 4 : 0);
-    L.part_ml = take(B > 0 ? static_cast<size_t>(W) * c.n_q_heads * 2 * 4 : 0);
-    const size_t crows = static_cast<size_t>(chunk_item_cap(c, C)) * c.n_kv_heads * 256;
-    L.cpart_o = take(crows * c.head_dim * 4);
-    L.cpart_ml = take(crows * 2 * 4);
+    // e4m3 pools: bf16 pages of the iteration's own rows, which the QKV
+    // projection's epilogue fills in the place of the pools
+    const size_t fresh = ctx.k_scale ? ceil_div(M, 16) * 16 * c.n_kv_heads * c.head_dim * 2 : 0;
+    L.new_k = take(fresh);
+    L.new_v = take(fresh);
+    L.meta = take(meta_ints(ctx, C, B) * 4);
+    L.part = part_layout(c, C, B, off);
+    off = L.part.end;
     L.gemm_part = off;  // split-K partials take the rest of the workspace
     L.end_fixed = off;
     return L;
@@ -229,6 +207,13 @@ int check_cfg(const slw_model_cfg& c) {
     if (c.block_size != 16) return fail(SLW_EUNSUPPORTED, "block_size must be 16");
     if (c.max_pos < 1 || c.max_pos > (1 << 20)) return fail(SLW_EINVAL, "max_pos out of range");
     if (!(c.rms_eps > 0.f) || !(c.rope_theta > 0.f)) return fail(SLW_EINVAL, "rms_eps and rope_theta must be > 0");
+    return SLW_OK;
+}
+
+int check_window(const slw_model_cfg& c, int32_t window, int32_t sinks) {
+    if (window < 0) return fail(SLW_EINVAL, "negative window");
+    if (sinks < 0 || sinks > c.max_pos) return fail(SLW_EINVAL, "sinks must be in [0, max_pos]");
+    if (window == 0 && sinks > 0) return fail(SLW_EINVAL, "sinks without a window");
     return SLW_OK;
 }
 
@@ -284,34 +269,12 @@ int ensure_stage_events(slw_ctx* ctx) {
     return SLW_OK;
 }
 
-int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void* x_out, void* ws,
-                      const Layout& L, const LayerPlans& plans, hipStream_t stream, bool no_alloc);
-
-// One iteration: validation, KV reservation (all or nothing), then the
-// metadata, its upload and the kernels.  A failure after the reservation
-// returns the reserved blocks, so a failed call leaves the block manager as
-// it found it.  no_alloc: the workspace is the static array, the metadata is
-// copied with hipMemcpyAsync from host memory the context holds, both
-// attentions run on `stream` and no stage events are recorded, so the call
-// creates no HIP object and allocates no memory of any kind on the device or
-// pinned on the host.
-int mixed_iteration_impl(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void* x_out, void* ws,
-                         size_t ws_bytes, hipStream_t stream, bool no_alloc = false) {
+// Validates a batch with rows: ctx->prefills receives its prefills in row
+// order, req the reservations it needs (sequence, length).
+int check_batch(slw_ctx* ctx, const slw_batch* bt, std::vector<std::pair<int64_t, int32_t>>& req) {
     const slw_model_cfg& c = ctx->cfg;
-    if (!bt) return fail(SLW_EINVAL, "null batch");
     const int C = bt->C, B = bt->B;
-    if (C < 0 || B < 0) return fail(SLW_EINVAL, "negative C or B");
-    if (C == 0 && B == 0) {
-        ctx->last_slots.clear();
-        return SLW_OK;
-    }
-    if (!ctx->kv_ready) return fail(SLW_EINVAL, "KV pools not attached (slw_kv_init)");
-    for (int l = 0; l < c.n_layers; ++l)
-        if (!ctx->have_w[l]) return fail(SLW_EINVAL, "weights of layer %d not set", l);
-    if (!x_in || !x_out || !ws) return fail(SLW_EINVAL, "null device buffer");
     if (B > 0 && (!bt->decode_seqs || !bt->context_lens)) return fail(SLW_EINVAL, "null decode arrays");
-
-    // validation; the chunk rows' prefills in row order
     std::vector<Prefill>& pre = ctx->prefills;
     pre.clear();
     if (bt->n_prefill > 1) {
@@ -327,7 +290,6 @@ int mixed_iteration_impl(slw_ctx* ctx, const slw_batch* bt, const void* x_in, vo
     } else if (C > 0) {
         pre.push_back({bt->prefill_seq, bt->prefix_len, C, 0});
     }
-    std::vector<std::pair<int64_t, int32_t>> req;
     req.reserve(B + pre.size());
     std::unordered_set<int64_t> seen;
     seen.reserve(2 * (B + pre.size()) + 2);
@@ -356,7 +318,38 @@ int mixed_iteration_impl(slw_ctx* ctx, const slw_batch* bt, const void* x_in, vo
             req.emplace_back(id, L + 1);
         }
     }
-    Layout L = layout(c, C, B);
+    return SLW_OK;
+}
+
+int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void* x_out, void* ws,
+                      const Layout& L, const LayerPlans& plans, hipStream_t stream, bool no_alloc);
+
+// One iteration: validation, KV reservation (all or nothing), then the
+// metadata, its upload and the kernels.  A failure after the reservation
+// returns the reserved blocks, so a failed call leaves the block manager as
+// it found it.  no_alloc: the workspace is the static array, the metadata is
+// copied with hipMemcpyAsync from host memory the context holds, both
+// attentions run on `stream` and no stage events are recorded, so the call
+// creates no HIP object and allocates no memory of any kind on the device or
+// pinned on the host.
+int mixed_iteration_impl(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void* x_out, void* ws,
+                         size_t ws_bytes, hipStream_t stream, bool no_alloc = false) {
+    const slw_model_cfg& c = ctx->cfg;
+    if (!bt) return fail(SLW_EINVAL, "null batch");
+    const int C = bt->C, B = bt->B;
+    if (C < 0 || B < 0) return fail(SLW_EINVAL, "negative C or B");
+    if (C == 0 && B == 0) {
+        ctx->last_slots.clear();
+        return SLW_OK;
+    }
+    if (!ctx->kv_ready) return fail(SLW_EINVAL, "KV pools not attached (slw_kv_init)");
+    for (int l = 0; l < c.n_layers; ++l)
+        if (!ctx->have_w[l]) return fail(SLW_EINVAL, "weights of layer %d not set", l);
+    if (!x_in || !x_out || !ws) return fail(SLW_EINVAL, "null device buffer");
+    std::vector<std::pair<int64_t, int32_t>> req;
+    int rc = check_batch(ctx, bt, req);
+    if (rc) return rc;
+    Layout L = layout(*ctx, C, B);
     const LayerPlans plans = plan_layer(c, C + B);
     if (!plans.ok(c, C + B)) return fail(SLW_EINVAL, "internal: GEMM plan");
     size_t need = L.end_fixed + plans.partial_bytes();
@@ -365,14 +358,13 @@ int mixed_iteration_impl(slw_ctx* ctx, const slw_batch* bt, const void* x_in, vo
     // no product runs beside, and the products run in blocks of as many rows
     // as fit there, with the same plans and so the same results.
     if (no_alloc && ws_bytes < need) {
-        L.gemm_part = L.part_o;
+        L.gemm_part = L.part.part_o;
         need = std::max(L.end_fixed, L.gemm_part + plans.partial_bytes() / (C + B));
     }
     if (ws_bytes < need)
         return fail(SLW_ENOMEM, "%s holds %zu bytes, this iteration needs %zu",
                     no_alloc ? "the static workspace (SLW_STATIC_WS_BYTES)" : "the workspace", ws_bytes, need);
     L.gemm_part_bytes = ws_bytes - L.gemm_part;
-    int rc = SLW_OK;
     if (!no_alloc) {
         rc = ensure_hip(ctx);
         if (rc) return rc;
@@ -389,189 +381,232 @@ int mixed_iteration_impl(slw_ctx* ctx, const slw_batch* bt, const void* x_in, vo
     return rc;
 }
 
+// Where a batch's attention metadata lies (32-bit words from its start) and
+// how long its lists are.
+struct AttnMeta {
+    int C = 0, B = 0, n_qt = 0, n_app = 0;
+    size_t kvlen = 0, btoff = 0, bt = 0, pre = 0, qt = 0, app = 0;
+    struct Class {  // the work lists of full ([0]) or windowed ([1]) layers
+        int n_work = 0, n_dslots = 0, n_items = 0, n_slots = 0;
+        size_t work = 0, skip = 0, item = 0, slot = 0, slot_items = 0, qtoff = 0, qt_skip = 0;
+        bool two_phase = false;
+    } cls[2];
+};
+
+// Appends the metadata of both attentions and of the append to m; offsets
+// count from m's start.
+int build_attn_meta(slw_ctx* ctx, const slw_batch* bt, std::vector<int32_t>& m, AttnMeta& am) {
+    const slw_model_cfg& c = ctx->cfg;
+    const int C = bt->C, B = bt->B;
+    const std::vector<Prefill>& pre = ctx->prefills;
+    int rc = SLW_OK;
+    auto put = [&](const std::vector<int32_t>& v) {
+        const size_t at = m.size();
+        m.insert(m.end(), v.begin(), v.end());
+        return at;
+    };
+    am.C = C;
+    am.B = B;
+    am.kvlen = m.size();
+    for (int b = 0; b < B; ++b) m.push_back(bt->context_lens[b] + 1);
+    am.btoff = m.size();
+    m.resize(m.size() + B + 1);
+    am.bt = m.size();
+    for (int b = 0; b < B; ++b) {
+        m[am.btoff + b] = static_cast<int32_t>(m.size() - am.bt);
+        const auto& t = ctx->kv.table(bt->decode_seqs[b]);
+        const int nb = static_cast<int>(ceil_div(bt->context_lens[b] + 1, 16));
+        m.insert(m.end(), t.begin(), t.begin() + nb);
+    }
+    m[am.btoff + B] = static_cast<int32_t>(m.size() - am.bt);
+    // block tables of the prefills, one after the other
+    am.pre = m.size();
+    std::vector<int32_t> pre_bt(pre.size());
+    for (size_t i = 0; i < pre.size(); ++i) {
+        pre_bt[i] = static_cast<int32_t>(m.size() - am.pre);
+        const auto& t = ctx->kv.table(pre[i].seq);
+        const int nb = static_cast<int>(ceil_div(pre[i].prefix + pre[i].c, 16));
+        m.insert(m.end(), t.begin(), t.begin() + nb);
+    }
+    // Each prefill's rows are cut into query tiles (a tile never mixes
+    // sequences); query tile q covers chunk rows qt_row0 .. + qt_rows at
+    // positions from qt_pos0 on and reads the block table at qt_bt, over keys
+    // 0 .. qt_pos0 + qt_rows - 1.
+    std::vector<int32_t> qt_row0, qt_rows, qt_pos0, qt_bt;
+    query_tiles(c, pre, qt_row0, qt_rows, qt_pos0, &qt_bt, pre_bt);
+    const int n_qt = static_cast<int>(qt_row0.size());
+    if (n_qt > chunk_tiles(c, C)) return fail(SLW_EINVAL, "internal: %d query tiles above cap", n_qt);
+    am.n_qt = n_qt;
+    am.qt = put(qt_row0);  // [4][n_qt]: first row, rows, first position, block-table offset
+    put(qt_rows);
+    put(qt_pos0);
+    put(qt_bt);
+    // [4][n_app]: block, first new token, new tokens, first row of each block appended to
+    std::vector<int32_t> app[4];
+    auto add = [&](int64_t seq, int at, int n, int row) {
+        const auto& t = ctx->kv.table(seq);
+        for (const int end = at + n; at < end;) {
+            const int k = std::min(16 - at % 16, end - at);
+            app[0].push_back(t[at / 16]);
+            app[1].push_back(at % 16);
+            app[2].push_back(k);
+            app[3].push_back(row);
+            at += k;
+            row += k;
+        }
+    };
+    for (const Prefill& f : pre) add(f.seq, f.prefix, f.c, f.row0);
+    for (int b = 0; b < B; ++b) add(bt->decode_seqs[b], bt->context_lens[b], 1, C + b);
+    am.n_app = static_cast<int>(app[0].size());
+    if (app[0].size() > append_cap(C, B)) return fail(SLW_EINVAL, "internal: %d blocks to append to above cap", am.n_app);
+    am.app = m.size();
+    for (const auto& v : app) put(v);
+
+    for (int k = 0; k < 2; ++k) {
+        if (!(k ? ctx->any_windowed : ctx->any_full)) continue;
+        AttnMeta::Class& cl = am.cls[k];
+        const Window w = k ? ctx->win : Window{};
+        DecodePlan& dp = ctx->dplan;
+        if ((rc = plan_decode(c, w, B, bt->context_lens, dp))) return rc;
+        cl.n_work = static_cast<int>(dp.b.size());
+        cl.n_dslots = static_cast<int>(dp.slot_off.size()) - 1;
+        cl.work = put(dp.b);
+        put(dp.kb);
+        put(dp.ke);
+        put(dp.off);
+        put(dp.slot_off);
+        cl.skip = put(dp.skip);
+        // plan_chunk hands the query tiles out to the work-groups.  A tile
+        // covered by one item is written directly, one covered by several is
+        // combined by the merge kernel.
+        ChunkPlan& cp = ctx->cplan;
+        if ((rc = plan_chunk(c, w, C, qt_pos0, qt_rows, cp))) return rc;
+        cl.n_items = static_cast<int>(cp.items.size() / 3);
+        cl.n_slots = static_cast<int>(cp.slot_off.size()) - 1;
+        cl.item = m.size();
+        m.resize(m.size() + cp.items.size());
+        for (int i = 0; i < cl.n_items; ++i)
+            for (int j = 0; j < 3; ++j) m[cl.item + static_cast<size_t>(j) * cl.n_items + i] = cp.items[3 * i + j];
+        cl.slot = put(cp.slot_off);
+        cl.slot_items = put(cp.slot_items);
+        cl.qtoff = put(cp.qt_off);
+        cl.qt_skip = put(cp.qt_skip);
+        cl.two_phase = cp.two_phase;
+    }
+    return SLW_OK;
+}
+
+CacheLayer cache_layer(const slw_ctx* ctx, int l) {
+    const size_t heads = static_cast<size_t>(ctx->kv.num_blocks()) * ctx->cfg.n_kv_heads * l;  // before the layer
+    const size_t at = heads * ctx->cfg.head_dim * 16 * (ctx->k_scale ? 1 : 2);
+    return {static_cast<char*>(ctx->k_pool) + at, static_cast<char*>(ctx->v_pool) + at,
+            ctx->k_scale ? ctx->k_scale + heads : nullptr, ctx->v_scale ? ctx->v_scale + heads : nullptr,
+            ctx->cfg.n_kv_heads, ctx->cfg.head_dim};
+}
+
+AppendArgs append_args(const slw_ctx* ctx, const AttnMeta& am, const int32_t* dmeta, int l, const void* k,
+                       const void* v, int ld) {
+    return {cache_layer(ctx, l), k, v, dmeta + am.app, am.n_app, ld};
+}
+
+// The attention of one layer: q rows of stride ld (chunk rows, then decodes),
+// out [rows][hq * hd], metadata at dmeta, partial sums at ws + P.
+struct AttnCall {
+    CacheAttnArgs a{};
+    bool cache = false;  // the kernels for e4m3 pools or a window
+    AttnCall(const slw_ctx* ctx, const AttnMeta& am, const int32_t* dmeta, char* ws, const PartLayout& P, int l,
+             const void* q, int ld, void* out) {
+        const slw_model_cfg& c = ctx->cfg;
+        const int hq = c.n_q_heads, hkv = c.n_kv_heads, hd = c.head_dim;
+        const AttnMeta::Class& cl = am.cls[ctx->windowed[l] ? 1 : 0];
+        const CacheLayer pool = cache_layer(ctx, l);
+        ChunkAttnArgs& ca = a.chunk;
+        if (am.C > 0) {
+            ca.qkv = q;
+            ca.out = out;
+            ca.k_pool = pool.k_pool;
+            ca.v_pool = pool.v_pool;
+            ca.bt = dmeta + am.pre;
+            ca.item_qt = dmeta + cl.item;
+            ca.item_kb = dmeta + cl.item + cl.n_items;
+            ca.item_ke = dmeta + cl.item + 2 * cl.n_items;
+            ca.qt_off = dmeta + cl.qtoff;
+            ca.part_o = reinterpret_cast<float*>(ws + P.cpart_o);
+            ca.part_ml = reinterpret_cast<float*>(ws + P.cpart_ml);
+            ca.c = am.C;
+            ca.n_qt = am.n_qt;
+            ca.qt_row0 = dmeta + am.qt;
+            ca.qt_rows = dmeta + am.qt + am.n_qt;
+            ca.qt_pos0 = dmeta + am.qt + 2 * am.n_qt;
+            ca.qt_bt = dmeta + am.qt + 3 * am.n_qt;
+            ca.hq = hq;
+            ca.hkv = hkv;
+            ca.hd = hd;
+            ca.ld_qkv = ld;
+            ca.slot_off = dmeta + cl.slot;
+            ca.slot_items = dmeta + cl.slot_items;
+            ca.n_items = cl.n_items;
+            ca.n_slots = cl.n_slots;
+            ca.split = cl.n_items > am.n_qt ? 1 : 0;
+            ca.pp = cl.two_phase ? 1 : 0;
+        }
+        DecodeAttnArgs& da = a.decode;
+        if (am.B > 0) {
+            da.q = static_cast<const char*>(q) + static_cast<size_t>(am.C) * ld * 2;
+            da.out = static_cast<char*>(out) + static_cast<size_t>(am.C) * hq * hd * 2;
+            da.k_pool = pool.k_pool;
+            da.v_pool = pool.v_pool;
+            da.kv_len = dmeta + am.kvlen;
+            da.bt_off = dmeta + am.btoff;
+            da.bt = dmeta + am.bt;
+            da.work_b = dmeta + cl.work;
+            da.work_kb = dmeta + cl.work + cl.n_work;
+            da.work_ke = dmeta + cl.work + 2 * cl.n_work;
+            da.work_off = dmeta + cl.work + 3 * cl.n_work;
+            da.slot_off = dmeta + cl.work + 3 * cl.n_work + am.B + 1;
+            da.n_slots = cl.n_dslots;
+            da.part_o = reinterpret_cast<float*>(ws + P.part_o);
+            da.part_ml = reinterpret_cast<float*>(ws + P.part_ml);
+            da.b = am.B;
+            da.n_work = cl.n_work;
+            da.hq = hq;
+            da.hkv = hkv;
+            da.hd = hd;
+            da.ld_q = ld;
+        }
+        cache = ctx->k_scale || ctx->windowed[l];
+        if (cache) {
+            a.k_scale = pool.k_scale;
+            a.v_scale = pool.v_scale;
+            a.qt_skip = dmeta + cl.qt_skip;
+            a.skip = dmeta + cl.skip;
+            const Window w = ctx->windowed[l] ? ctx->win : Window{};
+            a.window = w.window;
+            a.sinks = w.window > 0 ? w.sinks : 0;
+            a.sink_end = sink_end(w);
+        }
+    }
+    // The parts: chunk and decode in one launch, or each alone.
+    void both(hipStream_t s) const {
+        if (cache) launch_cache_attention(a, s);
+        else launch_attention(a.chunk, a.decode, s);
+    }
+    void chunk(hipStream_t s) const {
+        if (!cache) return launch_chunk_attention(a.chunk, s);
+        CacheAttnArgs x = a;
+        x.decode = DecodeAttnArgs{};
+        launch_cache_attention(x, s);
+    }
+    void decode(hipStream_t s) const {
+        if (!cache) return launch_decode_attention_split(a.decode, s);
+        CacheAttnArgs x = a;
+        x.chunk = ChunkAttnArgs{};
+        launch_cache_attention(x, s);
+    }
+    void merge(hipStream_t s) const { launch_attention_merge(&a.chunk, &a.decode, s); }
+};
+
 // Metadata, upload and kernels of an iteration whose blocks are reserved.
-// Query tiles of the chunk rows: each prefill's rows cut into tiles of
-// chunk_tile_positions(group) positions (a tile never mixes sequences).
-// Tile q: first chunk row, rows, first position and, when wanted, the offset
-// of its sequence's block table (bt_of_prefill[i] for prefill i).
-void query_tiles(const slw_model_cfg& c, const std::vector<Prefill>& pre, std::vector<int32_t>& row0,
-                 std::vector<int32_t>& rows, std::vector<int32_t>& pos0, std::vector<int32_t>* bt,
-                 const std::vector<int32_t>& bt_of_prefill) {
-    const int pwg = chunk_tile_positions(c.n_q_heads / c.n_kv_heads);
-    row0.clear();
-    rows.clear();
-    pos0.clear();
-    if (bt) bt->clear();
-    for (size_t i = 0; i < pre.size(); ++i)
-        for (int j = 0; j < pre[i].c; j += pwg) {
-            row0.push_back(pre[i].row0 + j);
-            rows.push_back(std::min(pwg, pre[i].c - j));
-            pos0.push_back(pre[i].prefix + j);
-            if (bt) bt->push_back(bt_of_prefill[i]);
-        }
-}
-
-// Decode attention work.  The keys of all decodes (decode b attends to
-// context_lens[b] + 1 of them), laid end to end with each decode's range
-// padded to a multiple of 64, are cut into equal runs (multiples of 64 keys,
-// so that every item starts on a page pair; at least kDecodeMinKeys each, at
-// most decode_slot_cap(c) runs), one per wave of each kv head; a run that
-// crosses decodes becomes one item per decode it touches, and padding alone
-// makes no item.  Items come out in decode order, so each decode's items are
-// contiguous for the merge.
-int plan_decode(const slw_model_cfg& c, int B, const int32_t* context_lens, DecodePlan& p) {
-    p.b.clear();
-    p.kb.clear();
-    p.ke.clear();
-    p.off.assign(B + 1, 0);
-    p.slot_off.assign(1, 0);
-    if (B <= 0) return SLW_OK;
-    int64_t padded = 0;
-    for (int b = 0; b < B; ++b) padded += ceil_div(context_lens[b] + 1, 64) * 64;
-    const int64_t want = std::min<int64_t>(decode_slot_cap(c), std::max<int64_t>(1, padded / kDecodeMinKeys));
-    const int64_t per = ceil_div(ceil_div(padded, want), 64) * 64;
-    const int n_slots = static_cast<int>(ceil_div(padded, per));
-    p.slot_off.clear();
-    int b = 0;
-    int64_t start_b = 0;  // first key of decode b in the padded layout
-    for (int sl = 0; sl < n_slots; ++sl) {
-        p.slot_off.push_back(static_cast<int32_t>(p.b.size()));
-        int64_t r0 = sl * per;
-        const int64_t r1 = std::min(padded, r0 + per);
-        while (r0 < r1) {
-            const int32_t len = context_lens[b] + 1;
-            const int64_t span = ceil_div(len, 64) * 64;
-            if (r0 >= start_b + span) {  // past decode b
-                start_b += span;
-                p.off[++b] = static_cast<int32_t>(p.b.size());
-                continue;
-            }
-            const int64_t k0 = r0 - start_b, k1 = std::min<int64_t>(r1 - start_b, span);
-            if (k0 < len) {
-                p.b.push_back(b);
-                p.kb.push_back(static_cast<int32_t>(k0));
-                p.ke.push_back(static_cast<int32_t>(std::min<int64_t>(k1, len)));
-            }
-            r0 = start_b + k1;
-        }
-    }
-    p.slot_off.push_back(static_cast<int32_t>(p.b.size()));
-    while (b < B) p.off[++b] = static_cast<int32_t>(p.b.size());
-    if (static_cast<int>(p.b.size()) > decode_work_cap(c, B) || n_slots > decode_slot_cap(c))
-        return fail(SLW_EINVAL, "internal: decode work %zu / slots %d above cap", p.b.size(), n_slots);
-    for (int d = 0; d < B; ++d) {  // the items of each decode tile its keys
-        int64_t at = 0;
-        for (int i = p.off[d]; i < p.off[d + 1]; ++i) {
-            if (p.b[i] != d || p.kb[i] != at || p.ke[i] <= at) return fail(SLW_EINVAL, "internal: decode plan");
-            at = p.ke[i];
-        }
-        if (at != context_lens[d] + 1) return fail(SLW_EINVAL, "internal: decode plan");
-    }
-    return SLW_OK;
-}
-
-// Chunk attention work over query tiles q (first position qt_pos0[q],
-// qt_rows[q] rows, keys 0 .. qt_pos0[q] + qt_rows[q] - 1).  Whole query tiles
-// where they balance: the tiles, longest first, each go to the least loaded
-// of `want` work-groups (LPT); when the largest load stays within
-// kChunkWholeSlack of an equal share, no tile is split and nothing is merged
-// (long prompts: many tiles of similar length).  Otherwise (fewer tiles than
-// work-groups, or tiles of very different lengths, as at the start of a
-// prompt) the 64-key tiles of every query tile, laid end to end, are cut into
-// equal runs, one per work-group of each kv head; a run that crosses query
-// tiles becomes one item per query tile it touches.  Items stay in query-tile
-// order; slot_items lists each work-group's items.
-int plan_chunk(const slw_model_cfg& c, int C, const std::vector<int32_t>& qt_pos0, const std::vector<int32_t>& qt_rows,
-               ChunkPlan& p) {
-    const int n_qt = static_cast<int>(qt_pos0.size());
-    p.items.clear();
-    p.slot_off.clear();
-    p.slot_items.clear();
-    p.whole = false;
-    auto key_end = [&](int q) { return static_cast<int64_t>(qt_pos0[q]) + qt_rows[q]; };
-    std::vector<int64_t> tile_end(n_qt + 1, 0);
-    for (int q = 0; q < n_qt; ++q) tile_end[q + 1] = tile_end[q] + ceil_div(key_end(q), 64);
-    const int64_t total_tiles = tile_end[n_qt];
-    std::vector<int32_t>& it = p.items;
-    int n_slots = 0;
-    if (n_qt > 0) {
-        const int64_t want = std::min<int64_t>(chunk_slot_cap(c), std::max<int64_t>(1, total_tiles / kChunkMinTiles));
-        const int64_t per = ceil_div(total_tiles, want);
-        if (n_qt >= want) {
-            std::vector<int32_t> order(n_qt);
-            for (int q = 0; q < n_qt; ++q) order[q] = q;
-            auto len = [&](int q) { return tile_end[q + 1] - tile_end[q]; };
-            std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return len(x) > len(y); });
-            std::vector<int64_t> load(want, 0);
-            std::vector<int32_t> owner(n_qt);
-            for (int q : order) {
-                const int g = static_cast<int>(std::min_element(load.begin(), load.end()) - load.begin());
-                load[g] += len(q);
-                owner[q] = g;
-            }
-            const int64_t mx = *std::max_element(load.begin(), load.end());
-            if (mx * kChunkWholeSlackDen <= per * kChunkWholeSlackNum) {
-                p.whole = true;
-                n_slots = static_cast<int>(want);
-                for (int q = 0; q < n_qt; ++q) {
-                    it.push_back(q);
-                    it.push_back(0);
-                    it.push_back(static_cast<int32_t>(key_end(q)));
-                }
-                p.slot_off.assign(n_slots + 1, 0);
-                for (int q = 0; q < n_qt; ++q) ++p.slot_off[owner[q] + 1];
-                for (int g = 0; g < n_slots; ++g) p.slot_off[g + 1] += p.slot_off[g];
-                p.slot_items.resize(n_qt);
-                std::vector<int32_t> fill(p.slot_off.begin(), p.slot_off.end() - 1);
-                for (int q = 0; q < n_qt; ++q) p.slot_items[fill[owner[q]]++] = q;
-            }
-        }
-        if (!p.whole) {
-            n_slots = static_cast<int>(ceil_div(total_tiles, per));
-            p.slot_off.resize(n_slots + 1);
-            int q = 0;
-            for (int sl = 0; sl < n_slots; ++sl) {
-                p.slot_off[sl] = static_cast<int32_t>(it.size() / 3);
-                int64_t t0 = sl * per;
-                const int64_t t1 = std::min(total_tiles, t0 + per);
-                while (t0 < t1) {
-                    while (tile_end[q + 1] <= t0) ++q;
-                    const int64_t seg_end = std::min(t1, tile_end[q + 1]);
-                    it.push_back(q);
-                    it.push_back(static_cast<int32_t>((t0 - tile_end[q]) * 64));
-                    it.push_back(static_cast<int32_t>(std::min(key_end(q), (seg_end - tile_end[q]) * 64)));
-                    t0 = seg_end;
-                }
-            }
-            p.slot_off[n_slots] = static_cast<int32_t>(it.size() / 3);
-            p.slot_items.resize(it.size() / 3);
-            for (size_t i = 0; i < p.slot_items.size(); ++i) p.slot_items[i] = static_cast<int32_t>(i);
-        }
-    } else {
-        p.slot_off.assign(1, 0);
-    }
-    const int n_items = static_cast<int>(it.size() / 3);
-    const int64_t blocks64 = std::max(1, chunk_tile_positions(c.n_q_heads / c.n_kv_heads) / 64);
-    p.two_phase = c.head_dim == 128 && n_items > 0 &&
-                  total_tiles >= (kTwoPhaseTiles + kTwoPhaseTilesPer64 * blocks64) * n_items;
-    p.qt_off.assign(n_qt + 1, 0);
-    for (int q = 0, i = 0; q <= n_qt; ++q) {
-        while (i < n_items && it[3 * i] < q) ++i;
-        p.qt_off[q] = i;
-    }
-    if (n_items > chunk_item_cap(c, C) || n_slots > chunk_slot_cap(c))
-        return fail(SLW_EINVAL, "internal: chunk items %d / slots %d above cap", n_items, n_slots);
-    for (int q = 0; q < n_qt; ++q) {  // the items of each query tile tile its key range
-        int64_t at = 0;
-        for (int i = p.qt_off[q]; i < p.qt_off[q + 1]; ++i) {
-            if (it[3 * i + 1] != at || it[3 * i + 2] <= at) return fail(SLW_EINVAL, "internal: chunk plan");
-            at = it[3 * i + 2];
-        }
-        if (at != key_end(q)) return fail(SLW_EINVAL, "internal: chunk plan");
-    }
-    return SLW_OK;
-}
-
 int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void* x_out, void* ws,
                       const Layout& L, const LayerPlans& plans, hipStream_t stream, bool no_alloc) {
     const slw_model_cfg& c = ctx->cfg;
@@ -584,86 +619,24 @@ int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void*
 
     std::vector<int32_t>& m = ctx->meta;
     m.clear();
-    m.reserve(meta_ints(c, C, B));
+    m.reserve(meta_ints(*ctx, C, B));
     // slot[M], pos[M]
     std::vector<int32_t>& slots = ctx->slots_build;
     slots.resize(M);
     for (const Prefill& f : pre)
         for (int j = 0; j < f.c; ++j) slots[f.row0 + j] = ctx->kv.slot(f.seq, f.prefix + j);
     for (int b = 0; b < B; ++b) slots[C + b] = ctx->kv.slot(bt->decode_seqs[b], bt->context_lens[b]);
-    m.insert(m.end(), slots.begin(), slots.end());
+    if (ctx->k_scale)  // the QKV projection writes its rows to pages of their own
+        for (int r = 0; r < M; ++r) m.push_back(r);
+    else
+        m.insert(m.end(), slots.begin(), slots.end());
     for (const Prefill& f : pre)
         for (int j = 0; j < f.c; ++j) m.push_back(f.prefix + j);
     for (int b = 0; b < B; ++b) m.push_back(bt->context_lens[b]);
-    const size_t o_kvlen = m.size();
-    for (int b = 0; b < B; ++b) m.push_back(bt->context_lens[b] + 1);
-    const size_t o_btoff = m.size();
-    m.resize(m.size() + B + 1);
-    const size_t o_bt = m.size();
-    for (int b = 0; b < B; ++b) {
-        m[o_btoff + b] = static_cast<int32_t>(m.size() - o_bt);
-        const auto& t = ctx->kv.table(bt->decode_seqs[b]);
-        const int nb = static_cast<int>(ceil_div(bt->context_lens[b] + 1, 16));
-        m.insert(m.end(), t.begin(), t.begin() + nb);
-    }
-    m[o_btoff + B] = static_cast<int32_t>(m.size() - o_bt);
-    // block tables of the prefills, one after the other
-    const size_t o_pre = m.size();
-    std::vector<int32_t> pre_bt(pre.size());
-    for (size_t i = 0; i < pre.size(); ++i) {
-        pre_bt[i] = static_cast<int32_t>(m.size() - o_pre);
-        const auto& t = ctx->kv.table(pre[i].seq);
-        const int nb = static_cast<int>(ceil_div(pre[i].prefix + pre[i].c, 16));
-        m.insert(m.end(), t.begin(), t.begin() + nb);
-    }
-    // Decode attention work (plan_decode).
-    const size_t o_workb = m.size();
-    DecodePlan& dp = ctx->dplan;
-    if ((rc = plan_decode(c, B, bt->context_lens, dp))) return rc;
-    const int n_work = static_cast<int>(dp.b.size()), n_dslots = static_cast<int>(dp.slot_off.size()) - 1;
-    m.insert(m.end(), dp.b.begin(), dp.b.end());
-    m.insert(m.end(), dp.kb.begin(), dp.kb.end());
-    m.insert(m.end(), dp.ke.begin(), dp.ke.end());
-    m.insert(m.end(), dp.off.begin(), dp.off.end());
-    m.insert(m.end(), dp.slot_off.begin(), dp.slot_off.end());
-    // Chunk attention work.  Each prefill's rows are cut into query tiles of
-    // pwg positions (a tile never mixes sequences); query tile q covers chunk
-    // rows qt_row0 .. + qt_rows at positions from qt_pos0 on and reads the
-    // block table at qt_bt, over keys 0 .. qt_pos0 + qt_rows - 1; plan_chunk
-    // hands the tiles out to the work-groups.  A query tile covered by one
-    // item is written directly, one covered by several is combined by the
-    // merge kernel.
-    std::vector<int32_t> qt_row0, qt_rows, qt_pos0, qt_bt;
-    query_tiles(c, pre, qt_row0, qt_rows, qt_pos0, &qt_bt, pre_bt);
-    const int n_qt = static_cast<int>(qt_row0.size());
-    if (n_qt > chunk_tiles(c, C)) return fail(SLW_EINVAL, "internal: %d query tiles above cap", n_qt);
-    ChunkPlan& cp = ctx->cplan;
-    if ((rc = plan_chunk(c, C, qt_pos0, qt_rows, cp))) return rc;
-    const std::vector<int32_t>& it = cp.items;
-    const std::vector<int32_t>& slot_off = cp.slot_off;
-    const std::vector<int32_t>& slot_items = cp.slot_items;
-    const std::vector<int32_t>& qt_off = cp.qt_off;
-    const int n_items = static_cast<int>(it.size() / 3), n_slots = static_cast<int>(slot_off.size()) - 1;
-    const size_t o_item = m.size();
-    m.resize(m.size() + 3 * static_cast<size_t>(n_items));
-    for (int i = 0; i < n_items; ++i) {
-        m[o_item + i] = it[3 * i];
-        m[o_item + n_items + i] = it[3 * i + 1];
-        m[o_item + 2 * n_items + i] = it[3 * i + 2];
-    }
-    const size_t o_slot = m.size();
-    m.insert(m.end(), slot_off.begin(), slot_off.end());
-    const size_t o_slot_items = m.size();
-    m.insert(m.end(), slot_items.begin(), slot_items.end());
-    const size_t o_qtoff = m.size();
-    m.insert(m.end(), qt_off.begin(), qt_off.end());
-    const size_t o_qt = m.size();  // [4][n_qt]: first row, rows, first position, block-table offset
-    m.insert(m.end(), qt_row0.begin(), qt_row0.end());
-    m.insert(m.end(), qt_rows.begin(), qt_rows.end());
-    m.insert(m.end(), qt_pos0.begin(), qt_pos0.end());
-    m.insert(m.end(), qt_bt.begin(), qt_bt.end());
+    AttnMeta am;
+    if ((rc = build_attn_meta(ctx, bt, m, am))) return rc;
 
-    if (m.size() > meta_ints(c, C, B)) return fail(SLW_EINVAL, "internal: metadata %zu ints above its region", m.size());
+    if (m.size() > meta_ints(*ctx, C, B)) return fail(SLW_EINVAL, "internal: metadata %zu ints above its region", m.size());
 
     // ---- upload ----
     const bool timing = !no_alloc && ctx->stage_depth > 0;
@@ -706,7 +679,6 @@ int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void*
 
     const int d = c.d_model, hq = c.n_q_heads, hkv = c.n_kv_heads, hd = c.head_dim, F = c.ffn_dim;
     const int qw = qkv_width(c);
-    const size_t layer_pool = static_cast<size_t>(ctx->kv.num_blocks()) * hkv * hd * 16 * 2;
 
     size_t set_base = 0;
     int set = 0;
@@ -724,8 +696,7 @@ int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void*
     for (int l = 0; l < c.n_layers; ++l) {
         const slw_layer_weights& wl = ctx->w[l];
         const void* cur = l == 0 ? x_in : x_out;
-        void* kp = static_cast<char*>(ctx->k_pool) + l * layer_pool;
-        void* vp = static_cast<char*>(ctx->v_pool) + l * layer_pool;
+        const CacheLayer pool = cache_layer(ctx, l);
 
         if ((rc = mark(l, 0))) return rc;
         if (l > 0 || !setup_x) launch_rmsnorm(cur, false, wl.g1, xn, M, d, c.rms_eps, stream);
@@ -735,78 +706,29 @@ int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void*
             GemmArgs ga{xn, wl.wqkv, qkv, nullptr, M, qw, d, d, qw, EPI_QKV};
             ga.rope_cs = rope;
             ga.slot = d_slot;
-            ga.k_pool = kp;
-            ga.v_pool = vp;
+            ga.k_pool = ctx->k_scale ? wsb + L.new_k : pool.k_pool;
+            ga.v_pool = ctx->k_scale ? wsb + L.new_v : pool.v_pool;
             ga.hq = hq;
             ga.hkv = hkv;
             ga.hd = hd;
             launch_gemm(ga, plans.qkv, gpartp, L.gemm_part_bytes, stream);
+            if (ctx->k_scale) {
+                const char* k = static_cast<const char*>(qkv) + static_cast<size_t>(hq) * hd * 2;
+                launch_cache_append(append_args(ctx, am, dmeta, l, k, k + static_cast<size_t>(hkv) * hd * 2, qw), stream);
+            }
         }
         if ((rc = mark(l, 3))) return rc;
         // Both attentions in one launch; per-stage events separate them.
-        ChunkAttnArgs ca{};
-        if (C > 0) {
-            ca.qkv = qkv;
-            ca.out = attn;
-            ca.k_pool = kp;
-            ca.v_pool = vp;
-            ca.bt = dmeta + o_pre;
-            ca.item_qt = dmeta + o_item;
-            ca.item_kb = dmeta + o_item + n_items;
-            ca.item_ke = dmeta + o_item + 2 * n_items;
-            ca.qt_off = dmeta + o_qtoff;
-            ca.part_o = reinterpret_cast<float*>(wsb + L.cpart_o);
-            ca.part_ml = reinterpret_cast<float*>(wsb + L.cpart_ml);
-            ca.c = C;
-            ca.n_qt = n_qt;
-            ca.qt_row0 = dmeta + o_qt;
-            ca.qt_rows = dmeta + o_qt + n_qt;
-            ca.qt_pos0 = dmeta + o_qt + 2 * n_qt;
-            ca.qt_bt = dmeta + o_qt + 3 * n_qt;
-            ca.hq = hq;
-            ca.hkv = hkv;
-            ca.hd = hd;
-            ca.ld_qkv = qw;
-            ca.slot_off = dmeta + o_slot;
-            ca.slot_items = dmeta + o_slot_items;
-            ca.n_items = n_items;
-            ca.n_slots = n_slots;
-            ca.split = n_items > n_qt ? 1 : 0;
-            ca.pp = cp.two_phase ? 1 : 0;
-        }
-        DecodeAttnArgs da{};
-        if (B > 0) {
-            da.q = static_cast<const char*>(qkv) + static_cast<size_t>(C) * qw * 2;
-            da.out = static_cast<char*>(attn) + static_cast<size_t>(C) * hq * hd * 2;
-            da.k_pool = kp;
-            da.v_pool = vp;
-            da.kv_len = dmeta + o_kvlen;
-            da.bt_off = dmeta + o_btoff;
-            da.bt = dmeta + o_bt;
-            da.work_b = dmeta + o_workb;
-            da.work_kb = dmeta + o_workb + n_work;
-            da.work_ke = dmeta + o_workb + 2 * n_work;
-            da.work_off = dmeta + o_workb + 3 * n_work;
-            da.slot_off = dmeta + o_workb + 3 * n_work + B + 1;
-            da.n_slots = n_dslots;
-            da.part_o = reinterpret_cast<float*>(wsb + L.part_o);
-            da.part_ml = reinterpret_cast<float*>(wsb + L.part_ml);
-            da.b = B;
-            da.n_work = n_work;
-            da.hq = hq;
-            da.hkv = hkv;
-            da.hd = hd;
-            da.ld_q = qw;
-        }
+        const AttnCall attention(ctx, am, dmeta, wsb, L.part, l, qkv, qw, attn);
         if (timing) {
-            if (C > 0) launch_chunk_attention(ca, stream);
+            if (C > 0) attention.chunk(stream);
             if ((rc = mark(l, 4))) return rc;
-            if (B > 0) launch_decode_attention_split(da, stream);
+            if (B > 0) attention.decode(stream);
         } else {
-            launch_attention(ca, da, stream);
+            attention.both(stream);
         }
         if ((rc = mark(l, 5))) return rc;
-        launch_attention_merge(&ca, &da, stream);
+        attention.merge(stream);
         if ((rc = mark(l, 6))) return rc;
         launch_gemm(GemmArgs{attn, wl.wo, hbuf, cur, M, d, hq * hd, hq * hd, d, EPI_RESID_F32OUT}, plans.o, gpartp,
                     L.gemm_part_bytes, stream);
@@ -824,7 +746,7 @@ int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void*
     HIP_TRY(hipGetLastError());
     if (timing) {
         // the merge stage (5) runs when decodes or split chunk query tiles need it
-        const bool merge = B > 0 || (C > 0 && n_items > n_qt);
+        const bool merge = B > 0 || am.cls[0].n_items > am.n_qt || am.cls[1].n_items > am.n_qt;
         ctx->stage_mask[set] = 0x3FFu & ~(C > 0 ? 0u : (1u << 3)) & ~(B > 0 ? 0u : (1u << 4)) &
                                ~(merge ? 0u : (1u << 5));
         ++ctx->stage_iter;
@@ -849,6 +771,7 @@ extern "C" int slw_create(const slw_model_cfg* cfg, slw_ctx** out) {
         ctx->cfg = *cfg;
         ctx->w.assign(cfg->n_layers, slw_layer_weights{});
         ctx->have_w.assign(cfg->n_layers, 0);
+        ctx->windowed.assign(cfg->n_layers, 0);
         *out = ctx.release();
         return SLW_OK;
     });
@@ -862,11 +785,18 @@ extern "C" int slw_destroy(slw_ctx* ctx) {
 extern "C" int slw_attention_plan(const slw_model_cfg* cfg, int32_t B, const int32_t* context_lens,
                                   int32_t n_prefill, const int32_t* prefix_lens, const int32_t* chunk_lens,
                                   int64_t out[12]) {
+    return slw_attention_plan_window(cfg, 0, 0, B, context_lens, n_prefill, prefix_lens, chunk_lens, out);
+}
+
+extern "C" int slw_attention_plan_window(const slw_model_cfg* cfg, int32_t window, int32_t sinks, int32_t B,
+                                         const int32_t* context_lens, int32_t n_prefill, const int32_t* prefix_lens,
+                                         const int32_t* chunk_lens, int64_t out[12]) {
     return guarded([&] {
         if (!cfg || !out || (B > 0 && !context_lens) || (n_prefill > 0 && (!prefix_lens || !chunk_lens)))
             return fail(SLW_EINVAL, "null argument");
         int rc = check_cfg(*cfg);
         if (rc) return rc;
+        if ((rc = check_window(*cfg, window, sinks))) return rc;
         if (B < 0 || n_prefill < 0 || n_prefill > SLW_MAX_PREFILLS)
             return fail(SLW_EINVAL, "B >= 0 and 0 <= n_prefill <= %d", SLW_MAX_PREFILLS);
         std::vector<Prefill> pre;
@@ -885,8 +815,9 @@ extern "C" int slw_attention_plan(const slw_model_cfg* cfg, int32_t B, const int
         ChunkPlan cp;
         std::vector<int32_t> row0, rows, pos0;
         query_tiles(*cfg, pre, row0, rows, pos0, nullptr, {});
-        if ((rc = plan_decode(*cfg, B, context_lens, dp))) return rc;
-        if ((rc = plan_chunk(*cfg, C, pos0, rows, cp))) return rc;
+        const Window win{window, sinks};
+        if ((rc = plan_decode(*cfg, win, B, context_lens, dp))) return rc;
+        if ((rc = plan_chunk(*cfg, win, C, pos0, rows, cp))) return rc;
         const int dslots = static_cast<int>(dp.slot_off.size()) - 1;
         int64_t dmax = 0, dmin = dslots > 0 ? std::numeric_limits<int64_t>::max() : 0;
         for (int sl = 0; sl < dslots; ++sl) {
@@ -938,18 +869,211 @@ extern "C" int slw_set_layer_weights(slw_ctx* ctx, int32_t layer, const slw_laye
     return SLW_OK;
 }
 
+namespace {
+
+std::atomic<uint64_t> g_kv_ids{0};
+
+int attach_pools(slw_ctx* ctx, void* k_pool, void* v_pool, void* k_scale, void* v_scale, int32_t num_blocks) {
+    if (num_blocks < 1) return fail(SLW_EINVAL, "num_blocks must be >= 1");
+    if (reinterpret_cast<uintptr_t>(k_pool) % 16 || reinterpret_cast<uintptr_t>(v_pool) % 16)
+        return fail(SLW_EINVAL, "pools must be 16-byte aligned");
+    ctx->kv_ready = false;
+    ctx->kv.reset(num_blocks, 16);
+    ctx->k_pool = k_pool;
+    ctx->v_pool = v_pool;
+    ctx->k_scale = static_cast<float*>(k_scale);
+    ctx->v_scale = static_cast<float*>(v_scale);
+    ctx->kv_id = ++g_kv_ids;
+    ctx->kv_ready = true;
+    return SLW_OK;
+}
+
+}  // namespace
+
 extern "C" int slw_kv_init(slw_ctx* ctx, void* k_pool, void* v_pool, int32_t num_blocks) {
     return guarded([&] {
         if (!ctx || !k_pool || !v_pool) return fail(SLW_EINVAL, "null argument");
-        if (num_blocks < 1) return fail(SLW_EINVAL, "num_blocks must be >= 1");
-        if (reinterpret_cast<uintptr_t>(k_pool) % 16 || reinterpret_cast<uintptr_t>(v_pool) % 16)
-            return fail(SLW_EINVAL, "pools must be 16-byte aligned");
-        ctx->k_pool = k_pool;
-        ctx->v_pool = v_pool;
-        ctx->kv.reset(num_blocks, 16);
-        ctx->kv_ready = true;
+        return attach_pools(ctx, k_pool, v_pool, nullptr, nullptr, num_blocks);
+    });
+}
+
+extern "C" int slw_kv_init_8bit(slw_ctx* ctx, void* k_pool, void* v_pool, void* k_scale, void* v_scale,
+                                int32_t num_blocks) {
+    return guarded([&] {
+        if (!ctx || !k_pool || !v_pool || !k_scale || !v_scale) return fail(SLW_EINVAL, "null argument");
+        if (reinterpret_cast<uintptr_t>(k_scale) % 4 || reinterpret_cast<uintptr_t>(v_scale) % 4)
+            return fail(SLW_EINVAL, "scales must be 4-byte aligned");
+        return attach_pools(ctx, k_pool, v_pool, k_scale, v_scale, num_blocks);
+    });
+}
+
+extern "C" int slw_set_window(slw_ctx* ctx, int32_t window, int32_t sinks, const uint8_t* layers) {
+    return guarded([&] {
+        if (!ctx) return fail(SLW_EINVAL, "null context");
+        int rc = check_window(ctx->cfg, window, sinks);
+        if (rc) return rc;
+        ctx->win = Window{window, sinks};
+        ctx->any_windowed = ctx->any_full = false;
+        for (int l = 0; l < ctx->cfg.n_layers; ++l) {
+            ctx->windowed[l] = window > 0 && (!layers || layers[l]);
+            (ctx->windowed[l] ? ctx->any_windowed : ctx->any_full) = true;
+        }
         return SLW_OK;
     });
+}
+
+// ---------------------------------------------------------------------------
+// The cache operators on their own: a batch handed over once, then appends and
+// attention per layer.
+// ---------------------------------------------------------------------------
+
+struct slw_attn {
+    uint64_t kv_id;               // of the pools it was made for
+    Window win;                   // and the windows
+    std::vector<char> windowed;
+    AttnMeta am;
+    PartLayout part;
+    char* ws;
+};
+
+namespace {
+
+struct AttnLayout {
+    size_t meta_bytes;
+    PartLayout part;
+};
+AttnLayout attn_layout(const slw_ctx& ctx, int C, int B) {
+    const size_t meta = align_up(attn_meta_ints(ctx, C, B) * 4);
+    return {meta, part_layout(ctx.cfg, C, B, meta)};
+}
+
+int check_attn(const slw_ctx* ctx, const slw_attn* plan, int32_t layer) {
+    if (!ctx || !plan) return fail(SLW_EINVAL, "null argument");
+    if (!ctx->kv_ready || plan->kv_id != ctx->kv_id)
+        return fail(SLW_EINVAL, "the batch was handed over for other KV pools");
+    if (plan->windowed != ctx->windowed || plan->win.window != ctx->win.window || plan->win.sinks != ctx->win.sinks)
+        return fail(SLW_EINVAL, "the window changed after the batch was handed over");
+    if (layer < 0 || layer >= ctx->cfg.n_layers) return fail(SLW_ERANGE, "layer %d out of range", layer);
+    return SLW_OK;
+}
+
+// Rows that the kernels read or write in 16-byte pieces.
+int check_rows(const void* p, int64_t ld, int64_t width, const char* what) {
+    if (!p) return fail(SLW_EINVAL, "null %s", what);
+    if (reinterpret_cast<uintptr_t>(p) % 16 || ld % 8 || ld < width || ld > INT32_MAX)
+        return fail(SLW_EINVAL, "%s rows: 16-byte aligned, stride a multiple of 8 and at least %lld (got %lld)", what,
+                    (long long)width, (long long)ld);
+    return SLW_OK;
+}
+
+}  // namespace
+
+extern "C" int slw_attn_workspace_size(slw_ctx* ctx, int32_t max_C, int32_t max_B, size_t* bytes) {
+    return guarded([&] {
+        if (!ctx || !bytes) return fail(SLW_EINVAL, "null argument");
+        if (max_C < 0 || max_B < 0) return fail(SLW_EINVAL, "negative size");
+        *bytes = attn_layout(*ctx, max_C, max_B).part.end;
+        return SLW_OK;
+    });
+}
+
+extern "C" int slw_attn_begin(slw_ctx* ctx, const slw_batch* batch, void* ws, size_t ws_bytes, void* stream,
+                              slw_attn** out) {
+    return guarded([&] {
+        if (!ctx || !batch || !out) return fail(SLW_EINVAL, "null argument");
+        *out = nullptr;
+        const int C = batch->C, B = batch->B;
+        if (C < 0 || B < 0) return fail(SLW_EINVAL, "negative C or B");
+        if (!ctx->kv_ready) return fail(SLW_EINVAL, "KV pools not attached");
+        hipStream_t s = static_cast<hipStream_t>(stream);
+        auto plan = std::make_unique<slw_attn>();
+        plan->kv_id = ctx->kv_id;
+        plan->win = ctx->win;
+        plan->windowed = ctx->windowed;
+        plan->ws = static_cast<char*>(ws);
+        if (C == 0 && B == 0) {
+            *out = plan.release();
+            return SLW_OK;
+        }
+        std::vector<std::pair<int64_t, int32_t>> req;
+        int rc = check_batch(ctx, batch, req);
+        if (rc) return rc;
+        const AttnLayout L = attn_layout(*ctx, C, B);
+        if (!ws) return fail(SLW_EINVAL, "null workspace");
+        if (reinterpret_cast<uintptr_t>(ws) % 16) return fail(SLW_EINVAL, "the workspace must be 16-byte aligned");
+        if (ws_bytes < L.part.end)
+            return fail(SLW_ENOMEM, "the workspace holds %zu bytes, this batch needs %zu", ws_bytes, L.part.end);
+        if (s) {
+            hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+            HIP_TRY(hipStreamIsCapturing(s, &st));
+            if (st != hipStreamCaptureStatusNone)
+                return fail(SLW_EINVAL, "a batch is handed over outside a capture: its metadata is uploaded once");
+        }
+        if ((rc = ensure_hip(ctx))) return rc;
+        KvManager::Undo undo;
+        if ((rc = ctx->kv.reserve_all(req, &undo))) return rc;
+        plan->part = L.part;
+        auto upload = [&]() -> int {
+            std::vector<int32_t>& m = ctx->meta;
+            m.clear();
+            int r = build_attn_meta(ctx, batch, m, plan->am);
+            if (r) return r;
+            if (m.size() * 4 > L.meta_bytes) return fail(SLW_EINVAL, "internal: metadata %zu ints above its region", m.size());
+            int32_t* stage = nullptr;
+            int slot = 0;
+            if ((r = next_staging(ctx, m.size(), &stage, &slot))) return r;
+            std::memcpy(stage, m.data(), m.size() * 4);
+            launch_iteration_setup(ws, ctx->staging_dev[slot], m.size(), nullptr, nullptr, 0, ctx->cfg.head_dim, 1.0,
+                                   nullptr, nullptr, nullptr, 0, 0.f, s);
+            HIP_TRY(hipGetLastError());
+            HIP_TRY(hipEventRecord(ctx->staged[slot], s));
+            return SLW_OK;
+        };
+        if ((rc = upload())) {
+            ctx->kv.rollback(undo);
+            return rc;
+        }
+        *out = plan.release();
+        return SLW_OK;
+    });
+}
+
+extern "C" int slw_attn_append(slw_ctx* ctx, const slw_attn* plan, int32_t layer, const void* k, const void* v,
+                               int64_t ld, void* stream) {
+    return guarded([&] {
+        int rc = check_attn(ctx, plan, layer);
+        if (rc) return rc;
+        if (plan->am.n_app == 0) return SLW_OK;
+        const int64_t width = static_cast<int64_t>(ctx->cfg.n_kv_heads) * ctx->cfg.head_dim;
+        if ((rc = check_rows(k, ld, width, "k")) || (rc = check_rows(v, ld, width, "v"))) return rc;
+        launch_cache_append(append_args(ctx, plan->am, reinterpret_cast<const int32_t*>(plan->ws), layer, k, v,
+                                        static_cast<int>(ld)), static_cast<hipStream_t>(stream));
+        HIP_TRY(hipGetLastError());
+        return SLW_OK;
+    });
+}
+
+extern "C" int slw_attn_attend(slw_ctx* ctx, const slw_attn* plan, int32_t layer, const void* q, int64_t ld,
+                               void* out, void* stream) {
+    return guarded([&] {
+        int rc = check_attn(ctx, plan, layer);
+        if (rc) return rc;
+        if (plan->am.C + plan->am.B == 0) return SLW_OK;
+        const int64_t width = static_cast<int64_t>(ctx->cfg.n_q_heads) * ctx->cfg.head_dim;
+        if ((rc = check_rows(q, ld, width, "q")) || (rc = check_rows(out, width, width, "out"))) return rc;
+        hipStream_t s = static_cast<hipStream_t>(stream);
+        const AttnCall attention(ctx, plan->am, reinterpret_cast<const int32_t*>(plan->ws), plan->ws, plan->part, layer,
+                                 q, static_cast<int>(ld), out);
+        attention.both(s);
+        attention.merge(s);
+        HIP_TRY(hipGetLastError());
+        return SLW_OK;
+    });
+}
+
+extern "C" int slw_attn_end(slw_attn* plan) {
+    delete plan;
+    return SLW_OK;
 }
 
 extern "C" int slw_kv_free_blocks(slw_ctx* ctx, int32_t* n_free) {
@@ -1007,7 +1131,7 @@ extern "C" int slw_workspace_size(slw_ctx* ctx, int32_t max_C, int32_t max_B, si
         // narrow kernel's, which has no partials), and partials grow with the rows
         const int rows = max_C + max_B;
         for (int m = 32; m < rows + 32; m += 32) gp = std::max(gp, plan_layer(ctx->cfg, std::min(m, rows)).partial_bytes());
-        *bytes = layout(ctx->cfg, max_C, max_B).end_fixed + gp;
+        *bytes = layout(*ctx, max_C, max_B).end_fixed + gp;
         return SLW_OK;
     });
 }
@@ -1017,7 +1141,7 @@ extern "C" int slw_workspace_view(slw_ctx* ctx, int32_t which, int32_t C, int32_
     if (!ctx || !offset || !bytes) return fail(SLW_EINVAL, "null argument");
     if (C < 0 || B < 0) return fail(SLW_EINVAL, "negative size");
     const slw_model_cfg& c = ctx->cfg;
-    const Layout L = layout(c, C, B);
+    const Layout L = layout(*ctx, C, B);
     const size_t M = static_cast<size_t>(C) + B;
     switch (which) {
         case SLW_VIEW_QKV: *offset = L.qkv; *bytes = M * qkv_width(c) * 2; break;

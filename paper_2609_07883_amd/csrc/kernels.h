@@ -126,6 +126,45 @@ void launch_attention(const ChunkAttnArgs& ca, const DecodeAttnArgs& da, hipStre
 // decode (da may be null or have b = 0).
 void launch_attention_merge(const ChunkAttnArgs* ca, const DecodeAttnArgs* da, hipStream_t s);
 
+// The cache operators beside the full bf16 ones above: attention over a paged
+// cache in bf16 or e4m3, with an optional window, and the append that fills
+// either cache.
+//
+// A layer's e4m3 pages hold the codes of 16 tokens, k_pool
+// [blocks][hkv][hd/64][16][64] and v_pool [blocks][hkv][hd][16], their values
+// scaled by k_scale / v_scale [blocks][hkv], powers of two.
+struct CacheLayer {
+    void* k_pool;
+    void* v_pool;
+    float* k_scale;  // null: a bf16 cache (layouts as above)
+    float* v_scale;
+    int hkv, hd;
+};
+// Append rows: item i takes n[i] rows from row0[i] on into tokens t0[i] .. of
+// block blk[i]; a block has one item.
+struct AppendArgs {
+    CacheLayer cache;
+    const void* k;         // bf16 [rows][hkv * hd], row stride ld
+    const void* v;
+    const int32_t* items;  // [4][n_items]: blk, t0, n, row0
+    int n_items, ld;
+};
+void launch_cache_append(const AppendArgs& a, hipStream_t s);
+// Both attentions; item key ranges are virtual (attn_plan.h): sink_end and a
+// decode's skip (or a query tile's qt_skip) map them to keys.  The pools in
+// `chunk` and `decode` are the cache's.
+struct CacheAttnArgs {
+    ChunkAttnArgs chunk;
+    DecodeAttnArgs decode;
+    const float* k_scale;    // null: a bf16 cache
+    const float* v_scale;
+    const int32_t* qt_skip;  // [n_qt]
+    const int32_t* skip;     // [b]
+    int window;              // 0: every earlier key
+    int sinks, sink_end;
+};
+void launch_cache_attention(const CacheAttnArgs& a, hipStream_t s);
+
 // One kernel: copy `words` 32-bit words from coherent, mapped host memory
 // (its device address; both pointers 16-byte aligned) to device memory, fill
 // the RoPE table: cs[r][i] = (cos, sin) of pos_host[r] * theta^(-2i/hd),

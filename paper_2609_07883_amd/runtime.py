@@ -88,12 +88,33 @@ def read_pages(k_pool: torch.Tensor, v_pool: torch.Tensor, blk: np.ndarray, tok:
     return k, v
 
 
+def read_pages_8bit(k_pool: torch.Tensor, v_pool: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                    blk: np.ndarray, tok: np.ndarray):
+    """(K, V) float64 [n][Hkv][hd]: the values at token tok[i] of block blk[i]
+    of one layer's 8-bit pools, k_pool [blocks][Hkv][hd/64][16][64] and v_pool
+    [blocks][Hkv][hd][16] (float8_e4m3fn), scales [blocks][Hkv]."""
+    b, t = np.asarray(blk, dtype=np.int64), np.asarray(tok, dtype=np.int64)
+    ids, at = np.unique(b, return_inverse=True)
+    sel = torch.from_numpy(ids).to(k_pool.device)
+    k, v = (p.view(torch.uint8)[sel].cpu().view(torch.float8_e4m3fn).float().double().numpy() for p in (k_pool, v_pool))
+    ks, vs = (s[sel].cpu().double().numpy() for s in (k_scale, v_scale))
+    hkv = k.shape[1]
+    k = k[at, :, :, t].reshape(len(b), hkv, -1) * ks[at][:, :, None]
+    v = v[at, :, :, t] * vs[at][:, :, None]
+    return k, v
+
+
 class Session:
     """One context with its device buffers for iterations up to (max_c, max_b)."""
 
     def __init__(self, shape: synth.ModelShape, num_blocks: int, max_c: int, max_b: int,
-                 layers=None, weight_seed: int = 0, qk_std=None, device_weights: bool = False):
-        """device_weights draws the weights on the GPU (the library's Philox
+                 layers=None, weight_seed: int = 0, qk_std=None, device_weights: bool = False,
+                 kv: str = "bf16", window: int = 0, sinks: int = 0, window_layers=None):
+        """kv: the cache's type, "bf16" or "e4m3" (8 bits, with scales).  window,
+        sinks, window_layers: sliding-window attention of the flagged layers
+        (None: all), see ``api.Context.set_window``.
+
+        device_weights draws the weights on the GPU (the library's Philox
         generator, seeds derived from weight_seed + 1000 * layer; N(0, 0.02)
         matrices, 1 + N(0, 0.02) gains) instead of the host recipe of
         ``synth.layer_weights``: for deep stacks whose outputs are timed but
@@ -103,11 +124,22 @@ class Session:
         self.ctx = api.Context.from_shape(shape)
         self.num_blocks = num_blocks
         s = shape
-        self.k_pool = torch.zeros((s.n_layers, num_blocks, s.n_kv_heads, s.head_dim // 32, 16, 32),
-                                  dtype=torch.bfloat16, device=self.dev)
+        if kv not in ("bf16", "e4m3"):
+            raise ValueError(f"kv must be 'bf16' or 'e4m3', not {kv!r}")
+        self.kv = kv
+        dtype, wide = (torch.bfloat16, 32) if kv == "bf16" else (torch.float8_e4m3fn, 64)
+        self.k_pool = torch.zeros((s.n_layers, num_blocks, s.n_kv_heads, s.head_dim // wide, 16, wide),
+                                  dtype=dtype, device=self.dev)
         self.v_pool = torch.zeros((s.n_layers, num_blocks, s.n_kv_heads, s.head_dim, 16),
-                                  dtype=torch.bfloat16, device=self.dev)
-        self.ctx.kv_init(self.k_pool.data_ptr(), self.v_pool.data_ptr(), num_blocks)
+                                  dtype=dtype, device=self.dev)
+        if kv == "bf16":
+            self.ctx.kv_init(self.k_pool.data_ptr(), self.v_pool.data_ptr(), num_blocks)
+        else:
+            self.k_scale = torch.ones((s.n_layers, num_blocks, s.n_kv_heads), dtype=torch.float32, device=self.dev)
+            self.v_scale = torch.ones_like(self.k_scale)
+            self.ctx.kv_init_8bit(self.k_pool.data_ptr(), self.v_pool.data_ptr(), self.k_scale.data_ptr(),
+                                  self.v_scale.data_ptr(), num_blocks)
+        self.ctx.set_window(window, sinks, window_layers)
         self.weights = []
         self.layer_bits = []
         for layer in range(s.n_layers):
@@ -181,7 +213,9 @@ class Session:
         return bt[pos // 16], pos % 16
 
     def write_kv(self, layer: int, sid: int, k_bits: np.ndarray, v_bits: np.ndarray, start: int = 0):
-        """Install K/V (uint16 [n][Hkv][hd]) at positions start..start+n-1 of sequence sid."""
+        """Install K/V (uint16 [n][Hkv][hd]) at positions start..start+n-1 of sequence sid (bf16 pools)."""
+        if self.kv != "bf16":
+            raise ValueError("the 8-bit cache is filled by appends")
         blk, tok = self._pages(sid, np.arange(start, start + k_bits.shape[0]))
         write_pages(self.k_pool[layer], self.v_pool[layer], blk, tok, k_bits, v_bits)
 
@@ -189,5 +223,8 @@ class Session:
         """(K, V) float64 [n][Hkv][hd] at the given positions of sequence sid."""
         torch.cuda.synchronize(self.dev)
         blk, tok = self._pages(sid, positions)
+        if self.kv != "bf16":
+            return read_pages_8bit(self.k_pool[layer], self.v_pool[layer], self.k_scale[layer], self.v_scale[layer],
+                                   blk, tok)
         k, v = read_pages(self.k_pool[layer], self.v_pool[layer], blk, tok)
         return synth.bf16_to_f64(k), synth.bf16_to_f64(v)
