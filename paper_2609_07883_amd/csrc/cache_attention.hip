@@ -75,14 +75,11 @@ __device__ __forceinline__ void cache_load(CacheStep<Q8, HD>& st, const CacheAtt
                                            int last_pg, int kvh, int col, int grp) {
     constexpr int PAGES = Q8 ? 4 : 2, PB = HD * 16 * (Q8 ? 1 : 2);  // pages of a step, bytes of a page
     const int pg0 = k0 >> 4;
-    int b[PAGES];
-#pragma unroll
-    for (int p = 0; p < PAGES; ++p) b[p] = bt_s[min(pg0 + p, last_pg)];
+    const int b0 = bt_s[min(pg0, last_pg)], b1 = bt_s[min(pg0 + 1, last_pg)];
+    const int b2 = PAGES == 4 ? bt_s[min(pg0 + 2, last_pg)] : 0, b3 = PAGES == 4 ? bt_s[min(pg0 + 3, last_pg)] : 0;
     auto pick = [&](int i) {
-        int r = b[0];
-#pragma unroll
-        for (int p = 1; p < PAGES; ++p) r = i == p ? b[p] : r;
-        return r;
+        const int lo = i & 1 ? b1 : b0, hi = i & 1 ? b3 : b2;
+        return PAGES == 4 && (i & 2) ? hi : lo;
     };
     const uint8_t* kpool = static_cast<const uint8_t*>(a.decode.k_pool);
     const uint8_t* vpool = static_cast<const uint8_t*>(a.decode.v_pool);
@@ -264,327 +261,258 @@ __global__ __launch_bounds__(64, 2) void cache_decode_kernel(CacheAttnArgs a) {
 // ---------------------------------------------------------------------------
 // Chunk attention: the rows of a query tile (256 / GROUP positions of one
 // prompt, GROUP q heads of one kv head) against its keys, 64 at a time, as in
-// the bf16 kernel: eight waves of 32 rows, K and V tiles in bf16 in LDS.
+// the bf16 kernels: eight waves of 32 rows, K and V tiles in bf16 in LDS.
 //
 // Tiles go through registers on their way to LDS, since e4m3 pages are widened
-// there, once per work-group instead of once per wave: the next tile's loads
-// are in flight while the current one is multiplied, and are widened and
-// written to the other of two buffers after it.
+// there, once per work-group instead of once per wave.
 //
 // A key that some rows of a wave see and others do not stays out of the
-// others' products through a zero probability, unless its V row is not
-// finite (0 times it would be NaN).  The waves say for each tile on an edge of
-// the mask whether they wrote such a value; a tile that has one takes a path
-// that multiplies the finite values alone, and adds what rows that see the
-// others get from them, counted with products of visibility and class.
+// others' products through a zero probability, unless its V row is not finite
+// (0 times it would be NaN).  The kernels watch for such values as they write
+// V to LDS; an item that met one is computed again by exact_item, which keeps
+// them apart.
 // ---------------------------------------------------------------------------
-template <bool Q8, int HD, int GROUP>
-__global__ __launch_bounds__(512) void cache_chunk_kernel(CacheAttnArgs a) {
-    const ChunkAttnArgs& c = a.chunk;
-    {   // decode waves behind the chunk work-groups, as in the bf16 kernel
-        const int n_chunk = c.n_slots * c.hkv;
-        if (static_cast<int>(blockIdx.x) >= n_chunk) {
-            const int v = (static_cast<int>(blockIdx.x) - n_chunk) * 8 +
-                          __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-            if (v < a.decode.n_slots * a.decode.hkv)
-                cache_decode_wave<Q8, HD>(a, v % a.decode.n_slots, v / a.decode.n_slots, threadIdx.x & 63);
-            return;
+
+// One work item of a work-group, and the wave's share of it.
+struct Item {
+    const const_i32* bt;
+    int item, row0, nrows, pos0, skip, v0, n_tiles;
+    int key_end, last_page;
+    int j0, lo, hi;         // the wave's first tile position, first and last sequence position
+    int window, sinks, sink_end;
+    bool live, whole;
+
+    __device__ __forceinline__ Item(const CacheAttnArgs& a, int index, int wave, int pw) {
+        const ChunkAttnArgs& c = a.chunk;
+        item = index;
+        const int qt = c.item_qt[item];
+        v0 = c.item_kb[item];
+        n_tiles = (c.item_ke[item] - v0 + 63) / 64;
+        row0 = c.qt_row0[qt];
+        nrows = c.qt_rows[qt];
+        pos0 = c.qt_pos0[qt];
+        skip = a.qt_skip[qt];
+        bt = (const const_i32*)(c.bt + c.qt_bt[qt]);
+        key_end = pos0 + nrows;
+        last_page = (key_end - 1) >> 4;
+        j0 = wave * pw;
+        lo = pos0 + j0;
+        hi = lo + pw - 1;
+        live = j0 < nrows;
+        whole = c.qt_off[qt + 1] - c.qt_off[qt] == 1;
+        window = a.window > 0 ? a.window : 0x7FFFFFFF;
+        sinks = a.sinks;
+        sink_end = a.sink_end;
+    }
+    __device__ __forceinline__ int key0(int t) const {
+        const int v = v0 + 64 * t;
+        return v < sink_end ? v : v + skip;
+    }
+    __device__ __forceinline__ int block(int key0, int page) const {
+        return bt[__builtin_amdgcn_readfirstlane(min((key0 >> 4) + page, last_page))];
+    }
+    // the wave's rows see no key of the tile / not every key of it
+    __device__ __forceinline__ bool unseen(int key0) const {
+        return key0 > hi || (lo - window >= key0 + 63 && key0 >= sinks);
+    }
+    __device__ __forceinline__ bool masked(int key0) const {
+        return key0 + 63 > lo || (hi - window >= key0 && key0 + 63 >= sinks);
+    }
+    __device__ __forceinline__ bool sees(int qpos, int kpos) const {
+        return kpos <= qpos && (kpos < sinks || kpos > qpos - window);
+    }
+};
+
+// Where the 16-byte pieces of a tile's pages go.  A tile has 4 PP pieces of K
+// and as many of V; those that a wave moves at once lie in one page.
+template <bool Q8, int HD>
+struct Pieces {
+    static constexpr int PAGE = HD * 16, PB = PAGE * (Q8 ? 1 : 2), PP = PB / 16;
+    static_assert(PP % 64 == 0, "a wave's pieces lie in one page");
+
+    // `first`: the piece's number among the K (or V) pieces, of the wave's lane 0
+    static __device__ __forceinline__ int page(int first) { return first / PP; }
+    static __device__ __forceinline__ int offset(int first, int lane) { return first % PP + lane; }
+
+    static __device__ __forceinline__ void put_k(bf16* tile, int first, int lane, u32x4 x, float scale) {
+        const int at = offset(first, lane), tok = (at & 63) >> 2;
+        bf16* base = tile + page(first) * PAGE + tok * 32;
+        if constexpr (Q8) {  // 16 dims of token tok: two of the four 8-dim pieces of a 32-dim slab
+            const int q4 = at & 3;
+            bf16* row = base + (2 * (at >> 6) + (q4 >> 1)) * 512;
+            *reinterpret_cast<bf16x8*>(row + kswz(tok, 2 * (q4 & 1)) * 8) = widen8(x[0], x[1], scale);
+            *reinterpret_cast<bf16x8*>(row + kswz(tok, 2 * (q4 & 1) + 1) * 8) = widen8(x[2], x[3], scale);
+        } else {
+            *reinterpret_cast<u32x4*>(base + (at >> 6) * 512 + kswz(tok, at & 3) * 8) = x;
         }
     }
-    constexpr int KK = HD / 32, NT = HD / 16, PAGE = HD * 16;
-    constexpr int PB = PAGE * (Q8 ? 1 : 2);     // bytes of a page
-    constexpr int HALF = 4 * PB / 16;           // 16-byte pieces of the K (or V) pages of a tile
-    constexpr int PT = 2 * HALF / 512;          // pieces a thread moves
-    constexpr int PP = PB / 16;                 // pieces of a page
-    static_assert(PT >= 1 && PP % 64 == 0, "a wave's pieces lie in one page");
-    constexpr int CT = 2, PW = 32 / GROUP;
-    __shared__ __attribute__((aligned(16))) bf16 Ks[2][4 * PAGE];
-    __shared__ __attribute__((aligned(16))) bf16 Vs[2][4 * PAGE];
-    __shared__ int odd[2][8];  // wave w wrote a V value that is not finite (edge tiles only)
-
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int grp = lane >> 4, col = lane & 15;
-    const int pos = xcd_order(blockIdx.x, c.n_slots * c.hkv);
-    const int kvh = pos / c.n_slots, slot = pos % c.n_slots;
-    const float sl2 = kLog2e / sqrtf(static_cast<float>(HD));
-    bf16x8 ones;
+    // Values of keys from key_end on (unwritten slots, stand-in pages) become
+    // 0; their scores are masked.  Nonzero result: a value is not finite.
+    static __device__ __forceinline__ uint32_t put_v(bf16* tile, int first, int lane, u32x4 x, float scale, int key0,
+                                                     int key_end) {
+        const int at = offset(first, lane);
+        if (key0 + 63 >= key_end) {
+            const int k = key0 + 16 * page(first) + (Q8 ? 0 : 8 * (at & 1));
+            const uint32_t live = low_bits(min(max(key_end - k, 0), 16));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ones[e] = bf16(1.0f);
-
-    // Piece i of a thread: piece j = 512 i + tid of the tile, K pages first.
-    auto piece = [&](int i, bool& is_v, int& page, int& at) {
-        const int j = 512 * i + wave * 64;  // wave-uniform part
-        is_v = j >= HALF;
-        const int jj = is_v ? j - HALF : j;
-        page = jj / PP;
-        at = jj % PP + lane;
-    };
-
-    const int i0 = c.slot_off[slot], i1 = c.slot_off[slot + 1];
-    for (int k = i0; k < i1; ++k) {
-        const int item = c.slot_items[k];
-        const int qt = c.item_qt[item], v0 = c.item_kb[item], v1 = c.item_ke[item];
-        const int row0 = c.qt_row0[qt], nrows = c.qt_rows[qt], pos0 = c.qt_pos0[qt], skip = a.qt_skip[qt];
-        const const_i32* bt_s = (const const_i32*)(c.bt + c.qt_bt[qt]);
-        const int key_end = pos0 + nrows, last_page = (key_end - 1) >> 4;
-        const int j0 = wave * PW;
-        const int n_tiles = (v1 - v0 + 63) / 64;
-        const int lo = pos0 + j0, hi = pos0 + j0 + PW - 1;  // the wave's positions
-        const bool wave_live = j0 < nrows;
-        const bool whole = c.qt_off[qt + 1] - c.qt_off[qt] == 1;
-        // rows at position p see sinks and keys past p - window
-        const int window = a.window > 0 ? a.window : 0x7FFFFFFF, sinks = a.sinks;
-        auto key0_of = [&](int t) {
-            const int v = v0 + 64 * t;
-            return v < a.sink_end ? v : v + skip;
-        };
-        // a key tile that some row from position p0 to p1 does not see whole
-        auto edge = [&](int key0, int p0, int p1) { return key0 + 63 > p0 || (p1 - window >= key0 && key0 + 63 >= sinks); };
-
-        bf16x8 qf[CT][KK];
-        const bf16* qkv = static_cast<const bf16*>(c.qkv);
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            const int r = ct * 16 + col, j = j0 + r / GROUP, h = kvh * GROUP + r % GROUP;
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk)
-                qf[ct][kk] = j < nrows ? *reinterpret_cast<const bf16x8*>(
-                                             qkv + static_cast<size_t>(row0 + j) * c.ld_qkv + h * HD + kk * 32 + grp * 8)
-                                       : bf16x8{};
+            for (int w = 0; w < 4; ++w) {
+                if constexpr (Q8) x[w] &= ((((live >> (4 * w)) & 0xFu) * 0x00204081u) & 0x01010101u) * 0xFFu;
+                else x[w] &= ((live >> (2 * w)) & 1u ? 0xFFFFu : 0u) | ((live >> (2 * w)) & 2u ? 0xFFFF0000u : 0u);
+            }
         }
+        uint32_t odd = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {  // an all-ones magnitude (exponent) carries into the sign
+            if constexpr (Q8) odd |= ((x[w] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+            else odd |= ((x[w] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+        }
+        bf16* base = tile + page(first) * PAGE;
+        if constexpr (Q8) {
+            *reinterpret_cast<bf16x8*>(base + at * 16 + vswz(at, 0) * 8) = widen8(x[0], x[1], scale);
+            *reinterpret_cast<bf16x8*>(base + at * 16 + vswz(at, 1) * 8) = widen8(x[2], x[3], scale);
+        } else {
+            const int d = at >> 1;
+            *reinterpret_cast<u32x4*>(base + d * 16 + vswz(d, at & 1) * 8) = x;
+        }
+        return odd;
+    }
+};
 
-        u32x4 raw[PT];
-        float rscale[PT];
-        auto load = [&](int t) {
-            const int pg0 = key0_of(t) >> 4;
-#pragma unroll
-            for (int i = 0; i < PT; ++i) {
-                bool is_v;
-                int page, at;
-                piece(i, is_v, page, at);
-                const size_t bh = static_cast<size_t>(bt_s[min(pg0 + page, last_page)]) * c.hkv + kvh;
-                raw[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(is_v ? c.v_pool : c.k_pool) + bh * PB + at * 16);
-                if constexpr (Q8) rscale[i] = ((const const_f32*)(is_v ? a.v_scale : a.k_scale))[bh];
-            }
-        };
-        // Widen and write a tile.  V values of keys past the sequence's end
-        // (unwritten slots, stand-in pages) become 0; their scores are masked.
-        auto store = [&](int t) {
-            const int key0 = key0_of(t), buf = t & 1;
-            bool bad = false;
-#pragma unroll
-            for (int i = 0; i < PT; ++i) {
-                bool is_v;
-                int page, at;
-                piece(i, is_v, page, at);
-                u32x4 x = raw[i];
-                if (is_v && key0 + 63 >= key_end) {
-                    const int first = key0 + 16 * page + (Q8 ? 0 : 8 * (at & 1));
-                    const uint32_t live = low_bits(min(max(key_end - first, 0), 16));
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        if constexpr (Q8) x[w] &= ((((live >> (4 * w)) & 0xFu) * 0x00204081u) & 0x01010101u) * 0xFFu;
-                        else x[w] &= ((live >> (2 * w)) & 1u ? 0xFFFFu : 0u) | ((live >> (2 * w)) & 2u ? 0xFFFF0000u : 0u);
-                    }
-                }
-                if (is_v) {
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        if constexpr (Q8) {
-                            bad |= (((x[w] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0u;
-                        } else {
-                            bad |= (x[w] & 0x7F80u) == 0x7F80u || (x[w] & 0x7F800000u) == 0x7F800000u;
-                        }
-                    }
-                }
-                bf16* base = &(is_v ? Vs : Ks)[buf][page * PAGE];
-                if constexpr (Q8) {
-                    const bf16x8 y0 = widen8(x[0], x[1], rscale[i]), y1 = widen8(x[2], x[3], rscale[i]);
-                    if (is_v) {
-                        *reinterpret_cast<bf16x8*>(base + at * 16 + vswz(at, 0) * 8) = y0;
-                        *reinterpret_cast<bf16x8*>(base + at * 16 + vswz(at, 1) * 8) = y1;
-                    } else {  // 16 dims of token tok: two of the four 8-dim pieces of a 32-dim slab
-                        const int tok = (at & 63) >> 2, q4 = at & 3;
-                        bf16* row = base + (2 * (at >> 6) + (q4 >> 1)) * 512 + tok * 32;
-                        *reinterpret_cast<bf16x8*>(row + kswz(tok, 2 * (q4 & 1)) * 8) = y0;
-                        *reinterpret_cast<bf16x8*>(row + kswz(tok, 2 * (q4 & 1) + 1) * 8) = y1;
-                    }
-                } else if (is_v) {
-                    const int d = at >> 1;
-                    *reinterpret_cast<u32x4*>(base + d * 16 + vswz(d, at & 1) * 8) = x;
-                } else {
-                    const int tok = (at & 63) >> 2;
-                    *reinterpret_cast<u32x4*>(base + (at >> 6) * 512 + tok * 32 + kswz(tok, at & 3) * 8) = x;
-                }
-            }
-            const int any = __any(bad);
-            if (lane == 0) odd[buf][wave] = any;
-        };
+// A tile on its way through a work-group's registers.
+template <bool Q8, int HD>
+struct Staged {
+    using P = Pieces<Q8, HD>;
+    static constexpr int HALF = 4 * P::PP, PT = 2 * HALF / 512;  // pieces of K (or V); pieces a thread moves
+    u32x4 raw[PT];
+    float scale[PT];
 
-        f32x4 o[CT][NT], l_acc[CT];
-        float m_run[CT];
-        int qpos[CT];  // position of row ct * 16 + col
+    __device__ __forceinline__ void load(const CacheAttnArgs& a, const Item& it, int kvh, int wave, int lane, int t) {
+        const int key0 = it.key0(t);
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
+        for (int i = 0; i < PT; ++i) {
+            const int j = 512 * i + 64 * wave;
+            const bool is_v = j >= HALF;
+            const int first = is_v ? j - HALF : j;
+            const size_t bh = static_cast<size_t>(it.block(key0, P::page(first))) * a.chunk.hkv + kvh;
+            const void* pool = is_v ? a.chunk.v_pool : a.chunk.k_pool;
+            raw[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(pool) + bh * P::PB + P::offset(first, lane) * 16);
+            if constexpr (Q8) scale[i] = ((const const_f32*)(is_v ? a.v_scale : a.k_scale))[bh];
+        }
+    }
+    __device__ __forceinline__ uint32_t store(bf16* ks, bf16* vs, const Item& it, int wave, int lane, int t) const {
+        uint32_t odd = 0;
+#pragma unroll
+        for (int i = 0; i < PT; ++i) {
+            const int j = 512 * i + 64 * wave;
+            if (j >= HALF) odd |= P::put_v(vs, j - HALF, lane, raw[i], scale[i], it.key0(t), it.key_end);
+            else P::put_k(ks, j, lane, raw[i], scale[i]);
+        }
+        return odd;
+    }
+};
+
+// Q^T operand: row r = ct * 16 + col is tile position j0 + r / GROUP, head kvh * GROUP + r % GROUP.
+template <int HD, int GROUP>
+__device__ __forceinline__ void load_q(bf16x8 (&qf)[2][HD / 32], const ChunkAttnArgs& c, const Item& it, int kvh, int col,
+                                       int grp) {
+    const bf16* q = static_cast<const bf16*>(c.qkv);
+#pragma unroll
+    for (int ct = 0; ct < 2; ++ct) {
+        const int r = ct * 16 + col, j = it.j0 + r / GROUP, h = kvh * GROUP + r % GROUP;
+#pragma unroll
+        for (int kk = 0; kk < HD / 32; ++kk)
+            qf[ct][kk] = j < it.nrows ? *reinterpret_cast<const bf16x8*>(
+                                            q + static_cast<size_t>(it.row0 + j) * c.ld_qkv + h * HD + kk * 32 + grp * 8)
+                                      : bf16x8{};
+    }
+}
+
+// A wave's rows of an item, in registers: running maximum of row ct * 16 + col,
+// row sums and outputs of rows ct * 16 + 4 grp + e, NT 16-dim tiles of them.
+template <int HD, int NT = HD / 16>
+struct Rows {
+    f32x4 o[2][NT], l[2];
+    float m[2];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int ct = 0; ct < 2; ++ct) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) o[ct][nt] = f32x4{};
-            l_acc[ct] = f32x4{};
-            m_run[ct] = -INFINITY;
-            qpos[ct] = lo + (ct * 16 + col) / GROUP;
+            l[ct] = f32x4{};
+            m[ct] = -INFINITY;
         }
-        auto sees = [&](int kpos, int ct) { return kpos <= qpos[ct] && (kpos < sinks || kpos > qpos[ct] - window); };
-
-        load(0);
-        store(0);
-        wait_lgkmcnt0();
-        barrier_only();
-        for (int t = 0; t < n_tiles; ++t) {
-            const int buf = t & 1, key0 = key0_of(t);
-            if (t + 1 < n_tiles) load(t + 1);
-            // tiles that lie past the wave's rows, or before all their windows
-            const bool skipped = !wave_live || key0 > hi || (lo - window >= key0 + 63 && key0 >= sinks);
-            if (!skipped) {
-                const bool masked = edge(key0, lo, hi);
-                f32x4 sc[4][CT];  // [2 pair + tile][ct]
+    }
+    // Scores of a tile, masked, to probabilities against the running maximum.
+    template <int GROUP>
+    __device__ __forceinline__ void softmax(f32x4 (&sc)[4][2], bf16x8 (&pf)[2][2], const Item& it, int key0, float sl2,
+                                            int col, int grp) {
+        if (it.masked(key0)) {
 #pragma unroll
-                for (int p = 0; p < 4; ++p) {
+            for (int p = 0; p < 4; ++p)
 #pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) sc[p][ct] = f32x4{};
-                    const int key = pair_key(col, p & 1), tok = key & 15;
-                    const int base = (2 * (p >> 1) + (key >> 4)) * PAGE + tok * 32 + kswz(tok, grp) * 8;
+                for (int e = 0; e < 4; ++e) {
+                    const int kpos = key0 + 32 * (p >> 1) + pair_key(4 * grp + e, p & 1);
 #pragma unroll
-                    for (int kk = 0; kk < KK; ++kk) {
-                        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(&Ks[buf][base + kk * 512]);
-#pragma unroll
-                        for (int ct = 0; ct < CT; ++ct) sc[p][ct] = mfma16(kf, qf[ct][kk], sc[p][ct]);
-                    }
+                    for (int ct = 0; ct < 2; ++ct)
+                        sc[p][ct][e] = it.sees(it.lo + (ct * 16 + col) / GROUP, kpos) ? sc[p][ct][e] : -INFINITY;
                 }
-                if (masked) {
+        }
+        float mx[2];
+        bool grow = false;
 #pragma unroll
-                    for (int p = 0; p < 4; ++p)
+        for (int ct = 0; ct < 2; ++ct) {
+            float x = -INFINITY;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int kpos = key0 + 32 * (p >> 1) + pair_key(4 * grp + e, p & 1);
+            for (int p = 0; p < 4; ++p)
 #pragma unroll
-                            for (int ct = 0; ct < CT; ++ct) sc[p][ct][e] = sees(kpos, ct) ? sc[p][ct][e] : -INFINITY;
-                        }
-                }
-                float mx[CT];
-                bool grow = false;
+                for (int e = 0; e < 4; ++e) x = fmaxf(x, sc[p][ct][e]);
+            mx[ct] = rows4_max(x) * sl2;
+            grow |= mx[ct] > m[ct] + kSlack;
+        }
+        if (__any(grow)) {
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    float m = -INFINITY;
+            for (int ct = 0; ct < 2; ++ct) {
+                const float m_new = fmaxf(m[ct], mx[ct]);
+                const float alpha = m_new == -INFINITY ? 1.f : fast_exp2(m[ct] - m_new);
+                m[ct] = m_new;
 #pragma unroll
-                    for (int p = 0; p < 4; ++p)
+                for (int e = 0; e < 4; ++e) {
+                    const float ae = __shfl(alpha, grp * 4 + e, 64);
+                    l[ct][e] *= ae;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) m = fmaxf(m, sc[p][ct][e]);
-                    mx[ct] = rows4_max(m) * sl2;
-                    grow |= mx[ct] > m_run[ct] + kSlack;
-                }
-                if (__any(grow)) {
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) {
-                        const float m_new = fmaxf(m_run[ct], mx[ct]);
-                        const float alpha = m_new == -INFINITY ? 1.f : fast_exp2(m_run[ct] - m_new);
-                        m_run[ct] = m_new;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float ae = __shfl(alpha, grp * 4 + e, 64);
-                            l_acc[ct][e] *= ae;
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) o[ct][nt][e] *= ae;
-                        }
-                    }
-                }
-                bf16x8 pf[2][CT];
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    const float m_use = m_run[ct] == -INFINITY ? 0.f : m_run[ct];
-#pragma unroll
-                    for (int p = 0; p < 4; ++p)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) sc[p][ct][e] = fast_exp2(fmaf(sc[p][ct][e], sl2, -m_use));
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) pf[j][ct] = to_bf16x8(sc[2 * j][ct], sc[2 * j + 1][ct]);
-                }
-                int any_odd = 0;
-                if (masked) {
-#pragma unroll
-                    for (int w = 0; w < 8; ++w) any_odd |= odd[buf][w];
-                    any_odd = __builtin_amdgcn_readfirstlane(any_odd);
-                }
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) l_acc[ct] = mfma16(pf[j][ct], ones, l_acc[ct]);
-                    bf16x8 vis[CT];
-                    if (any_odd) {
-#pragma unroll
-                        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                vis[ct][e] = bf16(sees(key0 + 32 * j + pair_key(4 * grp + (e & 3), e >> 2), ct) ? 1.0f : 0.0f);
-                    }
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const int d = nt * 16 + col;
-                        bf16x8 vf = *reinterpret_cast<const bf16x8*>(
-                            &Vs[buf][(2 * j + (grp >> 1)) * PAGE + d * 16 + vswz(d, grp & 1) * 8]);
-                        if (any_odd) {
-                            u32x4 bits = __builtin_bit_cast(u32x4, vf), pinf = {}, ninf = {}, nan = {};
-#pragma unroll
-                            for (int w = 0; w < 4; ++w)
-#pragma unroll
-                                for (int h = 0; h < 2; ++h) {
-                                    const uint32_t x = (bits[w] >> (16 * h)) & 0xFFFFu, one = 0x3F80u << (16 * h);
-                                    if ((x & 0x7F80u) != 0x7F80u) continue;
-                                    if (x == 0x7F80u) pinf[w] |= one;
-                                    else if (x == 0xFF80u) ninf[w] |= one;
-                                    else nan[w] |= one;
-                                    bits[w] &= ~(0xFFFFu << (16 * h));
-                                }
-                            vf = __builtin_bit_cast(bf16x8, bits);
-#pragma unroll
-                            for (int ct = 0; ct < CT; ++ct) {
-                                const f32x4 np = mfma16(vis[ct], __builtin_bit_cast(bf16x8, pinf), f32x4{});
-                                const f32x4 nn = mfma16(vis[ct], __builtin_bit_cast(bf16x8, ninf), f32x4{});
-                                const f32x4 nx = mfma16(vis[ct], __builtin_bit_cast(bf16x8, nan), f32x4{});
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    if (np[e] > 0.f) o[ct][nt][e] += INFINITY;
-                                    if (nn[e] > 0.f) o[ct][nt][e] -= INFINITY;
-                                    if (nx[e] > 0.f) o[ct][nt][e] = NAN;
-                                }
-                            }
-                        }
-#pragma unroll
-                        for (int ct = 0; ct < CT; ++ct) o[ct][nt] = mfma16(pf[j][ct], vf, o[ct][nt]);
-                    }
+                    for (int nt = 0; nt < NT; ++nt) o[ct][nt][e] *= ae;
                 }
             }
-            if (t + 1 < n_tiles) store(t + 1);
-            wait_lgkmcnt0();
-            barrier_only();
         }
-        if (!wave_live) continue;
-
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            if (!whole) {
-                const size_t rbase = (static_cast<size_t>(item) * c.hkv + kvh) * 256 + wave * 32 + ct * 16;
+        for (int ct = 0; ct < 2; ++ct) {
+            const float m_use = m[ct] == -INFINITY ? 0.f : m[ct];
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[p][ct][e] = fast_exp2(fmaf(sc[p][ct][e], sl2, -m_use));
+#pragma unroll
+            for (int j = 0; j < 2; ++j) pf[j][ct] = to_bf16x8(sc[2 * j][ct], sc[2 * j + 1][ct]);
+        }
+    }
+    // Normalised rows, or the item's partial sums, from dim d0 on.
+    template <int GROUP>
+    __device__ __forceinline__ void write(const ChunkAttnArgs& c, const Item& it, int kvh, int wave, int col, int grp,
+                                          int d0 = 0) const {
+#pragma unroll
+        for (int ct = 0; ct < 2; ++ct) {
+            if (!it.whole) {
+                const size_t rbase = (static_cast<size_t>(it.item) * c.hkv + kvh) * 256 + wave * 32 + ct * 16;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     // the maximum of row 4 grp + e sits in column 4 grp + e
-                    float m = __shfl(m_run[ct], grp * 4 + e, 64);
-                    const float l = l_acc[ct][e];
-                    m = m == -INFINITY && l != l ? 0.f : m;  // as in the decode kernel
-                    if (col == 0) {
-                        c.part_ml[(rbase + grp * 4 + e) * 2] = m;
-                        c.part_ml[(rbase + grp * 4 + e) * 2 + 1] = l;
+                    const float x = __shfl(m[ct], grp * 4 + e, 64), s = l[ct][e];
+                    if (col == 0) {  // a part of NaN scores alone, as in the decode kernel
+                        c.part_ml[(rbase + grp * 4 + e) * 2] = x == -INFINITY && s != s ? 0.f : x;
+                        c.part_ml[(rbase + grp * 4 + e) * 2 + 1] = s;
                     }
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-                        c.part_o[(rbase + grp * 4 + e) * HD + nt * 16 + col] = o[ct][nt][e];
+                    for (int nt = 0; nt < NT; ++nt) c.part_o[(rbase + grp * 4 + e) * HD + d0 + nt * 16 + col] = o[ct][nt][e];
                 }
             } else {
                 bf16* out = static_cast<bf16*>(c.out);
@@ -592,16 +520,273 @@ __global__ __launch_bounds__(512) void cache_chunk_kernel(CacheAttnArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int r = ct * 16 + grp * 4 + e;
-                    const int j = j0 + r / GROUP, h = kvh * GROUP + r % GROUP;
-                    const float inv = 1.0f / l_acc[ct][e];
-                    if (j < nrows) {
+                    const int j = it.j0 + r / GROUP, h = kvh * GROUP + r % GROUP;
+                    const float inv = 1.0f / l[ct][e];
+                    if (j < it.nrows) {
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
-                            out[static_cast<size_t>(row0 + j) * ldo + h * HD + nt * 16 + col] = f2bf(o[ct][nt][e] * inv);
+                            out[static_cast<size_t>(it.row0 + j) * ldo + h * HD + d0 + nt * 16 + col] = f2bf(o[ct][nt][e] * inv);
                     }
                 }
             }
         }
+    }
+};
+
+__device__ __forceinline__ bf16x8 ones8() {
+    bf16x8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = bf16(1.0f);
+    return r;
+}
+
+// An item whose V holds values that are not finite: the finite ones are
+// multiplied alone, and rows that see one of the others get what it makes of
+// their sums (counted by products of visibility and class).  Rare, so it is
+// built for few registers, beside the loop that it stands in for: 32 output
+// dims at a time, scores and all.
+template <bool Q8, int HD, int GROUP>
+__device__ __forceinline__ void exact_item(const CacheAttnArgs& a, const Item& it, int kvh, bf16* ks, bf16* vs, float sl2) {
+    constexpr int KK = HD / 32, NT = 2, PAGE = HD * 16, CT = 2;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));  // keeps what follows from it out of the loop that this stands in for
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int grp = lane >> 4, col = lane & 15;
+    const bf16x8 ones = ones8();
+    bf16x8 qf[CT][KK];
+    load_q<HD, GROUP>(qf, a.chunk, it, kvh, col, grp);
+#pragma unroll 1
+    for (int d0 = 0; d0 < HD; d0 += 16 * NT) {
+        Rows<HD, NT> rows;
+        rows.clear();
+#pragma unroll 1
+        for (int t = 0; t < it.n_tiles; ++t) {
+            const int key0 = it.key0(t);
+            barrier_only();
+            {
+                Staged<Q8, HD> st;
+                st.load(a, it, kvh, wave, lane, t);
+                st.store(ks, vs, it, wave, lane, t);
+            }
+            wait_lgkmcnt0();
+            barrier_only();
+            if (!it.live || it.unseen(key0)) continue;
+            f32x4 sc[4][CT];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) sc[p][ct] = f32x4{};
+                const int key = pair_key(col, p & 1), tok = key & 15;
+                const int base = (2 * (p >> 1) + (key >> 4)) * PAGE + tok * 32 + kswz(tok, grp) * 8;
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    const bf16x8 kf = *reinterpret_cast<const bf16x8*>(&ks[base + kk * 512]);
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) sc[p][ct] = mfma16(kf, qf[ct][kk], sc[p][ct]);
+                }
+            }
+            bf16x8 pf[2][CT];
+            rows.template softmax<GROUP>(sc, pf, it, key0, sl2, col, grp);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                bf16x8 vis[CT];
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    rows.l[ct] = mfma16(pf[j][ct], ones, rows.l[ct]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        vis[ct][e] = bf16(it.sees(it.lo + (ct * 16 + col) / GROUP,
+                                                  key0 + 32 * j + pair_key(4 * grp + (e & 3), e >> 2)) ? 1.0f : 0.0f);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int d = d0 + nt * 16 + col;
+                    u32x4 bits = *reinterpret_cast<const u32x4*>(&vs[(2 * j + (grp >> 1)) * PAGE + d * 16 + vswz(d, grp & 1) * 8]);
+                    u32x4 pinf = {}, ninf = {}, nan = {};
+#pragma unroll
+                    for (int w = 0; w < 4; ++w)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t x = (bits[w] >> (16 * h)) & 0xFFFFu, one = 0x3F80u << (16 * h);
+                            const bool odd = (x & 0x7F80u) == 0x7F80u;
+                            pinf[w] |= x == 0x7F80u ? one : 0u;
+                            ninf[w] |= x == 0xFF80u ? one : 0u;
+                            nan[w] |= odd && (x & 0x7Fu) ? one : 0u;
+                            bits[w] &= odd ? ~(0xFFFFu << (16 * h)) : 0xFFFFFFFFu;
+                        }
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        const f32x4 np = mfma16(vis[ct], __builtin_bit_cast(bf16x8, pinf), f32x4{});
+                        const f32x4 nn = mfma16(vis[ct], __builtin_bit_cast(bf16x8, ninf), f32x4{});
+                        const f32x4 nx = mfma16(vis[ct], __builtin_bit_cast(bf16x8, nan), f32x4{});
+                        f32x4& o = rows.o[ct][nt];
+                        o = mfma16(pf[j][ct], __builtin_bit_cast(bf16x8, bits), o);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (np[e] > 0.f) o[e] += INFINITY;
+                            if (nn[e] > 0.f) o[e] -= INFINITY;
+                            if (nx[e] > 0.f) o[e] = NAN;
+                        }
+                    }
+                }
+            }
+        }
+        if (it.live) rows.template write<GROUP>(a.chunk, it, kvh, wave, col, grp, d0);
+    }
+}
+
+// Whether a wave of the work-group met a V value that is not finite: `odd` is
+// nonzero in its lanes.  Every wave is past its last tile when this returns.
+__device__ __forceinline__ bool any_odd(uint32_t odd, int* flags) {
+    const int tid = threadIdx.x;
+    const int mine = __any(odd != 0);
+    if ((tid & 63) == 0) flags[tid >> 6] = mine;
+    wait_lgkmcnt0();
+    barrier_only();
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) all |= flags[w];
+    return __builtin_amdgcn_readfirstlane(all) != 0;
+}
+
+// Decode waves behind the chunk work-groups, as in the bf16 kernel; true in a
+// work-group of theirs.
+template <bool Q8, int HD>
+__device__ __forceinline__ bool decode_group(const CacheAttnArgs& a) {
+    const int n_chunk = a.chunk.n_slots * a.chunk.hkv;
+    if (static_cast<int>(blockIdx.x) < n_chunk) return false;
+    const int v = (static_cast<int>(blockIdx.x) - n_chunk) * 8 +
+                  __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    if (v < a.decode.n_slots * a.decode.hkv)
+        cache_decode_wave<Q8, HD>(a, v % a.decode.n_slots, v / a.decode.n_slots, threadIdx.x & 63);
+    return true;
+}
+
+// Two LDS buffers: the next tile's loads are in flight while the current one
+// is multiplied, and are widened and written to the other buffer after it.
+template <bool Q8, int HD, int GROUP>
+__global__ __launch_bounds__(512) void cache_chunk_kernel(CacheAttnArgs a) {
+    const ChunkAttnArgs& c = a.chunk;
+    if (decode_group<Q8, HD>(a)) return;
+    constexpr int KK = HD / 32, NT = HD / 16, PAGE = HD * 16, CT = 2, PW = 32 / GROUP;
+    __shared__ __attribute__((aligned(16))) bf16 Ks[2][4 * PAGE];
+    __shared__ __attribute__((aligned(16))) bf16 Vs[2][4 * PAGE];
+    __shared__ int flags[8];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int grp = lane >> 4, col = lane & 15;
+    const int pos = xcd_order(blockIdx.x, c.n_slots * c.hkv);
+    const int kvh = pos / c.n_slots, slot = pos % c.n_slots;
+    const float sl2 = kLog2e / sqrtf(static_cast<float>(HD));
+    const bf16x8 ones = ones8();
+
+    const int i0 = c.slot_off[slot], i1 = c.slot_off[slot + 1];
+    for (int k = i0; k < i1; ++k) {
+        const Item it(a, c.slot_items[k], wave, PW);
+        bf16x8 qf[CT][KK];
+        load_q<HD, GROUP>(qf, c, it, kvh, col, grp);
+        Rows<HD> rows;
+        rows.clear();
+        uint32_t odd = 0;
+        Staged<Q8, HD> st;
+        st.load(a, it, kvh, wave, lane, 0);
+        odd |= st.store(Ks[0], Vs[0], it, wave, lane, 0);
+        wait_lgkmcnt0();
+        barrier_only();
+        for (int t = 0; t < it.n_tiles; ++t) {
+            const int buf = t & 1, key0 = it.key0(t);
+            if (t + 1 < it.n_tiles) st.load(a, it, kvh, wave, lane, t + 1);
+            if (it.live && !it.unseen(key0)) {
+                f32x4 sc[4][CT];  // [2 pair + tile][ct]
+#pragma unroll
+                for (int p = 0; p < 4; ++p)
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) sc[p][ct] = f32x4{};
+                // LDS reads one step ahead of the MFMAs, in the order that the
+                // scheduling groups hold, as in the bf16 kernel
+                bf16x8 kf[2][KK], vf[2][4];
+                auto kread = [&](int p, bf16x8(&f)[KK]) {
+                    const int key = pair_key(col, p & 1), tok = key & 15;
+                    const int base = (2 * (p >> 1) + (key >> 4)) * PAGE + tok * 32 + kswz(tok, grp) * 8;
+#pragma unroll
+                    for (int kk = 0; kk < KK; ++kk) f[kk] = *reinterpret_cast<const bf16x8*>(&Ks[buf][base + kk * 512]);
+                };
+                // V group g: page pair g / (NT / 4), output dims 16 n0 .. + 63, n0 = 4 (g % (NT / 4))
+                constexpr int VG = 2 * NT / 4;
+                auto vread = [&](int g, bf16x8(&f)[4]) {
+                    const int j = g / (NT / 4), n0 = (g % (NT / 4)) * 4;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int d = (n0 + i) * 16 + col;
+                        f[i] = *reinterpret_cast<const bf16x8*>(
+                            &Vs[buf][(2 * j + (grp >> 1)) * PAGE + d * 16 + vswz(d, grp & 1) * 8]);
+                    }
+                };
+                kread(0, kf[0]);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    if (p + 1 < 4) kread(p + 1, kf[(p + 1) & 1]);
+#pragma unroll
+                    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct) sc[p][ct] = mfma16(kf[p & 1][kk], qf[ct][kk], sc[p][ct]);
+                }
+                vread(0, vf[0]);
+                __builtin_amdgcn_sched_group_barrier(0x100, KK, 0);  // 0x100: LDS reads
+#pragma unroll
+                for (int p = 0; p < 3; ++p) {
+#pragma unroll
+                    for (int r = 0; r < KK; ++r) {
+                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);  // 0x8: MFMA
+                        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    }
+                    if constexpr (KK * CT > KK) __builtin_amdgcn_sched_group_barrier(0x8, KK * CT - KK, 0);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                if constexpr (KK * CT > 4) __builtin_amdgcn_sched_group_barrier(0x8, KK * CT - 4, 0);
+                bf16x8 pf[2][CT];
+                rows.template softmax<GROUP>(sc, pf, it, key0, sl2, col, grp);
+#pragma unroll
+                for (int g = 0; g < VG; ++g) {
+                    const int j = g / (NT / 4), n0 = (g % (NT / 4)) * 4;
+                    if (g + 1 < VG) vread(g + 1, vf[(g + 1) & 1]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct)
+                            rows.o[ct][n0 + i] = mfma16(pf[j][ct], vf[g & 1][i], rows.o[ct][n0 + i]);
+                    if (n0 == 0) {
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct) rows.l[ct] = mfma16(pf[j][ct], ones, rows.l[ct]);
+                    }
+                }
+#pragma unroll
+                for (int g = 0; g < VG; ++g) {
+                    if (g + 1 < VG) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                        }
+                        if (g % (NT / 4) == 0) __builtin_amdgcn_sched_group_barrier(0x8, 5 * CT - 4, 0);
+                        else __builtin_amdgcn_sched_group_barrier(0x8, 4 * CT - 4, 0);
+                    } else {
+                        if (g % (NT / 4) == 0) __builtin_amdgcn_sched_group_barrier(0x8, 5 * CT, 0);
+                        else __builtin_amdgcn_sched_group_barrier(0x8, 4 * CT, 0);
+                    }
+                }
+            }
+            if (t + 1 < it.n_tiles) odd |= st.store(Ks[buf ^ 1], Vs[buf ^ 1], it, wave, lane, t + 1);
+            wait_lgkmcnt0();
+            barrier_only();
+        }
+        if (it.live) rows.template write<GROUP>(c, it, kvh, wave, col, grp);
+        if (any_odd(odd, flags)) exact_item<Q8, HD, GROUP>(a, it, kvh, Ks[0], Vs[0], sl2);  // writes its rows anew
+        barrier_only();
     }
 }
 
