@@ -16,6 +16,8 @@
 // P keep their precision, which an e4m3 product would cut to three bits.
 #include <math.h>
 
+#include <type_traits>
+
 #include "attn_device.h"
 #include "kernels.h"
 
@@ -790,9 +792,303 @@ __global__ __launch_bounds__(512) void cache_chunk_kernel(CacheAttnArgs a) {
     }
 }
 
+// ---------------------------------------------------------------------------
+// Long work items at head dim 128: two wave groups half a tile apart, as in
+// the bf16 kernel of that kind.  A tile's work is two phases with a barrier
+// after each,
+//   P1(t)  mask, running max, exponentials, P in bf16        (VALU)
+//   P2(t)  P V of tile t, then the scores of tile t + 1      (matrix cores)
+// and waves 4-7 run one phase behind waves 0-3, so that on every SIMD one
+// wave's softmax runs under the other's products.  Every wave computes every
+// tile; where its rows see no key of one, the scores are masked and the values
+// read from a tile of zeros.
+//
+// K and V have rings of four 16 KB tiles.  bf16: P2(t) issues the direct loads
+// of V(t + 3) and K(t + 4).  e4m3: P2(t) widens and writes V(t + 2) and
+// K(t + 3), which P2(t - 1) loaded into registers, and loads V(t + 3) and
+// K(t + 4), each between two groups of products.  In slots (phases of waves
+// 0-3) the writes of P2(t), slots 2t + 2 and 2t + 3, go to the buffers of
+// V(t - 2) and K(t - 1), last read in slot 2t - 1, and are first read in slot
+// 2t + 5.
+// ---------------------------------------------------------------------------
+template <bool Q8, int GROUP>
+__global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
+    constexpr int HD = 128, KK = HD / 32, NT = HD / 16, PAGE = HD * 16, CT = 2, PW = 32 / GROUP;
+    const ChunkAttnArgs& c = a.chunk;
+    if (decode_group<Q8, HD>(a)) return;
+    using P = Pieces<Q8, HD>;
+    constexpr int LW = 4 * P::PP / 512;  // 16-byte pieces of each of K and V that a thread moves per tile
+    __shared__ __attribute__((aligned(16))) bf16 Ks[4][4 * PAGE];
+    __shared__ __attribute__((aligned(16))) bf16 Vs[5][4 * PAGE];  // the last one: zeros
+    __shared__ int flags[8];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int behind = wave >> 2;  // 1: the group that runs one phase behind
+    const int grp = lane >> 4, col = lane & 15;
+    const int pos = xcd_order(blockIdx.x, c.n_slots * c.hkv);
+    const int kvh = pos / c.n_slots, slot = pos % c.n_slots;
+    const float sl2 = kLog2e / sqrtf(static_cast<float>(HD));
+    const bf16x8 ones = ones8();
+
+    // bf16: load i of a wave covers 1 KB slab j = wave + 8 i of K and of V, each
+    // lane the 16-byte piece that belongs at its swizzled place
+    const int l_k = (lane >> 2) * 32 + kswz(lane >> 2, lane & 3) * 8;
+    auto page_of = [&](int i) { return Q8 ? P::page(64 * wave) : (wave + 8 * i) / KK; };
+
+    for (int e = tid; e < 4 * PAGE / 8; e += 512) *reinterpret_cast<u32x4*>(&Vs[4][e * 8]) = u32x4{};
+    wait_lgkmcnt0();
+    const int i0 = c.slot_off[slot], i1 = c.slot_off[slot + 1];
+    for (int k = i0; k < i1; ++k) {
+        const Item it(a, c.slot_items[k], wave, PW);
+        const int n_tiles = it.n_tiles;
+        bf16x8 qf[CT][KK];
+        load_q<HD, GROUP>(qf, c, it, kvh, col, grp);
+        uint32_t odd = 0;
+
+        // Block ids of the pages a wave's loads read, through the scalar cache:
+        // blk_k of the tile whose K is loaded next, blk_v of the one before it,
+        // whose V is loaded at the same time.
+        int blk_k[LW], blk_v[LW];
+        auto fetch = [&](int t) {
+#pragma unroll
+            for (int i = 0; i < LW; ++i) blk_k[i] = it.block(it.key0(t), page_of(i));
+        };
+        auto shift = [&](int t) {  // the ids move up by a tile; tile t's come in
+#pragma unroll
+            for (int i = 0; i < LW; ++i) blk_v[i] = blk_k[i];
+            fetch(t);
+        };
+        auto heads = [&](int blk) { return static_cast<size_t>(blk) * c.hkv + kvh; };
+        // e4m3: the pieces on their way, with their scales
+        u32x4 kx, vx;
+        float ksc = 0.f, vsc = 0.f;
+        auto load_k = [&](int i, int t) {
+            if constexpr (Q8) {
+                kx = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(c.k_pool) + heads(blk_k[0]) * P::PB +
+                                                     P::offset(64 * wave, lane) * 16);
+            } else {
+                const int slab = (wave + 8 * i) % KK, at = page_of(i) * PAGE + slab * 512;
+                load_lds16(static_cast<const bf16*>(c.k_pool) + heads(blk_k[i]) * PAGE + slab * 512 + l_k, &Ks[t & 3][at]);
+            }
+        };
+        auto load_v = [&](int i, int t) {
+            if constexpr (Q8) {
+                vx = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(c.v_pool) + heads(blk_v[0]) * P::PB +
+                                                     P::offset(64 * wave, lane) * 16);
+            } else {
+                const int slab = (wave + 8 * i) % KK, at = page_of(i) * PAGE + slab * 512;
+                const int d = slab * 32 + (lane >> 1), h = (lane & 1) ^ ((d >> 2) & 1);
+                load_lds16(static_cast<const bf16*>(c.v_pool) + heads(blk_v[i]) * PAGE + d * 16 + h * 8, &Vs[t & 3][at]);
+            }
+        };
+        auto scales = [&]() {  // of the tiles whose loads were issued last
+            if constexpr (Q8) {
+                ksc = ((const const_f32*)a.k_scale)[heads(blk_k[0])];
+                vsc = ((const const_f32*)a.v_scale)[heads(blk_v[0])];
+            }
+        };
+        auto put_k = [&](int t) {
+            if constexpr (Q8) P::put_k(Ks[t & 3], 64 * wave, lane, kx, ksc);
+        };
+        auto put_v = [&](int t) {
+            if constexpr (Q8) odd |= P::put_v(Vs[t & 3], 64 * wave, lane, vx, vsc, it.key0(t), it.key_end);
+        };
+        // bf16: the pieces a lane loaded itself, once they have landed, on an
+        // edge of the mask: values of keys from key_end on become 0, others
+        // that are not finite are noted
+        const int last = it.pos0 + it.nrows - 1;
+        auto settle = [&](int t) {
+            if constexpr (!Q8) {
+                const int key0 = it.key0(t);
+                if (t < n_tiles && (key0 + 63 > it.pos0 || (last - it.window >= key0 && key0 + 63 >= it.sinks))) {
+#pragma unroll
+                    for (int i = 0; i < LW; ++i) {
+                        const int slab = (wave + 8 * i) % KK, d = slab * 32 + (lane >> 1), h = (lane & 1) ^ ((d >> 2) & 1);
+                        const int nv = min(max(it.key_end - (key0 + 16 * page_of(i) + 8 * h), 0), 8);
+                        u32x4* piece = reinterpret_cast<u32x4*>(&Vs[t & 3][page_of(i) * PAGE + slab * 512 + lane * 8]);
+                        u32x4 x = *piece;
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            x[w] &= (2 * w < nv ? 0x0000FFFFu : 0u) | (2 * w + 1 < nv ? 0xFFFF0000u : 0u);
+                            odd |= ((x[w] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+                        }
+                        *piece = x;
+                    }
+                    wait_lgkmcnt0();
+                }
+            }
+        };
+
+        Rows<HD> rows;
+        rows.clear();
+        f32x4 sc[4][CT];
+        bf16x8 pf[2][CT];
+        // P2 as a chain of fragment groups: VG groups of four V fragments, then
+        // the K fragments of the four score tiles.  Groups are read two ahead
+        // of their MFMAs; the first two are read at the end of P1.
+        constexpr int VG = 2 * NT / 4, NG = VG + 4;
+        bf16x8 fr[3][4];
+        static_assert(KK == 4, "a group is four fragments");
+        auto read = [&](int t, int s) {
+            bf16x8(&f)[4] = fr[s % 3];
+            if (s < VG) {
+                const int j = s / (NT / 4), n0 = (s % (NT / 4)) * 4, v_base = (2 * j + (grp >> 1)) * PAGE;
+                const int buf = it.unseen(it.key0(t)) ? 4 : t & 3;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int d = (n0 + i) * 16 + col;
+                    f[i] = *reinterpret_cast<const bf16x8*>(&Vs[buf][v_base + d * 16 + vswz(d, grp & 1) * 8]);
+                }
+            } else {
+                const int p = s - VG, key = pair_key(col, p & 1), tok = key & 15;
+                const int base = (2 * (p >> 1) + (key >> 4)) * PAGE + tok * 32 + kswz(tok, grp) * 8;
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) f[kk] = *reinterpret_cast<const bf16x8*>(&Ks[(t + 1) & 3][base + kk * 512]);
+            }
+        };
+        auto mma = [&](int s) {
+            const bf16x8(&f)[4] = fr[s % 3];
+            if (s < VG) {
+                const int j = s / (NT / 4), n0 = (s % (NT / 4)) * 4;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) rows.o[ct][n0 + i] = mfma16(pf[j][ct], f[i], rows.o[ct][n0 + i]);
+                if (n0 == 0) {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) rows.l[ct] = mfma16(pf[j][ct], ones, rows.l[ct]);
+                }
+            } else {
+                const int p = s - VG;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) sc[p][ct] = f32x4{};
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) sc[p][ct] = mfma16(f[kk], qf[ct][kk], sc[p][ct]);
+            }
+        };
+        // Groups first .. NG - 1, of which two are read, with four steps of
+        // moving tiles spread between them.
+        auto products = [&](int t, auto first) {
+            constexpr int S0 = decltype(first)::value, N = NG - S0;
+#pragma unroll
+            for (int s = S0; s < NG; ++s) {
+                if (s + 2 < NG) read(t, s + 2);
+                mma(s);
+#pragma unroll
+                for (int l = 0; l < 4; ++l)
+                    if ((2 * l + 1) * N / 8 == s - S0) {
+                        if constexpr (Q8) {
+                            if (l == 0) put_v(t + 2);
+                            else if (l == 1) put_k(t + 3);
+                            else if (l == 2) load_v(0, t + 3);
+                            else load_k(0, t + 4);
+                        } else {
+                            if (l < LW) load_v(l, t + 3);
+                            else load_k(l - LW, t + 4);
+                        }
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        // The item's K(0 .. 2), V(0) and V(1) (e4m3: the last of each in
+        // registers) before the first slot; the previous item's buffers are free.
+        if constexpr (Q8) {
+            u32x4 k0, k1, v0;
+            float k0s, k1s, v0s;
+            fetch(0);
+            load_k(0, 0);
+            k0 = kx;
+            shift(1);
+            load_v(0, 0);
+            load_k(0, 1);
+            v0 = vx;
+            k1 = kx;
+            k0s = ((const const_f32*)a.k_scale)[heads(blk_v[0])];
+            scales();
+            v0s = vsc;
+            k1s = ksc;
+            shift(2);
+            load_v(0, 1);
+            load_k(0, 2);
+            scales();
+            P::put_k(Ks[0], 64 * wave, lane, k0, k0s);
+            P::put_k(Ks[1], 64 * wave, lane, k1, k1s);
+            odd |= P::put_v(Vs[0], 64 * wave, lane, v0, v0s, it.key0(0), it.key_end);
+            shift(3);
+            wait_lgkmcnt0();
+        } else {
+            wait_vmcnt<0>();  // Q: the compiler then has no loads of its own pending
+            fetch(0);
+#pragma unroll
+            for (int i = 0; i < LW; ++i) load_k(i, 0);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                shift(t + 1);
+#pragma unroll
+                for (int i = 0; i < LW; ++i) {
+                    load_v(i, t);
+                    load_k(i, t + 1);
+                }
+            }
+            shift(3);
+            wait_vmcnt<0>();
+        }
+        barrier_only();
+        if (behind) {  // slot 0 of the group behind
+            settle(0);
+            barrier_only();
+        }
+        read(-1, VG);
+        read(-1, VG + 1);
+        products(-1, std::integral_constant<int, VG>{});
+        if (!behind) settle(0);
+        scales();
+        shift(4);
+        if constexpr (Q8) wait_lgkmcnt0();
+        barrier_only();
+        for (int t = 0; t < n_tiles; ++t) {
+            // P1
+            rows.template softmax<GROUP>(sc, pf, it, it.key0(t), sl2, col, grp);
+            if (behind) {  // V(t + 1) and K(t + 2) have landed; those of the tile after may not have
+                if constexpr (!Q8) wait_vmcnt<2 * LW>();
+                settle(t + 1);
+            }
+            read(t, 0);
+            read(t, 1);
+            barrier_only();
+            // P2, ahead of the other wave's softmax at every issue
+            __builtin_amdgcn_s_setprio(1);
+            products(t, std::integral_constant<int, 0>{});
+            __builtin_amdgcn_s_setprio(0);
+            if (!behind) {  // the same slot; two tiles' loads are younger
+                if constexpr (!Q8) wait_vmcnt<4 * LW>();
+                settle(t + 1);
+            }
+            scales();
+            shift(t + 5);
+            if constexpr (Q8) wait_lgkmcnt0();
+            else if (t + 1 == n_tiles) wait_vmcnt<0>();  // nothing in flight into the next item's buffers
+            barrier_only();
+        }
+        if (!behind) barrier_only();
+
+        if (it.live) rows.template write<GROUP>(c, it, kvh, wave, col, grp);
+        if (any_odd(odd, flags)) exact_item<Q8, HD, GROUP>(a, it, kvh, Ks[0], Vs[0], sl2);  // writes its rows anew
+        barrier_only();
+    }
+}
+
 template <bool Q8, int HD, int GROUP>
 void launch_g(const CacheAttnArgs& a, hipStream_t s) {
     const int blocks = a.chunk.n_slots * a.chunk.hkv + (a.decode.n_slots * a.decode.hkv + 7) / 8;
+    if constexpr (HD == 128) {
+        if (a.chunk.pp) {
+            cache_chunk_pp_kernel<Q8, GROUP><<<blocks, 512, 0, s>>>(a);
+            return;
+        }
+    }
     cache_chunk_kernel<Q8, HD, GROUP><<<blocks, 512, 0, s>>>(a);
 }
 

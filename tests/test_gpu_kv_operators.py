@@ -167,6 +167,54 @@ def test_long_prefix(cache, window, sinks):
     _run(rig, batch, q_std=2.0, rows={0, 1, 63, 64, 100, 198, 199, 200, 201})
 
 
+# (q heads, kv heads, chunk, prefix, window, sinks): work items long enough for the two-phase kernel
+LONG = [(16, 16, 257, 24001, 0, 0), (32, 16, 140, 20020, 0, 0), (32, 8, 200, 16390, 0, 0), (64, 8, 100, 16401, 0, 0),
+        (128, 8, 50, 16383, 0, 0), (16, 16, 4096, 5000, 4000, 3), (32, 16, 2048, 4000, 3001, 70), (64, 16, 1024, 5003, 3500, 0),
+        (128, 16, 512, 5000, 3001, 64), (256, 16, 256, 5000, 2100, 1)]
+
+
+def _long_rig(case, cache, grow=0):
+    hq, hkv, C, P, window, sinks = case
+    rig = Rig(hq, hkv, 128, {1: P, 2: 700, 3: 5}, cache, window=window, sinks=sinks, grow=C + 1, max_pos=32768)
+    from paper_2609_07883_amd.synth import ModelShape
+    shape = ModelShape(1, 256, hq, hkv, 128, 256, max_pos=32768)
+    plan = api.attention_plan(shape, [700, 5], [(P, C)], window, sinks)
+    assert plan["chunk_two_phase"]
+    tile = 256 * hkv // hq
+    rows = {0, 1, 33, tile - 1, tile, C // 2, C - 2, C - 1, C, C + 1}
+    return rig, api.Batch(C, 1, P, (2, 3), (700, 5)), {r for r in rows if 0 <= r < C + 2}
+
+
+def _with_caches(cases):  # full attention over bf16 pages is the iteration's own kernel
+    return [pytest.param(c, t, id=f"hq{c[0]}_hkv{c[1]}_w{c[4]}_{t}") for c in cases for t in ("e4m3", "bf16") if c[4] or t == "e4m3"]
+
+
+@pytest.mark.parametrize("case,cache", _with_caches(LONG))
+def test_long_items(case, cache):
+    """The two-phase kernel for every group size, whole and split query tiles, beside decodes."""
+    rig, batch, rows = _long_rig(case, cache)
+    _run(rig, batch, q_std=2.0, rows=rows)
+
+
+@pytest.mark.parametrize("case,cache", _with_caches([LONG[2], LONG[7], LONG[9]]))
+def test_long_items_with_tokens_that_are_not_finite(case, cache):
+    """V values that are not finite, cached and new, in tiles that some rows see whole, some in part and some not at
+    all: exactly the rows that see them have them."""
+    hq, hkv, C, P, window, sinks = case
+    rig, batch, rows = _long_rig(case, cache)
+    bt = rig.ctx.block_table(1)
+    bad = [P + C // 3 - window, P - 20] if window else [P - 20]
+    for i, t in enumerate(bad):
+        rig.v[0, bt[t // 16], :, t % 16, 3 + i] = np.nan if cache == "e4m3" else [np.inf, -np.inf][i]
+    rig.upload()
+    if window:
+        rows |= {C // 3 - 3, C // 3 - 2, C // 3 - 1, C // 3, C // 3 + 1}
+    x = rig.rng.standard_normal((batch.rows, hq + 2 * hkv, 128))
+    x[C // 2, hq + hkv:, 7] = np.nan
+    rows |= {C // 2 - 1, C // 2, C // 2 + 1}
+    _run(rig, batch, x=x, rows=rows)
+
+
 def test_large_values_and_far_scores():
     """Scores hundreds apart (the running maximum moves by more than the lazy threshold at every tile)."""
     rig = Rig(4, 2, 128, {1: 600, 2: 700}, "e4m3", window=0, grow=64)
