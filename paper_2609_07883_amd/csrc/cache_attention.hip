@@ -270,9 +270,9 @@ __global__ __launch_bounds__(64, 2) void cache_decode_kernel(CacheAttnArgs a) {
 //
 // A key that some rows of a wave see and others do not stays out of the
 // others' products through a zero probability, unless its V row is not finite
-// (0 times it would be NaN).  The kernels watch for such values as they write
-// V to LDS; an item that met one is computed again by exact_item, which keeps
-// them apart.
+// (0 times it would be NaN).  The kernels look for such values in the tiles that
+// some row does not see whole; an item that met one is computed again by
+// exact_item, which keeps them apart.
 // ---------------------------------------------------------------------------
 
 // One work item of a work-group, and the wave's share of it.
@@ -313,6 +313,10 @@ struct Item {
     __device__ __forceinline__ int block(int key0, int page) const {
         return bt[__builtin_amdgcn_readfirstlane(min((key0 >> 4) + page, last_page))];
     }
+    // some row of the query tile does not see every key of the tile
+    __device__ __forceinline__ bool edge(int key0) const {
+        return key0 + 63 > pos0 || (key_end - 1 - window >= key0 && key0 + 63 >= sinks);
+    }
     // the wave's rows see no key of the tile / not every key of it
     __device__ __forceinline__ bool unseen(int key0) const {
         return key0 > hi || (lo - window >= key0 + 63 && key0 >= sinks);
@@ -350,11 +354,9 @@ struct Pieces {
     }
     // Values of keys from key_end on (unwritten slots, stand-in pages) become
     // 0; their scores are masked.  Nonzero result: a value is not finite.
-    static __device__ __forceinline__ uint32_t put_v(bf16* tile, int first, int lane, u32x4 x, float scale, int key0,
-                                                     int key_end) {
-        const int at = offset(first, lane);
+    static __device__ __forceinline__ uint32_t settle_v(int first, int lane, u32x4& x, int key0, int key_end) {
         if (key0 + 63 >= key_end) {
-            const int k = key0 + 16 * page(first) + (Q8 ? 0 : 8 * (at & 1));
+            const int k = key0 + 16 * page(first) + (Q8 ? 0 : 8 * (offset(first, lane) & 1));
             const uint32_t live = low_bits(min(max(key_end - k, 0), 16));
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
@@ -365,9 +367,13 @@ struct Pieces {
         uint32_t odd = 0;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {  // an all-ones magnitude (exponent) carries into the sign
-            if constexpr (Q8) odd |= ((x[w] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-            else odd |= ((x[w] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+            if constexpr (Q8) odd |= (x[w] & 0x7F7F7F7Fu) + 0x01010101u;
+            else odd |= (x[w] & 0x7F807F80u) + 0x00800080u;
         }
+        return odd & (Q8 ? 0x80808080u : 0x80008000u);
+    }
+    static __device__ __forceinline__ void put_v(bf16* tile, int first, int lane, u32x4 x, float scale) {
+        const int at = offset(first, lane);
         bf16* base = tile + page(first) * PAGE;
         if constexpr (Q8) {
             *reinterpret_cast<bf16x8*>(base + at * 16 + vswz(at, 0) * 8) = widen8(x[0], x[1], scale);
@@ -376,7 +382,6 @@ struct Pieces {
             const int d = at >> 1;
             *reinterpret_cast<u32x4*>(base + d * 16 + vswz(d, at & 1) * 8) = x;
         }
-        return odd;
     }
 };
 
@@ -401,12 +406,21 @@ struct Staged {
             if constexpr (Q8) scale[i] = ((const const_f32*)(is_v ? a.v_scale : a.k_scale))[bh];
         }
     }
-    __device__ __forceinline__ uint32_t store(bf16* ks, bf16* vs, const Item& it, int wave, int lane, int t) const {
+    // nonzero: a V value of a tile on an edge of the mask is not finite
+    __device__ __forceinline__ uint32_t store(bf16* ks, bf16* vs, const Item& it, int wave, int lane, int t) {
+        const int key0 = it.key0(t);
         uint32_t odd = 0;
+        if (it.edge(key0)) {
+#pragma unroll
+            for (int i = 0; i < PT; ++i) {
+                const int j = 512 * i + 64 * wave;
+                if (j >= HALF) odd |= P::settle_v(j - HALF, lane, raw[i], key0, it.key_end);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < PT; ++i) {
             const int j = 512 * i + 64 * wave;
-            if (j >= HALF) odd |= P::put_v(vs, j - HALF, lane, raw[i], scale[i], it.key0(t), it.key_end);
+            if (j >= HALF) P::put_v(vs, j - HALF, lane, raw[i], scale[i]);
             else P::put_k(ks, j, lane, raw[i], scale[i]);
         }
         return odd;
@@ -800,16 +814,19 @@ __global__ __launch_bounds__(512) void cache_chunk_kernel(CacheAttnArgs a) {
 //   P2(t)  P V of tile t, then the scores of tile t + 1      (matrix cores)
 // and waves 4-7 run one phase behind waves 0-3, so that on every SIMD one
 // wave's softmax runs under the other's products.  Every wave computes every
-// tile; where its rows see no key of one, the scores are masked and the values
-// read from a tile of zeros.
+// tile; where its rows see no key of one, the scores are masked.
 //
-// K and V have rings of four 16 KB tiles.  bf16: P2(t) issues the direct loads
-// of V(t + 3) and K(t + 4).  e4m3: P2(t) widens and writes V(t + 2) and
-// K(t + 3), which P2(t - 1) loaded into registers, and loads V(t + 3) and
-// K(t + 4), each between two groups of products.  In slots (phases of waves
-// 0-3) the writes of P2(t), slots 2t + 2 and 2t + 3, go to the buffers of
-// V(t - 2) and K(t - 1), last read in slot 2t - 1, and are first read in slot
-// 2t + 5.
+// bf16: rings of four 16 KB tiles of K and of V; P2(t) issues the direct loads
+// of V(t + 3) and K(t + 4), as there.
+// e4m3: rings of three, and rings of three 8 KB tiles of codes, which direct
+// loads fill and where each thread finds the pieces it asked for itself.  P2(t)
+// takes the codes of V(t + 2) and K(t + 3) from there, widens and writes them,
+// and loads those of V(t + 5) and K(t + 6) in their place, each step between
+// two groups of products: a tile's loads have three of them to land.  In slots
+// (phases of waves 0-3) the writes of P2(t), slots 2t + 2 and 2t + 3, go to the
+// buffers of V(t - 1) and K(t), last read in slot 2t + 1, and are first read in
+// slot 2t + 5.  (With the codes in registers instead, one tile ahead, the loads
+// were late: 2050 us against 1671 for the bf16 cache at 4096 rows at 28 K.)
 // ---------------------------------------------------------------------------
 template <bool Q8, int GROUP>
 __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
@@ -818,8 +835,10 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
     if (decode_group<Q8, HD>(a)) return;
     using P = Pieces<Q8, HD>;
     constexpr int LW = 4 * P::PP / 512;  // 16-byte pieces of each of K and V that a thread moves per tile
-    __shared__ __attribute__((aligned(16))) bf16 Ks[4][4 * PAGE];
-    __shared__ __attribute__((aligned(16))) bf16 Vs[5][4 * PAGE];  // the last one: zeros
+    constexpr int RING = Q8 ? 3 : 4;
+    __shared__ __attribute__((aligned(16))) bf16 Ks[RING][4 * PAGE];
+    __shared__ __attribute__((aligned(16))) bf16 Vs[RING][4 * PAGE];
+    __shared__ __attribute__((aligned(16))) u32x4 codes[Q8 ? 2 : 1][Q8 ? 3 : 1][Q8 ? 512 : 1];  // [K, V][tile % 3][thread]
     __shared__ int flags[8];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -835,8 +854,6 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
     const int l_k = (lane >> 2) * 32 + kswz(lane >> 2, lane & 3) * 8;
     auto page_of = [&](int i) { return Q8 ? P::page(64 * wave) : (wave + 8 * i) / KK; };
 
-    for (int e = tid; e < 4 * PAGE / 8; e += 512) *reinterpret_cast<u32x4*>(&Vs[4][e * 8]) = u32x4{};
-    wait_lgkmcnt0();
     const int i0 = c.slot_off[slot], i1 = c.slot_off[slot + 1];
     for (int k = i0; k < i1; ++k) {
         const Item it(a, c.slot_items[k], wave, PW);
@@ -846,72 +863,70 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
         uint32_t odd = 0;
 
         // Block ids of the pages a wave's loads read, through the scalar cache:
-        // blk_k of the tile whose K is loaded next, blk_v of the one before it,
-        // whose V is loaded at the same time.
-        int blk_k[LW], blk_v[LW];
-        auto fetch = [&](int t) {
-#pragma unroll
-            for (int i = 0; i < LW; ++i) blk_k[i] = it.block(it.key0(t), page_of(i));
+        // ids[x] of tile t + AHEAD - x, of which P2(t) loads K of x = 0 and V of
+        // x = 1.  e4m3: the scales of the tiles that P2(t) writes, K(t + 3) and
+        // V(t + 2), are those of x = 3 and 4, and read a tile before.
+        constexpr int AHEAD = Q8 ? 6 : 4, IDS = Q8 ? 4 : 2;
+        int ids[IDS][LW];
+        float ksc = 0.f, vsc = 0.f;
+        auto heads = [&](int blk) { return static_cast<size_t>(blk) * c.hkv + kvh; };
+        auto scales = [&](int k_blk, int v_blk) {
+            if constexpr (Q8) {
+                ksc = ((const const_f32*)a.k_scale)[heads(k_blk)];
+                vsc = ((const const_f32*)a.v_scale)[heads(v_blk)];
+            }
         };
         auto shift = [&](int t) {  // the ids move up by a tile; tile t's come in
 #pragma unroll
-            for (int i = 0; i < LW; ++i) blk_v[i] = blk_k[i];
-            fetch(t);
+            for (int x = IDS - 1; x > 0; --x)
+#pragma unroll
+                for (int i = 0; i < LW; ++i) ids[x][i] = ids[x - 1][i];
+#pragma unroll
+            for (int i = 0; i < LW; ++i) ids[0][i] = it.block(it.key0(t), page_of(i));
         };
-        auto heads = [&](int blk) { return static_cast<size_t>(blk) * c.hkv + kvh; };
-        // e4m3: the pieces on their way, with their scales
-        u32x4 kx, vx;
-        float ksc = 0.f, vsc = 0.f;
-        auto load_k = [&](int i, int t) {
+        auto mod3 = [](int x) { return x >= 3 ? x - 3 : x; };
+        auto source = [&](bool is_v, int blk) {  // e4m3: the thread's piece of a page
+            return static_cast<const uint8_t*>(is_v ? c.v_pool : c.k_pool) + heads(blk) * P::PB + P::offset(64 * wave, lane) * 16;
+        };
+        // Loads of tile t (r: t % 3, e4m3) from the block(s) `blk`.
+        auto load_k = [&](int i, int t, int r, const int (&blk)[LW]) {
             if constexpr (Q8) {
-                kx = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(c.k_pool) + heads(blk_k[0]) * P::PB +
-                                                     P::offset(64 * wave, lane) * 16);
+                load_lds16(source(false, blk[0]), &codes[0][r][64 * wave]);
             } else {
                 const int slab = (wave + 8 * i) % KK, at = page_of(i) * PAGE + slab * 512;
-                load_lds16(static_cast<const bf16*>(c.k_pool) + heads(blk_k[i]) * PAGE + slab * 512 + l_k, &Ks[t & 3][at]);
+                load_lds16(static_cast<const bf16*>(c.k_pool) + heads(blk[i]) * PAGE + slab * 512 + l_k, &Ks[t & 3][at]);
             }
         };
-        auto load_v = [&](int i, int t) {
+        auto load_v = [&](int i, int t, int r, const int (&blk)[LW]) {
             if constexpr (Q8) {
-                vx = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(c.v_pool) + heads(blk_v[0]) * P::PB +
-                                                     P::offset(64 * wave, lane) * 16);
+                load_lds16(source(true, blk[0]), &codes[Q8 ? 1 : 0][r][64 * wave]);
             } else {
                 const int slab = (wave + 8 * i) % KK, at = page_of(i) * PAGE + slab * 512;
                 const int d = slab * 32 + (lane >> 1), h = (lane & 1) ^ ((d >> 2) & 1);
-                load_lds16(static_cast<const bf16*>(c.v_pool) + heads(blk_v[i]) * PAGE + d * 16 + h * 8, &Vs[t & 3][at]);
+                load_lds16(static_cast<const bf16*>(c.v_pool) + heads(blk[i]) * PAGE + d * 16 + h * 8, &Vs[t & 3][at]);
             }
         };
-        auto scales = [&]() {  // of the tiles whose loads were issued last
+        // The pieces of V that a lane loaded itself, on an edge of the mask, once
+        // they have landed: in the tile, or, e4m3, among the codes (r: t % 3).
+        auto settle = [&](int t, int r) {
+            const int key0 = it.key0(t);
             if constexpr (Q8) {
-                ksc = ((const const_f32*)a.k_scale)[heads(blk_k[0])];
-                vsc = ((const const_f32*)a.v_scale)[heads(blk_v[0])];
-            }
-        };
-        auto put_k = [&](int t) {
-            if constexpr (Q8) P::put_k(Ks[t & 3], 64 * wave, lane, kx, ksc);
-        };
-        auto put_v = [&](int t) {
-            if constexpr (Q8) odd |= P::put_v(Vs[t & 3], 64 * wave, lane, vx, vsc, it.key0(t), it.key_end);
-        };
-        // bf16: the pieces a lane loaded itself, once they have landed, on an
-        // edge of the mask: values of keys from key_end on become 0, others
-        // that are not finite are noted
-        const int last = it.pos0 + it.nrows - 1;
-        auto settle = [&](int t) {
-            if constexpr (!Q8) {
-                const int key0 = it.key0(t);
-                if (t < n_tiles && (key0 + 63 > it.pos0 || (last - it.window >= key0 && key0 + 63 >= it.sinks))) {
+                if (it.edge(key0)) {
+                    wait_vmcnt<4>();
+                    asm volatile("" ::: "memory");
+                    u32x4 x = codes[1][r][tid];
+                    odd |= P::settle_v(64 * wave, lane, x, key0, it.key_end);
+                    codes[1][r][tid] = x;
+                }
+            } else {
+                if (t < n_tiles && it.edge(key0)) {
 #pragma unroll
                     for (int i = 0; i < LW; ++i) {
-                        const int slab = (wave + 8 * i) % KK, d = slab * 32 + (lane >> 1), h = (lane & 1) ^ ((d >> 2) & 1);
-                        const int nv = min(max(it.key_end - (key0 + 16 * page_of(i) + 8 * h), 0), 8);
+                        const int slab = (wave + 8 * i) % KK, d = slab * 32 + (lane >> 1);
                         u32x4* piece = reinterpret_cast<u32x4*>(&Vs[t & 3][page_of(i) * PAGE + slab * 512 + lane * 8]);
                         u32x4 x = *piece;
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            x[w] &= (2 * w < nv ? 0x0000FFFFu : 0u) | (2 * w + 1 < nv ? 0xFFFF0000u : 0u);
-                            odd |= ((x[w] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-                        }
+                        // as the pieces number them: tokens 8 h .. of dim d is piece 2 d + h of its page
+                        odd |= P::settle_v(page_of(i) * P::PP, 2 * d + ((lane & 1) ^ ((d >> 2) & 1)), x, key0, it.key_end);
                         *piece = x;
                     }
                     wait_lgkmcnt0();
@@ -929,11 +944,11 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
         constexpr int VG = 2 * NT / 4, NG = VG + 4;
         bf16x8 fr[3][4];
         static_assert(KK == 4, "a group is four fragments");
-        auto read = [&](int t, int s) {
+        auto read = [&](int t, int r, int s) {
             bf16x8(&f)[4] = fr[s % 3];
             if (s < VG) {
                 const int j = s / (NT / 4), n0 = (s % (NT / 4)) * 4, v_base = (2 * j + (grp >> 1)) * PAGE;
-                const int buf = it.unseen(it.key0(t)) ? 4 : t & 3;
+                const int buf = Q8 ? r : t & 3;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int d = (n0 + i) * 16 + col;
@@ -943,7 +958,8 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
                 const int p = s - VG, key = pair_key(col, p & 1), tok = key & 15;
                 const int base = (2 * (p >> 1) + (key >> 4)) * PAGE + tok * 32 + kswz(tok, grp) * 8;
 #pragma unroll
-                for (int kk = 0; kk < KK; ++kk) f[kk] = *reinterpret_cast<const bf16x8*>(&Ks[(t + 1) & 3][base + kk * 512]);
+                for (int kk = 0; kk < KK; ++kk)
+                    f[kk] = *reinterpret_cast<const bf16x8*>(&Ks[Q8 ? mod3(r + 1) : (t + 1) & 3][base + kk * 512]);
             }
         };
         auto mma = [&](int s) {
@@ -969,107 +985,148 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
             }
         };
         // Groups first .. NG - 1, of which two are read, with four steps of
-        // moving tiles spread between them.
-        auto products = [&](int t, auto first) {
+        // moving tiles spread between them (r: t % 3).
+        u32x4 kx, vx;
+        auto products = [&](int t, int r, auto first) {
             constexpr int S0 = decltype(first)::value, N = NG - S0;
+            if constexpr (Q8) {  // the codes of V(t + 2) and K(t + 3) have landed, two tiles' loads are younger
+                wait_vmcnt<4>();
+                asm volatile("" ::: "memory");
+            }
 #pragma unroll
             for (int s = S0; s < NG; ++s) {
-                if (s + 2 < NG) read(t, s + 2);
+                if (s + 2 < NG) read(t, r, s + 2);
                 mma(s);
+                if constexpr (Q8) {
+                    if (s == S0) {
+                        vx = codes[1][mod3(r + 2)][tid];
+                        kx = codes[0][r][tid];
+                    }
+                    if (N / 4 == s - S0) P::put_v(Vs[mod3(r + 2)], 64 * wave, lane, vx, vsc);
+                    if (2 * N / 4 == s - S0) P::put_k(Ks[r], 64 * wave, lane, kx, ksc);
+                    if (3 * N / 4 == s - S0) {
+                        load_v(0, t + 5, mod3(r + 2), ids[1]);
+                        load_k(0, t + 6, r, ids[0]);
+                    }
+                    if (N / 4 == s - S0 || 2 * N / 4 == s - S0) {  // the widening between the MFMAs, not behind them
 #pragma unroll
-                for (int l = 0; l < 4; ++l)
-                    if ((2 * l + 1) * N / 8 == s - S0) {
-                        if constexpr (Q8) {
-                            if (l == 0) put_v(t + 2);
-                            else if (l == 1) put_k(t + 3);
-                            else if (l == 2) load_v(0, t + 3);
-                            else load_k(0, t + 4);
-                        } else {
-                            if (l < LW) load_v(l, t + 3);
-                            else load_k(l - LW, t + 4);
+                        for (int x = 0; x < 4; ++x) {
+                            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);    // 0x8: MFMA
+                            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // 0x100: LDS reads
+                            __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);    // 0x2: VALU
+                        }
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                            __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);
                         }
                     }
+                } else {
+#pragma unroll
+                    for (int l = 0; l < 2 * LW; ++l)
+                        if ((2 * l + 1) * N / (4 * LW) == s - S0) {
+                            if (l < LW) load_v(l, t + 3, 0, ids[1]);
+                            else load_k(l - LW, t + 4, 0, ids[0]);
+                        }
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
-        // The item's K(0 .. 2), V(0) and V(1) (e4m3: the last of each in
-        // registers) before the first slot; the previous item's buffers are free.
+        // Before the first slot: K(0 .. 2), V(0) and V(1) in LDS, of e4m3 the
+        // last of each and the next two as codes.  The previous item's buffers
+        // are free, and no load is in flight.
+        wait_vmcnt<0>();  // Q: the compiler then has no loads of its own pending
+        shift(0);
         if constexpr (Q8) {
-            u32x4 k0, k1, v0;
-            float k0s, k1s, v0s;
-            fetch(0);
-            load_k(0, 0);
-            k0 = kx;
+            const int b0 = ids[0][0];
             shift(1);
-            load_v(0, 0);
-            load_k(0, 1);
-            v0 = vx;
-            k1 = kx;
-            k0s = ((const const_f32*)a.k_scale)[heads(blk_v[0])];
-            scales();
-            v0s = vsc;
-            k1s = ksc;
+            const int b1 = ids[0][0];
             shift(2);
-            load_v(0, 1);
-            load_k(0, 2);
-            scales();
-            P::put_k(Ks[0], 64 * wave, lane, k0, k0s);
-            P::put_k(Ks[1], 64 * wave, lane, k1, k1s);
-            odd |= P::put_v(Vs[0], 64 * wave, lane, v0, v0s, it.key0(0), it.key_end);
+            load_v(0, 1, 1, ids[1]);
+            load_k(0, 2, 2, ids[0]);
             shift(3);
+            load_v(0, 2, 2, ids[1]);
+            load_k(0, 3, 0, ids[0]);
+            shift(4);
+            load_v(0, 3, 0, ids[1]);
+            load_k(0, 4, 1, ids[0]);
+            const u32x4 k0 = *reinterpret_cast<const u32x4*>(source(false, b0));
+            u32x4 v0 = *reinterpret_cast<const u32x4*>(source(true, b0));
+            const u32x4 k1 = *reinterpret_cast<const u32x4*>(source(false, b1));
+            scales(b0, b0);
+            P::put_k(Ks[0], 64 * wave, lane, k0, ksc);
+            if (it.edge(it.key0(0))) odd |= P::settle_v(64 * wave, lane, v0, it.key0(0), it.key_end);
+            P::put_v(Vs[0], 64 * wave, lane, v0, vsc);
+            scales(b1, b1);
+            P::put_k(Ks[1], 64 * wave, lane, k1, ksc);
+            scales(ids[2][0], b1);  // of K(2) and V(1)
+            shift(5);
             wait_lgkmcnt0();
         } else {
-            wait_vmcnt<0>();  // Q: the compiler then has no loads of its own pending
-            fetch(0);
 #pragma unroll
-            for (int i = 0; i < LW; ++i) load_k(i, 0);
+            for (int i = 0; i < LW; ++i) load_k(i, 0, 0, ids[0]);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 shift(t + 1);
 #pragma unroll
                 for (int i = 0; i < LW; ++i) {
-                    load_v(i, t);
-                    load_k(i, t + 1);
+                    load_v(i, t, 0, ids[1]);
+                    load_k(i, t + 1, 0, ids[0]);
                 }
             }
             shift(3);
-            wait_vmcnt<0>();
         }
+        wait_vmcnt<0>();
         barrier_only();
+        if constexpr (Q8) settle(1, 1);
         if (behind) {  // slot 0 of the group behind
-            settle(0);
+            if constexpr (!Q8) settle(0, 0);
             barrier_only();
         }
-        read(-1, VG);
-        read(-1, VG + 1);
-        products(-1, std::integral_constant<int, VG>{});
-        if (!behind) settle(0);
-        scales();
-        shift(4);
+        // ids[0] is that of tile t + AHEAD here and below, t = -1 to begin with
+        auto next = [&](int t) {
+            if constexpr (Q8) scales(ids[2][0], ids[3][0]);  // of K(t + 4) and V(t + 3)
+            shift(t + AHEAD + 1);
+        };
+        read(-1, 2, VG);
+        read(-1, 2, VG + 1);
+        products(-1, 2, std::integral_constant<int, VG>{});
+        if constexpr (!Q8) {
+            if (!behind) settle(0, 0);
+        }
+        next(-1);
         if constexpr (Q8) wait_lgkmcnt0();
         barrier_only();
-        for (int t = 0; t < n_tiles; ++t) {
+        for (int t = 0, r = 0; t < n_tiles; ++t, r = mod3(r + 1)) {
             // P1
+            if constexpr (Q8) settle(t + 2, mod3(r + 2));
             rows.template softmax<GROUP>(sc, pf, it, it.key0(t), sl2, col, grp);
-            if (behind) {  // V(t + 1) and K(t + 2) have landed; those of the tile after may not have
-                if constexpr (!Q8) wait_vmcnt<2 * LW>();
-                settle(t + 1);
+            // all of it before the barrier: the compiler would put the second
+            // half's exponentials off to where they are used
+#pragma unroll
+            for (int j = 0; j < 2; ++j) asm volatile("" ::"v"(pf[j][0]), "v"(pf[j][1]));
+            if constexpr (!Q8) {
+                if (behind) {  // V(t + 1) and K(t + 2) have landed; those of the tile after may not have
+                    wait_vmcnt<2 * LW>();
+                    settle(t + 1, 0);
+                }
             }
-            read(t, 0);
-            read(t, 1);
+            read(t, r, 0);
+            read(t, r, 1);
             barrier_only();
             // P2, ahead of the other wave's softmax at every issue
             __builtin_amdgcn_s_setprio(1);
-            products(t, std::integral_constant<int, 0>{});
+            products(t, r, std::integral_constant<int, 0>{});
             __builtin_amdgcn_s_setprio(0);
-            if (!behind) {  // the same slot; two tiles' loads are younger
-                if constexpr (!Q8) wait_vmcnt<4 * LW>();
-                settle(t + 1);
+            if constexpr (!Q8) {
+                if (!behind) {  // the same slot; two tiles' loads are younger
+                    wait_vmcnt<4 * LW>();
+                    settle(t + 1, 0);
+                }
             }
-            scales();
-            shift(t + 5);
+            next(t);
+            if (t + 1 == n_tiles) wait_vmcnt<0>();  // nothing in flight into the next item's buffers
             if constexpr (Q8) wait_lgkmcnt0();
-            else if (t + 1 == n_tiles) wait_vmcnt<0>();  // nothing in flight into the next item's buffers
             barrier_only();
         }
         if (!behind) barrier_only();
