@@ -392,18 +392,33 @@ struct Staged {
     static constexpr int HALF = 4 * P::PP, PT = 2 * HALF / 512;  // pieces of K (or V); pieces a thread moves
     u32x4 raw[PT];
     float scale[PT];
+    int blk[PT];
 
-    __device__ __forceinline__ void load(const CacheAttnArgs& a, const Item& it, int kvh, int wave, int lane, int t) {
+    // Block ids of a tile's pages, through the scalar cache, a tile before load() uses them.
+    __device__ __forceinline__ void fetch(const Item& it, int wave, int t) {
         const int key0 = it.key0(t);
 #pragma unroll
         for (int i = 0; i < PT; ++i) {
             const int j = 512 * i + 64 * wave;
+            blk[i] = it.block(key0, P::page(j >= HALF ? j - HALF : j));
+        }
+    }
+    // The scales come as vectors too: a scalar load in flight would make every
+    // wait for an LDS read of the tile before a wait for it.
+    __device__ __forceinline__ void load(const CacheAttnArgs& a, int kvh, int wave, int lane) {
+#pragma unroll
+        for (int i = 0; i < PT; ++i) {
+            const int j = 512 * i + 64 * wave;
             const bool is_v = j >= HALF;
-            const int first = is_v ? j - HALF : j;
-            const size_t bh = static_cast<size_t>(it.block(key0, P::page(first))) * a.chunk.hkv + kvh;
+            const size_t bh = static_cast<size_t>(blk[i]) * a.chunk.hkv + kvh;
             const void* pool = is_v ? a.chunk.v_pool : a.chunk.k_pool;
-            raw[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(pool) + bh * P::PB + P::offset(first, lane) * 16);
-            if constexpr (Q8) scale[i] = ((const const_f32*)(is_v ? a.v_scale : a.k_scale))[bh];
+            raw[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(pool) + bh * P::PB +
+                                                     P::offset(is_v ? j - HALF : j, lane) * 16);
+            if constexpr (Q8) {
+                uint32_t zero = 0;
+                asm volatile("" : "+v"(zero));  // an address in vector registers
+                scale[i] = (is_v ? a.v_scale : a.k_scale)[bh + zero];
+            }
         }
     }
     // nonzero: a V value of a tile on an edge of the mask is not finite
@@ -581,7 +596,8 @@ __device__ __forceinline__ void exact_item(const CacheAttnArgs& a, const Item& i
             barrier_only();
             {
                 Staged<Q8, HD> st;
-                st.load(a, it, kvh, wave, lane, t);
+                st.fetch(it, wave, t);
+                st.load(a, kvh, wave, lane);
                 st.store(ks, vs, it, wave, lane, t);
             }
             wait_lgkmcnt0();
@@ -705,13 +721,15 @@ __global__ __launch_bounds__(512) void cache_chunk_kernel(CacheAttnArgs a) {
         rows.clear();
         uint32_t odd = 0;
         Staged<Q8, HD> st;
-        st.load(a, it, kvh, wave, lane, 0);
+        st.fetch(it, wave, 0);
+        st.load(a, kvh, wave, lane);
+        st.fetch(it, wave, 1);
         odd |= st.store(Ks[0], Vs[0], it, wave, lane, 0);
         wait_lgkmcnt0();
         barrier_only();
         for (int t = 0; t < it.n_tiles; ++t) {
             const int buf = t & 1, key0 = it.key0(t);
-            if (t + 1 < it.n_tiles) st.load(a, it, kvh, wave, lane, t + 1);
+            if (t + 1 < it.n_tiles) st.load(a, kvh, wave, lane);
             if (it.live && !it.unseen(key0)) {
                 f32x4 sc[4][CT];  // [2 pair + tile][ct]
 #pragma unroll
@@ -798,6 +816,7 @@ __global__ __launch_bounds__(512) void cache_chunk_kernel(CacheAttnArgs a) {
             }
             if (t + 1 < it.n_tiles) odd |= st.store(Ks[buf ^ 1], Vs[buf ^ 1], it, wave, lane, t + 1);
             wait_lgkmcnt0();
+            st.fetch(it, wave, t + 2);
             barrier_only();
         }
         if (it.live) rows.template write<GROUP>(c, it, kvh, wave, col, grp);
@@ -863,26 +882,38 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
         uint32_t odd = 0;
 
         // Block ids of the pages a wave's loads read, through the scalar cache:
-        // ids[x] of tile t + AHEAD - x, of which P2(t) loads K of x = 0 and V of
-        // x = 1.  e4m3: the scales of the tiles that P2(t) writes, K(t + 3) and
-        // V(t + 2), are those of x = 3 and 4, and read a tile before.
-        constexpr int AHEAD = Q8 ? 6 : 4, IDS = Q8 ? 4 : 2;
-        int ids[IDS][LW];
-        float ksc = 0.f, vsc = 0.f;
+        // P2(t) loads K of ids[0], tile t + AHEAD, and V of ids[1], the tile
+        // before it.  e4m3: the scales that P2(t) widens K(t + 3) and V(t + 2)
+        // with are ksc[0] and vsc[0]; those of tile t + 5 come in before it,
+        // in time for memory to answer.  Ids and scales are asked for at the
+        // start of P1, which reads nothing from LDS before its end: a scalar
+        // load in flight makes a wait for LDS a wait for it (asked for at the
+        // end of P2, before its wait for the LDS writes, they cost 400 of
+        // 2100 cycles).
+        constexpr int AHEAD = Q8 ? 6 : 4;
+        int ids[2][LW];
+        float ksc[3], vsc[4];
         auto heads = [&](int blk) { return static_cast<size_t>(blk) * c.hkv + kvh; };
-        auto scales = [&](int k_blk, int v_blk) {
-            if constexpr (Q8) {
-                ksc = ((const const_f32*)a.k_scale)[heads(k_blk)];
-                vsc = ((const const_f32*)a.v_scale)[heads(v_blk)];
-            }
-        };
+        auto k_scale = [&](int blk) { return ((const const_f32*)a.k_scale)[heads(blk)]; };
+        auto v_scale = [&](int blk) { return ((const const_f32*)a.v_scale)[heads(blk)]; };
         auto shift = [&](int t) {  // the ids move up by a tile; tile t's come in
 #pragma unroll
-            for (int x = IDS - 1; x > 0; --x)
-#pragma unroll
-                for (int i = 0; i < LW; ++i) ids[x][i] = ids[x - 1][i];
-#pragma unroll
-            for (int i = 0; i < LW; ++i) ids[0][i] = it.block(it.key0(t), page_of(i));
+            for (int i = 0; i < LW; ++i) {
+                ids[1][i] = ids[0][i];
+                ids[0][i] = it.block(it.key0(t), page_of(i));
+            }
+        };
+        auto next = [&](int t) {  // from P2(t - 1)'s to P2(t)'s
+            if constexpr (Q8) {
+                ksc[0] = ksc[1];
+                ksc[1] = ksc[2];
+                ksc[2] = k_scale(ids[0][0]);
+                vsc[0] = vsc[1];
+                vsc[1] = vsc[2];
+                vsc[2] = vsc[3];
+                vsc[3] = v_scale(ids[0][0]);
+            }
+            shift(t + AHEAD);
         };
         auto mod3 = [](int x) { return x >= 3 ? x - 3 : x; };
         auto source = [&](bool is_v, int blk) {  // e4m3: the thread's piece of a page
@@ -1002,8 +1033,8 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
                         vx = codes[1][mod3(r + 2)][tid];
                         kx = codes[0][r][tid];
                     }
-                    if (N / 4 == s - S0) P::put_v(Vs[mod3(r + 2)], 64 * wave, lane, vx, vsc);
-                    if (2 * N / 4 == s - S0) P::put_k(Ks[r], 64 * wave, lane, kx, ksc);
+                    if (N / 4 == s - S0) P::put_v(Vs[mod3(r + 2)], 64 * wave, lane, vx, vsc[0]);
+                    if (2 * N / 4 == s - S0) P::put_k(Ks[r], 64 * wave, lane, kx, ksc[0]);
                     if (3 * N / 4 == s - S0) {
                         load_v(0, t + 5, mod3(r + 2), ids[1]);
                         load_k(0, t + 6, r, ids[0]);
@@ -1038,29 +1069,30 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
         wait_vmcnt<0>();  // Q: the compiler then has no loads of its own pending
         shift(0);
         if constexpr (Q8) {
-            const int b0 = ids[0][0];
-            shift(1);
-            const int b1 = ids[0][0];
-            shift(2);
-            load_v(0, 1, 1, ids[1]);
-            load_k(0, 2, 2, ids[0]);
-            shift(3);
-            load_v(0, 2, 2, ids[1]);
-            load_k(0, 3, 0, ids[0]);
-            shift(4);
-            load_v(0, 3, 0, ids[1]);
-            load_k(0, 4, 1, ids[0]);
-            const u32x4 k0 = *reinterpret_cast<const u32x4*>(source(false, b0));
-            u32x4 v0 = *reinterpret_cast<const u32x4*>(source(true, b0));
-            const u32x4 k1 = *reinterpret_cast<const u32x4*>(source(false, b1));
-            scales(b0, b0);
-            P::put_k(Ks[0], 64 * wave, lane, k0, ksc);
+            int b[5];
+#pragma unroll
+            for (int t = 0; t < 5; ++t) {
+                b[t] = ids[0][0];
+                shift(t + 1);
+            }
+            const int b1[LW] = {b[1]}, b2[LW] = {b[2]}, b3[LW] = {b[3]}, b4[LW] = {b[4]};
+            load_v(0, 1, 1, b1);
+            load_k(0, 2, 2, b2);
+            load_v(0, 2, 2, b2);
+            load_k(0, 3, 0, b3);
+            load_v(0, 3, 0, b3);
+            load_k(0, 4, 1, b4);
+            const u32x4 k0 = *reinterpret_cast<const u32x4*>(source(false, b[0]));
+            u32x4 v0 = *reinterpret_cast<const u32x4*>(source(true, b[0]));
+            const u32x4 k1 = *reinterpret_cast<const u32x4*>(source(false, b[1]));
+#pragma unroll
+            for (int x = 0; x < 3; ++x) ksc[x] = k_scale(b[2 + x]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) vsc[x] = v_scale(b[1 + x]);
+            P::put_k(Ks[0], 64 * wave, lane, k0, k_scale(b[0]));
             if (it.edge(it.key0(0))) odd |= P::settle_v(64 * wave, lane, v0, it.key0(0), it.key_end);
-            P::put_v(Vs[0], 64 * wave, lane, v0, vsc);
-            scales(b1, b1);
-            P::put_k(Ks[1], 64 * wave, lane, k1, ksc);
-            scales(ids[2][0], b1);  // of K(2) and V(1)
-            shift(5);
+            P::put_v(Vs[0], 64 * wave, lane, v0, v_scale(b[0]));
+            P::put_k(Ks[1], 64 * wave, lane, k1, k_scale(b[1]));
             wait_lgkmcnt0();
         } else {
 #pragma unroll
@@ -1083,22 +1115,17 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
             if constexpr (!Q8) settle(0, 0);
             barrier_only();
         }
-        // ids[0] is that of tile t + AHEAD here and below, t = -1 to begin with
-        auto next = [&](int t) {
-            if constexpr (Q8) scales(ids[2][0], ids[3][0]);  // of K(t + 4) and V(t + 3)
-            shift(t + AHEAD + 1);
-        };
         read(-1, 2, VG);
         read(-1, 2, VG + 1);
         products(-1, 2, std::integral_constant<int, VG>{});
         if constexpr (!Q8) {
             if (!behind) settle(0, 0);
         }
-        next(-1);
         if constexpr (Q8) wait_lgkmcnt0();
         barrier_only();
         for (int t = 0, r = 0; t < n_tiles; ++t, r = mod3(r + 1)) {
             // P1
+            next(t);
             if constexpr (Q8) settle(t + 2, mod3(r + 2));
             rows.template softmax<GROUP>(sc, pf, it, it.key0(t), sl2, col, grp);
             // all of it before the barrier: the compiler would put the second
@@ -1124,7 +1151,6 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
                     settle(t + 1, 0);
                 }
             }
-            next(t);
             if (t + 1 == n_tiles) wait_vmcnt<0>();  // nothing in flight into the next item's buffers
             if constexpr (Q8) wait_lgkmcnt0();
             barrier_only();
