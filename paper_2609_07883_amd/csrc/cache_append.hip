@@ -38,12 +38,28 @@ __device__ __forceinline__ int scale_exp(float s) {
     return min(max(static_cast<int>((__float_as_uint(s) >> 23) & 0xFFu) - 127, kMinExp), kMaxExp);
 }
 
-// Code of one bf16 value.  At e = 120 a code of 256 would stand for 2^128,
-// which is no finite float: the largest there is 240.
-__device__ __forceinline__ uint32_t quantise(uint32_t b, float inv, float lim) {
+// Codes of two bf16 values (a word's low and high half) in the low half of the
+// result, the other half kept from `keep`, or in the high half.  Nothing to
+// clamp: |x| 2^-e <= 448.
+template <bool HIGH>
+__device__ __forceinline__ uint32_t quantise2(uint32_t w, float inv, uint32_t keep) {
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(w << 16) * inv,
+                                                                 __uint_as_float(w & 0xFFFF0000u) * inv,
+                                                                 static_cast<int>(keep), HIGH));
+}
+__device__ __forceinline__ uint32_t quantise4(uint32_t w0, uint32_t w1, float inv) {
+    return quantise2<true>(w1, inv, quantise2<false>(w0, inv, 0u));
+}
+// Any value, where some are not finite or e is kMaxExp: there a code of 256
+// would stand for 2^128, which is no finite float, and the largest is 240.
+__device__ __forceinline__ uint32_t quantise_any(uint32_t b, float inv, float lim) {
     const float x = fminf(fmaxf(__uint_as_float(b << 16) * inv, -lim), lim);
     const uint32_t c = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x, 0.f, 0, false)) & 0xFFu;
     return not_finite(b) ? 0x7Fu : c;
+}
+__device__ __forceinline__ uint32_t quantise4_any(uint32_t w0, uint32_t w1, float inv, float lim) {
+    return quantise_any(w0 & 0xFFFFu, inv, lim) | quantise_any(w0 >> 16, inv, lim) << 8 |
+           quantise_any(w1 & 0xFFFFu, inv, lim) << 16 | quantise_any(w1 >> 16, inv, lim) << 24;
 }
 // Code at a scale 1 / f times as large (f <= 1).
 __device__ __forceinline__ uint32_t requantise(uint32_t c, float f) {
@@ -56,10 +72,39 @@ __device__ __forceinline__ uint32_t requantise4(uint32_t c, float f) {
            requantise(c >> 24, f) << 24;
 }
 
+// Largest value of the wave, in every lane: rotations within the rows of 16
+// lanes, then row swaps.
 __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
+    v = max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x128, 0xF, 0xF, false)));  // row_ror:8
+    v = max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x124, 0xF, 0xF, false)));
+    v = max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x122, 0xF, 0xF, false)));
+    v = max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x121, 0xF, 0xF, false)));
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max(b[0], b[1]);
+}
+
+// Largest magnitude of the wave's words of two bf16 values.  Magnitudes that
+// are not finite lie above all finite ones, so one pass tells whether there
+// are any (`odd`), and only then a second one leaves them out.
+template <int N>
+__device__ __forceinline__ uint32_t block_max(const uint32_t (&w)[N], bool& odd) {
+    uint32_t hi = 0, lo = 0;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), o, kWave)));
-    return v;
+    for (int i = 0; i < N; ++i) {
+        hi = max(hi, w[i] & 0x7FFF0000u);
+        lo = max(lo, w[i] & 0x7FFFu);
+    }
+    uint32_t m = wave_umax(max(hi >> 16, lo));
+    odd = m >= 0x7F80u;
+    if (odd) {
+        m = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) m = max(m, max(magnitude(w[i] & 0xFFFFu), magnitude(w[i] >> 16)));
+        m = wave_umax(m);
+    }
+    return m;
 }
 
 struct Item {
@@ -73,43 +118,79 @@ __device__ __forceinline__ void append_k8(const AppendArgs& a, const Item& it, i
     const bool fresh = t >= it.t0 && t < it.t0 + it.n, older = t < it.t0;
     const size_t bh = static_cast<size_t>(it.blk) * a.cache.hkv + kvh;
     uint32_t* page = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.cache.k_pool) + bh * HD * 16);
-    u32x4 x[S][2] = {}, held[S] = {};
+    const float s_old = a.cache.k_scale[bh];
+    alignas(16) uint32_t x[S * 8] = {};
     const uint16_t* row = static_cast<const uint16_t*>(a.k) + static_cast<size_t>(it.row0 + t - it.t0) * a.ld + kvh * HD;
+    if (fresh) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
+        for (int s = 0; s < S; ++s) {
+            *reinterpret_cast<u32x4*>(x + 8 * s) = *reinterpret_cast<const u32x4*>(row + 64 * s + 16 * c);
+            *reinterpret_cast<u32x4*>(x + 8 * s + 4) = *reinterpret_cast<const u32x4*>(row + 64 * s + 16 * c + 8);
+        }
+    }
+    bool odd;
+    int e = block_exp(block_max(x, odd));
+    const int e_old = it.t0 > 0 ? scale_exp(s_old) : kMinExp;
+    e = max(e, e_old);
+    const float inv = pow2(-e);
+    if (odd || e >= kMaxExp) {
+        const float lim = e >= kMaxExp ? 240.f : 448.f;
         if (fresh) {
-            x[s][0] = *reinterpret_cast<const u32x4*>(row + 64 * s + 16 * c);
-            x[s][1] = *reinterpret_cast<const u32x4*>(row + 64 * s + 16 * c + 8);
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                u32x4 out;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) out[w] = quantise4_any(x[8 * s + 2 * w], x[8 * s + 2 * w + 1], inv, lim);
+                *reinterpret_cast<u32x4*>(page + s * 256 + lane * 4) = out;
+            }
         }
-        if (older) held[s] = *reinterpret_cast<const u32x4*>(page + s * 256 + lane * 4);
-    }
-    uint32_t amax = 0;
+    } else if (fresh) {
 #pragma unroll
-    for (int s = 0; s < S; ++s)
+        for (int s = 0; s < S; ++s) {
+            u32x4 out;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-                amax = max(amax, max(magnitude(x[s][h][w] & 0xFFFFu), magnitude(x[s][h][w] >> 16)));
-    int e = block_exp(wave_umax(amax)), e_old = kMinExp;
-    if (it.t0 > 0) {
-        e_old = scale_exp(a.cache.k_scale[bh]);
-        e = max(e, e_old);
-    }
-    const float inv = pow2(-e), lim = e >= kMaxExp ? 240.f : 448.f, f = pow2(max(e_old - e, -126));
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-        u32x4 out;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const uint32_t p = x[s][w >> 1][(w & 1) * 2], q = x[s][w >> 1][(w & 1) * 2 + 1];
-            out[w] = quantise(p & 0xFFFFu, inv, lim) | quantise(p >> 16, inv, lim) << 8 |
-                     quantise(q & 0xFFFFu, inv, lim) << 16 | quantise(q >> 16, inv, lim) << 24;
-            if (older) out[w] = requantise4(held[s][w], f);
+            for (int w = 0; w < 4; ++w) out[w] = quantise4(x[8 * s + 2 * w], x[8 * s + 2 * w + 1], inv);
+            *reinterpret_cast<u32x4*>(page + s * 256 + lane * 4) = out;
         }
-        if (fresh || (older && e > e_old)) *reinterpret_cast<u32x4*>(page + s * 256 + lane * 4) = out;
+    }
+    if (e > e_old && older) {
+        const float f = pow2(max(e_old - e, -126));
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            u32x4 held = *reinterpret_cast<const u32x4*>(page + s * 256 + lane * 4);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) held[w] = requantise4(held[w], f);
+            *reinterpret_cast<u32x4*>(page + s * 256 + lane * 4) = held;
+        }
     }
     if (lane == 0) a.cache.k_scale[bh] = pow2(e);
+}
+
+// A lane's dims of an item's rows: w[t / 2 * D + d] holds dim d of tokens t
+// (low half) and t + 1, counted from the block's first; 0 where there is no row.
+template <int D>
+__device__ __forceinline__ void load_dims(uint32_t (&w)[8 * D], const void* rows, const AppendArgs& a, const Item& it,
+                                          int kvh, int lane) {
+    const uint16_t* first = static_cast<const uint16_t*>(rows) + static_cast<size_t>(it.row0) * a.ld + kvh * (64 * D);
+    uint32_t x[16] = {};
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+        if (t >= it.t0 && t < it.t0 + it.n) {
+            const uint16_t* row = first + static_cast<size_t>(t - it.t0) * a.ld;
+            x[t] = D == 2 ? reinterpret_cast<const uint32_t*>(row)[lane] : row[lane];
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+        w[p * D] = (x[2 * p] & 0xFFFFu) | x[2 * p + 1] << 16;
+        if constexpr (D == 2) w[p * D + 1] = (x[2 * p] >> 16) | (x[2 * p + 1] & 0xFFFF0000u);
+    }
+}
+
+// Mask of the bytes of word w that are tokens t0 .. t0 + n - 1.
+__device__ __forceinline__ uint32_t token_bytes(int w, const Item& it) {
+    const uint32_t live = ((1u << (it.t0 + it.n)) - (1u << it.t0)) >> (4 * w) & 0xFu;
+    return ((live * 0x00204081u) & 0x01010101u) * 0xFFu;
 }
 
 template <int HD>
@@ -117,55 +198,51 @@ __device__ __forceinline__ void append_v8(const AppendArgs& a, const Item& it, i
     constexpr int D = HD / 64;  // dims of a lane
     const size_t bh = static_cast<size_t>(it.blk) * a.cache.hkv + kvh;
     u32x4* page = reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.cache.v_pool) + bh * HD * 16) + lane * D;
+    const float s_old = a.cache.v_scale[bh];
     u32x4 held[D] = {};
     if (it.n < 16) {
 #pragma unroll
         for (int d = 0; d < D; ++d) held[d] = page[d];
     }
-    uint32_t x[16][D], amax = 0;
+    uint32_t x[8 * D];
+    load_dims<D>(x, a.v, a, it, kvh, lane);
+    bool odd;
+    int e = block_exp(block_max(x, odd));
+    const int e_old = it.t0 > 0 ? scale_exp(s_old) : kMinExp;
+    e = max(e, e_old);
+    const float inv = pow2(-e);
+    u32x4 out[D];
+    if (odd || e >= kMaxExp) {
+        const float lim = e >= kMaxExp ? 240.f : 448.f;
 #pragma unroll
-    for (int t = 0; t < 16; ++t) {
+        for (int d = 0; d < D; ++d)
 #pragma unroll
-        for (int d = 0; d < D; ++d) x[t][d] = 0;
-        if (t >= it.t0 && t < it.t0 + it.n) {
-            const uint16_t* row = static_cast<const uint16_t*>(a.v) + static_cast<size_t>(it.row0 + t - it.t0) * a.ld + kvh * HD;
-            if constexpr (D == 2) {
-                const uint32_t b = reinterpret_cast<const uint32_t*>(row)[lane];
-                x[t][0] = b & 0xFFFFu;
-                x[t][1] = b >> 16;
-            } else {
-                x[t][0] = row[lane];
+            for (int w = 0; w < 4; ++w) out[d][w] = quantise4_any(x[2 * w * D + d], x[(2 * w + 1) * D + d], inv, lim);
+    } else {
+#pragma unroll
+        for (int d = 0; d < D; ++d)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) out[d][w] = quantise4(x[2 * w * D + d], x[(2 * w + 1) * D + d], inv);
+    }
+    if (it.n < 16) {
+        if (e > e_old && it.t0 > 0) {
+            const float f = pow2(max(e_old - e, -126));
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t before = token_bytes(w, Item{0, 0, it.t0, 0});
+#pragma unroll
+                for (int d = 0; d < D; ++d) held[d][w] = (requantise4(held[d][w], f) & before) | (held[d][w] & ~before);
             }
         }
-    }
-#pragma unroll
-    for (int t = 0; t < 16; ++t)
-#pragma unroll
-        for (int d = 0; d < D; ++d) amax = max(amax, magnitude(x[t][d]));
-    int e = block_exp(wave_umax(amax)), e_old = kMinExp;
-    if (it.t0 > 0) {
-        e_old = scale_exp(a.cache.v_scale[bh]);
-        e = max(e, e_old);
-    }
-    const float inv = pow2(-e), lim = e >= kMaxExp ? 240.f : 448.f, f = pow2(max(e_old - e, -126));
-#pragma unroll
-    for (int d = 0; d < D; ++d) {
-        u32x4 out;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            uint32_t word = 0;
+            const uint32_t m = token_bytes(w, it);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = 4 * w + i;
-                const uint32_t c = (held[d][w] >> (8 * i)) & 0xFFu;
-                const uint32_t v = t < it.t0 ? (e > e_old ? requantise(c, f) : c)
-                                   : t < it.t0 + it.n ? quantise(x[t][d], inv, lim) : c;
-                word |= v << (8 * i);
-            }
-            out[w] = word;
+            for (int d = 0; d < D; ++d) out[d][w] = (out[d][w] & m) | (held[d][w] & ~m);
         }
-        page[d] = out;
     }
+#pragma unroll
+    for (int d = 0; d < D; ++d) page[d] = out[d];
     if (lane == 0) a.cache.v_scale[bh] = pow2(e);
 }
 
@@ -175,27 +252,32 @@ __device__ __forceinline__ void append_k16(const AppendArgs& a, const Item& it, 
     if (t < it.t0 || t >= it.t0 + it.n) return;
     uint16_t* page = static_cast<uint16_t*>(a.cache.k_pool) + (static_cast<size_t>(it.blk) * a.cache.hkv + kvh) * HD * 16;
     const uint16_t* row = static_cast<const uint16_t*>(a.k) + static_cast<size_t>(it.row0 + t - it.t0) * a.ld + kvh * HD;
+    u32x4 x[HD / 32];
 #pragma unroll
-    for (int s = 0; s < HD / 32; ++s)
-        *reinterpret_cast<u32x4*>(page + s * 512 + lane * 8) = *reinterpret_cast<const u32x4*>(row + 32 * s + 8 * c);
+    for (int s = 0; s < HD / 32; ++s) x[s] = *reinterpret_cast<const u32x4*>(row + 32 * s + 8 * c);
+#pragma unroll
+    for (int s = 0; s < HD / 32; ++s) *reinterpret_cast<u32x4*>(page + s * 512 + lane * 8) = x[s];
 }
 
 template <int HD>
 __device__ __forceinline__ void append_v16(const AppendArgs& a, const Item& it, int kvh, int lane) {
-    uint16_t* page = static_cast<uint16_t*>(a.cache.v_pool) + (static_cast<size_t>(it.blk) * a.cache.hkv + kvh) * HD * 16;
-    const uint16_t* v = static_cast<const uint16_t*>(a.v) + static_cast<size_t>(it.row0) * a.ld + kvh * HD;
+    constexpr int D = HD / 64;
+    uint16_t* page = static_cast<uint16_t*>(a.cache.v_pool) + (static_cast<size_t>(it.blk) * a.cache.hkv + kvh) * HD * 16 +
+                     lane * D * 16;
+    uint32_t x[8 * D];
+    load_dims<D>(x, a.v, a, it, kvh, lane);
 #pragma unroll
-    for (int d = lane; d < HD; d += kWave) {
+    for (int d = 0; d < D; ++d) {
         if (it.n == 16) {
             u32x4 out[2];
 #pragma unroll
-            for (int w = 0; w < 8; ++w)
-                out[w >> 2][w & 3] = v[static_cast<size_t>(2 * w) * a.ld + d] |
-                                     static_cast<uint32_t>(v[static_cast<size_t>(2 * w + 1) * a.ld + d]) << 16;
+            for (int w = 0; w < 8; ++w) out[w >> 2][w & 3] = x[w * D + d];
             *reinterpret_cast<u32x4*>(page + d * 16) = out[0];
             *reinterpret_cast<u32x4*>(page + d * 16 + 8) = out[1];
         } else {
-            for (int j = 0; j < it.n; ++j) page[d * 16 + it.t0 + j] = v[static_cast<size_t>(j) * a.ld + d];
+#pragma unroll
+            for (int t = 0; t < 16; ++t)
+                if (t >= it.t0 && t < it.t0 + it.n) page[d * 16 + t] = static_cast<uint16_t>(x[t / 2 * D + d] >> (16 * (t & 1)));
         }
     }
 }

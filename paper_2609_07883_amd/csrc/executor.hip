@@ -15,7 +15,6 @@
 #include <memory>
 #include <mutex>
 #include <random>
-#include <unordered_set>
 #include <vector>
 
 #include "attn_plan.h"
@@ -58,6 +57,8 @@ struct slw_ctx {
     std::vector<int32_t> last_slots;
     std::vector<int32_t> slots_build;  // slots of the iteration being built
     std::vector<Prefill> prefills;     // the iteration's prefills in row order
+    // the batch's sequences and the lengths they need: prefills, then decodes
+    std::vector<std::pair<KvManager::Seq*, int32_t>> batch_seqs;
     std::vector<int32_t> meta;  // host build area
     DecodePlan dplan;           // attention work of one class of layers (host build areas)
     ChunkPlan cplan;
@@ -270,8 +271,8 @@ int ensure_stage_events(slw_ctx* ctx) {
 }
 
 // Validates a batch with rows: ctx->prefills receives its prefills in row
-// order, req the reservations it needs (sequence, length).
-int check_batch(slw_ctx* ctx, const slw_batch* bt, std::vector<std::pair<int64_t, int32_t>>& req) {
+// order, ctx->batch_seqs its sequences and the lengths to reserve.
+int check_batch(slw_ctx* ctx, const slw_batch* bt) {
     const slw_model_cfg& c = ctx->cfg;
     const int C = bt->C, B = bt->B;
     if (B > 0 && (!bt->decode_seqs || !bt->context_lens)) return fail(SLW_EINVAL, "null decode arrays");
@@ -290,33 +291,34 @@ int check_batch(slw_ctx* ctx, const slw_batch* bt, std::vector<std::pair<int64_t
     } else if (C > 0) {
         pre.push_back({bt->prefill_seq, bt->prefix_len, C, 0});
     }
-    req.reserve(B + pre.size());
-    std::unordered_set<int64_t> seen;
-    seen.reserve(2 * (B + pre.size()) + 2);
+    auto& seqs = ctx->batch_seqs;
+    seqs.clear();
+    seqs.reserve(B + pre.size());
+    const uint64_t batch = ctx->kv.next_batch();  // a sequence that carries it was named before
     for (const Prefill& f : pre) {
         if (f.prefix < 0) return fail(SLW_EINVAL, "negative prefix_len");
         if (static_cast<int64_t>(f.prefix) + f.c > c.max_pos) return fail(SLW_ERANGE, "prefix_len + chunk exceeds max_pos");
-        if (!ctx->kv.exists(f.seq)) return fail(SLW_EINVAL, "prefill sequence %lld unknown", (long long)f.seq);
-        if (!seen.insert(f.seq).second)
-            return fail(SLW_EINVAL, "sequence %lld appears twice in the batch", (long long)f.seq);
-        if (ctx->kv.reserved(f.seq) < f.prefix)
+        KvManager::Seq* q = ctx->kv.find(f.seq);
+        if (!q) return fail(SLW_EINVAL, "prefill sequence %lld unknown", (long long)f.seq);
+        if (q->batch == batch) return fail(SLW_EINVAL, "sequence %lld appears twice in the batch", (long long)f.seq);
+        q->batch = batch;
+        if (q->reserved < f.prefix)
             return fail(SLW_EINVAL, "prefill sequence %lld holds %d positions, prefix_len is %d", (long long)f.seq,
-                        ctx->kv.reserved(f.seq), f.prefix);
-        req.emplace_back(f.seq, f.prefix + f.c);
+                        q->reserved, f.prefix);
+        seqs.emplace_back(q, f.prefix + f.c);
     }
-    {
-        for (int b = 0; b < B; ++b) {
-            const int64_t id = bt->decode_seqs[b];
-            const int32_t L = bt->context_lens[b];
-            if (!ctx->kv.exists(id)) return fail(SLW_EINVAL, "decode sequence %lld unknown", (long long)id);
-            if (!seen.insert(id).second)
-                return fail(SLW_EINVAL, "sequence %lld appears twice in the batch", (long long)id);
-            if (L < 0 || L + 1 > c.max_pos) return fail(SLW_ERANGE, "context_len %d out of range", L);
-            if (ctx->kv.reserved(id) < L)
-                return fail(SLW_EINVAL, "decode sequence %lld holds %d positions, context_len is %d",
-                            (long long)id, ctx->kv.reserved(id), L);
-            req.emplace_back(id, L + 1);
-        }
+    for (int b = 0; b < B; ++b) {
+        const int64_t id = bt->decode_seqs[b];
+        const int32_t L = bt->context_lens[b];
+        KvManager::Seq* q = ctx->kv.find(id);
+        if (!q) return fail(SLW_EINVAL, "decode sequence %lld unknown", (long long)id);
+        if (q->batch == batch) return fail(SLW_EINVAL, "sequence %lld appears twice in the batch", (long long)id);
+        q->batch = batch;
+        if (L < 0 || L + 1 > c.max_pos) return fail(SLW_ERANGE, "context_len %d out of range", L);
+        if (q->reserved < L)
+            return fail(SLW_EINVAL, "decode sequence %lld holds %d positions, context_len is %d", (long long)id,
+                        q->reserved, L);
+        seqs.emplace_back(q, L + 1);
     }
     return SLW_OK;
 }
@@ -346,8 +348,7 @@ int mixed_iteration_impl(slw_ctx* ctx, const slw_batch* bt, const void* x_in, vo
     for (int l = 0; l < c.n_layers; ++l)
         if (!ctx->have_w[l]) return fail(SLW_EINVAL, "weights of layer %d not set", l);
     if (!x_in || !x_out || !ws) return fail(SLW_EINVAL, "null device buffer");
-    std::vector<std::pair<int64_t, int32_t>> req;
-    int rc = check_batch(ctx, bt, req);
+    int rc = check_batch(ctx, bt);
     if (rc) return rc;
     Layout L = layout(*ctx, C, B);
     const LayerPlans plans = plan_layer(c, C + B);
@@ -374,7 +375,7 @@ int mixed_iteration_impl(slw_ctx* ctx, const slw_batch* bt, const void* x_in, vo
         }
     }
     KvManager::Undo undo;
-    rc = ctx->kv.reserve_all(req, &undo);
+    rc = ctx->kv.reserve_batch(ctx->batch_seqs, &undo);
     if (rc) return rc;
     rc = enqueue_iteration(ctx, bt, x_in, x_out, ws, L, plans, stream, no_alloc);
     if (rc) ctx->kv.rollback(undo);
@@ -414,7 +415,7 @@ int build_attn_meta(slw_ctx* ctx, const slw_batch* bt, std::vector<int32_t>& m, 
     am.bt = m.size();
     for (int b = 0; b < B; ++b) {
         m[am.btoff + b] = static_cast<int32_t>(m.size() - am.bt);
-        const auto& t = ctx->kv.table(bt->decode_seqs[b]);
+        const auto& t = ctx->batch_seqs[pre.size() + b].first->blocks;
         const int nb = static_cast<int>(ceil_div(bt->context_lens[b] + 1, 16));
         m.insert(m.end(), t.begin(), t.begin() + nb);
     }
@@ -424,7 +425,7 @@ int build_attn_meta(slw_ctx* ctx, const slw_batch* bt, std::vector<int32_t>& m, 
     std::vector<int32_t> pre_bt(pre.size());
     for (size_t i = 0; i < pre.size(); ++i) {
         pre_bt[i] = static_cast<int32_t>(m.size() - am.pre);
-        const auto& t = ctx->kv.table(pre[i].seq);
+        const auto& t = ctx->batch_seqs[i].first->blocks;
         const int nb = static_cast<int>(ceil_div(pre[i].prefix + pre[i].c, 16));
         m.insert(m.end(), t.begin(), t.begin() + nb);
     }
@@ -443,8 +444,9 @@ int build_attn_meta(slw_ctx* ctx, const slw_batch* bt, std::vector<int32_t>& m, 
     put(qt_bt);
     // [4][n_app]: block, first new token, new tokens, first row of each block appended to
     std::vector<int32_t> app[4];
-    auto add = [&](int64_t seq, int at, int n, int row) {
-        const auto& t = ctx->kv.table(seq);
+    for (auto& v : app) v.reserve(append_cap(C, B));
+    auto add = [&](const KvManager::Seq* q, int at, int n, int row) {
+        const auto& t = q->blocks;
         for (const int end = at + n; at < end;) {
             const int k = std::min(16 - at % 16, end - at);
             app[0].push_back(t[at / 16]);
@@ -455,8 +457,8 @@ int build_attn_meta(slw_ctx* ctx, const slw_batch* bt, std::vector<int32_t>& m, 
             row += k;
         }
     };
-    for (const Prefill& f : pre) add(f.seq, f.prefix, f.c, f.row0);
-    for (int b = 0; b < B; ++b) add(bt->decode_seqs[b], bt->context_lens[b], 1, C + b);
+    for (size_t i = 0; i < pre.size(); ++i) add(ctx->batch_seqs[i].first, pre[i].prefix, pre[i].c, pre[i].row0);
+    for (int b = 0; b < B; ++b) add(ctx->batch_seqs[pre.size() + b].first, bt->context_lens[b], 1, C + b);
     am.n_app = static_cast<int>(app[0].size());
     if (app[0].size() > append_cap(C, B)) return fail(SLW_EINVAL, "internal: %d blocks to append to above cap", am.n_app);
     am.app = m.size();
@@ -623,9 +625,9 @@ int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void*
     // slot[M], pos[M]
     std::vector<int32_t>& slots = ctx->slots_build;
     slots.resize(M);
-    for (const Prefill& f : pre)
-        for (int j = 0; j < f.c; ++j) slots[f.row0 + j] = ctx->kv.slot(f.seq, f.prefix + j);
-    for (int b = 0; b < B; ++b) slots[C + b] = ctx->kv.slot(bt->decode_seqs[b], bt->context_lens[b]);
+    for (size_t i = 0; i < pre.size(); ++i)
+        for (int j = 0; j < pre[i].c; ++j) slots[pre[i].row0 + j] = ctx->batch_seqs[i].first->slot(pre[i].prefix + j, 16);
+    for (int b = 0; b < B; ++b) slots[C + b] = ctx->batch_seqs[pre.size() + b].first->slot(bt->context_lens[b], 16);
     if (ctx->k_scale)  // the QKV projection writes its rows to pages of their own
         for (int r = 0; r < M; ++r) m.push_back(r);
     else
@@ -995,8 +997,7 @@ extern "C" int slw_attn_begin(slw_ctx* ctx, const slw_batch* batch, void* ws, si
             *out = plan.release();
             return SLW_OK;
         }
-        std::vector<std::pair<int64_t, int32_t>> req;
-        int rc = check_batch(ctx, batch, req);
+        int rc = check_batch(ctx, batch);
         if (rc) return rc;
         const AttnLayout L = attn_layout(*ctx, C, B);
         if (!ws) return fail(SLW_EINVAL, "null workspace");
@@ -1011,7 +1012,7 @@ extern "C" int slw_attn_begin(slw_ctx* ctx, const slw_batch* batch, void* ws, si
         }
         if ((rc = ensure_hip(ctx))) return rc;
         KvManager::Undo undo;
-        if ((rc = ctx->kv.reserve_all(req, &undo))) return rc;
+        if ((rc = ctx->kv.reserve_batch(ctx->batch_seqs, &undo))) return rc;
         plan->part = L.part;
         auto upload = [&]() -> int {
             std::vector<int32_t>& m = ctx->meta;

@@ -30,54 +30,55 @@ int KvManager::release(int64_t id) {
     return SLW_OK;
 }
 
+void KvManager::grow(Seq& s, int32_t len, Undo* undo) {
+    if (len < s.reserved) len = s.reserved;
+    const int64_t need = ceil_div(len, block_size_) - static_cast<int64_t>(s.blocks.size());
+    if (undo) undo->grown.push_back({&s, s.blocks.size(), s.reserved});
+    for (int64_t i = 0; i < need; ++i) {
+        s.blocks.push_back(free_.top());
+        free_.pop();
+    }
+    s.reserved = len;
+}
+
 int KvManager::reserve_all(const std::vector<std::pair<int64_t, int32_t>>& req, Undo* undo) {
     if (undo) undo->grown.clear();
-    // Largest request per sequence, then the total number of new blocks.
-    std::unordered_map<int64_t, int32_t> want;
+    // Largest request per sequence, in request order so block ids are deterministic.
+    std::vector<std::pair<Seq*, int32_t>> want;
+    std::unordered_map<Seq*, size_t> at;
     for (const auto& r : req) {
-        auto it = seqs_.find(r.first);
-        if (it == seqs_.end()) return fail(SLW_EINVAL, "sequence %lld unknown", (long long)r.first);
+        Seq* s = find(r.first);
+        if (!s) return fail(SLW_EINVAL, "sequence %lld unknown", (long long)r.first);
         if (r.second < 0) return fail(SLW_EINVAL, "negative length for sequence %lld", (long long)r.first);
-        auto w = want.find(r.first);
-        if (w == want.end()) want.emplace(r.first, r.second);
-        else if (r.second > w->second) w->second = r.second;
+        const auto w = at.emplace(s, want.size());
+        if (w.second) want.emplace_back(s, r.second);
+        else if (r.second > want[w.first->second].second) want[w.first->second].second = r.second;
     }
+    return reserve_batch(want, undo);
+}
+
+int KvManager::reserve_batch(const std::vector<std::pair<Seq*, int32_t>>& req, Undo* undo) {
+    if (undo) undo->grown.clear();
     int64_t total = 0;
-    for (const auto& w : want) {
-        const Seq& s = seqs_.at(w.first);
-        int64_t len = w.second > s.reserved ? w.second : s.reserved;
-        int64_t need = ceil_div(len, block_size_) - static_cast<int64_t>(s.blocks.size());
+    for (const auto& r : req) {
+        const int64_t len = r.second > r.first->reserved ? r.second : r.first->reserved;
+        const int64_t need = ceil_div(len, block_size_) - static_cast<int64_t>(r.first->blocks.size());
         if (need > 0) total += need;
     }
     if (total > static_cast<int64_t>(free_.size()))
         return fail(SLW_ENOMEM, "KV pool exhausted: need %lld blocks, %d free", (long long)total,
                     free_count());
-    // Grow in request order so block ids are deterministic.
-    for (const auto& r : req) {
-        auto w = want.find(r.first);
-        if (w == want.end()) continue;  // already grown
-        Seq& s = seqs_.at(r.first);
-        int32_t len = w->second > s.reserved ? w->second : s.reserved;
-        int64_t need = ceil_div(len, block_size_) - static_cast<int64_t>(s.blocks.size());
-        if (undo) undo->grown.push_back({r.first, s.blocks.size(), s.reserved});
-        for (int64_t i = 0; i < need; ++i) {
-            s.blocks.push_back(free_.top());
-            free_.pop();
-        }
-        s.reserved = len;
-        want.erase(w);
-    }
+    for (const auto& r : req) grow(*r.first, r.second, undo);
     return SLW_OK;
 }
 
 void KvManager::rollback(const Undo& undo) {
     for (auto e = undo.grown.rbegin(); e != undo.grown.rend(); ++e) {
-        Seq& s = seqs_.at(e->id);
-        while (s.blocks.size() > e->blocks) {
-            free_.push(s.blocks.back());
-            s.blocks.pop_back();
+        while (e->seq->blocks.size() > e->blocks) {
+            free_.push(e->seq->blocks.back());
+            e->seq->blocks.pop_back();
         }
-        s.reserved = e->reserved;
+        e->seq->reserved = e->reserved;
     }
 }
 

@@ -15,12 +15,26 @@ namespace slw {
 
 class KvManager {
 public:
+    struct Seq {
+        std::vector<int32_t> blocks;
+        int32_t reserved = 0;
+        uint64_t batch = 0;  // the last batch that named it (next_batch)
+        int32_t slot(int32_t pos, int32_t block_size) const {
+            return blocks[pos / block_size] * block_size + pos % block_size;
+        }
+    };
     void reset(int32_t num_blocks, int32_t block_size);
     int32_t num_blocks() const { return num_blocks_; }
     int32_t block_size() const { return block_size_; }
     int32_t free_count() const { return static_cast<int32_t>(free_.size()); }
 
     bool exists(int64_t id) const { return seqs_.count(id) != 0; }
+    // The sequence, or null.  Stays where it is until it is released.
+    Seq* find(int64_t id) {
+        const auto it = seqs_.find(id);
+        return it == seqs_.end() ? nullptr : &it->second;
+    }
+    uint64_t next_batch() { return ++batch_; }
     // Each returns an SLW_* code (and sets the error message on failure).
     int create(int64_t id);
     int release(int64_t id);
@@ -28,7 +42,7 @@ public:
     // reserved length before the call.
     struct Undo {
         struct Entry {
-            int64_t id;
+            Seq* seq;
             size_t blocks;
             int32_t reserved;
         };
@@ -37,22 +51,17 @@ public:
     // Grows every (id, new_len) in order; all or nothing.  With `undo`, the
     // changes are recorded so that rollback() can return them.
     int reserve_all(const std::vector<std::pair<int64_t, int32_t>>& req, Undo* undo = nullptr);
+    // The same for distinct sequences already looked up.
+    int reserve_batch(const std::vector<std::pair<Seq*, int32_t>>& req, Undo* undo);
     // Returns the blocks a reservation took and restores the lengths; the
     // free set, and so every later allocation, is as before the reservation.
     void rollback(const Undo& undo);
 
     const std::vector<int32_t>& table(int64_t id) const { return seqs_.at(id).blocks; }
-    int32_t reserved(int64_t id) const { return seqs_.at(id).reserved; }
-    int32_t slot(int64_t id, int32_t pos) const {
-        const auto& bt = seqs_.at(id).blocks;
-        return bt[pos / block_size_] * block_size_ + pos % block_size_;
-    }
 
 private:
-    struct Seq {
-        std::vector<int32_t> blocks;
-        int32_t reserved = 0;
-    };
+    void grow(Seq& s, int32_t len, Undo* undo);
+    uint64_t batch_ = 0;
     int32_t num_blocks_ = 0;
     int32_t block_size_ = 16;
     std::priority_queue<int32_t, std::vector<int32_t>, std::greater<int32_t>> free_;
