@@ -25,6 +25,9 @@ constexpr int kChunkMinTiles = 4;
 // Whole query tiles per work-group when the largest group's load is within
 // 11/10 of an equal share.
 constexpr int64_t kChunkWholeSlackNum = 11, kChunkWholeSlackDen = 10;
+// Cache kernels: what splitting query tiles costs, in 64-key tiles (plan_chunk);
+// an item costs kItemTiles5 / 5 for every 1024 values of a row.
+constexpr int64_t kMergeTiles = 4, kItemTiles5 = 2;
 // Work items of at least kTwoPhaseTiles + kTwoPhaseTilesPer64 (positions of a
 // query tile, at least 64, / 64) 64-key tiles on average run the two-phase
 // chunk kernel at head dim 128.  Its fill and extra phases are paid per item,
@@ -160,7 +163,14 @@ int plan_decode(const slw_model_cfg& c, const Window& w, int B, const int32_t* c
 // equal runs, one per work-group of each kv head; a run that crosses query
 // tiles becomes one item per query tile it touches.  Items stay in query-tile
 // order; slot_items lists each work-group's items.
-int plan_chunk(const slw_model_cfg& c, const Window& w, int C, const std::vector<int32_t>& qt_pos0,
+//
+// Layers on the cache kernels (`cache`) weigh the two instead: whole query
+// tiles on up to one work-group each against equal runs, whose partial sums are
+// written and merged.  In units of a 64-key tile (about 1.2 us), the merge's
+// launch takes 4 and an item of 1024 values a row (all kv heads) 0.4: four
+// prompts of 1500 rows under a window of 512 took 40 + 16 us (merge) in equal
+// runs and 35 + 4 us whole; 77 rows at 50, two query tiles, 14 against 20.
+int plan_chunk(const slw_model_cfg& c, const Window& w, bool cache, int C, const std::vector<int32_t>& qt_pos0,
                const std::vector<int32_t>& qt_rows, ChunkPlan& p) {
     const int n_qt = static_cast<int>(qt_pos0.size());
     p.items.clear();
@@ -178,12 +188,13 @@ int plan_chunk(const slw_model_cfg& c, const Window& w, int C, const std::vector
     if (n_qt > 0) {
         const int64_t want = std::min<int64_t>(chunk_slot_cap(c), std::max<int64_t>(1, total_tiles / kChunkMinTiles));
         const int64_t per = ceil_div(total_tiles, want);
-        if (n_qt >= want) {
+        const int64_t spread = cache ? std::min<int64_t>(n_qt, chunk_slot_cap(c)) : want;  // work-groups for whole tiles
+        if (cache || n_qt >= want) {
             std::vector<int32_t> order(n_qt);
             for (int q = 0; q < n_qt; ++q) order[q] = q;
             auto len = [&](int q) { return tile_end[q + 1] - tile_end[q]; };
             std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return len(x) > len(y); });
-            std::vector<int64_t> load(want, 0);
+            std::vector<int64_t> load(spread, 0);
             std::vector<int32_t> owner(n_qt);
             for (int q : order) {
                 const int g = static_cast<int>(std::min_element(load.begin(), load.end()) - load.begin());
@@ -191,9 +202,14 @@ int plan_chunk(const slw_model_cfg& c, const Window& w, int C, const std::vector
                 owner[q] = g;
             }
             const int64_t mx = *std::max_element(load.begin(), load.end());
-            if (mx * kChunkWholeSlackDen <= per * kChunkWholeSlackNum) {
+            bool whole = mx * kChunkWholeSlackDen <= per * kChunkWholeSlackNum;
+            if (cache) {
+                const int64_t runs = ceil_div(total_tiles, per);
+                whole = mx <= per + kMergeTiles + kItemTiles5 * (n_qt + runs - 1) * c.n_kv_heads * c.head_dim / (5 * 1024);
+            }
+            if (whole) {
                 p.whole = true;
-                n_slots = static_cast<int>(want);
+                n_slots = static_cast<int>(spread);
                 for (int q = 0; q < n_qt; ++q) {
                     it.push_back(q);
                     it.push_back(0);

@@ -56,7 +56,7 @@ void query_tiles(const slw_model_cfg& c, const std::vector<Prefill>& pre, std::v
                  std::vector<int32_t>& rows, std::vector<int32_t>& pos0, std::vector<int32_t>* bt,
                  const std::vector<int32_t>& bt_of_prefill);
 int plan_decode(const slw_model_cfg& c, const Window& w, int B, const int32_t* context_lens, DecodePlan& p);
-int plan_chunk(const slw_model_cfg& c, const Window& w, int C, const std::vector<int32_t>& qt_pos0,
+int plan_chunk(const slw_model_cfg& c, const Window& w, bool cache, int C, const std::vector<int32_t>& qt_pos0,
                const std::vector<int32_t>& qt_rows, ChunkPlan& p);
 
 }  // namespace slw

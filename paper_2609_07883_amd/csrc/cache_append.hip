@@ -268,16 +268,24 @@ __device__ __forceinline__ void append_v16(const AppendArgs& a, const Item& it, 
     load_dims<D>(x, a.v, a, it, kvh, lane);
 #pragma unroll
     for (int d = 0; d < D; ++d) {
-        if (it.n == 16) {
-            u32x4 out[2];
-#pragma unroll
-            for (int w = 0; w < 8; ++w) out[w >> 2][w & 3] = x[w * D + d];
-            *reinterpret_cast<u32x4*>(page + d * 16) = out[0];
-            *reinterpret_cast<u32x4*>(page + d * 16 + 8) = out[1];
-        } else {
+        if (it.n == 1) {  // a decode's token
 #pragma unroll
             for (int t = 0; t < 16; ++t)
-                if (t >= it.t0 && t < it.t0 + it.n) page[d * 16 + t] = static_cast<uint16_t>(x[t / 2 * D + d] >> (16 * (t & 1)));
+                if (t == it.t0) page[d * 16 + t] = static_cast<uint16_t>(x[t / 2 * D + d] >> (16 * (t & 1)));
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4* piece = reinterpret_cast<u32x4*>(page + d * 16 + 8 * h);
+                u32x4 held = {}, out;
+                if (it.n < 16) held = *piece;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t live = (((1u << (it.t0 + it.n)) - (1u << it.t0)) >> (8 * h + 2 * w)) & 3u;
+                    const uint32_t m = (live & 1u ? 0xFFFFu : 0u) | (live & 2u ? 0xFFFF0000u : 0u);
+                    out[w] = (x[(4 * h + w) * D + d] & m) | (held[w] & ~m);
+                }
+                *piece = out;
+            }
         }
     }
 }

@@ -213,11 +213,23 @@ __device__ __forceinline__ void cache_decode_wave(const CacheAttnArgs& a, int sl
 #pragma unroll
             for (int j = 0; j < TAU / 2; ++j) {
                 const bf16x8 pf = to_bf16x8(s[2 * j], s[2 * j + 1]);  // the lane group's keys 8 j .. 8 j + 7
+                // e4m3: P in two bf16 terms, whose sum has 16 bits; the matrix
+                // cores have time to spare here (bf16 V can hold infinities,
+                // which a second term of 0 or less would turn into NaN)
+                bf16x8 pr;
+                if constexpr (Q8) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) pr[e] = f2bf(s[2 * j + (e >> 2)][e & 3] - bf2f(pf[e]));
+                }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const u32x4 x = st.v[nt] & vmask;
-                    if constexpr (Q8) o[nt] = mfma16(pf, widen8(x[2 * j], x[2 * j + 1], st.vs), o[nt]);
-                    else o[nt] = mfma16(pf, __builtin_bit_cast(bf16x8, x), o[nt]);
+                    if constexpr (Q8) {
+                        const bf16x8 v = widen8(x[2 * j], x[2 * j + 1], st.vs);
+                        o[nt] = mfma16(pf, v, mfma16(pr, v, o[nt]));
+                    } else {
+                        o[nt] = mfma16(pf, __builtin_bit_cast(bf16x8, x), o[nt]);
+                    }
                 }
             }
         };

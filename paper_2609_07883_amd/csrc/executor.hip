@@ -482,7 +482,7 @@ int build_attn_meta(slw_ctx* ctx, const slw_batch* bt, std::vector<int32_t>& m, 
         // covered by one item is written directly, one covered by several is
         // combined by the merge kernel.
         ChunkPlan& cp = ctx->cplan;
-        if ((rc = plan_chunk(c, w, C, qt_pos0, qt_rows, cp))) return rc;
+        if ((rc = plan_chunk(c, w, k || ctx->k_scale, C, qt_pos0, qt_rows, cp))) return rc;
         cl.n_items = static_cast<int>(cp.items.size() / 3);
         cl.n_slots = static_cast<int>(cp.slot_off.size()) - 1;
         cl.item = m.size();
@@ -819,7 +819,7 @@ extern "C" int slw_attention_plan_window(const slw_model_cfg* cfg, int32_t windo
         query_tiles(*cfg, pre, row0, rows, pos0, nullptr, {});
         const Window win{window, sinks};
         if ((rc = plan_decode(*cfg, win, B, context_lens, dp))) return rc;
-        if ((rc = plan_chunk(*cfg, win, C, pos0, rows, cp))) return rc;
+        if ((rc = plan_chunk(*cfg, win, window > 0, C, pos0, rows, cp))) return rc;
         const int dslots = static_cast<int>(dp.slot_off.size()) - 1;
         int64_t dmax = 0, dmin = dslots > 0 ? std::numeric_limits<int64_t>::max() : 0;
         for (int sl = 0; sl < dslots; ++sl) {
