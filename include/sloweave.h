@@ -499,13 +499,15 @@ int slw_attention_plan(const slw_model_cfg* cfg, int32_t B, const int32_t* conte
                        const int32_t* prefix_lens, const int32_t* chunk_lens, int64_t out[12]);
 
 /*
- * The same for windowed layers (slw_set_window's window and sinks; window 0:
- * as above): keys and tiles counted are those left by the window, without the
- * 64-key tiles between the sinks and the window.
+ * The same for the layers of an 8-bit or windowed cache, whose chunk attention
+ * divides its work by rules of its own: window and sinks as for slw_set_window,
+ * window 0 for full attention over the 8-bit cache.  Keys and tiles counted are
+ * those left by the window, without the 64-key tiles between the sinks and the
+ * window.
  */
-int slw_attention_plan_window(const slw_model_cfg* cfg, int32_t window, int32_t sinks, int32_t B,
-                              const int32_t* context_lens, int32_t n_prefill, const int32_t* prefix_lens,
-                              const int32_t* chunk_lens, int64_t out[12]);
+int slw_cache_attention_plan(const slw_model_cfg* cfg, int32_t window, int32_t sinks, int32_t B,
+                             const int32_t* context_lens, int32_t n_prefill, const int32_t* prefix_lens,
+                             const int32_t* chunk_lens, int64_t out[12]);
 
 /* ------------------------------------------------------------------------ */
 /* Controller (Eq. 1 solved by bisection as Alg. 1 does; margin of Sec. 3.3) */

@@ -37,7 +37,7 @@ EXPORTS = (
     "slw_serve", "slw_cost_table_analytic", "slw_build_cost_table_ctx", "slw_cost_table_from_samples_ctx",
     "slw_cost_table_prefixes", "slw_cost_table_lookup_ctx", "slw_select_chunk_ctx",
     "slw_mixed_iteration_static", "slw_flush_cache", "slw_fill_normal", "slw_gemm_plan",
-    "slw_attention_plan", "slw_attention_plan_window", "slw_kv_init_8bit", "slw_set_window",
+    "slw_attention_plan", "slw_cache_attention_plan", "slw_kv_init_8bit", "slw_set_window",
     "slw_attn_workspace_size", "slw_attn_begin", "slw_attn_append", "slw_attn_attend", "slw_attn_end",
 )
 STATIC_WS_BYTES = 128 << 20
@@ -154,7 +154,7 @@ def lib() -> C.CDLL:
         "slw_fill_normal": ([vp, sz, C.c_uint64, C.c_float, C.c_float, vp], C.c_int),
         "slw_gemm_plan": ([i32, i32, i32, P(i32)], C.c_int),
         "slw_attention_plan": ([P(ModelCfg), i32, P(i32), i32, P(i32), P(i32), P(i64)], C.c_int),
-        "slw_attention_plan_window": ([P(ModelCfg), i32, i32, i32, P(i32), i32, P(i32), P(i32), P(i64)], C.c_int),
+        "slw_cache_attention_plan": ([P(ModelCfg), i32, i32, i32, P(i32), i32, P(i32), P(i32), P(i64)], C.c_int),
         "slw_last_slots": ([vp, P(i32), i32, P(i32)], C.c_int),
         "slw_workspace_view": ([vp, i32, i32, i32, P(sz), P(sz)], C.c_int),
         "slw_build_cost_table": ([vp, P(i32), i32, P(i32), i32, P(ProfileOpts), P(vp)], C.c_int),
@@ -347,20 +347,20 @@ ATTENTION_PLAN_FIELDS = ("decode_items", "decode_slots", "decode_max_keys", "dec
                          "chunk_max_tiles", "chunk_min_tiles", "chunk_tiles", "chunk_two_phase")
 
 
-def attention_plan(shape, context_lens, prefills=(), window: int = 0, sinks: int = 0) -> dict:
+def attention_plan(shape, context_lens, prefills=(), window: int = 0, sinks: int = 0, kv: str = "bf16") -> dict:
     """The attention work lists an iteration would build (host only).
 
     shape: a model shape (synth.ModelShape); context_lens: cached tokens of
     each decode; prefills: (prefix_len, chunk_len) per prompt; window and
-    sinks: those of a windowed layer."""
+    sinks: those of a windowed layer; kv: the cache's type, "bf16" or "e4m3"."""
     cfg = ModelCfg(shape.n_layers, shape.d_model, shape.n_q_heads, shape.n_kv_heads, shape.head_dim,
                    shape.ffn_dim, shape.rms_eps, shape.rope_theta, 16, shape.max_pos)
     cl = _i32(context_lens)
     pp = _i32([p for p, _ in prefills])
     pc = _i32([c for _, c in prefills])
     out = np.zeros(12, np.int64)
-    if window or sinks:
-        _check(lib().slw_attention_plan_window(C.byref(cfg), int(window), int(sinks), len(cl), _ptr(cl, C.c_int32),
+    if kv != "bf16" or window or sinks:
+        _check(lib().slw_cache_attention_plan(C.byref(cfg), int(window), int(sinks), len(cl), _ptr(cl, C.c_int32),
                                                len(pp), _ptr(pp, C.c_int32), _ptr(pc, C.c_int32),
                                                _ptr(out, C.c_int64)))
     else:

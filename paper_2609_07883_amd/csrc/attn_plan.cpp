@@ -42,6 +42,13 @@ constexpr int64_t kMergeTiles = 4, kItemTiles5 = 2;
 //   1 head: 31: 73.6 / 77.0, 36: 81.3 / 85.4, 51: 109.5 / 109.4, 84: 310 / 293;
 //   head dim 64: 1 head, 59: 102 / 108; 8 heads, 72: 108 / 110; 16 heads, 464: 1130 / 1152.
 constexpr int64_t kTwoPhaseTiles = 21, kTwoPhaseTilesPer64 = 5;
+// The cache kernels' line; one-phase / two-phase us at n tiles per item, 4096
+// rows at 8192 under windows:
+//   4 heads a group: 9: 63.3 / 68.5, 12: 76.9 / 79.8, 15: 90.1 / 90.0,
+//   18: 104.9 / 102.5; 256 rows at 8192 over the whole context, 8: 59.0 / 56.2;
+//   8 heads: 11.5: 159 / 149; 2 heads: 19: 109.2 / 108.6, 28: 157 / 147;
+//   1 head: 21: 118 / 130, 45: 225.6 / 224.6.
+constexpr int64_t kCacheTwoPhaseTiles = 5, kCacheTwoPhaseTilesPer64 = 10;
 
 }  // namespace
 
@@ -250,7 +257,8 @@ int plan_chunk(const slw_model_cfg& c, const Window& w, bool cache, int C, const
     const int n_items = static_cast<int>(it.size() / 3);
     const int64_t blocks64 = std::max(1, chunk_tile_positions(c.n_q_heads / c.n_kv_heads) / 64);
     p.two_phase = c.head_dim == 128 && n_items > 0 &&
-                  total_tiles >= (kTwoPhaseTiles + kTwoPhaseTilesPer64 * blocks64) * n_items;
+                  total_tiles >= (cache ? kCacheTwoPhaseTiles + kCacheTwoPhaseTilesPer64 * blocks64
+                                        : kTwoPhaseTiles + kTwoPhaseTilesPer64 * blocks64) * n_items;
     p.qt_off.assign(n_qt + 1, 0);
     for (int q = 0, i = 0; q <= n_qt; ++q) {
         while (i < n_items && it[3 * i] < q) ++i;

@@ -784,15 +784,11 @@ extern "C" int slw_destroy(slw_ctx* ctx) {
     return SLW_OK;
 }
 
-extern "C" int slw_attention_plan(const slw_model_cfg* cfg, int32_t B, const int32_t* context_lens,
-                                  int32_t n_prefill, const int32_t* prefix_lens, const int32_t* chunk_lens,
-                                  int64_t out[12]) {
-    return slw_attention_plan_window(cfg, 0, 0, B, context_lens, n_prefill, prefix_lens, chunk_lens, out);
-}
+namespace {
 
-extern "C" int slw_attention_plan_window(const slw_model_cfg* cfg, int32_t window, int32_t sinks, int32_t B,
-                                         const int32_t* context_lens, int32_t n_prefill, const int32_t* prefix_lens,
-                                         const int32_t* chunk_lens, int64_t out[12]) {
+int attention_plan(const slw_model_cfg* cfg, bool cache, int32_t window, int32_t sinks, int32_t B,
+                   const int32_t* context_lens, int32_t n_prefill, const int32_t* prefix_lens,
+                   const int32_t* chunk_lens, int64_t out[12]) {
     return guarded([&] {
         if (!cfg || !out || (B > 0 && !context_lens) || (n_prefill > 0 && (!prefix_lens || !chunk_lens)))
             return fail(SLW_EINVAL, "null argument");
@@ -819,7 +815,7 @@ extern "C" int slw_attention_plan_window(const slw_model_cfg* cfg, int32_t windo
         query_tiles(*cfg, pre, row0, rows, pos0, nullptr, {});
         const Window win{window, sinks};
         if ((rc = plan_decode(*cfg, win, B, context_lens, dp))) return rc;
-        if ((rc = plan_chunk(*cfg, win, window > 0, C, pos0, rows, cp))) return rc;
+        if ((rc = plan_chunk(*cfg, win, cache, C, pos0, rows, cp))) return rc;
         const int dslots = static_cast<int>(dp.slot_off.size()) - 1;
         int64_t dmax = 0, dmin = dslots > 0 ? std::numeric_limits<int64_t>::max() : 0;
         for (int sl = 0; sl < dslots; ++sl) {
@@ -846,6 +842,20 @@ extern "C" int slw_attention_plan_window(const slw_model_cfg* cfg, int32_t windo
         for (int i = 0; i < 12; ++i) out[i] = v[i];
         return SLW_OK;
     });
+}
+
+}  // namespace
+
+extern "C" int slw_attention_plan(const slw_model_cfg* cfg, int32_t B, const int32_t* context_lens,
+                                  int32_t n_prefill, const int32_t* prefix_lens, const int32_t* chunk_lens,
+                                  int64_t out[12]) {
+    return attention_plan(cfg, false, 0, 0, B, context_lens, n_prefill, prefix_lens, chunk_lens, out);
+}
+
+extern "C" int slw_cache_attention_plan(const slw_model_cfg* cfg, int32_t window, int32_t sinks, int32_t B,
+                                        const int32_t* context_lens, int32_t n_prefill, const int32_t* prefix_lens,
+                                        const int32_t* chunk_lens, int64_t out[12]) {
+    return attention_plan(cfg, true, window, sinks, B, context_lens, n_prefill, prefix_lens, chunk_lens, out);
 }
 
 extern "C" int slw_gemm_plan(int32_t m, int32_t n, int32_t k, int32_t out[6]) {

@@ -168,7 +168,7 @@ def test_long_prefix(cache, window, sinks):
 
 
 # (q heads, kv heads, chunk, prefix, window, sinks): work items long enough for the two-phase kernel
-LONG = [(16, 16, 257, 24001, 0, 0), (32, 16, 140, 20020, 0, 0), (32, 8, 200, 16390, 0, 0), (64, 8, 100, 16401, 0, 0),
+LONG = [(16, 16, 257, 25001, 0, 0), (32, 16, 140, 20020, 0, 0), (32, 8, 200, 16390, 0, 0), (64, 8, 100, 16401, 0, 0),
         (128, 8, 50, 16383, 0, 0), (16, 16, 4096, 5000, 4000, 3), (32, 16, 2048, 4000, 3001, 70), (64, 16, 1024, 5003, 3500, 0),
         (128, 16, 512, 5000, 3001, 64), (256, 16, 256, 5000, 2100, 1)]
 
@@ -178,7 +178,7 @@ def _long_rig(case, cache, grow=0):
     rig = Rig(hq, hkv, 128, {1: P, 2: 700, 3: 5}, cache, window=window, sinks=sinks, grow=C + 1, max_pos=32768)
     from paper_2609_07883_amd.synth import ModelShape
     shape = ModelShape(1, 256, hq, hkv, 128, 256, max_pos=32768)
-    plan = api.attention_plan(shape, [700, 5], [(P, C)], window, sinks)
+    plan = api.attention_plan(shape, [700, 5], [(P, C)], window, sinks, kv=cache)
     assert plan["chunk_two_phase"]
     tile = 256 * hkv // hq
     rows = {0, 1, 33, tile - 1, tile, C // 2, C - 2, C - 1, C, C + 1}

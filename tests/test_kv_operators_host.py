@@ -108,9 +108,13 @@ def test_window_work_lists(window, sinks, seed):
     shape = ModelShape(1, 256, 8, 2, 64, 256, max_pos=8192)
     ctxs = rng.integers(0, 8000, rng.integers(0, 20)).tolist()
     pre = [(int(rng.integers(0, 4000)), int(rng.integers(1, 900))) for _ in range(rng.integers(0, 4))]
-    plan = api.attention_plan(shape, ctxs, pre, window, sinks)
-    if not window:
-        assert plan == api.attention_plan(shape, ctxs, pre)
+    plan = api.attention_plan(shape, ctxs, pre, window, sinks, kv="e4m3")
+    if window:
+        assert plan == api.attention_plan(shape, ctxs, pre, window, sinks)
+    else:  # the keys of full attention, divided by other rules
+        full = api.attention_plan(shape, ctxs, pre)
+        assert plan["chunk_tiles"] == full["chunk_tiles"]
+        assert {k: v for k, v in plan.items() if "decode" in k} == {k: v for k, v in full.items() if "decode" in k}
     chunk = sum(_tiles(p + j, min(p + j + 64, p + c) - 1, window, sinks) for p, c in pre for j in range(0, c, 64))
     assert plan["chunk_tiles"] == chunk
     assert plan["decode_max_keys"] * plan["decode_slots"] >= 0
