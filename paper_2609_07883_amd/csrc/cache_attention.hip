@@ -60,8 +60,21 @@ __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xFFFFFFF
 // K scale of the lane group's page multiplies its scores, the V scale is
 // applied where the codes are widened.
 //
-// Bound by HBM.
+// Bound by HBM.  The waves of a slot's kv heads lie next to each other in the
+// launch, since the heads' pages of a block do in memory; where the layers'
+// pages exceed the 256 MB last-level cache (a.once), they are loaded as data
+// that nobody reads again.  256 chat decodes over the 8-bit cache, 505 MB:
+// 110.6 -> 98.2 us, 5.15 TB/s, where a large copy reaches 5.16 (the first alone
+// 109.5, the second alone 99.9); beside a chunk of 64 rows 142 -> 132.  Data that
+// is still there is read slower so: 32 decodes of 84 MB beside 256 rows 46
+// against 38 us.
 // ---------------------------------------------------------------------------
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load_page(const uint8_t* p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+    else return *reinterpret_cast<const u32x4*>(p);
+}
+
 template <bool Q8, int HD>
 struct CacheStep {
     static constexpr int TAU = Q8 ? 4 : 2;                // score tiles
@@ -72,7 +85,7 @@ struct CacheStep {
     float ks, vs;  // e4m3: scales of the lane group's page
 };
 
-template <bool Q8, int HD>
+template <bool Q8, int HD, bool ONCE>
 __device__ __forceinline__ void cache_load(CacheStep<Q8, HD>& st, const CacheAttnArgs& a, const const_i32* bt_s, int k0,
                                            int last_pg, int kvh, int col, int grp) {
     constexpr int PAGES = Q8 ? 4 : 2, PB = HD * 16 * (Q8 ? 1 : 2);  // pages of a step, bytes of a page
@@ -94,21 +107,21 @@ __device__ __forceinline__ void cache_load(CacheStep<Q8, HD>& st, const CacheAtt
         const int tok = (kpl * (col >> 2) + 4 * tau + (col & 3)) & 15;
 #pragma unroll
         for (int s = 0; s < CacheStep<Q8, HD>::KL; ++s)
-            st.k[tau][s] = *reinterpret_cast<const u32x4*>(kpage + s * 1024 + tok * 64 + grp * 16);
+            st.k[tau][s] = load_page<ONCE>(kpage + s * 1024 + tok * 64 + grp * 16);
     }
     const size_t vbh = static_cast<size_t>(pick(Q8 ? grp : grp >> 1)) * hkv + kvh;
     const uint8_t* vpage = vpool + vbh * PB;
 #pragma unroll
     for (int nt = 0; nt < CacheStep<Q8, HD>::VL; ++nt)
-        st.v[nt] = *reinterpret_cast<const u32x4*>(vpage + (nt * 16 + col) * (Q8 ? 16 : 32) + (Q8 ? 0 : 16 * (grp & 1)));
+        st.v[nt] = load_page<ONCE>(vpage + (nt * 16 + col) * (Q8 ? 16 : 32) + (Q8 ? 0 : 16 * (grp & 1)));
     if constexpr (Q8) {
         st.ks = a.k_scale[vbh];
         st.vs = a.v_scale[vbh];
     }
 }
 
-template <bool Q8, int HD>
-__device__ __forceinline__ void cache_decode_wave(const CacheAttnArgs& a, int slot, int kvh, int lane) {
+template <bool Q8, int HD, bool ONCE>
+__device__ __forceinline__ void cache_decode_items(const CacheAttnArgs& a, int slot, int kvh, int lane) {
     using Step = CacheStep<Q8, HD>;
     constexpr int TAU = Step::TAU, KL = Step::KL, NT = HD / 16, KPL = 4 * TAU, KEYS = 4 * KPL;
     const DecodeAttnArgs& d = a.decode;
@@ -237,12 +250,12 @@ __device__ __forceinline__ void cache_decode_wave(const CacheAttnArgs& a, int sl
         // Loads one step ahead, also past the item's end (they re-read a page
         // of the sequence), so that no branch skips a load.
         Step sa, sb;
-        cache_load<Q8, HD>(sa, a, bt_s, key_of(v0), last_pg, kvh, col, grp);
+        cache_load<Q8, HD, ONCE>(sa, a, bt_s, key_of(v0), last_pg, kvh, col, grp);
         for (int c0 = v0;; c0 += 2 * KEYS) {
-            cache_load<Q8, HD>(sb, a, bt_s, key_of(c0 + KEYS), last_pg, kvh, col, grp);
+            cache_load<Q8, HD, ONCE>(sb, a, bt_s, key_of(c0 + KEYS), last_pg, kvh, col, grp);
             compute(sa, c0);
             if (c0 + KEYS >= v1) break;
-            cache_load<Q8, HD>(sa, a, bt_s, key_of(c0 + 2 * KEYS), last_pg, kvh, col, grp);
+            cache_load<Q8, HD, ONCE>(sa, a, bt_s, key_of(c0 + 2 * KEYS), last_pg, kvh, col, grp);
             compute(sb, c0 + KEYS);
             if (c0 + 2 * KEYS >= v1) break;
         }
@@ -268,8 +281,14 @@ __device__ __forceinline__ void cache_decode_wave(const CacheAttnArgs& a, int sl
 }
 
 template <bool Q8, int HD>
+__device__ __forceinline__ void cache_decode_wave(const CacheAttnArgs& a, int slot, int kvh, int lane) {
+    if (a.once) cache_decode_items<Q8, HD, true>(a, slot, kvh, lane);
+    else cache_decode_items<Q8, HD, false>(a, slot, kvh, lane);
+}
+
+template <bool Q8, int HD>
 __global__ __launch_bounds__(64, 2) void cache_decode_kernel(CacheAttnArgs a) {
-    cache_decode_wave<Q8, HD>(a, blockIdx.x, blockIdx.y, threadIdx.x);
+    cache_decode_wave<Q8, HD>(a, blockIdx.y, blockIdx.x, threadIdx.x);
 }
 
 // ---------------------------------------------------------------------------
@@ -702,7 +721,7 @@ __device__ __forceinline__ bool decode_group(const CacheAttnArgs& a) {
     const int v = (static_cast<int>(blockIdx.x) - n_chunk) * 8 +
                   __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     if (v < a.decode.n_slots * a.decode.hkv)
-        cache_decode_wave<Q8, HD>(a, v % a.decode.n_slots, v / a.decode.n_slots, threadIdx.x & 63);
+        cache_decode_wave<Q8, HD>(a, v / a.decode.hkv, v % a.decode.hkv, threadIdx.x & 63);
     return true;
 }
 
@@ -1190,7 +1209,7 @@ void launch_g(const CacheAttnArgs& a, hipStream_t s) {
 template <bool Q8, int HD>
 void launch_hd(const CacheAttnArgs& a, hipStream_t s) {
     if (a.chunk.n_items <= 0) {
-        if (a.decode.b > 0) cache_decode_kernel<Q8, HD><<<dim3(a.decode.n_slots, a.decode.hkv), 64, 0, s>>>(a);
+        if (a.decode.b > 0) cache_decode_kernel<Q8, HD><<<dim3(a.decode.hkv, a.decode.n_slots), 64, 0, s>>>(a);
         return;
     }
     switch (a.chunk.hq / a.chunk.hkv) {

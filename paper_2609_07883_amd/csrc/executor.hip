@@ -29,6 +29,7 @@ namespace {
 
 constexpr int kRing = 4;                 // pinned staging buffers in flight
 constexpr size_t kAlign = 256;
+constexpr int64_t kLastLevelCache = 256 << 20;
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
@@ -391,6 +392,7 @@ struct AttnMeta {
         int n_work = 0, n_dslots = 0, n_items = 0, n_slots = 0;
         size_t work = 0, skip = 0, item = 0, slot = 0, slot_items = 0, qtoff = 0, qt_skip = 0;
         bool two_phase = false;
+        int64_t decode_keys = 0;
     } cls[2];
 };
 
@@ -478,6 +480,7 @@ int build_attn_meta(slw_ctx* ctx, const slw_batch* bt, std::vector<int32_t>& m, 
         put(dp.off);
         put(dp.slot_off);
         cl.skip = put(dp.skip);
+        for (int b = 0; b < B; ++b) cl.decode_keys += bt->context_lens[b] + 1 - dp.skip[b];
         // plan_chunk hands the query tiles out to the work-groups.  A tile
         // covered by one item is written directly, one covered by several is
         // combined by the merge kernel.
@@ -586,6 +589,10 @@ struct AttnCall {
             a.window = w.window;
             a.sinks = w.window > 0 ? w.sinks : 0;
             a.sink_end = sink_end(w);
+            // the decodes' keys and values of all layers against the last-level cache
+            const int64_t windowed = std::count_if(ctx->windowed.begin(), ctx->windowed.end(), [](char f) { return f != 0; });
+            const int64_t keys = am.cls[0].decode_keys * (c.n_layers - windowed) + am.cls[1].decode_keys * windowed;
+            a.once = keys * 2 * hkv * hd * (ctx->k_scale ? 1 : 2) > kLastLevelCache;
         }
     }
     // The parts: chunk and decode in one launch, or each alone.

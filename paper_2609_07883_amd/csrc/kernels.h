@@ -162,6 +162,7 @@ struct CacheAttnArgs {
     const int32_t* skip;     // [b]
     int window;              // 0: every earlier key
     int sinks, sink_end;
+    int once;                // the decodes' pages are not in a cache by their next use
 };
 void launch_cache_attention(const CacheAttnArgs& a, hipStream_t s);
 
