@@ -258,6 +258,66 @@ def test_every_score_seen_not_a_number(cache):
     _run(rig, api.Batch(20, 1, 3000, (2,), (3000,)))
 
 
+@pytest.mark.parametrize("cache,window", [("e4m3", 0), ("bf16", 30)])
+def test_query_that_is_not_a_number(cache, window):
+    """One head of one row's query holds NaN: that head of that row is NaN, every other output is as it was."""
+    rig = Rig(8, 2, 128, {1: 100, 2: 60}, cache, window=window, grow=40)
+    batch = api.Batch(40, 1, 100, (2,), (60,))
+    x = rig.rng.standard_normal((41, 12, 128))
+    x[7, 3, 5] = np.nan
+    x[40, 6, 0] = np.nan
+    _run(rig, batch, x=x)
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+def test_pools_past_32_bits(cache):
+    """Blocks whose pages lie more than 2^32 bytes into the pools: the same bits as in a small pool."""
+    hq, hkv, hd, page = 8, 8, 128, 16 * 128 * (1 if cache == "e4m3" else 2)
+    first = 2**32 // (hkv * page) + 5
+    outs = []
+    for spare in (0, first):
+        blocks = spare + 40
+        ctx = api.Context(1, 256, hq, hkv, hd, 256, 1e-5, 10000.0, 1 << 20)
+        k = torch.empty(blocks * hkv * page, dtype=torch.uint8, device="cuda")
+        v = torch.empty_like(k)
+        k[-40 * hkv * page:].fill_(0x7F)
+        v[-40 * hkv * page:].fill_(0x7F)
+        if cache == "e4m3":
+            ks = torch.full((blocks * hkv,), float("nan"), device="cuda")
+            vs = torch.full_like(ks, float("nan"))
+            ctx.kv_init_8bit(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), blocks)
+        else:
+            ctx.kv_init(k.data_ptr(), v.data_ptr(), blocks)
+        ctx.set_window(200, 3)
+        left, sid = spare, 100
+        while left > 0:
+            ctx.seq_create(sid)
+            ctx.seq_reserve(sid, 16 * min(left, 65536))
+            left, sid = left - min(left, 65536), sid + 1
+        ctx.seq_create(1)
+        ctx.seq_create(2)
+        gen = torch.Generator(device="cuda").manual_seed(3)
+        got = []
+        for batch in (api.Batch.batched([(1, 0, 300), (2, 0, 70)]), api.Batch(90, 1, 300, (2,), (70,))):
+            x = torch.randn((batch.rows, 3 * hq * hd), device="cuda", generator=gen).bfloat16()
+            n = ctx.attn_workspace_size(batch.chunk, len(batch.decode_seqs))
+            ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+            out = torch.empty((batch.rows, hq * hd), dtype=torch.bfloat16, device="cuda")
+            plan = ctx.attn_begin(batch, ws.data_ptr(), n)
+            p = x.data_ptr()
+            plan.append(0, p + 2 * hq * hd, p + 4 * hq * hd, 3 * hq * hd)
+            plan.attend(0, p, 3 * hq * hd, out.data_ptr())
+            torch.cuda.synchronize()
+            got.append(out.clone())
+        got += [k[-40 * hkv * page:].clone(), v[-40 * hkv * page:].clone()]
+        outs.append(got)
+        assert min(ctx.block_table(1)) >= spare
+        del k, v
+    assert torch.isfinite(outs[0][0]).all() and torch.isfinite(outs[0][1]).all()
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+
+
 # -- use ------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("cache", ["e4m3", "bf16"])
