@@ -499,7 +499,7 @@ int slw_attention_plan(const slw_model_cfg* cfg, int32_t B, const int32_t* conte
                        const int32_t* prefix_lens, const int32_t* chunk_lens, int64_t out[12]);
 
 /*
- * The same for the layers of an 8-bit or windowed cache, whose chunk attention
+ * The same for the layers of an 8-bit or windowed cache, whose attention
  * divides its work by rules of its own: window and sinks as for slw_set_window,
  * window 0 for full attention over the 8-bit cache.  Keys and tiles counted are
  * those left by the window, without the 64-key tiles between the sinks and the

@@ -1058,6 +1058,7 @@ __global__ __launch_bounds__(64, 2) void decode_attn_kernel(DecodeAttnArgs a) {
 template <int HD>
 __device__ __forceinline__ void decode_merge_row(const DecodeAttnArgs& a, int b, int h) {
     const int w0 = a.work_off[b], w1 = a.work_off[b + 1];
+    if (a.direct && w1 - w0 == 1) return;  // written by the attention kernel
     merge_row<HD>(a.part_ml, a.part_o, static_cast<size_t>(w0) * a.hq + h, a.hq, w1 - w0,
                   static_cast<bf16*>(a.out) + static_cast<size_t>(b) * a.hq * HD + h * HD);
 }

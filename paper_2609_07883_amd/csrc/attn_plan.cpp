@@ -16,6 +16,23 @@ namespace {
 // wave of the launch finishes at about the same time.
 constexpr int kDecodeWaves = 2048;
 constexpr int kDecodeMinKeys = 128;
+// The cache kernels' decodes with no chunk beside them: runs for this many
+// waves, or one for each decode where the longest is at most 1.5 runs + 128
+// keys, which leaves nothing to merge.  us a layer with its append and merge
+// for 2048 / 768 / 512 waves: 64 chat decodes (8-bit) 44.9 / 44.3 / 44.7, 256
+// 114.4 / 108.0 / 116.5, 4 of 1 K to 10 K 35.2 / 28.7 / 28.7, 32 of 0.5 K to 2 K
+// 32.9 / 28.4 / 31.0; in bf16, 32 in a window of 1024 43.2 / 41.3 / 40.4, 256 chat
+// decodes 197.6 / 188.8 / 186.7.  768 waves / one run a decode, decodes of equal
+// length, two layers: one of 190 tokens 29.9 / 25.3, of 250 27.8 / 26.8, of 380
+// 27.8 / 31.7; 32 of 250 32.4 / 29.8, of 830 49.4 / 53.5; 64 of 380 47.1 / 37.9,
+// of 830 72.2 / 57.1; 128 of 1200 137.5 / 119.2; 256 of 830 217.8 / 189.7.
+// Beside a chunk, eight waves share a CU, and fewer waves are fewer CUs: 256
+// decodes beside 64 rows 116.1 / 159.6 with 2048 / 768.
+constexpr int kCacheDecodeWaves = 768;
+// Beside a chunk that needs no merge, decodes of up to so many keys get one run
+// each: 5 beside 77 rows, split / one run, of 120 tokens 25.4 / 21.7, of 190
+// 25.3 / 22.8, of 250 24.9 / 26.1.
+constexpr int64_t kBesideWhole = 3 * 64;
 // Chunk attention runs one work-group per CU (its register use allows no
 // more), so a launch of kChunkSlots work-groups with equal work finishes in
 // one round on a 256-CU part.  A work-group takes at least kChunkMinTiles
@@ -97,14 +114,18 @@ void query_tiles(const slw_model_cfg& c, const std::vector<Prefill>& pre, std::v
 }
 
 // Decode attention work.  The keys of all decodes (decode b attends to
-// context_lens[b] + 1 of them, or those left by the window), laid end to end with each decode's range
-// padded to a multiple of 64, are cut into equal runs (multiples of 64 keys,
-// so that every item starts on a page pair; at least kDecodeMinKeys each, at
-// most decode_slot_cap(c) runs), one per wave of each kv head; a run that
-// crosses decodes becomes one item per decode it touches, and padding alone
-// makes no item.  Items come out in decode order, so each decode's items are
-// contiguous for the merge.
-int plan_decode(const slw_model_cfg& c, const Window& w, int B, const int32_t* context_lens, DecodePlan& p) {
+// context_lens[b] + 1 of them, or those left by the window), laid end to end
+// with each decode's range padded to a multiple of 64, are cut into equal runs
+// (multiples of 64 keys, so that every item starts on a page pair; at least
+// kDecodeMinKeys each, at most decode_slot_cap(c) runs), one per wave of each
+// kv head; a run that crosses decodes becomes one item per decode it touches,
+// and padding alone makes no item.  Items come out in decode order, so each
+// decode's items are contiguous for the merge.
+//
+// Layers on the cache kernels (kind) write a decode of one item without a
+// merge, and decodes of similar length get one run each (kCacheDecodeWaves).
+int plan_decode(const slw_model_cfg& c, const Window& w, DecodeKind kind, int B, const int32_t* context_lens,
+                DecodePlan& p) {
     p.b.clear();
     p.kb.clear();
     p.ke.clear();
@@ -114,37 +135,54 @@ int plan_decode(const slw_model_cfg& c, const Window& w, int B, const int32_t* c
     if (B <= 0) return SLW_OK;
     for (int b = 0; b < B; ++b) p.skip[b] = window_skip(w, context_lens[b]);
     auto keys = [&](int b) { return context_lens[b] + 1 - p.skip[b]; };  // virtual
-    int64_t padded = 0;
-    for (int b = 0; b < B; ++b) padded += ceil_div(keys(b), 64) * 64;
-    const int64_t want = std::min<int64_t>(decode_slot_cap(c), std::max<int64_t>(1, padded / kDecodeMinKeys));
+    int64_t padded = 0, longest = 0;
+    for (int b = 0; b < B; ++b) {
+        const int64_t span = ceil_div(keys(b), 64) * 64;
+        padded += span;
+        longest = std::max(longest, span);
+    }
+    const int64_t slots = kind == DecodeKind::cache_alone ? std::max(1, kCacheDecodeWaves / c.n_kv_heads) : decode_slot_cap(c);
+    const int64_t want = std::min<int64_t>(slots, std::max<int64_t>(1, padded / kDecodeMinKeys));
     const int64_t per = ceil_div(ceil_div(padded, want), 64) * 64;
-    const int n_slots = static_cast<int>(ceil_div(padded, per));
+    const bool whole = B <= decode_slot_cap(c) && ((kind == DecodeKind::cache_alone && 2 * longest <= 3 * per + 4 * 64) ||
+                                                   (kind == DecodeKind::cache_beside && longest <= kBesideWhole));
+    const int n_slots = whole ? B : static_cast<int>(ceil_div(padded, per));
     p.slot_off.clear();
-    int b = 0;
-    int64_t start_b = 0;  // first key of decode b in the padded layout
-    for (int sl = 0; sl < n_slots; ++sl) {
-        p.slot_off.push_back(static_cast<int32_t>(p.b.size()));
-        int64_t r0 = sl * per;
-        const int64_t r1 = std::min(padded, r0 + per);
-        while (r0 < r1) {
-            const int32_t len = keys(b);
-            const int64_t span = ceil_div(len, 64) * 64;
-            if (r0 >= start_b + span) {  // past decode b
-                start_b += span;
-                p.off[++b] = static_cast<int32_t>(p.b.size());
-                continue;
-            }
-            const int64_t k0 = r0 - start_b, k1 = std::min<int64_t>(r1 - start_b, span);
-            if (k0 < len) {
-                p.b.push_back(b);
-                p.kb.push_back(static_cast<int32_t>(k0));
-                p.ke.push_back(static_cast<int32_t>(std::min<int64_t>(k1, len)));
-            }
-            r0 = start_b + k1;
+    if (whole) {
+        for (int d = 0; d < B; ++d) {
+            p.b.push_back(d);
+            p.kb.push_back(0);
+            p.ke.push_back(keys(d));
+            p.off[d + 1] = d + 1;
+            p.slot_off.push_back(d);
         }
+    } else {
+        int b = 0;
+        int64_t start_b = 0;  // first key of decode b in the padded layout
+        for (int sl = 0; sl < n_slots; ++sl) {
+            p.slot_off.push_back(static_cast<int32_t>(p.b.size()));
+            int64_t r0 = sl * per;
+            const int64_t r1 = std::min(padded, r0 + per);
+            while (r0 < r1) {
+                const int32_t len = keys(b);
+                const int64_t span = ceil_div(len, 64) * 64;
+                if (r0 >= start_b + span) {  // past decode b
+                    start_b += span;
+                    p.off[++b] = static_cast<int32_t>(p.b.size());
+                    continue;
+                }
+                const int64_t k0 = r0 - start_b, k1 = std::min<int64_t>(r1 - start_b, span);
+                if (k0 < len) {
+                    p.b.push_back(b);
+                    p.kb.push_back(static_cast<int32_t>(k0));
+                    p.ke.push_back(static_cast<int32_t>(std::min<int64_t>(k1, len)));
+                }
+                r0 = start_b + k1;
+            }
+        }
+        while (b < B) p.off[++b] = static_cast<int32_t>(p.b.size());
     }
     p.slot_off.push_back(static_cast<int32_t>(p.b.size()));
-    while (b < B) p.off[++b] = static_cast<int32_t>(p.b.size());
     if (static_cast<int>(p.b.size()) > decode_work_cap(c, B) || n_slots > decode_slot_cap(c))
         return fail(SLW_EINVAL, "internal: decode work %zu / slots %d above cap", p.b.size(), n_slots);
     for (int d = 0; d < B; ++d) {  // the items of each decode tile its keys

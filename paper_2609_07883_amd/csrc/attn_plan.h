@@ -55,7 +55,16 @@ int chunk_item_cap(const slw_model_cfg& c, int C);
 void query_tiles(const slw_model_cfg& c, const std::vector<Prefill>& pre, std::vector<int32_t>& row0,
                  std::vector<int32_t>& rows, std::vector<int32_t>& pos0, std::vector<int32_t>* bt,
                  const std::vector<int32_t>& bt_of_prefill);
-int plan_decode(const slw_model_cfg& c, const Window& w, int B, const int32_t* context_lens, DecodePlan& p);
+// Which kernels the decodes run on, and beside what: a chunk whose query tiles
+// are split is merged by a launch that the decodes then share.
+enum class DecodeKind { bf16, cache_alone, cache_beside, cache_split };
+inline DecodeKind decode_kind(bool cache, const ChunkPlan& chunk) {
+    if (!cache) return DecodeKind::bf16;
+    if (chunk.items.empty()) return DecodeKind::cache_alone;
+    return chunk.items.size() / 3 + 1 > chunk.qt_off.size() ? DecodeKind::cache_split : DecodeKind::cache_beside;
+}
+int plan_decode(const slw_model_cfg& c, const Window& w, DecodeKind kind, int B, const int32_t* context_lens,
+                DecodePlan& p);
 int plan_chunk(const slw_model_cfg& c, const Window& w, bool cache, int C, const std::vector<int32_t>& qt_pos0,
                const std::vector<int32_t>& qt_rows, ChunkPlan& p);
 

@@ -63,11 +63,17 @@ __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xFFFFFFF
 // Bound by HBM.  The waves of a slot's kv heads lie next to each other in the
 // launch, since the heads' pages of a block do in memory; where the layers'
 // pages exceed the 256 MB last-level cache (a.once), they are loaded as data
-// that nobody reads again.  256 chat decodes over the 8-bit cache, 505 MB:
-// 110.6 -> 98.2 us, 5.15 TB/s, where a large copy reaches 5.16 (the first alone
-// 109.5, the second alone 99.9); beside a chunk of 64 rows 142 -> 132.  Data that
+// that nobody reads again.  256 chat decodes over the 8-bit cache, 505 MB, in
+// runs for 2048 waves: 110.6 -> 98.2 us (the first alone 109.5, the second alone
+// 99.9); with runs for 768 (attn_plan.cpp) 91.4 us, 5.5 TB/s, where a large copy
+// reaches 5.16; beside a chunk of 64 rows 142 -> 132.  Data that
 // is still there is read slower so: 32 decodes of 84 MB beside 256 rows 46
 // against 38 us.
+//
+// A decode of one item is written as its rows, the others as partial sums for
+// the merge's launch.  Combining those by the last wave to finish instead took
+// longer: with release and acquire fences 45 -> 111 us for 64 decodes, with
+// partial sums written through and read past the L2s 45 -> 53.
 // ---------------------------------------------------------------------------
 template <bool ONCE>
 __device__ __forceinline__ u32x4 load_page(const uint8_t* p) {
@@ -129,14 +135,19 @@ __device__ __forceinline__ void cache_decode_items(const CacheAttnArgs& a, int s
     const int group = d.hq / d.hkv;
     const float sl2 = kLog2e / sqrtf(static_cast<float>(HD));
 
+    // Lists through the scalar cache: 0.3 to 1 us less than through vector loads.
+    // (Asked for an item ahead, under the first keys of the one before, they
+    // took 0.5 to 1 us longer: most waves have one item or two.)
+    auto of = [](const int32_t* p, int i) { return ((const const_i32*)p)[i]; };
     const int i0 = d.slot_off[slot], i1 = d.slot_off[slot + 1];
     for (int w = i0; w < i1; ++w) {
-        const int b = d.work_b[w], v0 = d.work_kb[w], v1 = d.work_ke[w];
-        const int len = d.kv_len[b], skip = a.skip[b];
+        const int b = of(d.work_b, w), v0 = of(d.work_kb, w), v1 = of(d.work_ke, w);
+        const int len = of(d.kv_len, b), skip = of(a.skip, b);
+        const bool whole = of(d.work_off, b + 1) - of(d.work_off, b) == 1;  // all of the decode
         const int last_pg = (len - 1) >> 4;
         // keys below w_lo are seen only if they are sinks
         const int w_lo = a.window > 0 ? max(len - a.window, 0) : 0;
-        const const_i32* bt_s = (const const_i32*)(d.bt + d.bt_off[b]);
+        const const_i32* bt_s = (const const_i32*)(d.bt + of(d.bt_off, b));
         auto key_of = [&](int v) { return v < a.sink_end ? v : v + skip; };
 
         // Q^T operand: the dims that a lane's K pieces hold
@@ -247,23 +258,38 @@ __device__ __forceinline__ void cache_decode_items(const CacheAttnArgs& a, int s
             }
         };
 
-        // Loads one step ahead, also past the item's end (they re-read a page
-        // of the sequence), so that no branch skips a load.
+        // A step's loads follow the products of the step two before it, so one or
+        // two steps are in flight; past the item's end they re-read a page of
+        // the sequence, so that no branch skips a load.
         Step sa, sb;
         cache_load<Q8, HD, ONCE>(sa, a, bt_s, key_of(v0), last_pg, kvh, col, grp);
+        cache_load<Q8, HD, ONCE>(sb, a, bt_s, key_of(v0 + KEYS), last_pg, kvh, col, grp);
         for (int c0 = v0;; c0 += 2 * KEYS) {
-            cache_load<Q8, HD, ONCE>(sb, a, bt_s, key_of(c0 + KEYS), last_pg, kvh, col, grp);
             compute(sa, c0);
             if (c0 + KEYS >= v1) break;
             cache_load<Q8, HD, ONCE>(sa, a, bt_s, key_of(c0 + 2 * KEYS), last_pg, kvh, col, grp);
             compute(sb, c0 + KEYS);
             if (c0 + 2 * KEYS >= v1) break;
+            cache_load<Q8, HD, ONCE>(sb, a, bt_s, key_of(c0 + 3 * KEYS), last_pg, kvh, col, grp);
         }
 
         const float l = rows4_sum(l_run);
         // a maximum of -inf marks a part that saw no key: where every score
         // seen was NaN, the sum says so instead
         const float m = m_run == -INFINITY && l != l ? 0.f : m_run;
+        if (whole) {  // its rows
+            bf16* out = static_cast<bf16*>(d.out) + (static_cast<size_t>(b) * d.hq + kvh * group) * HD;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int h = grp * 4 + e;
+                const float inv = 1.0f / __shfl(l, h, 64);
+                if (h < group) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) out[h * HD + nt * 16 + col] = f2bf(o[nt][e] * inv);
+                }
+            }
+            continue;
+        }
         const size_t hbase = static_cast<size_t>(w) * d.hq + kvh * group;
         if (grp == 0 && col < group) {
             d.part_ml[(hbase + col) * 2 + 0] = m;

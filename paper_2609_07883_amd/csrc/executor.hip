@@ -470,22 +470,12 @@ int build_attn_meta(slw_ctx* ctx, const slw_batch* bt, std::vector<int32_t>& m, 
         if (!(k ? ctx->any_windowed : ctx->any_full)) continue;
         AttnMeta::Class& cl = am.cls[k];
         const Window w = k ? ctx->win : Window{};
-        DecodePlan& dp = ctx->dplan;
-        if ((rc = plan_decode(c, w, B, bt->context_lens, dp))) return rc;
-        cl.n_work = static_cast<int>(dp.b.size());
-        cl.n_dslots = static_cast<int>(dp.slot_off.size()) - 1;
-        cl.work = put(dp.b);
-        put(dp.kb);
-        put(dp.ke);
-        put(dp.off);
-        put(dp.slot_off);
-        cl.skip = put(dp.skip);
-        for (int b = 0; b < B; ++b) cl.decode_keys += bt->context_lens[b] + 1 - dp.skip[b];
+        const bool cache = k || ctx->k_scale;
         // plan_chunk hands the query tiles out to the work-groups.  A tile
         // covered by one item is written directly, one covered by several is
         // combined by the merge kernel.
         ChunkPlan& cp = ctx->cplan;
-        if ((rc = plan_chunk(c, w, k || ctx->k_scale, C, qt_pos0, qt_rows, cp))) return rc;
+        if ((rc = plan_chunk(c, w, cache, C, qt_pos0, qt_rows, cp))) return rc;
         cl.n_items = static_cast<int>(cp.items.size() / 3);
         cl.n_slots = static_cast<int>(cp.slot_off.size()) - 1;
         cl.item = m.size();
@@ -497,6 +487,17 @@ int build_attn_meta(slw_ctx* ctx, const slw_batch* bt, std::vector<int32_t>& m, 
         cl.qtoff = put(cp.qt_off);
         cl.qt_skip = put(cp.qt_skip);
         cl.two_phase = cp.two_phase;
+        DecodePlan& dp = ctx->dplan;
+        if ((rc = plan_decode(c, w, decode_kind(cache, cp), B, bt->context_lens, dp))) return rc;
+        cl.n_work = static_cast<int>(dp.b.size());
+        cl.n_dslots = static_cast<int>(dp.slot_off.size()) - 1;
+        cl.work = put(dp.b);
+        put(dp.kb);
+        put(dp.ke);
+        put(dp.off);
+        put(dp.slot_off);
+        cl.skip = put(dp.skip);
+        for (int b = 0; b < B; ++b) cl.decode_keys += bt->context_lens[b] + 1 - dp.skip[b];
     }
     return SLW_OK;
 }
@@ -581,6 +582,7 @@ struct AttnCall {
         }
         cache = ctx->k_scale || ctx->windowed[l];
         if (cache) {
+            da.direct = 1;
             a.k_scale = pool.k_scale;
             a.v_scale = pool.v_scale;
             a.qt_skip = dmeta + cl.qt_skip;
@@ -612,7 +614,10 @@ struct AttnCall {
         x.chunk = ChunkAttnArgs{};
         launch_cache_attention(x, s);
     }
-    void merge(hipStream_t s) const { launch_attention_merge(&a.chunk, &a.decode, s); }
+    void merge(hipStream_t s) const {
+        const bool decodes = !a.decode.direct || a.decode.n_work > a.decode.b;
+        launch_attention_merge(&a.chunk, decodes ? &a.decode : nullptr, s);
+    }
 };
 
 // Metadata, upload and kernels of an iteration whose blocks are reserved.
@@ -755,7 +760,11 @@ int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void*
     HIP_TRY(hipGetLastError());
     if (timing) {
         // the merge stage (5) runs when decodes or split chunk query tiles need it
-        const bool merge = B > 0 || am.cls[0].n_items > am.n_qt || am.cls[1].n_items > am.n_qt;
+        bool merge = false;
+        for (int l = 0; l < c.n_layers; ++l) {
+            const AttnMeta::Class& cl = am.cls[ctx->windowed[l] ? 1 : 0];
+            merge |= cl.n_items > am.n_qt || (ctx->k_scale || ctx->windowed[l] ? cl.n_work > B : B > 0);
+        }
         ctx->stage_mask[set] = 0x3FFu & ~(C > 0 ? 0u : (1u << 3)) & ~(B > 0 ? 0u : (1u << 4)) &
                                ~(merge ? 0u : (1u << 5));
         ++ctx->stage_iter;
@@ -821,8 +830,8 @@ int attention_plan(const slw_model_cfg* cfg, bool cache, int32_t window, int32_t
         std::vector<int32_t> row0, rows, pos0;
         query_tiles(*cfg, pre, row0, rows, pos0, nullptr, {});
         const Window win{window, sinks};
-        if ((rc = plan_decode(*cfg, win, B, context_lens, dp))) return rc;
         if ((rc = plan_chunk(*cfg, win, cache, C, pos0, rows, cp))) return rc;
+        if ((rc = plan_decode(*cfg, win, decode_kind(cache, cp), B, context_lens, dp))) return rc;
         const int dslots = static_cast<int>(dp.slot_off.size()) - 1;
         int64_t dmax = 0, dmin = dslots > 0 ? std::numeric_limits<int64_t>::max() : 0;
         for (int sl = 0; sl < dslots; ++sl) {

@@ -116,6 +116,7 @@ struct DecodeAttnArgs {
     float* part_o;           // [n_work][hq][hd]
     float* part_ml;          // [n_work][hq][2]
     int b, n_work, n_slots, hq, hkv, hd, ld_q;
+    int direct;              // a decode of one item is written as its rows, not as a partial (cache kernels)
 };
 void launch_decode_attention_split(const DecodeAttnArgs& a, hipStream_t s);
 // Both attentions of a layer in one launch (chunk work-groups first, decode
@@ -123,7 +124,8 @@ void launch_decode_attention_split(const DecodeAttnArgs& a, hipStream_t s);
 void launch_attention(const ChunkAttnArgs& ca, const DecodeAttnArgs& da, hipStream_t s);
 // Combine the partials of both attentions in one launch: chunk rows of
 // query tiles split over several items (ca may be null or unsplit) and every
-// decode (da may be null or have b = 0).
+// decode, or with `direct` those of several items (da may be null or have
+// b = 0).
 void launch_attention_merge(const ChunkAttnArgs* ca, const DecodeAttnArgs* da, hipStream_t s);
 
 // The cache operators beside the full bf16 ones above: attention over a paged

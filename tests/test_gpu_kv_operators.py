@@ -146,6 +146,16 @@ def test_decodes(hq, hkv, hd, cache, window, sinks):
     _run(rig, api.Batch(0, 0, 0, tuple(seqs), tuple(ctxs)), q_std=2.0)
 
 
+@pytest.mark.parametrize("cache,window", [("e4m3", 0), ("bf16", 400)])
+@pytest.mark.parametrize("hq,hkv,ctxs", [(16, 16, [3 * i % 130 for i in range(150)]), (8, 4, [600 + 3 * i for i in range(64)]),
+                                         (8, 4, [30 + i for i in range(63)] + [1900])])
+def test_many_decodes(hq, hkv, ctxs, cache, window):
+    """More decodes than a launch has runs, decodes of like lengths, one long decode among short ones."""
+    seqs = {10 + i: n for i, n in enumerate(ctxs)}
+    rig = Rig(hq, hkv, 64, seqs, cache, window=window, grow=1, max_pos=2048)
+    _run(rig, api.Batch(0, 0, 0, tuple(seqs), tuple(ctxs)), q_std=2.0)
+
+
 @pytest.mark.parametrize("cache,window,sinks", [(c, *w) for c in WINDOWS for w in WINDOWS[c]])
 @pytest.mark.parametrize("hq,hkv,hd", HEADS)
 def test_chunks(hq, hkv, hd, cache, window, sinks):

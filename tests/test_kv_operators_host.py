@@ -114,13 +114,31 @@ def test_window_work_lists(window, sinks, seed):
     else:  # the keys of full attention, divided by other rules
         full = api.attention_plan(shape, ctxs, pre)
         assert plan["chunk_tiles"] == full["chunk_tiles"]
-        assert {k: v for k, v in plan.items() if "decode" in k} == {k: v for k, v in full.items() if "decode" in k}
     chunk = sum(_tiles(p + j, min(p + j + 64, p + c) - 1, window, sinks) for p, c in pre for j in range(0, c, 64))
     assert plan["chunk_tiles"] == chunk
     assert plan["decode_max_keys"] * plan["decode_slots"] >= 0
     if ctxs:
         keys = sum(64 * _tiles(c, c, window, sinks) for c in ctxs)
         assert plan["decode_min_keys"] <= keys / plan["decode_slots"] <= plan["decode_max_keys"] + 64
+        assert len(ctxs) <= plan["decode_items"] < plan["decode_slots"] + len(ctxs)
+
+
+def test_decode_runs():
+    shape = ModelShape(1, 4096, 32, 8, 128, 256, max_pos=1 << 15)
+
+    def runs(ctxs, pre=()):
+        p = api.attention_plan(shape, ctxs, pre, kv="e4m3")
+        return p["decode_items"], p["decode_slots"]
+
+    assert runs([250]) == (1, 1) and runs([500]) == (4, 4)  # short: one run; else 128 keys each
+    assert runs([830] * 64) == (64, 64)                     # alike: one run each, also where the lengths differ a little
+    assert runs([600, 830] * 32) == (64, 64)
+    items, slots = runs([300] * 63 + [8000])                # unlike: equal runs for 768 waves
+    assert slots <= 96 and items > 64
+    assert runs([3000] * 300)[1] <= 96                      # more decodes than wave slots
+    full = api.attention_plan(shape, [300] * 63 + [8000], [(8192, 300)])
+    assert runs([300] * 63 + [8000], [(8192, 300)]) == (full["decode_items"], full["decode_slots"])
+    assert runs([190] * 5, [(50, 77)]) == (5, 5) and runs([300] * 5, [(50, 77)])[0] > 5
 
 
 def test_plan_window_refusals():
