@@ -2,6 +2,7 @@
 #include "attn_plan.h"
 
 #include <algorithm>
+#include <functional>
 
 #include "common.h"
 #include "kernels.h"
@@ -66,6 +67,8 @@ constexpr int64_t kTwoPhaseTiles = 21, kTwoPhaseTilesPer64 = 5;
 //   8 heads: 11.5: 159 / 149; 2 heads: 19: 109.2 / 108.6, 28: 157 / 147;
 //   1 head: 21: 118 / 130, 45: 225.6 / 224.6.
 constexpr int64_t kCacheTwoPhaseTiles = 5, kCacheTwoPhaseTilesPer64 = 10;
+
+inline int64_t span64(int64_t keys) { return (keys + 63) & ~static_cast<int64_t>(63); }
 
 }  // namespace
 
@@ -132,66 +135,61 @@ int plan_decode(const slw_model_cfg& c, const Window& w, DecodeKind kind, int B,
     p.off.assign(B + 1, 0);
     p.slot_off.assign(1, 0);
     p.skip.resize(std::max(B, 0));
+    p.keys.resize(std::max(B, 0));
     if (B <= 0) return SLW_OK;
-    for (int b = 0; b < B; ++b) p.skip[b] = window_skip(w, context_lens[b]);
-    auto keys = [&](int b) { return context_lens[b] + 1 - p.skip[b]; };  // virtual
-    int64_t padded = 0, longest = 0;
+    int64_t padded = 0;
+    int32_t longest = 0;
     for (int b = 0; b < B; ++b) {
-        const int64_t span = ceil_div(keys(b), 64) * 64;
-        padded += span;
-        longest = std::max(longest, span);
+        p.skip[b] = window_skip(w, context_lens[b]);
+        p.keys[b] = context_lens[b] + 1 - p.skip[b];
+        padded += span64(p.keys[b]);
+        longest = std::max(longest, p.keys[b]);
     }
-    const int64_t slots = kind == DecodeKind::cache_alone ? std::max(1, kCacheDecodeWaves / c.n_kv_heads) : decode_slot_cap(c);
+    const int cap = decode_work_cap(c, B), slot_cap = decode_slot_cap(c);
+    const int64_t slots = kind == DecodeKind::cache_alone ? std::max(1, kCacheDecodeWaves / c.n_kv_heads) : slot_cap;
     const int64_t want = std::min<int64_t>(slots, std::max<int64_t>(1, padded / kDecodeMinKeys));
-    const int64_t per = ceil_div(ceil_div(padded, want), 64) * 64;
-    const bool whole = B <= decode_slot_cap(c) && ((kind == DecodeKind::cache_alone && 2 * longest <= 3 * per + 4 * 64) ||
-                                                   (kind == DecodeKind::cache_beside && longest <= kBesideWhole));
+    const int64_t per = span64(ceil_div(padded, want));
+    const bool whole = B <= slot_cap && ((kind == DecodeKind::cache_alone && 2 * span64(longest) <= 3 * per + 4 * 64) ||
+                                         (kind == DecodeKind::cache_beside && longest <= kBesideWhole));
     const int n_slots = whole ? B : static_cast<int>(ceil_div(padded, per));
-    p.slot_off.clear();
-    if (whole) {
-        for (int d = 0; d < B; ++d) {
-            p.b.push_back(d);
-            p.kb.push_back(0);
-            p.ke.push_back(keys(d));
-            p.off[d + 1] = d + 1;
-            p.slot_off.push_back(d);
-        }
-    } else {
-        int b = 0;
-        int64_t start_b = 0;  // first key of decode b in the padded layout
-        for (int sl = 0; sl < n_slots; ++sl) {
-            p.slot_off.push_back(static_cast<int32_t>(p.b.size()));
-            int64_t r0 = sl * per;
-            const int64_t r1 = std::min(padded, r0 + per);
-            while (r0 < r1) {
-                const int32_t len = keys(b);
-                const int64_t span = ceil_div(len, 64) * 64;
-                if (r0 >= start_b + span) {  // past decode b
-                    start_b += span;
-                    p.off[++b] = static_cast<int32_t>(p.b.size());
-                    continue;
-                }
-                const int64_t k0 = r0 - start_b, k1 = std::min<int64_t>(r1 - start_b, span);
-                if (k0 < len) {
-                    p.b.push_back(b);
-                    p.kb.push_back(static_cast<int32_t>(k0));
-                    p.ke.push_back(static_cast<int32_t>(std::min<int64_t>(k1, len)));
-                }
-                r0 = start_b + k1;
+    if (n_slots > slot_cap) return fail(SLW_EINVAL, "internal: %d decode slots above cap", n_slots);
+    // at most one item for each end of a slot or of a decode: n_slots + B
+    p.b.resize(n_slots + B);
+    p.kb.resize(n_slots + B);
+    p.ke.resize(n_slots + B);
+    p.slot_off.resize(n_slots + 1);
+    int n = 0, sl = 0;
+    int64_t room = 0;  // keys that the slot can still take
+    for (int b = 0; b < B; ++b) {
+        const int32_t len = p.keys[b];
+        const int64_t span = span64(len);
+        for (int64_t k = 0; k < span;) {
+            if (room == 0) {
+                p.slot_off[sl++] = n;
+                room = whole ? span : per;
             }
+            const int64_t take = std::min(room, span - k);
+            p.b[n] = b;
+            p.kb[n] = static_cast<int32_t>(k);
+            p.ke[n] = static_cast<int32_t>(std::min<int64_t>(k + take, len));
+            ++n;
+            k += take;
+            room -= take;
         }
-        while (b < B) p.off[++b] = static_cast<int32_t>(p.b.size());
+        p.off[b + 1] = n;
     }
-    p.slot_off.push_back(static_cast<int32_t>(p.b.size()));
-    if (static_cast<int>(p.b.size()) > decode_work_cap(c, B) || n_slots > decode_slot_cap(c))
-        return fail(SLW_EINVAL, "internal: decode work %zu / slots %d above cap", p.b.size(), n_slots);
+    p.slot_off[sl] = n;
+    p.b.resize(n);
+    p.kb.resize(n);
+    p.ke.resize(n);
+    if (n > cap || sl != n_slots) return fail(SLW_EINVAL, "internal: decode work %d above cap, or %d slots of %d", n, sl, n_slots);
     for (int d = 0; d < B; ++d) {  // the items of each decode tile its keys
         int64_t at = 0;
         for (int i = p.off[d]; i < p.off[d + 1]; ++i) {
             if (p.b[i] != d || p.kb[i] != at || p.ke[i] <= at) return fail(SLW_EINVAL, "internal: decode plan");
             at = p.ke[i];
         }
-        if (at != keys(d)) return fail(SLW_EINVAL, "internal: decode plan");
+        if (at != p.keys[d]) return fail(SLW_EINVAL, "internal: decode plan");
     }
     return SLW_OK;
 }
@@ -239,14 +237,18 @@ int plan_chunk(const slw_model_cfg& c, const Window& w, bool cache, int C, const
             for (int q = 0; q < n_qt; ++q) order[q] = q;
             auto len = [&](int q) { return tile_end[q + 1] - tile_end[q]; };
             std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return len(x) > len(y); });
-            std::vector<int64_t> load(spread, 0);
+            // (load, work-group) heap: the least loaded on top, the lowest of equals
+            std::vector<std::pair<int64_t, int32_t>> load(spread);
+            for (int64_t g = 0; g < spread; ++g) load[g] = {0, static_cast<int32_t>(g)};
             std::vector<int32_t> owner(n_qt);
+            int64_t mx = 0;
             for (int q : order) {
-                const int g = static_cast<int>(std::min_element(load.begin(), load.end()) - load.begin());
-                load[g] += len(q);
-                owner[q] = g;
+                std::pop_heap(load.begin(), load.end(), std::greater<>());
+                load.back().first += len(q);
+                owner[q] = load.back().second;
+                mx = std::max(mx, load.back().first);
+                std::push_heap(load.begin(), load.end(), std::greater<>());
             }
-            const int64_t mx = *std::max_element(load.begin(), load.end());
             bool whole = mx * kChunkWholeSlackDen <= per * kChunkWholeSlackNum;
             if (cache) {
                 const int64_t runs = ceil_div(total_tiles, per);

@@ -35,6 +35,7 @@ struct DecodePlan {
     std::vector<int32_t> off;        // [B + 1] first item of each decode
     std::vector<int32_t> slot_off;   // [slots + 1] first item of each wave slot
     std::vector<int32_t> skip;       // [B] keys between each decode's sinks and its window that are left out
+    std::vector<int32_t> keys;       // [B] virtual keys of each decode
 };
 struct ChunkPlan {
     std::vector<int32_t> items;       // [3 n]: query tile, first virtual key, virtual key past the last
