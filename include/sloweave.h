@@ -268,8 +268,10 @@ int slw_mixed_iteration_static(slw_ctx* ctx, const slw_batch* batch, const void*
  * (device, 16-byte aligned, ws_bytes >= slw_attn_workspace_size(ctx, C, B); a
  * first kernel on `stream` copies it from a pinned staging ring) and returns a
  * plan (host memory, freed by slw_attn_end).  It is not for streams under
- * capture (SLW_EINVAL).  C == 0 and B == 0 together gives a plan whose calls do
- * nothing.
+ * capture (SLW_EINVAL), nor to be called while another stream captures in global
+ * mode; calls of the plan on other streams are ordered after it by the caller.
+ * A batch that is refused leaves no plan (*plan = NULL).  C == 0 and B == 0
+ * together gives a plan whose calls do nothing.
  *   The plan stays usable, any number of times, while its sequences live, `ws`
  * is left alone and neither pools nor windows are set anew (then SLW_EINVAL).
  * Its calls are asynchronous, allocate nothing and may be captured into
