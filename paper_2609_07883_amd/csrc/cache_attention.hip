@@ -27,6 +27,9 @@ namespace {
 typedef const float __attribute__((address_space(4))) const_f32;
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
+// Lists through the scalar cache.
+__device__ __forceinline__ int of(const int32_t* p, int i) { return ((const const_i32*)p)[i]; }
+
 constexpr float kSlack = 8.0f;  // lazy rescaling threshold (log2 units), as in the bf16 kernels
 
 // Four e4m3 codes times a power of two, in bf16 (exact; NaN stays NaN).
@@ -135,11 +138,9 @@ __device__ __forceinline__ void cache_decode_items(const CacheAttnArgs& a, int s
     const int group = d.hq / d.hkv;
     const float sl2 = kLog2e / sqrtf(static_cast<float>(HD));
 
-    // Lists through the scalar cache: 0.3 to 1 us less than through vector loads.
-    // (Asked for an item ahead, under the first keys of the one before, they
+    // Through the scalar cache an item's lists take 0.3 to 1 us less.  (Asked for an item ahead, under the first keys of the one before, they
     // took 0.5 to 1 us longer: most waves have one item or two.)
-    auto of = [](const int32_t* p, int i) { return ((const const_i32*)p)[i]; };
-    const int i0 = d.slot_off[slot], i1 = d.slot_off[slot + 1];
+    const int i0 = of(d.slot_off, slot), i1 = of(d.slot_off, slot + 1);
     for (int w = i0; w < i1; ++w) {
         const int b = of(d.work_b, w), v0 = of(d.work_kb, w), v1 = of(d.work_ke, w);
         const int len = of(d.kv_len, b), skip = of(a.skip, b);
@@ -344,21 +345,21 @@ struct Item {
     __device__ __forceinline__ Item(const CacheAttnArgs& a, int index, int wave, int pw) {
         const ChunkAttnArgs& c = a.chunk;
         item = index;
-        const int qt = c.item_qt[item];
-        v0 = c.item_kb[item];
-        n_tiles = (c.item_ke[item] - v0 + 63) / 64;
-        row0 = c.qt_row0[qt];
-        nrows = c.qt_rows[qt];
-        pos0 = c.qt_pos0[qt];
-        skip = a.qt_skip[qt];
-        bt = (const const_i32*)(c.bt + c.qt_bt[qt]);
+        const int qt = of(c.item_qt, item);
+        v0 = of(c.item_kb, item);
+        n_tiles = (of(c.item_ke, item) - v0 + 63) / 64;
+        row0 = of(c.qt_row0, qt);
+        nrows = of(c.qt_rows, qt);
+        pos0 = of(c.qt_pos0, qt);
+        skip = of(a.qt_skip, qt);
+        bt = (const const_i32*)(c.bt + of(c.qt_bt, qt));
         key_end = pos0 + nrows;
         last_page = (key_end - 1) >> 4;
         j0 = wave * pw;
         lo = pos0 + j0;
         hi = lo + pw - 1;
         live = j0 < nrows;
-        whole = c.qt_off[qt + 1] - c.qt_off[qt] == 1;
+        whole = of(c.qt_off, qt + 1) - of(c.qt_off, qt) == 1;
         window = a.window > 0 ? a.window : 0x7FFFFFFF;
         sinks = a.sinks;
         sink_end = a.sink_end;
@@ -769,9 +770,9 @@ __global__ __launch_bounds__(512) void cache_chunk_kernel(CacheAttnArgs a) {
     const float sl2 = kLog2e / sqrtf(static_cast<float>(HD));
     const bf16x8 ones = ones8();
 
-    const int i0 = c.slot_off[slot], i1 = c.slot_off[slot + 1];
+    const int i0 = of(c.slot_off, slot), i1 = of(c.slot_off, slot + 1);
     for (int k = i0; k < i1; ++k) {
-        const Item it(a, c.slot_items[k], wave, PW);
+        const Item it(a, of(c.slot_items, k), wave, PW);
         bf16x8 qf[CT][KK];
         load_q<HD, GROUP>(qf, c, it, kvh, col, grp);
         Rows<HD> rows;
@@ -930,9 +931,9 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
     const int l_k = (lane >> 2) * 32 + kswz(lane >> 2, lane & 3) * 8;
     auto page_of = [&](int i) { return Q8 ? P::page(64 * wave) : (wave + 8 * i) / KK; };
 
-    const int i0 = c.slot_off[slot], i1 = c.slot_off[slot + 1];
+    const int i0 = of(c.slot_off, slot), i1 = of(c.slot_off, slot + 1);
     for (int k = i0; k < i1; ++k) {
-        const Item it(a, c.slot_items[k], wave, PW);
+        const Item it(a, of(c.slot_items, k), wave, PW);
         const int n_tiles = it.n_tiles;
         bf16x8 qf[CT][KK];
         load_q<HD, GROUP>(qf, c, it, kvh, col, grp);
