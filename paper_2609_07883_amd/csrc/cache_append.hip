@@ -15,7 +15,8 @@
 // once.  One wave per (block, kv head, K or V): K pages are token-major, so a
 // lane takes 16 dims of one token from the row to the page; V pages are
 // dim-major, so a lane takes its dims of all 16 tokens, which transposes in
-// registers.
+// registers.  8B heads: 4096 rows 6.6 us (25 MB, 3.8 TB/s); one token of each of
+// 256 sequences 5.7 us, start and latency, for 5.6 MB.
 #include "device.h"
 #include "kernels.h"
 
@@ -198,7 +199,9 @@ __device__ __forceinline__ void append_v8(const AppendArgs& a, const Item& it, i
     constexpr int D = HD / 64;  // dims of a lane
     const size_t bh = static_cast<size_t>(it.blk) * a.cache.hkv + kvh;
     u32x4* page = reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.cache.v_pool) + bh * HD * 16) + lane * D;
-    const float s_old = a.cache.v_scale[bh];
+    uint32_t zero = 0;
+    asm volatile("" : "+v"(zero));  // a vector load, issued here: a scalar one is put off to its use (+0.2 us)
+    const float s_old = a.cache.v_scale[bh + zero];
     u32x4 held[D] = {};
     if (it.n < 16) {
 #pragma unroll
