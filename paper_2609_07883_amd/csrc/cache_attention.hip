@@ -29,6 +29,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // Lists through the scalar cache.
 __device__ __forceinline__ int of(const int32_t* p, int i) { return ((const const_i32*)p)[i]; }
+__device__ __forceinline__ const const_i32* record(const int32_t* p, int i) { return (const const_i32*)p + 8 * i; }
 
 constexpr float kSlack = 8.0f;  // lazy rescaling threshold (log2 units), as in the bf16 kernels
 
@@ -142,13 +143,13 @@ __device__ __forceinline__ void cache_decode_items(const CacheAttnArgs& a, int s
     // took 0.5 to 1 us longer: most waves have one item or two.)
     const int i0 = of(d.slot_off, slot), i1 = of(d.slot_off, slot + 1);
     for (int w = i0; w < i1; ++w) {
-        const int b = of(d.work_b, w), v0 = of(d.work_kb, w), v1 = of(d.work_ke, w);
-        const int len = of(d.kv_len, b), skip = of(a.skip, b);
-        const bool whole = of(d.work_off, b + 1) - of(d.work_off, b) == 1;  // all of the decode
+        const const_i32* rec = record(a.decode_items, w);
+        const int b = rec[0], v0 = rec[1], v1 = rec[2], len = rec[3], skip = rec[4], at = rec[5];
+        const bool whole = rec[6] != 0;  // all of the decode
         const int last_pg = (len - 1) >> 4;
         // keys below w_lo are seen only if they are sinks
         const int w_lo = a.window > 0 ? max(len - a.window, 0) : 0;
-        const const_i32* bt_s = (const const_i32*)(d.bt + of(d.bt_off, b));
+        const const_i32* bt_s = (const const_i32*)(d.bt + at);
         auto key_of = [&](int v) { return v < a.sink_end ? v : v + skip; };
 
         // Q^T operand: the dims that a lane's K pieces hold
@@ -344,22 +345,22 @@ struct Item {
 
     __device__ __forceinline__ Item(const CacheAttnArgs& a, int index, int wave, int pw) {
         const ChunkAttnArgs& c = a.chunk;
-        item = index;
-        const int qt = of(c.item_qt, item);
-        v0 = of(c.item_kb, item);
-        n_tiles = (of(c.item_ke, item) - v0 + 63) / 64;
-        row0 = of(c.qt_row0, qt);
-        nrows = of(c.qt_rows, qt);
-        pos0 = of(c.qt_pos0, qt);
-        skip = of(a.qt_skip, qt);
-        bt = (const const_i32*)(c.bt + of(c.qt_bt, qt));
+        const const_i32* rec = record(a.chunk_items, index);
+        whole = rec[0] < 0;
+        item = whole ? ~rec[0] : rec[0];
+        v0 = rec[1];
+        n_tiles = (rec[2] - v0 + 63) / 64;
+        row0 = rec[3];
+        nrows = rec[4];
+        pos0 = rec[5];
+        skip = rec[6];
+        bt = (const const_i32*)(c.bt + rec[7]);
         key_end = pos0 + nrows;
         last_page = (key_end - 1) >> 4;
         j0 = wave * pw;
         lo = pos0 + j0;
         hi = lo + pw - 1;
         live = j0 < nrows;
-        whole = of(c.qt_off, qt + 1) - of(c.qt_off, qt) == 1;
         window = a.window > 0 ? a.window : 0x7FFFFFFF;
         sinks = a.sinks;
         sink_end = a.sink_end;
@@ -772,7 +773,7 @@ __global__ __launch_bounds__(512) void cache_chunk_kernel(CacheAttnArgs a) {
 
     const int i0 = of(c.slot_off, slot), i1 = of(c.slot_off, slot + 1);
     for (int k = i0; k < i1; ++k) {
-        const Item it(a, of(c.slot_items, k), wave, PW);
+        const Item it(a, k, wave, PW);
         bf16x8 qf[CT][KK];
         load_q<HD, GROUP>(qf, c, it, kvh, col, grp);
         Rows<HD> rows;
@@ -933,7 +934,7 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
 
     const int i0 = of(c.slot_off, slot), i1 = of(c.slot_off, slot + 1);
     for (int k = i0; k < i1; ++k) {
-        const Item it(a, of(c.slot_items, k), wave, PW);
+        const Item it(a, k, wave, PW);
         const int n_tiles = it.n_tiles;
         bf16x8 qf[CT][KK];
         load_q<HD, GROUP>(qf, c, it, kvh, col, grp);

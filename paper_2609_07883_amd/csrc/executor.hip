@@ -109,11 +109,12 @@ size_t attn_meta_ints(const slw_ctx& ctx, int C, int B) {
     const slw_model_cfg& c = ctx.cfg;
     const size_t mb = static_cast<size_t>(max_blocks(c));
     const size_t np = C > 0 ? static_cast<size_t>(std::min(C, static_cast<int>(SLW_MAX_PREFILLS))) : 0;
-    const size_t per_class = 3 * static_cast<size_t>(decode_work_cap(c, B)) + (B + 1) + decode_slot_cap(c) + 1 + B +
-                             4 * static_cast<size_t>(chunk_item_cap(c, C)) + 2 * static_cast<size_t>(chunk_tiles(c, C)) + 1 +
-                             chunk_slot_cap(c) + 1;
+    const size_t work = decode_work_cap(c, B), items = chunk_item_cap(c, C);
+    const size_t per_class = (B + 1) + decode_slot_cap(c) + 1 + static_cast<size_t>(chunk_tiles(c, C)) + 1 + chunk_slot_cap(c) + 1;
+    const size_t cache_classes = ctx.any_windowed + (ctx.any_full && ctx.k_scale);
     return B + (B + 1) + static_cast<size_t>(B) * mb + np * mb + 4 * static_cast<size_t>(chunk_tiles(c, C)) +
-           4 * append_cap(C, B) + per_class * (ctx.any_full + ctx.any_windowed);
+           4 * append_cap(C, B) + per_class * (ctx.any_full + ctx.any_windowed) +
+           (ctx.any_full && !ctx.k_scale ? 3 * work + 4 * items : 0) + 8 * (work + items) * cache_classes;
 }
 
 size_t meta_ints(const slw_ctx& ctx, int C, int B) {
@@ -390,7 +391,7 @@ struct AttnMeta {
     size_t kvlen = 0, btoff = 0, bt = 0, pre = 0, qt = 0, app = 0;
     struct Class {  // the work lists of full ([0]) or windowed ([1]) layers
         int n_work = 0, n_dslots = 0, n_items = 0, n_slots = 0;
-        size_t work = 0, skip = 0, item = 0, slot = 0, slot_items = 0, qtoff = 0, qt_skip = 0;
+        size_t work = 0, work_off = 0, decode_slot = 0, item = 0, slot = 0, slot_items = 0, qtoff = 0;
         bool two_phase = false;
         int64_t decode_keys = 0;
     } cls[2];
@@ -478,25 +479,47 @@ int build_attn_meta(slw_ctx* ctx, const slw_batch* bt, std::vector<int32_t>& m, 
         if ((rc = plan_chunk(c, w, cache, C, qt_pos0, qt_rows, cp))) return rc;
         cl.n_items = static_cast<int>(cp.items.size() / 3);
         cl.n_slots = static_cast<int>(cp.slot_off.size()) - 1;
-        cl.item = m.size();
-        m.resize(m.size() + cp.items.size());
-        for (int i = 0; i < cl.n_items; ++i)
-            for (int j = 0; j < 3; ++j) m[cl.item + static_cast<size_t>(j) * cl.n_items + i] = cp.items[3 * i + j];
         cl.slot = put(cp.slot_off);
-        cl.slot_items = put(cp.slot_items);
         cl.qtoff = put(cp.qt_off);
-        cl.qt_skip = put(cp.qt_skip);
+        cl.item = m.size();
+        if (!cache) {
+            m.resize(m.size() + cp.items.size());
+            for (int i = 0; i < cl.n_items; ++i)
+                for (int j = 0; j < 3; ++j) m[cl.item + static_cast<size_t>(j) * cl.n_items + i] = cp.items[3 * i + j];
+            cl.slot_items = put(cp.slot_items);
+        } else {  // CacheAttnArgs::chunk_items
+            m.resize(m.size() + 8 * cp.slot_items.size());
+            int32_t* at = m.data() + cl.item;
+            for (const int32_t i : cp.slot_items) {
+                const int q = cp.items[3 * i];
+                const bool whole = cp.qt_off[q + 1] - cp.qt_off[q] == 1;
+                const int32_t rec[8] = {whole ? ~i : i, cp.items[3 * i + 1], cp.items[3 * i + 2], qt_row0[q],
+                                        qt_rows[q], qt_pos0[q], cp.qt_skip[q], qt_bt[q]};
+                at = std::copy(rec, rec + 8, at);
+            }
+        }
         cl.two_phase = cp.two_phase;
         DecodePlan& dp = ctx->dplan;
         if ((rc = plan_decode(c, w, decode_kind(cache, cp), B, bt->context_lens, dp))) return rc;
         cl.n_work = static_cast<int>(dp.b.size());
         cl.n_dslots = static_cast<int>(dp.slot_off.size()) - 1;
-        cl.work = put(dp.b);
-        put(dp.kb);
-        put(dp.ke);
-        put(dp.off);
-        put(dp.slot_off);
-        cl.skip = put(dp.skip);
+        cl.work_off = put(dp.off);
+        cl.decode_slot = put(dp.slot_off);
+        if (!cache) {
+            cl.work = put(dp.b);
+            put(dp.kb);
+            put(dp.ke);
+        } else {  // CacheAttnArgs::decode_items
+            cl.work = m.size();
+            m.resize(m.size() + 8 * dp.b.size());
+            int32_t* at = m.data() + cl.work;
+            for (int i = 0; i < cl.n_work; ++i) {
+                const int b = dp.b[i];
+                const int32_t rec[8] = {b, dp.kb[i], dp.ke[i], bt->context_lens[b] + 1, dp.skip[b], m[am.btoff + b],
+                                        dp.off[b + 1] - dp.off[b] == 1, 0};
+                at = std::copy(rec, rec + 8, at);
+            }
+        }
         for (int b = 0; b < B; ++b) cl.decode_keys += bt->context_lens[b] + 1 - dp.skip[b];
     }
     return SLW_OK;
@@ -533,9 +556,6 @@ struct AttnCall {
             ca.k_pool = pool.k_pool;
             ca.v_pool = pool.v_pool;
             ca.bt = dmeta + am.pre;
-            ca.item_qt = dmeta + cl.item;
-            ca.item_kb = dmeta + cl.item + cl.n_items;
-            ca.item_ke = dmeta + cl.item + 2 * cl.n_items;
             ca.qt_off = dmeta + cl.qtoff;
             ca.part_o = reinterpret_cast<float*>(ws + P.cpart_o);
             ca.part_ml = reinterpret_cast<float*>(ws + P.cpart_ml);
@@ -550,7 +570,6 @@ struct AttnCall {
             ca.hd = hd;
             ca.ld_qkv = ld;
             ca.slot_off = dmeta + cl.slot;
-            ca.slot_items = dmeta + cl.slot_items;
             ca.n_items = cl.n_items;
             ca.n_slots = cl.n_slots;
             ca.split = cl.n_items > am.n_qt ? 1 : 0;
@@ -565,11 +584,8 @@ struct AttnCall {
             da.kv_len = dmeta + am.kvlen;
             da.bt_off = dmeta + am.btoff;
             da.bt = dmeta + am.bt;
-            da.work_b = dmeta + cl.work;
-            da.work_kb = dmeta + cl.work + cl.n_work;
-            da.work_ke = dmeta + cl.work + 2 * cl.n_work;
-            da.work_off = dmeta + cl.work + 3 * cl.n_work;
-            da.slot_off = dmeta + cl.work + 3 * cl.n_work + am.B + 1;
+            da.work_off = dmeta + cl.work_off;
+            da.slot_off = dmeta + cl.decode_slot;
             da.n_slots = cl.n_dslots;
             da.part_o = reinterpret_cast<float*>(ws + P.part_o);
             da.part_ml = reinterpret_cast<float*>(ws + P.part_ml);
@@ -585,8 +601,8 @@ struct AttnCall {
             da.direct = 1;
             a.k_scale = pool.k_scale;
             a.v_scale = pool.v_scale;
-            a.qt_skip = dmeta + cl.qt_skip;
-            a.skip = dmeta + cl.skip;
+            a.chunk_items = dmeta + cl.item;
+            a.decode_items = dmeta + cl.work;
             const Window w = ctx->windowed[l] ? ctx->win : Window{};
             a.window = w.window;
             a.sinks = w.window > 0 ? w.sinks : 0;
@@ -595,6 +611,14 @@ struct AttnCall {
             const int64_t windowed = std::count_if(ctx->windowed.begin(), ctx->windowed.end(), [](char f) { return f != 0; });
             const int64_t keys = am.cls[0].decode_keys * (c.n_layers - windowed) + am.cls[1].decode_keys * windowed;
             a.once = keys * 2 * hkv * hd * (ctx->k_scale ? 1 : 2) > kLastLevelCache;
+        } else {
+            ca.item_qt = dmeta + cl.item;
+            ca.item_kb = dmeta + cl.item + cl.n_items;
+            ca.item_ke = dmeta + cl.item + 2 * cl.n_items;
+            ca.slot_items = dmeta + cl.slot_items;
+            da.work_b = dmeta + cl.work;
+            da.work_kb = dmeta + cl.work + cl.n_work;
+            da.work_ke = dmeta + cl.work + 2 * cl.n_work;
         }
     }
     // The parts: chunk and decode in one launch, or each alone.

@@ -152,16 +152,22 @@ struct AppendArgs {
     int n_items, ld;
 };
 void launch_cache_append(const AppendArgs& a, hipStream_t s);
-// Both attentions; item key ranges are virtual (attn_plan.h): sink_end and a
-// decode's skip (or a query tile's qt_skip) map them to keys.  The pools in
-// `chunk` and `decode` are the cache's.
+// Both attentions; item key ranges are virtual (attn_plan.h): sink_end and an
+// item's keys left out map them to keys.  The pools in `chunk` and `decode` are
+// the cache's; what an item is stands in the lists here, not in theirs.
 struct CacheAttnArgs {
     ChunkAttnArgs chunk;
     DecodeAttnArgs decode;
     const float* k_scale;    // null: a bf16 cache
     const float* v_scale;
-    const int32_t* qt_skip;  // [n_qt]
-    const int32_t* skip;     // [b]
+    // What an item is, in one load: [n_items][8] in the order of the work-groups
+    // (item, or ~item where it is all of its query tile; first virtual key and
+    // virtual key past the last; first row, rows, first position, keys left out
+    // and block-table offset of its query tile) and [n_work][8] (decode, first
+    // virtual key and virtual key past the last; keys, keys left out,
+    // block-table offset of the decode; 1 where it is all of the decode)
+    const int32_t* chunk_items;
+    const int32_t* decode_items;
     int window;              // 0: every earlier key
     int sinks, sink_end;
     int once;                // the decodes' pages are not in a cache by their next use
