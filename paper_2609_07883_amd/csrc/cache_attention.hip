@@ -202,7 +202,11 @@ __device__ __forceinline__ void cache_decode_items(const CacheAttnArgs& a, int s
                     }
                 }
             }
-            const float scale = Q8 ? sl2 * st.ks : sl2;
+            // A page with no seen key has no part through its scales either: -inf
+            // times one that is 0, NaN or negative (a page never written) is not
+            // -inf, and a code of 0 times NaN not 0.
+            const float scale = Q8 ? (seen ? sl2 * st.ks : 1.f) : sl2;
+            const float v_scale = Q8 && seen ? st.vs : 1.f;
             float mx = -INFINITY;
 #pragma unroll
             for (int tau = 0; tau < TAU; ++tau)
@@ -251,7 +255,7 @@ __device__ __forceinline__ void cache_decode_items(const CacheAttnArgs& a, int s
                 for (int nt = 0; nt < NT; ++nt) {
                     const u32x4 x = st.v[nt] & vmask;
                     if constexpr (Q8) {
-                        const bf16x8 v = widen8(x[2 * j], x[2 * j + 1], st.vs);
+                        const bf16x8 v = widen8(x[2 * j], x[2 * j + 1], v_scale);
                         o[nt] = mfma16(pf, v, mfma16(pr, v, o[nt]));
                     } else {
                         o[nt] = mfma16(pf, __builtin_bit_cast(bf16x8, x), o[nt]);
