@@ -152,7 +152,8 @@ int slw_kv_init_8bit(slw_ctx* ctx, void* k_pool, void* v_pool, void* k_scale, vo
  * other layers attend to every t <= p.  window 0 (the state after slw_create)
  * turns windows off.  0 <= sinks <= max_pos, sinks only with a window.  Keys
  * outside are neither read nor waited for (in steps of 64), whatever the pools
- * hold there, but their blocks stay the sequence's.
+ * and the scales of blocks that lie outside whole hold there, but their blocks
+ * stay the sequence's.
  * Workspace sizes depend on the pools attached and the windows set: ask again
  * after either call.
  */

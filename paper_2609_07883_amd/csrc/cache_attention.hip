@@ -416,8 +416,11 @@ struct Pieces {
         }
     }
     // Values of keys from key_end on (unwritten slots, stand-in pages) become
-    // 0; their scores are masked.  Nonzero result: a value is not finite.
-    static __device__ __forceinline__ uint32_t settle_v(int first, int lane, u32x4& x, int key0, int key_end) {
+    // 0; their scores are masked.  Nonzero result: a value is not finite, or
+    // may not be once widened: 448 times 2^120 and more, which a scale of a page
+    // that no row sees can be.
+    static __device__ __forceinline__ uint32_t settle_v(int first, int lane, u32x4& x, int key0, int key_end,
+                                                        float scale) {
         if (key0 + 63 >= key_end) {
             const int k = key0 + 16 * page(first) + (Q8 ? 0 : 8 * (offset(first, lane) & 1));
             const uint32_t live = low_bits(min(max(key_end - k, 0), 16));
@@ -433,7 +436,9 @@ struct Pieces {
             if constexpr (Q8) odd |= (x[w] & 0x7F7F7F7Fu) + 0x01010101u;
             else odd |= (x[w] & 0x7F807F80u) + 0x00800080u;
         }
-        return odd & (Q8 ? 0x80808080u : 0x80008000u);
+        odd &= Q8 ? 0x80808080u : 0x80008000u;
+        if constexpr (Q8) odd |= ((__float_as_uint(scale) >> 23) & 0xFFu) >= 127u + 120u ? 1u : 0u;
+        return odd;
     }
     static __device__ __forceinline__ void put_v(bf16* tile, int first, int lane, u32x4 x, float scale) {
         const int at = offset(first, lane);
@@ -492,7 +497,7 @@ struct Staged {
 #pragma unroll
             for (int i = 0; i < PT; ++i) {
                 const int j = 512 * i + 64 * wave;
-                if (j >= HALF) odd |= P::settle_v(j - HALF, lane, raw[i], key0, it.key_end);
+                if (j >= HALF) odd |= P::settle_v(j - HALF, lane, raw[i], key0, it.key_end, Q8 ? scale[i] : 1.f);
             }
         }
 #pragma unroll
@@ -1001,7 +1006,8 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
             }
         };
         // The pieces of V that a lane loaded itself, on an edge of the mask, once
-        // they have landed: in the tile, or, e4m3, among the codes (r: t % 3).
+        // they have landed: in the tile, or, e4m3, among the codes (r: t % 3),
+        // which are the next to be widened, with vsc[0].
         auto settle = [&](int t, int r) {
             const int key0 = it.key0(t);
             if constexpr (Q8) {
@@ -1009,7 +1015,7 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
                     wait_vmcnt<4>();
                     asm volatile("" ::: "memory");
                     u32x4 x = codes[1][r][tid];
-                    odd |= P::settle_v(64 * wave, lane, x, key0, it.key_end);
+                    odd |= P::settle_v(64 * wave, lane, x, key0, it.key_end, vsc[0]);
                     codes[1][r][tid] = x;
                 }
             } else {
@@ -1020,7 +1026,8 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
                         u32x4* piece = reinterpret_cast<u32x4*>(&Vs[t & 3][page_of(i) * PAGE + slab * 512 + lane * 8]);
                         u32x4 x = *piece;
                         // as the pieces number them: tokens 8 h .. of dim d is piece 2 d + h of its page
-                        odd |= P::settle_v(page_of(i) * P::PP, 2 * d + ((lane & 1) ^ ((d >> 2) & 1)), x, key0, it.key_end);
+                        odd |= P::settle_v(page_of(i) * P::PP, 2 * d + ((lane & 1) ^ ((d >> 2) & 1)), x, key0,
+                                           it.key_end, 1.f);
                         *piece = x;
                     }
                     wait_lgkmcnt0();
@@ -1153,8 +1160,9 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) vsc[x] = v_scale(b[1 + x]);
             P::put_k(Ks[0], 64 * wave, lane, k0, k_scale(b[0]));
-            if (it.edge(it.key0(0))) odd |= P::settle_v(64 * wave, lane, v0, it.key0(0), it.key_end);
-            P::put_v(Vs[0], 64 * wave, lane, v0, v_scale(b[0]));
+            const float vs0 = v_scale(b[0]);
+            if (it.edge(it.key0(0))) odd |= P::settle_v(64 * wave, lane, v0, it.key0(0), it.key_end, vs0);
+            P::put_v(Vs[0], 64 * wave, lane, v0, vs0);
             P::put_k(Ks[1], 64 * wave, lane, k1, k_scale(b[1]));
             wait_lgkmcnt0();
         } else {

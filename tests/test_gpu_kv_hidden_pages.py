@@ -61,3 +61,26 @@ def test_long_decodes(scale):
     """Decodes of several items, whose partial sums are merged."""
     rig = _rig(8, 2, 128, {2: 4095, 3: 6001}, window=2500, sinks=5, grow=1)
     _check(rig, api.Batch(0, 0, 0, (2, 3), (4095, 6001)), scale)
+
+
+@pytest.mark.parametrize("scale", SCALES)
+@pytest.mark.parametrize("hq,hkv,hd,window,sinks", [(4, 4, 64, 50, 3), (8, 2, 128, 200, 70), (16, 1, 128, 1, 0), (8, 1, 64, 333, 0)])
+def test_chunks(hq, hkv, hd, window, sinks, scale):
+    """Prompts behind cached prefixes beside decodes."""
+    pre = [(1, 90, 1), (2, 155, 65), (3, 333, 40), (4, 430, 70)]
+    rig = _rig(hq, hkv, hd, {1: 90, 2: 155, 3: 333, 4: 430, 20: 90, 21: 700}, window=window, sinks=sinks, grow=80)
+    _check(rig, api.Batch.batched(pre, (20, 21), (90, 700)), scale)
+
+
+@pytest.mark.parametrize("scale", SCALES)
+@pytest.mark.parametrize("hq,hkv,C,P,window,sinks", [(64, 16, 1024, 5003, 3500, 0), (128, 16, 512, 5000, 3001, 64),
+                                                      (256, 16, 256, 5000, 2100, 1), (32, 8, 200, 16390, 9001, 5)])
+def test_long_items(hq, hkv, C, P, window, sinks, scale):
+    """The two-phase kernel, query tiles whole and split."""
+    from paper_2609_07883_amd.synth import ModelShape
+    shape = ModelShape(1, 256, hq, hkv, 128, 256, max_pos=32768)
+    assert api.attention_plan(shape, [700], [(P, C)], window, sinks, kv="e4m3")["chunk_two_phase"]
+    rig = _rig(hq, hkv, 128, {1: P, 2: 700}, window=window, sinks=sinks, grow=C + 1, max_pos=32768)
+    tile = 256 * hkv // hq
+    rows = {0, 1, 15, 16, 17, 31, 33, tile - 1, tile, C // 2, C - 1, C}
+    _check(rig, api.Batch(C, 1, P, (2,), (700,)), scale, rows)
