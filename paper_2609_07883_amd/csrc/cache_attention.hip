@@ -139,8 +139,9 @@ __device__ __forceinline__ void cache_decode_items(const CacheAttnArgs& a, int s
     const int group = d.hq / d.hkv;
     const float sl2 = kLog2e / sqrtf(static_cast<float>(HD));
 
-    // Through the scalar cache an item's lists take 0.3 to 1 us less.  (Asked for an item ahead, under the first keys of the one before, they
-    // took 0.5 to 1 us longer: most waves have one item or two.)
+    // Through the scalar cache an item's lists take 0.3 to 1 us less.  (Asked
+    // for an item ahead, under the first keys of the one before, they took 0.5
+    // to 1 us longer: most waves have one item or two.)
     const int i0 = of(d.slot_off, slot), i1 = of(d.slot_off, slot + 1);
     for (int w = i0; w < i1; ++w) {
         const const_i32* rec = record(a.decode_items, w);
@@ -1011,7 +1012,7 @@ __global__ __launch_bounds__(512) void cache_chunk_pp_kernel(CacheAttnArgs a) {
         auto settle = [&](int t, int r) {
             const int key0 = it.key0(t);
             if constexpr (Q8) {
-                if (it.edge(key0)) {
+                if (t < n_tiles && it.edge(key0)) {
                     wait_vmcnt<4>();
                     asm volatile("" ::: "memory");
                     u32x4 x = codes[1][r][tid];
