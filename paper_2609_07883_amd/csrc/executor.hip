@@ -102,10 +102,10 @@ size_t append_cap(int C, int B) {
     return std::min<size_t>(C, C / 16 + 2 * np) + B;
 }
 
-// Metadata of the two attentions and the append (32-bit words): block tables,
-// query tiles, blocks to append to, and the work lists of each class of
-// layers (full attention, windowed).
-size_t attn_meta_ints(const slw_ctx& ctx, int C, int B) {
+// Metadata of the two attentions and, where wanted, the append (32-bit words):
+// block tables, query tiles, blocks to append to, and the work lists of each
+// class of layers (full attention, windowed).
+size_t attn_meta_ints(const slw_ctx& ctx, int C, int B, bool append) {
     const slw_model_cfg& c = ctx.cfg;
     const size_t mb = static_cast<size_t>(max_blocks(c));
     const size_t np = C > 0 ? static_cast<size_t>(std::min(C, static_cast<int>(SLW_MAX_PREFILLS))) : 0;
@@ -113,12 +113,15 @@ size_t attn_meta_ints(const slw_ctx& ctx, int C, int B) {
     const size_t per_class = (B + 1) + decode_slot_cap(c) + 1 + static_cast<size_t>(chunk_tiles(c, C)) + 1 + chunk_slot_cap(c) + 1;
     const size_t cache_classes = ctx.any_windowed + (ctx.any_full && ctx.k_scale);
     return B + (B + 1) + static_cast<size_t>(B) * mb + np * mb + 4 * static_cast<size_t>(chunk_tiles(c, C)) +
-           4 * append_cap(C, B) + per_class * (ctx.any_full + ctx.any_windowed) +
+           (append ? 4 * append_cap(C, B) : 0) + per_class * (ctx.any_full + ctx.any_windowed) +
            (ctx.any_full && !ctx.k_scale ? 3 * work + 4 * items : 0) + 8 * (work + items) * cache_classes;
 }
 
+// An iteration appends to bf16 pools in the QKV projection's epilogue.
+bool iteration_appends(const slw_ctx& ctx) { return ctx.k_scale != nullptr; }
+
 size_t meta_ints(const slw_ctx& ctx, int C, int B) {
-    return 2 * (static_cast<size_t>(C) + B) + attn_meta_ints(ctx, C, B);
+    return 2 * (static_cast<size_t>(C) + B) + attn_meta_ints(ctx, C, B, iteration_appends(ctx));
 }
 
 // Partial sums of the two attentions, after `off`.
@@ -397,9 +400,9 @@ struct AttnMeta {
     } cls[2];
 };
 
-// Appends the metadata of both attentions and of the append to m; offsets
-// count from m's start.
-int build_attn_meta(slw_ctx* ctx, const slw_batch* bt, std::vector<int32_t>& m, AttnMeta& am) {
+// Appends the metadata of both attentions and, with `append`, of the append to
+// m; offsets count from m's start.
+int build_attn_meta(slw_ctx* ctx, const slw_batch* bt, bool append, std::vector<int32_t>& m, AttnMeta& am) {
     const slw_model_cfg& c = ctx->cfg;
     const int C = bt->C, B = bt->B;
     const std::vector<Prefill>& pre = ctx->prefills;
@@ -445,27 +448,28 @@ int build_attn_meta(slw_ctx* ctx, const slw_batch* bt, std::vector<int32_t>& m, 
     put(qt_rows);
     put(qt_pos0);
     put(qt_bt);
-    // [4][n_app]: block, first new token, new tokens, first row of each block appended to
-    std::vector<int32_t> app[4];
-    for (auto& v : app) v.reserve(append_cap(C, B));
-    auto add = [&](const KvManager::Seq* q, int at, int n, int row) {
-        const auto& t = q->blocks;
-        for (const int end = at + n; at < end;) {
-            const int k = std::min(16 - at % 16, end - at);
-            app[0].push_back(t[at / 16]);
-            app[1].push_back(at % 16);
-            app[2].push_back(k);
-            app[3].push_back(row);
-            at += k;
-            row += k;
-        }
-    };
-    for (size_t i = 0; i < pre.size(); ++i) add(ctx->batch_seqs[i].first, pre[i].prefix, pre[i].c, pre[i].row0);
-    for (int b = 0; b < B; ++b) add(ctx->batch_seqs[pre.size() + b].first, bt->context_lens[b], 1, C + b);
-    am.n_app = static_cast<int>(app[0].size());
-    if (app[0].size() > append_cap(C, B)) return fail(SLW_EINVAL, "internal: %d blocks to append to above cap", am.n_app);
-    am.app = m.size();
-    for (const auto& v : app) put(v);
+    if (append) {  // [4][n_app]: block, first new token, new tokens, first row of each block appended to
+        std::vector<int32_t> app[4];
+        for (auto& v : app) v.reserve(append_cap(C, B));
+        auto add = [&](const KvManager::Seq* q, int at, int n, int row) {
+            const auto& t = q->blocks;
+            for (const int end = at + n; at < end;) {
+                const int k = std::min(16 - at % 16, end - at);
+                app[0].push_back(t[at / 16]);
+                app[1].push_back(at % 16);
+                app[2].push_back(k);
+                app[3].push_back(row);
+                at += k;
+                row += k;
+            }
+        };
+        for (size_t i = 0; i < pre.size(); ++i) add(ctx->batch_seqs[i].first, pre[i].prefix, pre[i].c, pre[i].row0);
+        for (int b = 0; b < B; ++b) add(ctx->batch_seqs[pre.size() + b].first, bt->context_lens[b], 1, C + b);
+        am.n_app = static_cast<int>(app[0].size());
+        if (app[0].size() > append_cap(C, B)) return fail(SLW_EINVAL, "internal: %d blocks to append to above cap", am.n_app);
+        am.app = m.size();
+        for (const auto& v : app) put(v);
+    }
 
     for (int k = 0; k < 2; ++k) {
         if (!(k ? ctx->any_windowed : ctx->any_full)) continue;
@@ -672,7 +676,7 @@ int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void*
         for (int j = 0; j < f.c; ++j) m.push_back(f.prefix + j);
     for (int b = 0; b < B; ++b) m.push_back(bt->context_lens[b]);
     AttnMeta am;
-    if ((rc = build_attn_meta(ctx, bt, m, am))) return rc;
+    if ((rc = build_attn_meta(ctx, bt, iteration_appends(*ctx), m, am))) return rc;
 
     if (m.size() > meta_ints(*ctx, C, B)) return fail(SLW_EINVAL, "internal: metadata %zu ints above its region", m.size());
 
@@ -995,7 +999,7 @@ struct AttnLayout {
     PartLayout part;
 };
 AttnLayout attn_layout(const slw_ctx& ctx, int C, int B) {
-    const size_t meta = align_up(attn_meta_ints(ctx, C, B) * 4);
+    const size_t meta = align_up(attn_meta_ints(ctx, C, B, true) * 4);
     return {meta, part_layout(ctx.cfg, C, B, meta)};
 }
 
@@ -1067,7 +1071,7 @@ extern "C" int slw_attn_begin(slw_ctx* ctx, const slw_batch* batch, void* ws, si
         auto upload = [&]() -> int {
             std::vector<int32_t>& m = ctx->meta;
             m.clear();
-            int r = build_attn_meta(ctx, batch, m, plan->am);
+            int r = build_attn_meta(ctx, batch, true, m, plan->am);
             if (r) return r;
             if (m.size() * 4 > L.meta_bytes) return fail(SLW_EINVAL, "internal: metadata %zu ints above its region", m.size());
             int32_t* stage = nullptr;
