@@ -146,7 +146,7 @@ PartLayout part_layout(const slw_model_cfg& c, int C, int B, size_t off) {
 }
 
 struct Layout {
-    size_t xn, qkv, attn, h, act, rope, new_k, new_v, meta, gemm_part, end_fixed;
+    size_t xn, qkv, attn, h, act, rope, meta, gemm_part, end_fixed;
     PartLayout part;
     size_t gemm_part_bytes;  // from gemm_part on; set where the workspace is known
 };
@@ -167,11 +167,6 @@ Layout layout(const slw_ctx& ctx, int C, int B) {
     L.h = take(M * c.d_model * 4);  // fp32 residual stream inside the layer
     L.act = take(M * c.ffn_dim * 2);
     L.rope = take(M * (c.head_dim / 2) * 8);
-    // e4m3 pools: bf16 pages of the iteration's own rows, which the QKV
-    // projection's epilogue fills in the place of the pools
-    const size_t fresh = ctx.k_scale ? ceil_div(M, 16) * 16 * c.n_kv_heads * c.head_dim * 2 : 0;
-    L.new_k = take(fresh);
-    L.new_v = take(fresh);
     L.meta = take(meta_ints(ctx, C, B) * 4);
     L.part = part_layout(c, C, B, off);
     off = L.part.end;
@@ -668,10 +663,7 @@ int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void*
     for (size_t i = 0; i < pre.size(); ++i)
         for (int j = 0; j < pre[i].c; ++j) slots[pre[i].row0 + j] = ctx->batch_seqs[i].first->slot(pre[i].prefix + j, 16);
     for (int b = 0; b < B; ++b) slots[C + b] = ctx->batch_seqs[pre.size() + b].first->slot(bt->context_lens[b], 16);
-    if (ctx->k_scale)  // the QKV projection writes its rows to pages of their own
-        for (int r = 0; r < M; ++r) m.push_back(r);
-    else
-        m.insert(m.end(), slots.begin(), slots.end());
+    m.insert(m.end(), slots.begin(), slots.end());
     for (const Prefill& f : pre)
         for (int j = 0; j < f.c; ++j) m.push_back(f.prefix + j);
     for (int b = 0; b < B; ++b) m.push_back(bt->context_lens[b]);
@@ -748,13 +740,15 @@ int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void*
             GemmArgs ga{xn, wl.wqkv, qkv, nullptr, M, qw, d, d, qw, EPI_QKV};
             ga.rope_cs = rope;
             ga.slot = d_slot;
-            ga.k_pool = ctx->k_scale ? wsb + L.new_k : pool.k_pool;
-            ga.v_pool = ctx->k_scale ? wsb + L.new_v : pool.v_pool;
+            if (!ctx->k_scale) {
+                ga.k_pool = pool.k_pool;
+                ga.v_pool = pool.v_pool;
+            }
             ga.hq = hq;
             ga.hkv = hkv;
             ga.hd = hd;
             launch_gemm(ga, plans.qkv, gpartp, L.gemm_part_bytes, stream);
-            if (ctx->k_scale) {
+            if (ctx->k_scale) {  // e4m3 pools take the rows from the projection's output
                 const char* k = static_cast<const char*>(qkv) + static_cast<size_t>(hq) * hd * 2;
                 launch_cache_append(append_args(ctx, am, dmeta, l, k, k + static_cast<size_t>(hkv) * hd * 2, qw), stream);
             }

@@ -37,7 +37,7 @@ __device__ __forceinline__ int qkv_dim(int cw, int hd) {
 
 // Rotate (x0, x1) = dims (d0, d0 + hd/2) of head hg of row `row` by the
 // iteration's table (q and k heads; v heads are not rotated) and store; k and
-// v also go to their KV page at slot[row].
+// v also go to their KV page at slot[row], where there are bf16 pools.
 __device__ __forceinline__ void qkv_store(const GemmArgs& g, int row, int hg, int d0, float x0, float x1) {
     const int d1 = d0 + g.hd / 2, slot = hg < g.hq ? 0 : g.slot[row];
     bf16* out = static_cast<bf16*>(g.out) + static_cast<size_t>(row) * g.ldo + hg * g.hd;
@@ -51,7 +51,7 @@ __device__ __forceinline__ void qkv_store(const GemmArgs& g, int row, int hg, in
     const bf16 b0 = f2bf(x0), b1 = f2bf(x1);
     out[d0] = b0;
     out[d1] = b1;
-    if (hg < g.hq) return;
+    if (hg < g.hq || !g.k_pool) return;
     const size_t blk = slot >> 4, t = slot & 15;
     if (hg < g.hq + g.hkv) {
         bf16* pg = static_cast<bf16*>(g.k_pool) + (blk * g.hkv + (hg - g.hq)) * g.hd * 16;
@@ -243,7 +243,7 @@ __device__ __forceinline__ void tile_store(const GemmArgs& g, int m0, int n0, in
         }
     } else if constexpr (EPI == EPI_QKV) {
         const int half = g.hd >> 1, hg = c0 / g.hd, d0 = c0 % g.hd, d1 = d0 + half;
-        const bool rot = hg < g.hq + g.hkv, paged = hg >= g.hq;
+        const bool rot = hg < g.hq + g.hkv, paged = hg >= g.hq && g.k_pool;
         constexpr int IC = 2;  // row groups whose tables are read at once
 #pragma unroll
         for (int i0 = 0; i0 < HA; i0 += IC) {

@@ -19,6 +19,7 @@ void launch_rmsnorm(const void* x, bool x_f32, const void* g, void* y, int rows,
 //   EPI_SWIGLU        W holds gate rows then up rows (n = 2f); out bf16 [m][f] = silu(gate) * up
 //   EPI_QKV           W is the fused q/k/v projection; out bf16 [m][n] holds q and k rotated by
 //                     RoPE and v; k and v are also appended to the paged pools at slot[r]
+//                     where there are bf16 pools (k_pool and v_pool, else null)
 enum GemmEpilogue { EPI_RESID_F32OUT = 0, EPI_RESID_F32IN = 1, EPI_SWIGLU = 2, EPI_QKV = 3 };
 struct GemmArgs {
     const void* a;      // bf16 [m][k], row stride lda

@@ -22,3 +22,15 @@ def test_bf16_iteration(shape):
     c = _ctx(shape)
     c.kv_init(64, 64, 4)
     assert tuple(c.workspace_size(*r) for r in ROWS) == BF16[shape]
+
+
+@pytest.mark.parametrize("shape", BF16)
+def test_8bit_iteration(shape):
+    """Over the 8-bit cache an iteration's workspace holds longer lists and no second copy of its K/V rows."""
+    c = _ctx(shape)
+    for C, B in ROWS:
+        c.kv_init(64, 64, 4)
+        it, op = c.workspace_size(C, B), c.attn_workspace_size(C, B)
+        c.kv_init_8bit(64, 64, 64, 64, 4)
+        lists = c.attn_workspace_size(C, B) - op + 16 * (C + B) + 2 * 256     # at most one append (four words) a row
+        assert it <= c.workspace_size(C, B) <= it + lists
