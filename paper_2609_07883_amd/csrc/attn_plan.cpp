@@ -209,10 +209,12 @@ int plan_decode(const slw_model_cfg& c, const Window& w, DecodeKind kind, int B,
 //
 // Layers on the cache kernels (`cache`) weigh the two instead: whole query
 // tiles on up to one work-group each against equal runs, whose partial sums are
-// written and merged.  In units of a 64-key tile (about 1.2 us), the merge's
-// launch takes 4 and an item of 1024 values a row (all kv heads) 0.4: four
-// prompts of 1500 rows under a window of 512 took 40 + 16 us (merge) in equal
-// runs and 35 + 4 us whole; 77 rows at 50, two query tiles, 14 against 20.
+// written and merged.  In units of a 64-key tile (1.9 us where few CUs work,
+// 2.3 where all do), the rule counts 4 for the merge's launch and 0.4 for an
+// item of 1024 values a row (all kv heads).  The two numbers were chosen on two
+// shapes, whose both sides they get right, and are no fit: four prompts of 1500
+// rows under a window of 512 took 40 + 16 us (merge) in equal runs and 35 + 4 us
+// whole; 77 rows at 50, two query tiles, 14 whole against 20.
 int plan_chunk(const slw_model_cfg& c, const Window& w, bool cache, int C, const std::vector<int32_t>& qt_pos0,
                const std::vector<int32_t>& qt_rows, ChunkPlan& p) {
     const int n_qt = static_cast<int>(qt_pos0.size());

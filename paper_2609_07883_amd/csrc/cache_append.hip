@@ -15,8 +15,10 @@
 // once.  One wave per (block, kv head, K or V): K pages are token-major, so a
 // lane takes 16 dims of one token from the row to the page; V pages are
 // dim-major, so a lane takes its dims of all 16 tokens, which transposes in
-// registers.  8B heads: 4096 rows 6.6 us (25 MB, 3.8 TB/s); one token of each of
-// 256 sequences 5.7 us, start and latency, for 5.6 MB.
+// registers.  8B heads: 4096 rows 6.6 to 7.5 us (25 MB, 3.4 to 3.8 TB/s); one
+// token of each of 256 sequences 5.7 us, start and latency, for 5.6 MB.  In bf16
+// 4096 rows take 10.8 us (34 MB, 3.1 TB/s; 6.5 at a large copy's rate) and 1500
+// rows 5.6 to 6.4 (12.4 MB; 2.4), of which a launch with one token takes 2 to 3.
 #include "device.h"
 #include "kernels.h"
 

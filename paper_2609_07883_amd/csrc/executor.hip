@@ -5,8 +5,9 @@
 // metadata) is: host-side reservation and slot mapping, one upload of the
 // per-iteration metadata through a pinned staging ring, a RoPE table for the
 // iteration's positions, then per layer: RMSNorm, QKV GEMM (RoPE and KV
-// append in its epilogue), chunk and decode attention, output GEMM into an
-// fp32 residual, RMSNorm, gate/up GEMM (SiLU*mul epilogue), down GEMM.
+// append in its epilogue; over 8-bit pools the append is a kernel of its own),
+// chunk and decode attention, output GEMM into an fp32 residual, RMSNorm,
+// gate/up GEMM (SiLU*mul epilogue), down GEMM.
 #include <algorithm>
 #include <atomic>
 #include <chrono>
