@@ -328,8 +328,8 @@ int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void*
                       const Layout& L, const LayerPlans& plans, hipStream_t stream, bool no_alloc);
 
 // One iteration: validation, KV reservation (all or nothing), then the
-// metadata, its upload and the kernels.  A failure after the reservation
-// returns the reserved blocks, so a failed call leaves the block manager as
+// metadata, its upload and the kernels.  A failure after the reservation, an
+// exception too, returns the reserved blocks, so a failed call leaves the block manager as
 // it found it.  no_alloc: the workspace is the static array, the metadata is
 // copied with hipMemcpyAsync from host memory the context holds, both
 // attentions run on `stream` and no stage events are recorded, so the call
@@ -375,12 +375,11 @@ int mixed_iteration_impl(slw_ctx* ctx, const slw_batch* bt, const void* x_in, vo
             if (rc) return rc;
         }
     }
-    KvManager::Undo undo;
-    rc = ctx->kv.reserve_batch(ctx->batch_seqs, &undo);
-    if (rc) return rc;
-    rc = enqueue_iteration(ctx, bt, x_in, x_out, ws, L, plans, stream, no_alloc);
-    if (rc) ctx->kv.rollback(undo);
-    return rc;
+    KvManager::Reservation room(ctx->kv);
+    if ((rc = room.reserve(ctx->batch_seqs))) return rc;
+    if ((rc = enqueue_iteration(ctx, bt, x_in, x_out, ws, L, plans, stream, no_alloc))) return rc;
+    room.keep();
+    return SLW_OK;
 }
 
 // Where a batch's attention metadata lies (32-bit words from its start) and
@@ -1060,29 +1059,22 @@ extern "C" int slw_attn_begin(slw_ctx* ctx, const slw_batch* batch, void* ws, si
                 return fail(SLW_EINVAL, "a batch is handed over outside a capture: its metadata is uploaded once");
         }
         if ((rc = ensure_hip(ctx))) return rc;
-        KvManager::Undo undo;
-        if ((rc = ctx->kv.reserve_batch(ctx->batch_seqs, &undo))) return rc;
+        KvManager::Reservation room(ctx->kv);
+        if ((rc = room.reserve(ctx->batch_seqs))) return rc;
         plan->part = L.part;
-        auto upload = [&]() -> int {
-            std::vector<int32_t>& m = ctx->meta;
-            m.clear();
-            int r = build_attn_meta(ctx, batch, true, m, plan->am);
-            if (r) return r;
-            if (m.size() * 4 > L.meta_bytes) return fail(SLW_EINVAL, "internal: metadata %zu ints above its region", m.size());
-            int32_t* stage = nullptr;
-            int slot = 0;
-            if ((r = next_staging(ctx, m.size(), &stage, &slot))) return r;
-            std::memcpy(stage, m.data(), m.size() * 4);
-            launch_iteration_setup(ws, ctx->staging_dev[slot], m.size(), nullptr, nullptr, 0, ctx->cfg.head_dim, 1.0,
-                                   nullptr, nullptr, nullptr, 0, 0.f, s);
-            HIP_TRY(hipGetLastError());
-            HIP_TRY(hipEventRecord(ctx->staged[slot], s));
-            return SLW_OK;
-        };
-        if ((rc = upload())) {
-            ctx->kv.rollback(undo);
-            return rc;
-        }
+        std::vector<int32_t>& m = ctx->meta;
+        m.clear();
+        if ((rc = build_attn_meta(ctx, batch, true, m, plan->am))) return rc;
+        if (m.size() * 4 > L.meta_bytes) return fail(SLW_EINVAL, "internal: metadata %zu ints above its region", m.size());
+        int32_t* stage = nullptr;
+        int slot = 0;
+        if ((rc = next_staging(ctx, m.size(), &stage, &slot))) return rc;
+        std::memcpy(stage, m.data(), m.size() * 4);
+        launch_iteration_setup(ws, ctx->staging_dev[slot], m.size(), nullptr, nullptr, 0, ctx->cfg.head_dim, 1.0, nullptr,
+                               nullptr, nullptr, 0, 0.f, s);
+        HIP_TRY(hipGetLastError());
+        HIP_TRY(hipEventRecord(ctx->staged[slot], s));
+        room.keep();
         *out = plan.release();
         return SLW_OK;
     });

@@ -1,6 +1,7 @@
 // Host-side paged-KV block manager (Table 1, "KV manager").
 #include "kv_manager.h"
 
+#include <algorithm>
 #include <unordered_map>
 
 #include "common.h"
@@ -30,6 +31,7 @@ int KvManager::release(int64_t id) {
     return SLW_OK;
 }
 
+// Room for the blocks is there (reserve_batch), so nothing here can fail.
 void KvManager::grow(Seq& s, int32_t len, Undo* undo) {
     if (len < s.reserved) len = s.reserved;
     const int64_t need = ceil_div(len, block_size_) - static_cast<int64_t>(s.blocks.size());
@@ -68,6 +70,13 @@ int KvManager::reserve_batch(const std::vector<std::pair<Seq*, int32_t>>& req, U
     if (total > static_cast<int64_t>(free_.size()))
         return fail(SLW_ENOMEM, "KV pool exhausted: need %lld blocks, %d free", (long long)total,
                     free_count());
+    // every allocation before the first block is taken
+    if (undo) undo->grown.reserve(req.size());
+    for (const auto& r : req) {
+        std::vector<int32_t>& blocks = r.first->blocks;
+        const size_t need = static_cast<size_t>(ceil_div(std::max(r.second, r.first->reserved), block_size_));
+        if (need > blocks.capacity()) blocks.reserve(std::max(need, 2 * blocks.capacity()));
+    }
     for (const auto& r : req) grow(*r.first, r.second, undo);
     return SLW_OK;
 }

@@ -48,14 +48,33 @@ public:
         };
         std::vector<Entry> grown;
     };
-    // Grows every (id, new_len) in order; all or nothing.  With `undo`, the
-    // changes are recorded so that rollback() can return them.
+    // Grows every (id, new_len) in order; all or nothing, also where host memory
+    // runs out.  With `undo`, the changes are recorded so that rollback() can
+    // return them.
     int reserve_all(const std::vector<std::pair<int64_t, int32_t>>& req, Undo* undo = nullptr);
     // The same for distinct sequences already looked up.
     int reserve_batch(const std::vector<std::pair<Seq*, int32_t>>& req, Undo* undo);
     // Returns the blocks a reservation took and restores the lengths; the
     // free set, and so every later allocation, is as before the reservation.
     void rollback(const Undo& undo);
+    // A reservation for a call that may still fail: returned when the call
+    // leaves without keep(), by an exception too.
+    class Reservation {
+    public:
+        explicit Reservation(KvManager& kv) : kv_(kv) {}
+        Reservation(const Reservation&) = delete;
+        Reservation& operator=(const Reservation&) = delete;
+        ~Reservation() {
+            if (!kept_) kv_.rollback(undo_);
+        }
+        int reserve(const std::vector<std::pair<Seq*, int32_t>>& req) { return kv_.reserve_batch(req, &undo_); }
+        void keep() { kept_ = true; }
+
+    private:
+        KvManager& kv_;
+        Undo undo_;
+        bool kept_ = false;
+    };
 
     const std::vector<int32_t>& table(int64_t id) const { return seqs_.at(id).blocks; }
 

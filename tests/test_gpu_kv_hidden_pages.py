@@ -1,6 +1,5 @@
 """GPU tests of windowed attention over the 8-bit cache where blocks that the window hides whole hold scales that are no
 powers of two, as where a caller installs the window's tokens alone."""
-import numpy as np
 import pytest
 
 from paper_2609_07883_amd import api

@@ -1,6 +1,5 @@
 """GPU tests of decode batches whose keys and values exceed the last-level cache (256 MB over all layers), where the
 cache kernels load pages as data that is read once."""
-import numpy as np
 import pytest
 
 from paper_2609_07883_amd import api
