@@ -329,10 +329,10 @@ int enqueue_iteration(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void*
 
 // One iteration: validation, KV reservation (all or nothing), then the
 // metadata, its upload and the kernels.  A failure after the reservation, an
-// exception too, returns the reserved blocks, so a failed call leaves the block manager as
-// it found it.  no_alloc: the workspace is the static array, the metadata is
-// copied with hipMemcpyAsync from host memory the context holds, both
-// attentions run on `stream` and no stage events are recorded, so the call
+// exception too, returns the reserved blocks, so a failed call leaves the block
+// manager as it found it.  no_alloc: the workspace is the static array, the
+// metadata is copied with hipMemcpyAsync from host memory the context holds,
+// both attentions run on `stream` and no stage events are recorded, so the call
 // creates no HIP object and allocates no memory of any kind on the device or
 // pinned on the host.
 int mixed_iteration_impl(slw_ctx* ctx, const slw_batch* bt, const void* x_in, void* x_out, void* ws,
