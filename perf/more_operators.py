@@ -301,8 +301,9 @@ def _own_rotate(s, case, api):
     s["k_pool"], s["v_pool"] = (torch.empty(pool, dtype=torch.bfloat16, device="cuda") for _ in range(2))
     ctx.kv_init(s["k_pool"].data_ptr(), s["v_pool"].data_ptr(), blocks)
     ids = list(range(1, 1 + len(prompts) + len(decodes)))
-    for sid in ids:
+    for sid, p in zip(ids, [p for p, _ in prompts] + decodes):  # the tokens before the batch's
         ctx.seq_create(sid)
+        ctx.seq_reserve(sid, p)
     batch = api.Batch.batched([(sid, p, n) for sid, (p, n) in zip(ids, prompts)], ids[len(prompts):], decodes)
     s["ws"] = torch.empty(ctx.attn_workspace_size(case["chunk"], case["decodes"]), dtype=torch.uint8, device="cuda")
     s["plan"] = ctx.attn_begin(batch, s["ws"].data_ptr(), s["ws"].numel(), s["stream"])
