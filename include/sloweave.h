@@ -301,6 +301,163 @@ int slw_attn_attend(slw_ctx* ctx, const slw_attn* plan, int32_t layer, const voi
                     void* out, void* stream);
 int slw_attn_end(slw_attn* plan);
 
+/* ------------------------------------------------------------------------ */
+/* Operators round the cache's, for blocks other than the iteration's, and   */
+/* behind the last one (none is in the paper, which schedules such blocks     */
+/* unmodified, Sec. 5.1)                                                     */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * These calls keep no state: everything belongs to the caller, nothing is
+ * allocated, all work is enqueued on `stream` of the current device and may be
+ * captured into a graph.  Outputs do not overlap inputs unless said.  Rows are
+ * strided: ld* counts elements.
+ *
+ * Rotary positions of a plan's rows: the rows' positions are the batch's, so a
+ * block rotates q and k with the plan, then appends k and attends with q.
+ *   Of each head, the first rot_dim values turn in pairs, pair i being values
+ * (i, i + rot_dim/2), or (2i, 2i + 1) with `interleaved`: at position p,
+ *   x' = mscale (x cos(p f_i) - y sin(p f_i)),  y' = mscale (y cos(p f_i) + x sin(p f_i)),
+ * angles formed in double; the others stay as they are.  f_i, by `scaling`, with
+ * g_i = theta^(-2i/rot_dim):
+ *   NONE      g_i
+ *   LINEAR    g_i / factor
+ *   NTK       g_i with theta * factor^(rot_dim / (rot_dim - 2)) for theta
+ *   BY_PARTS  g_i ((1 - h) / factor + h), h = clamp((t - low) / (high - low), 0, 1),
+ *             t = original_len * g_i / 2 pi the turns within the original length
+ *   TABLE     freq[i], device memory, radians a position
+ * rot_dim is a multiple of 16 up to head_dim.  Fields a kind does not name are
+ * ignored.
+ */
+#define SLW_ROPE_NONE 0
+#define SLW_ROPE_LINEAR 1
+#define SLW_ROPE_NTK 2
+#define SLW_ROPE_BY_PARTS 3
+#define SLW_ROPE_TABLE 4
+typedef struct slw_rope {
+    int32_t rot_dim;
+    int32_t interleaved;  /* 0 or 1                                               */
+    int32_t scaling;      /* SLW_ROPE_*                                           */
+    int32_t original_len; /* BY_PARTS: >= 1                                       */
+    double theta;         /* > 0                                                  */
+    double factor;        /* > 0                                                  */
+    double low, high;     /* BY_PARTS: low < high                                 */
+    const double* freq;   /* TABLE: device [rot_dim / 2]                          */
+    float mscale;
+} slw_rope;
+/*
+ * q device bf16 [C + B][Hq * hd] and k [C + B][Hkv * hd] (chunk rows first, as
+ * for slw_attn_append), both with row stride ld, to q_out and k_out, both with
+ * stride ld_out; either pair may be NULL.  In place where the outputs are the
+ * inputs with the same stride.  Alignment as for slw_attn_append.
+ */
+int slw_attn_rotate(slw_ctx* ctx, const slw_attn* plan, const slw_rope* rope, const void* q, const void* k,
+                    int64_t ld, void* q_out, void* k_out, int64_t ld_out, void* stream);
+
+/*
+ * The residual stream between two blocks:
+ *   r' = r + scale * gate * P(o),  y = r' / sqrt(mean(r'^2) + eps) * gain
+ * with o a block's output, P(o) = o, or with post_gain
+ * o / sqrt(mean(o^2) + eps) * post_gain.  fp32 arithmetic; y is taken of r'
+ * before r' is rounded to the stream's type.
+ *   resid      [rows][d], bf16, or fp32 with resid_f32 = 1
+ *   block      bf16 [rows][d], or NULL: r' = r (then no post_gain and no gate)
+ *   post_gain  bf16 [d], or NULL;  gate  bf16 [rows][d], or [d] with ld_gate = 0, or NULL
+ *   gain       bf16 [d]
+ *   resid_out  as resid, or NULL: r' is not written;  out  bf16 [rows][d], or NULL: only r'
+ * resid_out may be resid, and out may be block, each with the same stride.  d is a
+ * multiple of 8 up to SLW_NORM_MAX_D; rows and gains are 16-byte aligned, strides
+ * multiples of 8.
+ */
+#define SLW_NORM_MAX_D 32768
+typedef struct slw_norm_args {
+    const void* resid;
+    const void* block;
+    const void* post_gain;
+    const void* gate;
+    const void* gain;
+    void* resid_out;
+    void* out;
+    int64_t ld_resid, ld_block, ld_gate, ld_resid_out, ld_out;
+    int32_t rows, d;
+    int32_t resid_f32;
+    float scale, eps;
+} slw_norm_args;
+int slw_residual_norm(const slw_norm_args* args, void* stream);
+
+/*
+ * Products with weights in 4 bits: out = a W^T, W[n][k] in the OCP MX format
+ * (e2m1 codes: bit 3 the sign, then 0, 1/2, 1, 3/2, 2, 3, 4, 6; one e8m0 scale
+ * byte b, 2^(b - 127), for 32 values of a row).  A weight is its value as a bf16
+ * number: exact for 1 <= b <= 252, infinite where it exceeds bf16's range, NaN for
+ * b = 255.  Products are exact, sums fp32.
+ *   Gated weights hold n/2 gate rows, then n/2 up rows, and
+ * out[m][n/2] = silu(a Wg^T) * (a Wu^T), silu(x) = x / (1 + e^-x).
+ *   slw_w4_pack lays weights out once, as the products read them:
+ *     codes   device [n][k/2], two a byte, the even one in the low bits, 16-byte aligned
+ *     scales  device [n][k/32]
+ *     packed  device, slw_w4_packed_bytes of it, 16-byte aligned
+ * 1 <= n <= SLW_W4_MAX_N (even if gated), k a multiple of 32 up to SLW_W4_MAX_K.
+ *   slw_w4_product: a device bf16 [m][k], row stride lda (a multiple of 8), 16-byte
+ * aligned; out bf16, or fp32 with out_f32 = 1, row stride ldo; ws device, 16-byte
+ * aligned, ws_bytes >= slw_w4_workspace_size for at least m rows (NULL where
+ * that is 0).  Calls that share a workspace run in one stream's order, or in an
+ * order the caller sees to.  0 <= m <= SLW_W4_MAX_M; 0 does nothing.
+ */
+#define SLW_W4_MAX_N (1 << 22)
+#define SLW_W4_MAX_K 65536
+#define SLW_W4_MAX_M (1 << 20)
+typedef struct slw_w4 {
+    const void* packed;
+    int32_t n, k;
+    int32_t gated;  /* 0 or 1 */
+} slw_w4;
+int slw_w4_packed_bytes(int32_t n, int32_t k, int32_t gated, size_t* bytes);
+int slw_w4_pack(const void* codes, const void* scales, int32_t n, int32_t k, int32_t gated, void* packed,
+                void* stream);
+int slw_w4_workspace_size(int32_t n, int32_t k, int32_t gated, int32_t max_m, size_t* bytes);
+int slw_w4_product(const slw_w4* w, const void* a, int64_t lda, int32_t m, void* out, int64_t ldo,
+                   int32_t out_f32, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The next token of each row of logits, drawn with a given random number.  With
+ * w_t = exp((x_t - max x) / temperature), the tokens sorted by logit, largest
+ * first (equal ones by index) are cut to the first top_k; of those, the ones with
+ * less than top_p of those tokens' mass before them (the first one always); of
+ * those, the ones with w >= min_p.  The token is the first, by index, at which the
+ * running sum of the kept w exceeds u times their sum; logprob is ln(w / sum).
+ * Masses are held in 64 bits, so that the result is the definition's.
+ *   logits   device bf16, or fp32 with logits_f32 = 1, [rows][vocab], row stride ld,
+ *            aligned to their type; NaN counts as -inf
+ *   temperature, top_k, top_p, min_p   device [rows], each may be NULL (1, off, off, off).
+ *            temperature <= 0 or NaN: the largest logit, the first of equal ones,
+ *            logprob 0.  top_k <= 0 or >= vocab: off.  top_p >= 1 or NaN: off; <= 0: one token.
+ *            min_p <= 0 or NaN: off; > 1 counts as 1.
+ *   u        device [rows] in [0, 1): beyond that the nearest inside, NaN as 0
+ *   tokens   device int32 [rows]: -1 for a row of nothing but -inf
+ *   logprob  device fp32 [rows], or NULL; -inf for such a row
+ *   ws       device, 16-byte aligned, ws_bytes >= slw_sample_workspace_size for at
+ *            least these rows and this vocab (NULL where that is 0); shared as
+ *            slw_w4_product's
+ * 1 <= vocab <= SLW_SAMPLE_MAX_VOCAB.
+ */
+#define SLW_SAMPLE_MAX_VOCAB (1 << 20)
+typedef struct slw_sample_args {
+    const void* logits;
+    int64_t ld;
+    int32_t rows, vocab;
+    int32_t logits_f32;
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+    const float* u;
+    int32_t* tokens;
+    float* logprob;
+} slw_sample_args;
+int slw_sample_workspace_size(int32_t max_rows, int32_t vocab, size_t* bytes);
+int slw_sample(const slw_sample_args* args, void* ws, size_t ws_bytes, void* stream);
+
 /* Slot of every row of the last slw_mixed_iteration (host int32, chunk rows first). */
 int slw_last_slots(slw_ctx* ctx, int32_t* out, int32_t cap, int32_t* n);
 

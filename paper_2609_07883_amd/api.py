@@ -39,6 +39,8 @@ EXPORTS = (
     "slw_mixed_iteration_static", "slw_flush_cache", "slw_fill_normal", "slw_gemm_plan",
     "slw_attention_plan", "slw_cache_attention_plan", "slw_kv_init_8bit", "slw_set_window",
     "slw_attn_workspace_size", "slw_attn_begin", "slw_attn_append", "slw_attn_attend", "slw_attn_end",
+    "slw_attn_rotate", "slw_residual_norm", "slw_w4_packed_bytes", "slw_w4_pack", "slw_w4_workspace_size",
+    "slw_w4_product", "slw_sample_workspace_size", "slw_sample",
 )
 STATIC_WS_BYTES = 128 << 20
 STAGES = ("rmsnorm_attn", "rope_table", "qkv_gemm", "chunk_attn", "decode_attn", "attn_merge",
@@ -72,6 +74,33 @@ class BatchC(C.Structure):
 
 
 MAX_PREFILLS = 16
+
+
+class RopeC(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scaling", C.c_int32),
+                ("original_len", C.c_int32), ("theta", C.c_double), ("factor", C.c_double), ("low", C.c_double),
+                ("high", C.c_double), ("freq", C.c_void_p), ("mscale", C.c_float)]
+
+
+class NormArgsC(C.Structure):
+    _fields_ = [("resid", C.c_void_p), ("block", C.c_void_p), ("post_gain", C.c_void_p), ("gate", C.c_void_p),
+                ("gain", C.c_void_p), ("resid_out", C.c_void_p), ("out", C.c_void_p), ("ld_resid", C.c_int64),
+                ("ld_block", C.c_int64), ("ld_gate", C.c_int64), ("ld_resid_out", C.c_int64), ("ld_out", C.c_int64),
+                ("rows", C.c_int32), ("d", C.c_int32), ("resid_f32", C.c_int32), ("scale", C.c_float),
+                ("eps", C.c_float)]
+
+
+class W4C(C.Structure):
+    _fields_ = [("packed", C.c_void_p), ("n", C.c_int32), ("k", C.c_int32), ("gated", C.c_int32)]
+
+
+class SampleArgsC(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("ld", C.c_int64), ("rows", C.c_int32), ("vocab", C.c_int32),
+                ("logits_f32", C.c_int32), ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p),
+                ("min_p", C.c_void_p), ("u", C.c_void_p), ("tokens", C.c_void_p), ("logprob", C.c_void_p)]
+
+
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3, "table": 4}
 
 
 class ProfileOpts(C.Structure):
@@ -142,6 +171,14 @@ def lib() -> C.CDLL:
         "slw_attn_append": ([vp, vp, i32, vp, vp, i64, vp], C.c_int),
         "slw_attn_attend": ([vp, vp, i32, vp, i64, vp, vp], C.c_int),
         "slw_attn_end": ([vp], C.c_int),
+        "slw_attn_rotate": ([vp, vp, P(RopeC), vp, vp, i64, vp, vp, i64, vp], C.c_int),
+        "slw_residual_norm": ([P(NormArgsC), vp], C.c_int),
+        "slw_w4_packed_bytes": ([i32, i32, i32, P(sz)], C.c_int),
+        "slw_w4_pack": ([vp, vp, i32, i32, i32, vp, vp], C.c_int),
+        "slw_w4_workspace_size": ([i32, i32, i32, i32, P(sz)], C.c_int),
+        "slw_w4_product": ([P(W4C), vp, i64, i32, vp, i64, i32, vp, sz, vp], C.c_int),
+        "slw_sample_workspace_size": ([i32, i32, P(sz)], C.c_int),
+        "slw_sample": ([P(SampleArgsC), vp, sz, vp], C.c_int),
         "slw_kv_free_blocks": ([vp, P(i32)], C.c_int),
         "slw_seq_create": ([vp, i64], C.c_int),
         "slw_seq_free": ([vp, i64], C.c_int),
@@ -505,9 +542,84 @@ class AttnPlan:
         """Enqueue the append of the batch's K/V rows (row stride ld elements) to one layer's cache."""
         _check(lib().slw_attn_append(self._ctx._h, self._h, layer, k or None, v or None, ld, stream or None))
 
+    def rotate(self, rope: "Rope", q: int, k: int, ld: int, q_out: int, k_out: int, ld_out: int, stream: int = 0):
+        """Enqueue the rotation of the batch's query and key rows to their positions (0: not these)."""
+        _check(lib().slw_attn_rotate(self._ctx._h, self._h, C.byref(rope.c), q or None, k or None, ld, q_out or None,
+                                     k_out or None, ld_out, stream or None))
+
     def attend(self, layer: int, q: int, ld: int, out: int, stream: int = 0):
         """Enqueue one layer's attention of the batch's query rows (row stride ld elements)."""
         _check(lib().slw_attn_attend(self._ctx._h, self._h, layer, q or None, ld, out or None, stream or None))
+
+
+class Rope:
+    """Rotary positions (slw_rope): the first rot_dim values of a head, in pairs half of them apart or next to each
+    other (interleaved); scaling "none", "linear", "ntk", "by_parts" (low and high: turns within original_len
+    between which frequencies are blended) or "table" (freq: address of rot_dim / 2 doubles on the device)."""
+
+    def __init__(self, rot_dim: int, theta: float = 0.0, *, interleaved: bool = False, scaling: str = "none",
+                 factor: float = 1.0, low: float = 1.0, high: float = 4.0, original_len: int = 0, freq: int = 0,
+                 mscale: float = 1.0):
+        self.c = RopeC(int(rot_dim), int(interleaved), ROPE_SCALINGS[scaling], int(original_len), float(theta),
+                       float(factor), float(low), float(high), freq or None, float(mscale))
+
+
+def residual_norm(rows: int, d: int, resid: int, block: int, resid_out: int, gain: int, out: int, *,
+                  resid_f32: bool = False, eps: float = 1e-5, post_gain: int = 0, gate: int = 0, ld_gate: int = 0,
+                  scale: float = 1.0, ld_resid: int | None = None, ld_block: int | None = None,
+                  ld_resid_out: int | None = None, ld_out: int | None = None, stream: int = 0) -> None:
+    """Enqueue r' = r + scale * gate * P(o) and y = RMSNorm(r') * gain (slw_residual_norm); addresses that are 0 are
+    left out, strides that are None are d."""
+    a = NormArgsC(resid or None, block or None, post_gain or None, gate or None, gain or None, resid_out or None,
+                  out or None, d if ld_resid is None else ld_resid, d if ld_block is None else ld_block, ld_gate,
+                  d if ld_resid_out is None else ld_resid_out, d if ld_out is None else ld_out, rows, d,
+                  int(resid_f32), scale, eps)
+    _check(lib().slw_residual_norm(C.byref(a), stream or None))
+
+
+def w4_packed_bytes(n: int, k: int, gated: bool = False) -> int:
+    b = C.c_size_t()
+    _check(lib().slw_w4_packed_bytes(n, k, int(gated), C.byref(b)))
+    return b.value
+
+
+class W4:
+    """Weights [n][k] in 4 bits at `packed` (w4_packed_bytes(n, k, gated) of device memory, the caller's)."""
+
+    def __init__(self, packed: int, n: int, k: int, gated: bool = False):
+        self.c = W4C(packed or None, int(n), int(k), int(gated))
+        self._ref = C.byref(self.c)
+
+    def pack(self, codes: int, scales: int, stream: int = 0) -> None:
+        """Enqueue the layout of codes [n][k/2] and scale bytes [n][k/32] into `packed`."""
+        _check(lib().slw_w4_pack(codes or None, scales or None, self.c.n, self.c.k, self.c.gated, self.c.packed,
+                                 stream or None))
+
+    def workspace_size(self, max_m: int) -> int:
+        b = C.c_size_t()
+        _check(lib().slw_w4_workspace_size(self.c.n, self.c.k, self.c.gated, max_m, C.byref(b)))
+        return b.value
+
+    def product(self, a: int, lda: int, m: int, out: int, ldo: int, *, out_f32: bool = False, ws: int = 0,
+                ws_bytes: int = 0, stream: int = 0) -> None:
+        """Enqueue out = a W^T, or silu(a Wg^T) * (a Wu^T) for gated weights."""
+        _check(lib().slw_w4_product(self._ref, a or None, lda, m, out or None, ldo, int(out_f32), ws or None, ws_bytes,
+                                    stream or None))
+
+
+def sample_workspace_size(max_rows: int, vocab: int) -> int:
+    b = C.c_size_t()
+    _check(lib().slw_sample_workspace_size(max_rows, vocab, C.byref(b)))
+    return b.value
+
+
+def sample(logits: int, rows: int, vocab: int, ld: int, u: int, tokens: int, *, logits_f32: bool = False,
+           temperature: int = 0, top_k: int = 0, top_p: int = 0, min_p: int = 0, logprob: int = 0, ws: int = 0,
+           ws_bytes: int = 0, stream: int = 0) -> None:
+    """Enqueue the draw of each row's next token (slw_sample); the parameters are addresses of [rows], 0: left out."""
+    a = SampleArgsC(logits or None, ld, rows, vocab, int(logits_f32), temperature or None, top_k or None, top_p or None,
+                    min_p or None, u or None, tokens or None, logprob or None)
+    _check(lib().slw_sample(C.byref(a), ws or None, ws_bytes, stream or None))
 
 
 class Context:

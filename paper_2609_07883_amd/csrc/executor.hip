@@ -11,6 +11,7 @@
 #include <algorithm>
 #include <atomic>
 #include <chrono>
+#include <cmath>
 #include <cstring>
 #include <limits>
 #include <memory>
@@ -21,6 +22,7 @@
 #include "attn_plan.h"
 #include "common.h"
 #include "cost_table.h"
+#include "hip_try.h"
 #include "kernels.h"
 #include "kv_manager.h"
 
@@ -33,12 +35,6 @@ constexpr size_t kAlign = 256;
 constexpr int64_t kLastLevelCache = 256 << 20;
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-
-#define HIP_TRY(expr)                                                                      \
-    do {                                                                                   \
-        hipError_t e_ = (expr);                                                            \
-        if (e_ != hipSuccess) return fail(SLW_EHIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-    } while (0)
 
 }  // namespace
 
@@ -981,6 +977,7 @@ struct slw_attn {
     uint64_t kv_id;               // of the pools it was made for
     Window win;                   // and the windows
     std::vector<char> windowed;
+    std::vector<Prefill> prompts; // of the batch, in row order
     AttnMeta am;
     PartLayout part;
     char* ws;
@@ -1062,6 +1059,7 @@ extern "C" int slw_attn_begin(slw_ctx* ctx, const slw_batch* batch, void* ws, si
         KvManager::Reservation room(ctx->kv);
         if ((rc = room.reserve(ctx->batch_seqs))) return rc;
         plan->part = L.part;
+        plan->prompts = ctx->prefills;
         std::vector<int32_t>& m = ctx->meta;
         m.clear();
         if ((rc = build_attn_meta(ctx, batch, true, m, plan->am))) return rc;
@@ -1108,6 +1106,89 @@ extern "C" int slw_attn_attend(slw_ctx* ctx, const slw_attn* plan, int32_t layer
                                  q, static_cast<int>(ld), out);
         attention.both(s);
         attention.merge(s);
+        HIP_TRY(hipGetLastError());
+        return SLW_OK;
+    });
+}
+
+namespace {
+
+int rope_args(const slw_model_cfg& c, const slw_rope& r, RopeArgs* out) {
+    if (r.rot_dim < 16 || r.rot_dim % 16 || r.rot_dim > c.head_dim)
+        return fail(SLW_EUNSUPPORTED, "rot_dim must be a multiple of 16 in [16, head_dim = %d] (got %d)", c.head_dim, r.rot_dim);
+    if (r.interleaved != 0 && r.interleaved != 1) return fail(SLW_EINVAL, "interleaved must be 0 or 1");
+    if (!std::isfinite(r.mscale)) return fail(SLW_EINVAL, "mscale must be finite");
+    auto positive = [](double x) { return x > 0.0 && std::isfinite(x); };
+    RopeArgs a{};
+    a.mscale = r.mscale;
+    a.rot = r.rot_dim;
+    a.interleaved = r.interleaved != 0;
+    a.first = 1.0;
+    double theta = r.theta;
+    if (r.scaling != SLW_ROPE_TABLE && !positive(theta)) return fail(SLW_EINVAL, "theta must be positive and finite");
+    if (r.scaling == SLW_ROPE_LINEAR || r.scaling == SLW_ROPE_NTK || r.scaling == SLW_ROPE_BY_PARTS)
+        if (!positive(r.factor)) return fail(SLW_EINVAL, "factor must be positive and finite");
+    switch (r.scaling) {
+        case SLW_ROPE_NONE: break;
+        case SLW_ROPE_LINEAR: a.first = 1.0 / r.factor; break;
+        case SLW_ROPE_NTK: theta *= std::pow(r.factor, r.rot_dim / (r.rot_dim - 2.0)); break;
+        case SLW_ROPE_BY_PARTS:
+            if (!std::isfinite(r.low) || !std::isfinite(r.high) || !(r.low < r.high))
+                return fail(SLW_EINVAL, "low and high must be finite, low below high");
+            if (r.original_len < 1) return fail(SLW_EINVAL, "original_len must be >= 1");
+            a.by_parts = true;
+            a.turns_in_original = r.original_len / 6.283185307179586477;
+            a.low = r.low;
+            a.inv_width = 1.0 / (r.high - r.low);
+            a.inv_factor = 1.0 / r.factor;
+            break;
+        case SLW_ROPE_TABLE:
+            if (!r.freq || reinterpret_cast<uintptr_t>(r.freq) % 8) return fail(SLW_EINVAL, "freq: 8-byte aligned device memory");
+            a.freq = r.freq;
+            break;
+        default: return fail(SLW_EINVAL, "unknown scaling %d", r.scaling);
+    }
+    if (!a.freq) a.step = -2.0 * std::log2(theta) / r.rot_dim;
+    *out = a;
+    return SLW_OK;
+}
+
+}  // namespace
+
+extern "C" int slw_attn_rotate(slw_ctx* ctx, const slw_attn* plan, const slw_rope* rope, const void* q, const void* k,
+                               int64_t ld, void* q_out, void* k_out, int64_t ld_out, void* stream) {
+    return guarded([&] {
+        int rc = check_attn(ctx, plan, 0);
+        if (rc) return rc;
+        if (!rope) return fail(SLW_EINVAL, "null argument");
+        const slw_model_cfg& c = ctx->cfg;
+        RopeArgs ra;
+        if ((rc = rope_args(c, *rope, &ra))) return rc;
+        if (!q && !k) return fail(SLW_EINVAL, "neither q nor k rows");
+        if (!q != !q_out || !k != !k_out) return fail(SLW_EINVAL, "rows without their outputs, or outputs without rows");
+        const int64_t qw = static_cast<int64_t>(c.n_q_heads) * c.head_dim, kw = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
+        if (q && ((rc = check_rows(q, ld, qw, "q")) || (rc = check_rows(q_out, ld_out, qw, "q output")))) return rc;
+        if (k && ((rc = check_rows(k, ld, kw, "k")) || (rc = check_rows(k_out, ld_out, kw, "k output")))) return rc;
+        if (plan->am.C + plan->am.B == 0) return SLW_OK;
+        RotateRows a{};
+        a.q = q;
+        a.k = k;
+        a.q_out = q_out;
+        a.k_out = k_out;
+        a.kv_len = reinterpret_cast<const int32_t*>(plan->ws) + plan->am.kvlen;
+        a.ld = ld;
+        a.ld_out = ld_out;
+        a.rows = plan->am.C + plan->am.B;
+        a.chunk = plan->am.C;
+        a.hq = c.n_q_heads;
+        a.hkv = c.n_kv_heads;
+        a.hd = c.head_dim;
+        for (const Prefill& f : plan->prompts) {
+            a.row_end[a.n_prompts] = f.row0 + f.c;
+            a.shift[a.n_prompts++] = f.prefix - f.row0;
+        }
+        a.in_place = ld == ld_out && q == q_out && k == k_out;
+        launch_rotate(a, ra, static_cast<hipStream_t>(stream));
         HIP_TRY(hipGetLastError());
         return SLW_OK;
     });

@@ -175,6 +175,47 @@ struct CacheAttnArgs {
 };
 void launch_cache_attention(const CacheAttnArgs& a, hipStream_t s);
 
+// The residual stream's update and the norms round it (slw_residual_norm).
+struct NormRows {
+    const void* resid;
+    const void* block;      // may be null
+    const void* post_gain;  // may be null
+    const void* gate;       // may be null; ld_gate 0: one row for all
+    const void* gain;
+    void* resid_out;        // may be null
+    void* out;              // may be null
+    int64_t ld_resid, ld_block, ld_gate, ld_resid_out, ld_out;
+    int rows, d;
+    bool resid_f32;
+    float scale, eps;
+};
+void launch_residual_norm(const NormRows& a, hipStream_t s);
+
+// Rotary positions of a batch's query and key rows (slw_attn_rotate).  Pair i
+// turns by freq[i] a position where there is a table, else by
+// first * 2^(i step); by_parts blends that with its 1 / factor.
+struct RopeArgs {
+    const double* freq;
+    double step, first;
+    double turns_in_original, low, inv_width, inv_factor;  // by_parts
+    float mscale;
+    int rot;
+    bool interleaved, by_parts;
+};
+struct RotateRows {
+    const void* q;  // null: the other alone
+    const void* k;
+    void* q_out;
+    void* k_out;
+    const int32_t* kv_len;  // [decodes]: position + 1
+    int64_t ld, ld_out;
+    int rows, chunk, hq, hkv, hd;
+    int n_prompts;          // rows up to row_end[i] of prompt i sit at position row + shift[i]
+    int row_end[16], shift[16];
+    bool in_place;          // q_out and k_out are q and k: values that do not turn stay
+};
+void launch_rotate(const RotateRows& a, const RopeArgs& rope, hipStream_t s);
+
 // One kernel: copy `words` 32-bit words from coherent, mapped host memory
 // (its device address; both pointers 16-byte aligned) to device memory, fill
 // the RoPE table: cs[r][i] = (cos, sin) of pos_host[r] * theta^(-2i/hd),
