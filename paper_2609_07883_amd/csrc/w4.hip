@@ -8,13 +8,13 @@
 // before the output.
 //
 // Layout (slw_w4_pack).  W's rows are cut into tiles of 16, k into steps of 128;
-// a tile's step is 1024 bytes, 16 for each lane of a wave: lane l holds row
-// l % 16, the 32 codes of the group l / 16, in the order of the source.  A lane's
-// 16 bytes are the weight operands of four 16x16x32 MFMAs (j = 0..3: values 8 j
-// .. 8 j + 7 of every group; the activations are read in the same order) and
-// share one scale; the scale bytes of four steps make one word for each lane.
-// Gated weights have gate tiles and up tiles in turn, so that a wave holds the
-// two members of a pair in the same lane.
+// a tile's step is 1024 bytes, 16 for each lane of a wave, the weight operands of
+// four 16x16x32 MFMAs: word j of lane l holds row l % 16, values 8 (l / 16) .. + 7
+// of the step's group j.  So an MFMA takes one group of 32, whose scale is one
+// for the row, and the activations' operands are 64 consecutive bytes of a row.
+// The four scale bytes of a row's step make a word, the words of four steps 16
+// consecutive bytes.  Gated weights have gate tiles and up tiles in turn, so that a
+// wave holds the two members of a pair in the same lane.
 #include <math.h>
 
 #include <algorithm>
@@ -26,23 +26,28 @@
 namespace slw {
 namespace {
 
+constexpr int64_t kMostTileStride = 1 << 22;  // the tile kernel's row offsets are 32 bits
+constexpr int kMostSplitRows = 4096;  // k is split for fewer rows only
+constexpr int kStep = 128;   // k of a step: a lane's 16 bytes of four groups
+
 struct W4Args {
     const u32x4* codes;      // [tiles][steps][64]
-    const uint32_t* scales;  // [tiles][words][64]
+    const uint32_t* scales;  // [tiles][words][16][4]: row, step of four
     const bf16* a;
     void* out;
     int64_t lda, ldo;
     int m, n, k;             // n: columns of out
     int tiles, steps, words;
     bool vec;                // four columns of out in one store
+    bool gated, f32;
+    float* part;             // tile kernel with its k split: [splits][m][16 tiles] sums
+    int splits;
 };
 
 __device__ __forceinline__ float silu(float g) { return g / (1.0f + expf(-g)); }
 
-// The scale 2^(byte i of w - 127) as a float whose exponent bits are the byte.
-__device__ __forceinline__ float step_scale(uint32_t w, int i) {
-    return __uint_as_float((w >> (8 * i) & 0xFFu) << 23);
-}
+// The scale 2^(byte j of w - 127) as a float whose exponent bits are the byte.
+__device__ __forceinline__ float group_scale(uint32_t w, int j) { return __uint_as_float((w >> (8 * j) & 0xFFu) << 23); }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -75,52 +80,134 @@ __device__ __forceinline__ void store_cols(const W4Args& g, int row, int n0, f32
     }
 }
 
-// A work-group: NT tiles of weights and 16 MT rows; its waves share the k steps
-// and add their sums through LDS.
-template <int MT, int NT, bool GATED, class Out>
-__global__ __launch_bounds__(512) void w4_stream_kernel(W4Args g) {
+// The outputs of one row in the lane of a wave: NB tiles' sums, from tile `tile` on.
+template <int NB>
+__device__ __forceinline__ void store_row(const W4Args& g, int row, int tile, int grp, const f32x4 (&v)[NB]) {
+    if (NB > 1 && g.gated) {
+#pragma unroll
+        for (int t = 0; t + 1 < NB; t += 2) {
+            f32x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = silu(v[t][e]) * v[t + 1][e];
+            const int n0 = (tile + t) / 2 * 16 + 4 * grp;
+            if (g.f32) store_cols<float>(g, row, n0, o);
+            else store_cols<bf16>(g, row, n0, o);
+        }
+    } else {
+#pragma unroll
+        for (int t = 0; t < NB; ++t) {
+            const int n0 = (tile + t) * 16 + 4 * grp;
+            if (g.f32) store_cols<float>(g, row, n0, v[t]);
+            else store_cols<bf16>(g, row, n0, v[t]);
+        }
+    }
+}
+
+// The same, or where k is split over work-groups this one's sums, [split][m][16 tiles].
+template <int NB>
+__device__ __forceinline__ void store_sums(const W4Args& g, int row, int tile, int grp, const f32x4 (&v)[NB]) {
+    if (g.splits == 1) {
+        store_row<NB>(g, row, tile, grp, v);
+        return;
+    }
+    float* p = g.part + (static_cast<size_t>(blockIdx.z) * g.m + row) * (16 * static_cast<size_t>(g.tiles)) + 4 * grp;
+#pragma unroll
+    for (int t = 0; t < NB; ++t)
+        if (tile + t < g.tiles) *reinterpret_cast<f32x4*>(p + (tile + t) * 16) = v[t];
+}
+
+// Words of N consecutive steps (of four that are loaded together).
+template <int N>
+struct Words {
+    uint32_t w[N];
+    __device__ __forceinline__ void load(const uint32_t* p) {
+        if constexpr (N == 4) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+            w[0] = v[0], w[1] = v[1], w[2] = v[2], w[3] = v[3];
+        } else if constexpr (N == 2) {
+            const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+            w[0] = v[0], w[1] = v[1];
+        } else {
+            w[0] = *p;
+        }
+    }
+};
+
+// Stream kernel, for a few rows: a work-group has NT tiles of weights and 16 MT
+// rows, its waves share the k steps and add their sums through LDS; k may be
+// split over work-groups too.  A wave takes D steps at a time, 4 KB of codes,
+// which it loads a turn ahead; the rows' operands come straight from the caches.
+template <int MT, int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void w4_stream_kernel(W4Args g) {
+    constexpr int D = 4 / NT;
     extern __shared__ f32x4 red[];  // [waves][NT * MT][64]
-    const int wave = threadIdx.x / kWave, waves = blockDim.x / kWave, lane = threadIdx.x % kWave;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x / kWave));
+    const int waves = blockDim.x / kWave;
     const int tile0 = blockIdx.x * NT, row0 = blockIdx.y * 16 * MT;
     const int col = lane & 15, grp = lane >> 4;
     const bf16* a[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) a[i] = g.a + min(row0 + 16 * i + col, g.m - 1) * g.lda + 32 * grp;
+    for (int i = 0; i < MT; ++i) a[i] = g.a + min(row0 + 16 * i + col, g.m - 1) * g.lda + 8 * grp;
+    const u32x4* codes[NT];
+    const uint32_t* scales[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const size_t tile = min(tile0 + t, g.tiles - 1);
+        codes[t] = g.codes + tile * g.steps * 64 + lane;
+        scales[t] = g.scales + tile * g.words * 64 + col * 4;
+    }
     f32x4 acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int b = wave; b < g.words; b += waves) {
-        uint32_t sc[NT];
+    u32x4 c[NT][D];
+    Words<D> s[NT];
+    auto load = [&](int step, u32x4 (&to)[NT][D], Words<D> (&sc)[NT]) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-            sc[t] = g.scales[(static_cast<size_t>(min(tile0 + t, g.tiles - 1)) * g.words + b) * 64 + lane];
+        for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-            const int step = 4 * b + i4;
-            if (step >= g.steps) break;
-            u32x4 c[NT];
+            for (int d = 0; d < D; ++d) to[t][d] = codes[t][static_cast<size_t>(min(step + d, g.steps - 1)) * 64];
+            sc[t].load(scales[t] + step / 4 * 64 + step % 4);
+        }
+    };
+    const int stride = D * waves * gridDim.z, last = g.k % kStep ? g.k % kStep / 32 : 4;  // groups of the last step
+    int step = D * (blockIdx.z * waves + wave);
+    if (step < g.steps) load(step, c, s);
+    for (; step < g.steps; step += stride) {
+        bf16x8 x[D][MT][4];
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                c[t] = g.codes[(static_cast<size_t>(min(tile0 + t, g.tiles - 1)) * g.steps + step) * 64 + lane];
-            bf16x8 x[MT][4];
-            const bool in_k = step * 128 + 32 * grp < g.k;
+        for (int d = 0; d < D; ++d)
+            if (step + d < g.steps) {
+                const int groups = step + d == g.steps - 1 ? last : 4;
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (j < groups) x[d][i][j] = *reinterpret_cast<const bf16x8*>(a[i] + (step + d) * kStep + 32 * j);
+            }
+        u32x4 c_next[NT][D];
+        Words<D> s_next[NT];
+        if (step + stride < g.steps) load(step + stride, c_next, s_next);
+#pragma unroll
+        for (int d = 0; d < D; ++d)
+            if (step + d < g.steps) {
+                const int groups = step + d == g.steps - 1 ? last : 4;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    x[i][j] = in_k ? *reinterpret_cast<const bf16x8*>(a[i] + step * 128 + 8 * j) : bf16x8{};
+                    if (j < groups)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const float s = step_scale(sc[t], i4);
+                        for (int t = 0; t < NT; ++t) {
+                            const bf16x8 w = widen(c[t][d][j], group_scale(s[t].w[d], j));
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bf16x8 w = widen(c[t][j], s);
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) acc[i][t] = mfma16(w, x[i][j], acc[i][t]);
-                }
+                            for (int i = 0; i < MT; ++i) acc[i][t] = mfma16(w, x[d][i][j], acc[i][t]);
+                        }
             }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            s[t] = s_next[t];
+#pragma unroll
+            for (int d = 0; d < D; ++d) c[t][d] = c_next[t][d];
         }
     }
 #pragma unroll
@@ -128,45 +215,173 @@ __global__ __launch_bounds__(512) void w4_stream_kernel(W4Args g) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) red[(wave * MT * NT + i * NT + t) * 64 + lane] = acc[i][t];
     __syncthreads();
-    constexpr int kPer = GATED ? 2 : 1;
+    // a wave adds a row tile's pair of column tiles (or its only one)
+    constexpr int kPer = NT > 1 ? 2 : 1;
     for (int u = wave; u < MT * NT / kPer; u += waves) {
-        const int i = u / (NT / kPer), t = u % (NT / kPer) * kPer;
+        const int i = u / (NT / kPer), t = u % (NT / kPer) * kPer, row = row0 + 16 * i + col;
         f32x4 v[kPer];
 #pragma unroll
         for (int p = 0; p < kPer; ++p) {
             v[p] = f32x4{0.f, 0.f, 0.f, 0.f};
             for (int w = 0; w < waves; ++w) v[p] += red[(w * MT * NT + i * NT + t + p) * 64 + lane];
         }
-        f32x4 o = v[0];
-        if (GATED)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = silu(v[0][e]) * v[kPer - 1][e];
-        const int row = row0 + 16 * i + col, n0 = (tile0 + t) / kPer * 16 + 4 * grp;
-        if (row < g.m) store_cols<Out>(g, row, n0, o);
+        if (row < g.m) store_sums<kPer>(g, row, tile0 + t, grp, v);
     }
 }
 
-// One thread for each lane of each tile's step: 16 bytes of codes; the first
-// step of four also makes the lane's scale word.
+// Tile kernel: 2 x WN waves compute 32 HA rows times 64 WN columns of W; a wave
+// holds HA x 4 tiles.  The rows of a step of k come through LDS (two buffers,
+// direct global->LDS loads), chunk c of row r at c ^ (r % 16) so that a read
+// serves 16 rows on distinct banks.  The weights never pass through LDS: a
+// wave's operands of a step are 4 KB of consecutive codes, loaded a step ahead
+// into registers and widened there.
+template <int HA, int WN>
+__global__ __launch_bounds__(128 * WN, 2) void w4_tile_kernel(W4Args g, int nt_m, int nt_n, int steps_per_split) {
+    constexpr int BM = 32 * HA, NW = 2 * WN, BUF = BM * 256, LOADS = BM / 4 / NW;
+    static_assert(BM / 4 % NW == 0, "whole loads for every wave");
+    __shared__ __attribute__((aligned(1024))) char smem[2 * BUF];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    const int wm = wave / WN, wn = wave % WN, col = lane & 15, grp = lane >> 4;
+    int tm, tn;
+    tile_coords(xcd_order(blockIdx.x, nt_m * nt_n), nt_m, nt_n, tm, tn);
+    const int m0 = tm * BM, tile0 = (tn * WN + wn) * 4;
+    const int t0 = blockIdx.z * steps_per_split, t1 = min(t0 + steps_per_split, g.steps);
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&smem[0])));
+
+    // loads: piece x of this wave is 4 rows; lane l brings chunk (l % 16) ^ (row % 16) of row l / 16.
+    // Rows past m read row m - 1, chunks past k the step's first chunk (no product takes them).
+    const char* base = reinterpret_cast<const char*>(g.a + m0 * g.lda);
+    const int tail = g.k % kStep / 8;  // chunks of a last step that is not whole
+    uint32_t off[LOADS];
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) {
+        const int row = (x * NW + wave) * 4 + (lane >> 4);
+        off[x] = static_cast<uint32_t>(min(row, g.m - 1 - m0)) * static_cast<uint32_t>(g.lda * 2) + (((lane & 15) ^ (row & 15)) << 4);
+    }
+    auto load_rows = [&](int t) {
+        const char* from = base + static_cast<size_t>(t) * 256;
+        const bool cut = tail && t == g.steps - 1;
+#pragma unroll
+        for (int x = 0; x < LOADS; ++x) {
+            uint32_t o = off[x];
+            if (cut) {
+                const int row = (x * NW + wave) * 4 + (lane >> 4), c = (lane & 15) ^ (row & 15);
+                if (c >= tail) o -= c << 4;
+            }
+            load_lds16(from, o, lds0 + (t - t0 & 1) * BUF + (x * NW + wave) * 1024);
+        }
+    };
+    const u32x4* codes[4];
+    const uint32_t* scales[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const size_t tile = min(tile0 + b, g.tiles - 1);
+        codes[b] = g.codes + tile * g.steps * 64 + lane;
+        scales[b] = g.scales + tile * g.words * 64 + col * 4;
+    }
+    u32x4 next[4];
+    uint32_t sc[4], sc_next[4];
+    auto load_weights = [&](int t) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) next[b] = codes[b][static_cast<size_t>(t) * 64];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) sc_next[b] = scales[b][t / 4 * 64 + t % 4];
+    };
+    const char* frag[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) frag[j] = smem + (wm * 16 * HA + col) * 256 + (((4 * j + grp) ^ col) << 4);
+    f32x4 acc[HA][4];
+#pragma unroll
+    for (int i = 0; i < HA; ++i)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    load_weights(t0);
+    load_rows(t0);
+    for (int t = t0; t < t1; ++t) {
+        wait_vmcnt<0>();
+        barrier_only();
+        u32x4 c[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            c[b] = next[b];
+            sc[b] = sc_next[b];
+        }
+        if (t + 1 < t1) {
+            load_weights(t + 1);
+            load_rows(t + 1);
+        }
+        const int at = (t - t0 & 1) * BUF, groups = t == g.steps - 1 && tail ? tail / 4 : 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j >= groups) break;
+            bf16x8 x[HA], w[4];
+#pragma unroll
+            for (int i = 0; i < HA; ++i) x[i] = *reinterpret_cast<const bf16x8*>(frag[j] + at + i * 4096);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) w[b] = widen(c[b][j], group_scale(sc[b], j));
+#pragma unroll
+            for (int i = 0; i < HA; ++i)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) acc[i][b] = mfma16(w[b], x[i], acc[i][b]);
+        }
+        // this wave's reads of the buffer are in registers before another wave refills it
+        wait_lgkmcnt<0>();
+    }
+    const int row0 = m0 + wm * 16 * HA + col;
+#pragma unroll
+    for (int i = 0; i < HA; ++i) {
+        const int row = row0 + 16 * i;
+        if (row >= g.m) continue;
+        store_sums<4>(g, row, tile0, grp, acc[i]);
+    }
+}
+
+// Adds a split product's sums, four columns (or pairs) of a row a thread, and stores them.
+__global__ __launch_bounds__(256) void w4_join_kernel(W4Args g) {
+    const int per = g.gated ? 2 : 1, quads = g.tiles / per * 4;
+    const int i = blockIdx.x * 256 + threadIdx.x, row = blockIdx.y;
+    if (i >= quads) return;
+    const int tile = i / 4 * per, grp = i % 4;
+    const size_t ld = 16 * static_cast<size_t>(g.tiles);
+    f32x4 v[2] = {};
+    for (int s = 0; s < g.splits; ++s) {
+        const float* p = g.part + (static_cast<size_t>(s) * g.m + row) * ld + tile * 16 + 4 * grp;
+        v[0] += *reinterpret_cast<const f32x4*>(p);
+        if (g.gated) v[1] += *reinterpret_cast<const f32x4*>(p + 16);
+    }
+    if (g.gated) {
+        store_row<2>(g, row, tile, grp, v);
+    } else {
+        f32x4 one[1] = {v[0]};
+        store_row<1>(g, row, tile, grp, one);
+    }
+}
+
+// One thread for each lane of each tile's step: four words of codes; the first 16
+// lanes of every step make the row's scale word.
 __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                       u32x4* __restrict__ to_codes, uint32_t* __restrict__ to_scales,
                                                       int rows, int k, int tiles, int steps, int words, bool gated) {
     const size_t i = blockIdx.x * static_cast<size_t>(256) + threadIdx.x;
-    const int lane = i % 64, step = i / 64 % steps;
-    const size_t tile = i / 64 / steps;
+    const int lane = i % 64, step = i / 64 % (4 * words);
+    const size_t tile = i / 64 / (4 * words);
     if (tile >= static_cast<size_t>(tiles)) return;
     const int r = (gated ? tile / 2 : tile) * 16 + (lane & 15);  // of the gate or up rows, or of all
     const int groups = k / 32;
     const size_t row = gated && tile % 2 ? static_cast<size_t>(rows) + r : r;
-    const int group = step * 4 + lane / 16;
-    u32x4 c = {0u, 0u, 0u, 0u};
-    if (r < rows && group < groups) c = *reinterpret_cast<const u32x4*>(codes + row * (k / 2) + group * 16);
-    to_codes[(tile * steps + step) * 64 + lane] = c;
-    if (step % 4) return;
+    if (step < steps) {
+        u32x4 c = {0u, 0u, 0u, 0u};
+        for (int j = 0; j < 4; ++j)
+            if (r < rows && 4 * step + j < groups)
+                c[j] = *reinterpret_cast<const uint32_t*>(codes + row * (k / 2) + (4 * step + j) * 16 + 4 * (lane / 16));
+        to_codes[(tile * steps + step) * 64 + lane] = c;
+    }
+    if (lane >= 16) return;
     uint32_t w = 0;
     for (int j = 0; j < 4; ++j)
-        if (r < rows && group + 4 * j < groups) w |= static_cast<uint32_t>(scales[row * groups + group + 4 * j]) << (8 * j);
-    to_scales[(tile * words + step / 4) * 64 + lane] = w;
+        if (r < rows && 4 * step + j < groups) w |= static_cast<uint32_t>(scales[row * groups + 4 * step + j]) << (8 * j);
+    to_scales[((tile * words + step / 4) * 16 + lane) * 4 + step % 4] = w;
 }
 
 struct W4Shape {
@@ -183,18 +398,101 @@ W4Shape w4_shape(int n, int k, bool gated) {
     return s;
 }
 
-template <int MT, int NT, bool GATED, class Out>
-void stream_launch(const W4Args& g, int waves, hipStream_t s) {
-    const dim3 grid(static_cast<unsigned>(ceil_div(g.tiles, NT)), static_cast<unsigned>(ceil_div(g.m, 16 * MT)));
-    w4_stream_kernel<MT, NT, GATED, Out><<<grid, 64 * waves, static_cast<size_t>(waves) * MT * NT * 1024, s>>>(g);
+// Most waves of a stream work-group.
+constexpr int kStreamWaves = 8;
+
+// Which kernel a product runs on.
+struct W4Plan {
+    int kind;    // 0: stream, 1: tile
+    int mt, nt;  // stream: row and column tiles of a work-group; tile: HA, WN
+    int waves;   // stream
+    int splits;
+};
+
+W4Plan plan_w4(const W4Shape& s, int m, bool gated) {
+    W4Plan p{};
+    if (m <= 32) {
+        p.mt = m <= 16 ? 1 : 2;
+        p.nt = m > 16 || s.tiles >= 1024 ? 4 : gated || s.tiles >= 384 ? 2 : 1;
+        // one work-group a CU at least, by splitting k
+        const int64_t groups = ceil_div(s.tiles, p.nt);
+        p.splits = 1;
+        while (m > 16 && groups * p.splits < 256 && p.splits * 2 * 8 <= s.steps) p.splits *= 2;
+        p.waves = std::min(p.nt == 4 && p.splits == 1 ? 4 : 8, s.words);
+        return p;
+    }
+    // Work-groups of 2 WN waves, eight waves on a CU; a wave's step costs its
+    // MFMAs (two waves share a matrix unit) or the wait for the next step.
+    p.kind = 1;
+    double best = 0;
+    for (int wn = 4; wn >= 1; wn /= 2)
+        for (int ha = 1; ha <= (wn == 4 ? 8 : wn == 2 ? 4 : 2); ++ha) {
+            if (ha == 7 || 4 * ha % wn) continue;
+            const int64_t tiles = ceil_div(m, 32 * ha) * ceil_div(s.tiles, 4 * wn), slots = 256 * 4 / wn;
+            for (int sp = 1; sp == 1 || (sp <= 16 && sp * 4 <= s.steps && m <= kMostSplitRows); sp *= 2) {
+                const int64_t per = ceil_div(s.steps, sp), rounds = ceil_div(tiles * sp, slots);
+                const double t = rounds * (per * std::max(512.0 * ha + 200, 900.0) + 4000.0) +
+                                 (sp > 1 ? 8000.0 + sp * static_cast<double>(m) * s.tiles * 16 * 4 * 2 / 2000 : 0.0);
+                if (best == 0 || t < best) {
+                    best = t;
+                    p.mt = ha;
+                    p.nt = wn;
+                    p.splits = static_cast<int>(ceil_div(s.steps, per));
+                }
+            }
+        }
+    return p;
 }
 
-template <bool GATED, class Out>
-void stream_by_rows(const W4Args& g, hipStream_t s) {
-    const int waves = std::min(8, g.words);
-    if (g.m <= 16) stream_launch<1, 2, GATED, Out>(g, waves, s);
-    else if (g.m <= 32) stream_launch<2, 2, GATED, Out>(g, waves, s);
-    else stream_launch<4, 2, GATED, Out>(g, waves, s);
+size_t w4_partial_bytes(const W4Shape& s, const W4Plan& p, int m) {
+    return p.splits > 1 ? static_cast<size_t>(p.splits) * m * s.tiles * 64 : 0;
+}
+
+template <int MT, int NT>
+void stream_launch(const W4Args& g, int waves, hipStream_t s) {
+    const dim3 grid(static_cast<unsigned>(ceil_div(g.tiles, NT)), static_cast<unsigned>(ceil_div(g.m, 16 * MT)),
+                    static_cast<unsigned>(g.splits));
+    w4_stream_kernel<MT, NT, kStreamWaves><<<grid, 64 * waves, static_cast<size_t>(waves) * MT * NT * 1024, s>>>(g);
+}
+
+template <int NT>
+void stream_by_rows(const W4Args& g, const W4Plan& p, hipStream_t s) {
+    if (p.mt == 1) stream_launch<1, NT>(g, p.waves, s);
+    else stream_launch<2, NT>(g, p.waves, s);
+}
+
+template <int HA, int WN>
+void tile_launch(const W4Args& g, hipStream_t s) {
+    const int nt_m = static_cast<int>(ceil_div(g.m, 32 * HA)), nt_n = static_cast<int>(ceil_div(g.tiles, 4 * WN));
+    const int per = static_cast<int>(ceil_div(g.steps, g.splits));
+    w4_tile_kernel<HA, WN><<<dim3(static_cast<unsigned>(nt_m * nt_n), 1, static_cast<unsigned>(g.splits)), 128 * WN, 0, s>>>(
+        g, nt_m, nt_n, per);
+}
+
+void launch_w4(const W4Args& g, const W4Plan& p, hipStream_t s) {
+    if (p.kind == 0) {
+        if (p.nt == 1) stream_by_rows<1>(g, p, s);
+        else if (p.nt == 2) stream_by_rows<2>(g, p, s);
+        else stream_by_rows<4>(g, p, s);
+    } else switch (p.nt * 16 + p.mt) {
+        case 64 + 1: tile_launch<1, 4>(g, s); break;
+        case 64 + 2: tile_launch<2, 4>(g, s); break;
+        case 64 + 3: tile_launch<3, 4>(g, s); break;
+        case 64 + 4: tile_launch<4, 4>(g, s); break;
+        case 64 + 5: tile_launch<5, 4>(g, s); break;
+        case 64 + 6: tile_launch<6, 4>(g, s); break;
+        case 64 + 8: tile_launch<8, 4>(g, s); break;
+        case 32 + 1: tile_launch<1, 2>(g, s); break;
+        case 32 + 2: tile_launch<2, 2>(g, s); break;
+        case 32 + 3: tile_launch<3, 2>(g, s); break;
+        case 32 + 4: tile_launch<4, 2>(g, s); break;
+        case 16 + 1: tile_launch<1, 1>(g, s); break;
+        default: tile_launch<2, 1>(g, s); break;
+    }
+    if (p.splits > 1) {
+        const int quads = g.tiles / (g.gated ? 2 : 1) * 4;
+        w4_join_kernel<<<dim3(static_cast<unsigned>(ceil_div(quads, 256)), static_cast<unsigned>(g.m)), 256, 0, s>>>(g);
+    }
 }
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -231,7 +529,7 @@ extern "C" int slw_w4_pack(const void* codes, const void* scales, int32_t n, int
         if (!codes || !scales || !packed) return fail(SLW_EINVAL, "null argument");
         if (!aligned16(codes) || !aligned16(packed)) return fail(SLW_EINVAL, "codes and packed weights must be 16-byte aligned");
         const W4Shape w = w4_shape(n, k, gated);
-        const size_t threads = w.code_bytes / 16;
+        const size_t threads = static_cast<size_t>(w.tiles) * w.words * 256;
         w4_pack_kernel<<<static_cast<unsigned>((threads + 255) / 256), 256, 0, static_cast<hipStream_t>(stream)>>>(
             static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), static_cast<u32x4*>(packed),
             reinterpret_cast<uint32_t*>(static_cast<char*>(packed) + w.code_bytes), gated ? n / 2 : n, k, w.tiles, w.steps,
@@ -247,7 +545,10 @@ extern "C" int slw_w4_workspace_size(int32_t n, int32_t k, int32_t gated, int32_
         int rc = check_w4(n, k, gated);
         if (rc) return rc;
         if (max_m < 0) return fail(SLW_EINVAL, "negative rows");
+        const W4Shape s = w4_shape(n, k, gated);
         *bytes = 0;
+        for (int m = 1; m <= max_m && m <= kMostSplitRows; ++m)
+            *bytes = std::max(*bytes, w4_partial_bytes(s, plan_w4(s, m, gated), m));
         return SLW_OK;
     });
 }
@@ -284,9 +585,18 @@ extern "C" int slw_w4_product(const slw_w4* w, const void* a, int64_t lda, int32
         g.steps = sh.steps;
         g.words = sh.words;
         g.vec = ldo % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (out_f32 ? 16 : 8) == 0;
-        hipStream_t s = static_cast<hipStream_t>(stream);
-        if (w->gated) out_f32 ? stream_by_rows<true, float>(g, s) : stream_by_rows<true, bf16>(g, s);
-        else out_f32 ? stream_by_rows<false, float>(g, s) : stream_by_rows<false, bf16>(g, s);
+        g.gated = w->gated != 0;
+        g.f32 = out_f32 != 0;
+        W4Plan plan = plan_w4(sh, lda > kMostTileStride ? std::min(m, 32) : m, g.gated);
+        if (lda > kMostTileStride) plan.splits = 1;
+        const size_t need = w4_partial_bytes(sh, plan, m);
+        if (need) {
+            if (!ws || !aligned16(ws)) return fail(SLW_EINVAL, "the workspace must be 16-byte aligned device memory");
+            if (ws_bytes < need) return fail(SLW_ENOMEM, "the workspace holds %zu bytes, %d rows need %zu", ws_bytes, m, need);
+        }
+        g.part = static_cast<float*>(ws);
+        g.splits = plan.splits;
+        launch_w4(g, plan, static_cast<hipStream_t>(stream));
         HIP_TRY(hipGetLastError());
         return SLW_OK;
     });

@@ -193,6 +193,18 @@ def test_product_of_every_scale():
     assert got[127].isnan().all() and zero_inf[126].all()
 
 
+@pytest.mark.parametrize("m", [1, 30, 40])
+def test_product_of_rows_far_apart(m):
+    """A row stride past what 32-bit offsets within a tile reach."""
+    w = Weights(48, 64)
+    ld = (1 << 22) + 8
+    buf = torch.zeros(m * ld, dtype=torch.bfloat16, device="cuda").view(m, ld)
+    a, av = _bf16(np.random.default_rng(m).standard_normal((m, 64)))
+    buf[:, :64] = a
+    want, bound = O.product(av, w.values)
+    _within(_f64(w.product(buf, m, ld, True)), want, bound, "f32")
+
+
 def test_product_rows_keep_to_themselves():
     """Infinities and NaN in a row of a, and rows behind the last, stay out of the others."""
     w = Weights(320, 512)
