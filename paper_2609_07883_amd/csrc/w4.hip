@@ -258,18 +258,13 @@ __global__ __launch_bounds__(128 * WN, 2) void w4_tile_kernel(W4Args g, int nt_m
         const int row = (x * NW + wave) * 4 + (lane >> 4);
         off[x] = static_cast<uint32_t>(min(row, g.m - 1 - m0)) * static_cast<uint32_t>(g.lda * 2) + (((lane & 15) ^ (row & 15)) << 4);
     }
-    auto load_rows = [&](int t) {
-        const char* from = base + static_cast<size_t>(t) * 256;
-        const bool cut = tail && t == g.steps - 1;
-#pragma unroll
-        for (int x = 0; x < LOADS; ++x) {
-            uint32_t o = off[x];
-            if (cut) {
-                const int row = (x * NW + wave) * 4 + (lane >> 4), c = (lane & 15) ^ (row & 15);
-                if (c >= tail) o -= c << 4;
-            }
-            load_lds16(from, o, lds0 + (t - t0 & 1) * BUF + (x * NW + wave) * 1024);
+    auto load_row = [&](int x, int t) {
+        uint32_t o = off[x];
+        if (tail && t == g.steps - 1) {
+            const int row = (x * NW + wave) * 4 + (lane >> 4), c = (lane & 15) ^ (row & 15);
+            if (c >= tail) o -= c << 4;
         }
+        load_lds16(base + static_cast<size_t>(t) * 256, o, lds0 + (t - t0 & 1) * BUF + (x * NW + wave) * 1024);
     };
     const u32x4* codes[4];
     const uint32_t* scales[4];
@@ -297,36 +292,69 @@ __global__ __launch_bounds__(128 * WN, 2) void w4_tile_kernel(W4Args g, int nt_m
         for (int b = 0; b < 4; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     load_weights(t0);
-    load_rows(t0);
-    for (int t = t0; t < t1; ++t) {
-        wait_vmcnt<0>();
-        barrier_only();
-        u32x4 c[4];
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) load_row(x, t0);
+    // A step is four groups of two units, a unit the products of half of the wave's
+    // rows.  Operands are read a unit ahead, a group's weights widened under the unit
+    // before it, the next step's rows asked for in the first units (issued together
+    // they held up the MFMAs; with a step's order left to the compiler it read all
+    // rows at once and spilled).  The one barrier of a step stands before its last
+    // unit, whose operands are in registers by then: the next step's first operands
+    // are read, from rows that every wave has waited for, while that unit computes,
+    // and the buffer of this step is free.
+    constexpr int H0 = (HA + 1) / 2, H1 = HA - H0, UNITS = H1 ? 8 : 4, PER = UNITS / 4, EACH = (LOADS + UNITS / 2 - 1) / (UNITS / 2);
+    bf16x8 x[2][H0], w[2][4];
+    u32x4 c[4];
+    auto read = [&](int u, int at) {  // into x[u % 2]
+        const int j = u / PER, h = u % PER;
+#pragma unroll
+        for (int i = 0; i < (h ? H1 : H0); ++i)
+            x[u & 1][i] = *reinterpret_cast<const bf16x8*>(frag[j] + at + (h * H0 + i) * 4096);
+    };
+    auto widen_group = [&](int j) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) w[j & 1][b] = widen(c[b][j], group_scale(sc[b], j));
+    };
+    auto take_weights = [&] {
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             c[b] = next[b];
             sc[b] = sc_next[b];
         }
-        if (t + 1 < t1) {
-            load_weights(t + 1);
-            load_rows(t + 1);
+        widen_group(0);
+    };
+    wait_vmcnt<0>();
+    barrier_only();
+    read(0, 0);
+    take_weights();
+    for (int t = t0; t < t1; ++t) {
+        const int at = (t - t0 & 1) * BUF;
+        const int groups = tail && t == g.steps - 1 ? tail / 4 : 4;
+        const bool more = t + 1 < t1;
+        if (more) load_weights(t + 1);
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const int j = u / PER, h = u % PER;
+            if (u + 1 < UNITS) {
+                read(u + 1, at);
+            } else {
+                wait_lgkmcnt<0>();
+                wait_vmcnt<0>();
+                barrier_only();
+                if (more) read(0, BUF - at);
+            }
+            if (more)
+#pragma unroll
+                for (int q = u * EACH; q < (u + 1) * EACH && q < LOADS; ++q) load_row(q, t + 1);
+            if (h == PER - 1 && j < 3) widen_group(j + 1);
+            if (u + 1 == UNITS && more) take_weights();
+            if (j < groups)
+#pragma unroll
+                for (int i = 0; i < (h ? H1 : H0); ++i)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) acc[h * H0 + i][b] = mfma16(w[j & 1][b], x[u & 1][i], acc[h * H0 + i][b]);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        const int at = (t - t0 & 1) * BUF, groups = t == g.steps - 1 && tail ? tail / 4 : 4;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (j >= groups) break;
-            bf16x8 x[HA], w[4];
-#pragma unroll
-            for (int i = 0; i < HA; ++i) x[i] = *reinterpret_cast<const bf16x8*>(frag[j] + at + i * 4096);
-#pragma unroll
-            for (int b = 0; b < 4; ++b) w[b] = widen(c[b][j], group_scale(sc[b], j));
-#pragma unroll
-            for (int i = 0; i < HA; ++i)
-#pragma unroll
-                for (int b = 0; b < 4; ++b) acc[i][b] = mfma16(w[b], x[i], acc[i][b]);
-        }
-        // this wave's reads of the buffer are in registers before another wave refills it
-        wait_lgkmcnt<0>();
     }
     const int row0 = m0 + wm * 16 * HA + col;
 #pragma unroll
@@ -421,18 +449,23 @@ W4Plan plan_w4(const W4Shape& s, int m, bool gated) {
         p.waves = std::min(p.nt == 4 && p.splits == 1 ? 4 : 8, s.words);
         return p;
     }
-    // Work-groups of 2 WN waves, eight waves on a CU; a wave's step costs its
-    // MFMAs (two waves share a matrix unit) or the wait for the next step.
+    // Rounds of the work-groups that run together (eight waves a CU) times their steps.  us a step, fitted at 512 .. 2080 rows of the 8B
+    // layer's products: 0.75 + 0.29 HA with WN 4 (3.09 at HA 8, 1.91 at 4), 0.40 +
+    // 0.33 HA with WN 2 (1.71 at HA 4), never below 1.05, the wait for a step;
+    // work-groups alone on their CU take 0.65 of that.  A split's sums are written
+    // and read at 6 TB/s, by one launch more.
     p.kind = 1;
     double best = 0;
     for (int wn = 4; wn >= 1; wn /= 2)
         for (int ha = 1; ha <= (wn == 4 ? 8 : wn == 2 ? 4 : 2); ++ha) {
             if (ha == 7 || 4 * ha % wn) continue;
             const int64_t tiles = ceil_div(m, 32 * ha) * ceil_div(s.tiles, 4 * wn), slots = 256 * 4 / wn;
-            for (int sp = 1; sp == 1 || (sp <= 16 && sp * 4 <= s.steps && m <= kMostSplitRows); sp *= 2) {
-                const int64_t per = ceil_div(s.steps, sp), rounds = ceil_div(tiles * sp, slots);
-                const double t = rounds * (per * std::max(512.0 * ha + 200, 900.0) + 4000.0) +
-                                 (sp > 1 ? 8000.0 + sp * static_cast<double>(m) * s.tiles * 16 * 4 * 2 / 2000 : 0.0);
+            for (int sp = 1; sp == 1 || (sp <= 8 && sp * 4 <= s.steps && m <= kMostSplitRows); sp *= 2) {
+                const int64_t per = ceil_div(s.steps, sp), groups = tiles * sp;
+                double step = std::max(1.05, wn == 4 ? 0.75 + 0.29 * ha : wn == 2 ? 0.40 + 0.33 * ha : 0.45 + 0.35 * ha);
+                if (wn < 4 && groups <= 256) step *= 0.65;
+                const double t = ceil_div(groups, slots) * (per * step + 1.5) +
+                                 (sp > 1 ? 2.0 + sp * static_cast<double>(m) * s.tiles * 16 * 4 * 2 / 6e6 : 0.0);
                 if (best == 0 || t < best) {
                     best = t;
                     p.mt = ha;
