@@ -4,23 +4,29 @@
 // of the tokens sorted by (logit descending, index ascending): the first top_k;
 // of those, the ones with less than top_p of their mass before them; of those,
 // w >= min_p.  So every filter is a cut in that order, (key, index) of the last
-// token kept, and no row is ever sorted whole.  One work-group a row:
-//   1. a pass finds M, and each thread's largest logit;
-//   2. top_k up to the number of threads: the k-th largest of the threads' largest
-//      bounds the k-th largest logit from below, and a pass collects what is not
-//      below it, a little more than k tokens, in LDS; they are sorted, cut, sorted
-//      by index, and the token is drawn;
-//   3. top_p: a pass weighs the tokens in bins of 1/16 octave of w; the running sum
-//      over bins says in which one the cut is.  The tokens down to that bin are
-//      collected as above, or where they are too many those of the bin alone, which
-//      gives the cut;
-//   4. with no filter, or a cut of more tokens than LDS holds, the token is found by
-//      sums of the kept w over sixteenths of the row, then of that sixteenth, ...
+// token kept, and no row is ever sorted.  A row is cut into slices, so that a few
+// rows fill the chip, and dealt with by two kernels:
+//   1. a slice's largest logit and, as the row needs them, the largest of every
+//      thread (top_k), the mass of the tokens in bins of 1/16 octave of w (top_p),
+//      or the mass of sixteenths of the slice (no filter);
+//   2. a row's token.  top_k up to the number of threads: the k-th largest of the
+//      threads' largest bounds the k-th largest logit from below, and what is not
+//      below it, a little more than k tokens, is collected in LDS.  top_p: the running sum
+//      over bins says in which one the cut is; the tokens down to that bin are
+//      collected, or where they are too many those of the bin alone.  Cuts and the
+//      draw are one thing there, the first value of an order at which a running sum
+//      reaches a target, found digit by digit with a histogram: by logit and count
+//      for top_k, by logit and mass for top_p, by index and mass for the draw.  Where
+//      more tokens are kept than were collected, or all, sums over ranges of the row
+//      say in which the running sum passes u Z, then over sixteenths of that range,
+//      and so on.
+// The second kernel is a chain of short steps that meet their code cold, so it is
+// written in loops of few instructions rather than unrolled.
 //
-// Every mass is held in 64 bits: w from an exponential good to 2^-37, bins in
-// fixed point (integer sums: the order of the atomics does not matter), all else
-// in doubles summed in a fixed order.  With fp32 sums one draw in a few hundred
-// would be another token; a result depends on the row alone.
+// Every mass is held in 64 bits: w from an exponential good to 2^-37, bins and
+// lists in fixed point (integer sums: the order of the atomics does not matter),
+// all else in doubles summed in a fixed order.  With fp32 sums one draw in a few
+// hundred would be another token.
 #include <math.h>
 
 #include <algorithm>
@@ -35,6 +41,7 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 constexpr int kBins = 768;          // 16 for an octave; the last one holds w < 2^-47 and is weighed nowhere
 constexpr int kQueue = 8 * kWave + 64;  // logits a wave has queued: a piece of every lane beside 63 left over
+constexpr int kMost = 4096;         // most groups of threads of a row whose largest logits are kept
 constexpr int kList = 4096;         // tokens sorted in LDS
 
 struct SampleArgs {
@@ -47,7 +54,14 @@ struct SampleArgs {
     const float* u;
     int32_t* tokens;
     float* logprob;
-    int vocab;
+    int vocab, rows;
+    // workspace; a slice is slices * row + its number
+    int slices;
+    uint64_t* best;     // [slice]: its largest logit's key, ~ the first index that has it; 0: nothing but -inf
+    int32_t* ref;       // [slice]: top_p: sixteenths of an octave from logit 0 that its masses count from
+    double* sums;       // [slice][16]
+    uint64_t* bins;     // [slice][kBins]
+    uint32_t* most;     // [row][kMost]: the largest keys of groups of threads
 };
 
 // Ascending with the value; both zeros alike, NaN as -inf.
@@ -75,12 +89,19 @@ struct Row {
     }
     // 2^(t / 16): t = 16 q + i + f, |f| <= 1/2, 2^(f / 16) by a polynomial fitted to
     // 5e-12, 2^(i / 16) from the table, whose 16 entries lie on distinct banks.
-    __device__ __forceinline__ double weight(double t, int& n) const {
+    __device__ __forceinline__ double weight(double t, int& n) const { return weight_from(t, 0, n); }
+    // 2^((t - ref) / 16), n: t - ref to the nearest whole
+    __device__ __forceinline__ double weight_from(double t, int ref, int& n) const {
+        const double p = of_sixteenth(t, n);
+        n -= ref;
+        return ldexp(p * root[n & 15], n >> 4);
+    }
+    // 2^((t - n) / 16), n the nearest whole number
+    static __device__ __forceinline__ double of_sixteenth(double t, int& n) {
         const double whole = rint(t), f = t - whole;
         n = static_cast<int>(whole);
-        const double p = fma(f, fma(f, fma(f, fma(f, 0x1.3b2c4ac7eb38ap-23, 0x1.c6b3488226c3bp-17), 0x1.ebfbdff6988cep-11),
-                                    0x1.62e42fee4615cp-5), 1.0);
-        return ldexp(p * root[n & 15], n >> 4);
+        return fma(f, fma(f, fma(f, fma(f, 0x1.3b2c4ac7eb38ap-23, 0x1.c6b3488226c3bp-17), 0x1.ebfbdff6988cep-11),
+                          0x1.62e42fee4615cp-5), 1.0);
     }
     __device__ __forceinline__ double w(float x) const {
         int n;
@@ -91,23 +112,62 @@ struct Row {
 
 struct Shared {
     union {
-        uint64_t list[kList];
+        struct {
+            uint64_t list[kList];  // key, index
+            double w[kList];
+        };
         float queue[kWaves][kQueue];
     };
     uint64_t mass[kBins];
     double root[16];
     double red_d[kWaves];
-    uint64_t red_u[kWaves];
-    int n_list, found, digit;
-    uint64_t before;
+    uint64_t best[16];  // of the slices
+    int32_t ref[16];
+    uint64_t goal, sum, before;
     double found_d, above_d;
+    int n_list, found, digit;
 };
 
-__device__ __forceinline__ double wave_sum_d(double v) {
+// Inclusive sums over the lanes of a wave by data-parallel moves: within rows of 16
+// lanes, then the last lane of a row onto the next one, then of the first half onto
+// the second.  A shuffle goes through LDS, several times as long.
+template <int CTRL, int ROWS, class V>
+__device__ __forceinline__ V moved(V v) {
+    static_assert(sizeof(V) == 4 || sizeof(V) == 8, "one or two registers");
+    union {
+        V v;
+        int w[sizeof(V) / 4];
+    } from{v}, to;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+    for (size_t i = 0; i < sizeof(V) / 4; ++i) to.w[i] = __builtin_amdgcn_update_dpp(0, from.w[i], CTRL, ROWS, 0xf, false);
+    return to.v;
+}
+template <class V>
+__device__ __forceinline__ V wave_scan(V v) {
+    v += moved<0x111, 0xf>(v);  // one lane up
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);  // lane 15 of a row
+    v += moved<0x143, 0xc>(v);  // lane 31
     return v;
 }
+// A lane's value, on every lane.
+template <class V>
+__device__ __forceinline__ V of_lane(V v, int lane) {
+    union {
+        V v;
+        int w[sizeof(V) / 4];
+    } x{v};
+#pragma unroll
+    for (size_t i = 0; i < sizeof(V) / 4; ++i) x.w[i] = __builtin_amdgcn_readlane(x.w[i], lane);
+    return x.v;
+}
+// A value that is the same on every lane, in scalar registers.
+template <class V>
+__device__ __forceinline__ V uniform(V v) { return of_lane(v, 0); }
+template <class V>
+__device__ __forceinline__ V wave_total(V v) { return of_lane(wave_scan(v), kWave - 1); }
 
 // LDS accesses of the lanes of one wave keep their order across it.
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
@@ -121,23 +181,11 @@ struct Group {
         wave_fence();
         if (!solo) __syncthreads();
     }
-    __device__ __forceinline__ uint64_t sum(uint64_t v, Shared& sh) const {
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
-        if (solo) return v;
-        __syncthreads();
-        if (threadIdx.x % kWave == 0) sh.red_u[threadIdx.x / kWave] = v;
-        __syncthreads();
-        v = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) v += sh.red_u[w];
-        return v;
-    }
 };
 
 // Sum over the work-group, in a fixed order, on every thread.
 __device__ __forceinline__ double block_sum(double v, Shared& sh) {
-    v = wave_sum_d(v);
+    v = wave_total(v);
     __syncthreads();
     if (threadIdx.x % kWave == 0) sh.red_d[threadIdx.x / kWave] = v;
     __syncthreads();
@@ -150,11 +198,7 @@ __device__ __forceinline__ double block_sum(double v, Shared& sh) {
 // Inclusive sums over the work-group's threads, in thread order.
 __device__ __forceinline__ double block_scan(double v, Shared& sh) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const double p = __shfl_up(v, o, kWave);
-        if (lane >= o) v += p;
-    }
+    v = wave_scan(v);
     __syncthreads();
     if (lane == kWave - 1) sh.red_d[wave] = v;
     __syncthreads();
@@ -162,20 +206,6 @@ __device__ __forceinline__ double block_scan(double v, Shared& sh) {
 #pragma unroll
     for (int w = 0; w < kWaves - 1; ++w) before += w < wave ? sh.red_d[w] : 0.0;
     return before + v;
-}
-
-__device__ __forceinline__ uint64_t block_max(uint64_t v, Shared& sh) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const uint64_t p = __shfl_xor(v, o, kWave);
-        v = p > v ? p : v;
-    }
-    __syncthreads();
-    if (threadIdx.x % kWave == 0) sh.red_u[threadIdx.x / kWave] = v;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) v = sh.red_u[w] > v ? sh.red_u[w] : v;
-    return v;
 }
 
 // The row in pieces of 8 tokens, aligned to 16 bytes as far as the row's start
@@ -210,19 +240,18 @@ struct Pieces {
     }
 };
 
-// Every token of the row, f(x, index); a row with +inf as Row::fix has it.  Up to 14
-// places outside the row come too, as -inf.
+__device__ __forceinline__ float largest(const float (&x)[8]) {
+    return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+}
+
+// Every token of the row, f(x, index); a row with +inf as Row::fix has it.  One at a
+// time: for what few rows come to.
 template <class T, class F>
 __device__ __forceinline__ void each(const Pieces<T>& p, const Row& r, F&& f) {
 #pragma unroll 1
-    for (int v = threadIdx.x; v < p.count; v += kThreads) {
-        float x[8];
-        p.load(v, x);
-        if (r.at_inf)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = r.fix(x[e]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f(x[e], 8 * v - p.shift + e);
+    for (int i = threadIdx.x; i < p.n; i += kThreads) {
+        const float x = static_cast<float>(p.row[i]);
+        f(r.at_inf ? r.fix(x) : x, i);
     }
 }
 
@@ -243,7 +272,7 @@ __device__ __forceinline__ Cut bisect(const Pieces<T>& p, const Row& r, const Cu
         double s = 0.0;
         each(p, r, [&](float x, int i) {
             const uint32_t k = key_of(x);
-            if (i >= 0 && i < p.n && in.keeps(k, i) && c.keeps(k, i)) s += by_mass ? r.w(x) : 1.0;
+            if (in.keeps(k, i) && c.keeps(k, i)) s += by_mass ? r.w(x) : 1.0;
         });
         return block_sum(s, sh);
     };
@@ -265,33 +294,36 @@ __device__ __forceinline__ Cut bisect(const Pieces<T>& p, const Row& r, const Cu
     return Cut{lo, a};
 }
 
-// Tokens of `in` with lo <= key < hi, in LDS (in any order); how many there are, of which the first kList are there.
+// Tokens of `in` from `lo` up and below `hi` (none: +inf), in LDS (in any order); how many there are, of
+// which the first kList are there.
 template <class T>
-__device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, uint32_t lo, uint32_t hi, const Cut& in, Shared& sh) {
+__device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float lo, float hi, const Cut& in, Shared& sh) {
     __syncthreads();
     if (threadIdx.x == 0) sh.n_list = 0;
     __syncthreads();
+    // a piece is loaded before the one ahead of it is looked at
+    float x[8], y[8];
+    if (static_cast<int>(threadIdx.x) < p.count) p.load(threadIdx.x, y);
 #pragma unroll 1
     for (int v = threadIdx.x; v < p.count; v += kThreads) {
-        float x[8];
-        p.load(v, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = y[e];
+        if (v + kThreads < p.count) p.load(v + kThreads, y);
         if (r.at_inf)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = r.fix(x[e]);
         uint32_t keeps = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t k = key_of(x[e]);
-            keeps |= k >= lo && k < hi && in.keeps(k, 8 * v - p.shift + e) ? 1u << e : 0u;
-        }
-        if (keeps) {
-            int at = atomicAdd(&sh.n_list, __popc(keeps));
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (keeps >> e & 1) {
-                    if (at < kList) sh.list[at] = static_cast<uint64_t>(key_of(x[e])) << 32 | static_cast<uint32_t>(8 * v - p.shift + e);
-                    ++at;
-                }
+        for (int e = 0; e < 8; ++e) keeps |= x[e] >= lo && x[e] < hi ? 1u << e : 0u;
+#pragma unroll 1
+        for (; keeps; keeps &= keeps - 1) {
+            const int i = 8 * v - p.shift + __ffs(keeps) - 1;
+            float one = static_cast<float>(p.row[i]);
+            if (r.at_inf) one = r.fix(one);
+            const uint32_t k = key_of(one);
+            if (!in.keeps(k, i)) continue;
+            const int at = atomicAdd(&sh.n_list, 1);
+            if (at < kList) sh.list[at] = static_cast<uint64_t>(k) << 32 | static_cast<uint32_t>(i);
         }
     }
     __syncthreads();
@@ -300,15 +332,16 @@ __device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, uint32_
     return n;
 }
 
-// The smallest key whose token falls into bin `bin` or one before it: every wave
-// tries 64 keys at a time.
-__device__ __forceinline__ uint32_t bin_edge(const Row& r, int bin) {
-    uint32_t lo = 0x00800000u, hi = key_of(r.M);  // lo: the lowest finite key; hi is in the bin or before it
+// The smallest key whose value `holds`, as every larger one does, M's too:
+// every wave tries 64 keys at a time.
+template <class F>
+__device__ __forceinline__ uint32_t edge(const Row& r, F&& holds) {
+    uint32_t lo = 0x00800000u, hi = key_of(r.M);  // lo: the lowest finite key; hi holds
     const uint32_t lane = threadIdx.x % kWave;
 #pragma unroll 1
     while (lo < hi) {
         const uint32_t step = max((hi - lo) / kWave, 1u), key = lo + lane * step;
-        const uint64_t in = __ballot(key < hi && r.bin_of(value_of(key)) <= bin);
+        const uint64_t in = __ballot(key < hi && holds(value_of(key)));
         // keys below the first that is in are not; it is not below the one before it
         const uint32_t first = in ? static_cast<uint32_t>(__ffsll(static_cast<unsigned long long>(in)) - 1) : kWave;
         if (in) hi = lo + first * step;
@@ -323,137 +356,108 @@ __device__ __forceinline__ uint32_t bin_edge(const Row& r, int bin) {
 constexpr int kSolo = 256;  // tokens that one wave deals with alone
 constexpr int kDigit = 9;
 
-// w in units of 2^-50: the low bits of w + 4.
-__device__ __forceinline__ uint64_t fixed(double w) {
-    return static_cast<uint64_t>(__double_as_longlong(w + 4.0) - __double_as_longlong(4.0));
-}
-
-// The least value v[] (of `bits` bits) of the tokens that are `in` up to which their
-// amounts add up to the target, 0 < target <= their sum, and what lies before it:
-// nine bits at a time, by sums over the values of the next nine.
-__device__ __forceinline__ uint32_t select(const Group& g, const uint32_t (&v)[4], const uint64_t (&amount)[4],
-                                           const bool (&in)[4], int bits, uint64_t target, uint64_t& before, Shared& sh) {
-    constexpr uint32_t kMask = (1u << kDigit) - 1;
-    const int tid = threadIdx.x;
-    uint32_t prefix = 0;
-    before = 0;
-#pragma unroll 1
-    for (int shift = (bits - 1) / kDigit * kDigit; shift >= 0; shift -= kDigit) {
-        g.sync();
-        for (int b = tid; b <= static_cast<int>(kMask); b += g.size()) sh.mass[b] = 0;
-        g.sync();
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (in[e] && (shift + kDigit >= 32 || v[e] >> (shift + kDigit) == prefix))
-                atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[v[e] >> shift & kMask]), static_cast<unsigned long long>(amount[e]));
-        g.sync();
-        if (tid < kWave) {  // eight digits a lane
-            uint64_t m[8], sum = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                m[i] = sh.mass[8 * tid + i];
-                sum += m[i];
-            }
-            uint64_t upto = sum;
-#pragma unroll
-            for (int o = 1; o < kWave; o <<= 1) {
-                const uint64_t q = __shfl_up(upto, o, kWave);
-                if (tid >= o) upto += q;
-            }
-            const uint64_t reach = __ballot(before + upto >= target);
-            if (reach && tid == __ffsll(static_cast<unsigned long long>(reach)) - 1) {
-                uint64_t run = before + upto - sum;
-                int d = 0;
-#pragma unroll
-                for (int i = 0; i < 7; ++i)
-                    if (d == i && run + m[i] < target) {
-                        run += m[i];
-                        d = i + 1;
-                    }
-                sh.digit = 8 * tid + d;
-                sh.before = run;
-            }
-        }
-        g.sync();
-        prefix = prefix << kDigit | static_cast<uint32_t>(sh.digit);
-        before = sh.before;
+// By wave 0: the first of 512 amounts up to which they add up to the goal (with
+// what lies before them; 512: none), and what lies before that one.
+__device__ __forceinline__ void find_digit(uint64_t before, uint64_t goal, uint64_t sum8, Shared& sh) {
+    const int lane = threadIdx.x;
+    const uint64_t upto = before + wave_scan(sum8);
+    const uint64_t reach = __ballot(upto >= goal);
+    const int l = reach ? __ffsll(static_cast<unsigned long long>(reach)) - 1 : kWave - 1;
+    const uint64_t one = lane < 8 ? sh.mass[8 * l + lane] : 0, run = of_lane(upto - sum8, l) + wave_scan(one);
+    const uint64_t hit = __ballot(lane < 8 && run >= goal);
+    if (lane == (hit ? __ffsll(static_cast<unsigned long long>(hit)) - 1 : 7)) {
+        sh.digit = reach ? 8 * l + lane : 512;
+        sh.before = run - one;
     }
-    return prefix;
+}
+// The lane's eight amounts of those.
+__device__ __forceinline__ uint64_t eight(const Shared& sh) {
+    uint64_t s = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += sh.mass[8 * threadIdx.x + i];
+    return s;
 }
 
-// The collected tokens, four a thread: cut to a count (count > 0), then to a mass
-// (mass > 0, as it is or as a share of theirs), each by key and among equals by
-// index; then, if the rest is all that the row keeps, the token is drawn.  Returns
-// the last cut made.
+// The collected tokens: cut to a count (count > 0), then to a mass (mass > 0, as it
+// is or as a share of theirs), each by key and among equals by index; then, if the
+// rest is all that the row keeps, the token is drawn.  Returns the last cut made.
+// No key is below `least`.
 struct Targets {
     double count, mass;
     bool share, draw;
 };
-__device__ __forceinline__ Cut cut_list(const Row& r, int n, const Targets& to, double u, int32_t* token, float* logprob,
-                                        Shared& sh) {
+// Of bf16 logits the keys' upper 16 bits say which (low_bits 16).
+__device__ __forceinline__ Cut cut_list(const Row& r, int n, uint32_t least, int low_bits, const Targets& to, double u,
+                                        int32_t* token, float* logprob, Shared& sh) {
+    constexpr uint32_t kDigits = 1u << kDigit;
     const Group g{to.draw && n <= kSolo};
+    const int tid = threadIdx.x;
     Cut cut{0, r.n};
-    if (g.solo && threadIdx.x >= kWave) return cut;
-    uint32_t key[4], idx[4];
-    double w[4];
-    bool in[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int i = threadIdx.x + e * g.size();
-        in[e] = i < n;
-        const uint64_t t = in[e] ? sh.list[i] : 0;
-        key[e] = static_cast<uint32_t>(t >> 32);
-        idx[e] = static_cast<uint32_t>(t);
-        w[e] = in[e] ? r.w(value_of(key[e])) : 0.0;
-    }
-    const uint32_t top = key_of(r.M);
-    const int index_bits = 32 - __clz(r.n);
-    uint64_t target = 0, before = 0, all = 0;
-    uint32_t found = 0;
-    bool ties = false;
+    if (g.solo && tid >= kWave) return cut;
+#pragma unroll 1
+    for (int i = tid; i < n; i += g.size()) sh.w[i] = r.w(value_of(static_cast<uint32_t>(sh.list[i] >> 32)));
+    const uint32_t top = key_of(r.M) >> low_bits, depth = top - (least >> low_bits);
+    uint64_t rest = 0;  // of the goal, for the ones that equal the last by key
     // 0, 1: count by key, by index; 2, 3: mass; 4: the draw
 #pragma unroll 1
     for (int step = 0; step < 5; ++step) {
-        if ((step < 2 && !(to.count > 0.0)) || (step >= 2 && step < 4 && !(to.mass > 0.0)) || (step == 4 && !to.draw)) continue;
-        const bool by_key = step == 0 || step == 2;
-        if ((step == 1 || step == 3) && !ties) continue;
-        uint32_t v[4];
-        uint64_t amount[4], sum = 0;
-        bool some[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (step == 4) in[e] = in[e] && w[e] >= r.min_p;
-            v[e] = by_key ? top - key[e] : idx[e];
-            amount[e] = step < 2 ? 1 : fixed(w[e]);
-            some[e] = in[e] && (step == 4 || by_key || key[e] == found);
-            sum += some[e] ? amount[e] : 0;
-        }
-        sum = g.sum(sum, sh);
-        if (by_key) {
-            const double t = step == 0 ? to.count : to.share ? to.mass * static_cast<double>(sum) : to.mass * 0x1p50;
-            target = min(t >= 1.0 ? static_cast<uint64_t>(ceil(t)) : 1, sum);
-        } else if (step < 4) {
-            target -= before;
-            if (sum <= target) continue;  // all of the equal ones
-        } else {
-            all = sum;
-            target = min(static_cast<uint64_t>(u * static_cast<double>(sum)) + 1, sum);
-        }
-        const uint32_t got = select(g, v, amount, some, by_key ? 32 : index_bits, target, before, sh);
-        if (by_key) {
-            found = top - got;
-            ties = true;
-            cut = Cut{found, r.n};
-        } else {
-            cut.last = static_cast<int>(got);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (step < 4) in[e] = in[e] && (key[e] > cut.key || (key[e] == cut.key && static_cast<int>(idx[e]) <= cut.last));
-            else if (in[e] && idx[e] == got) {
-                *token = static_cast<int32_t>(got);
-                if (logprob) *logprob = static_cast<float>(log(w[e] * 0x1p50 / static_cast<double>(all)));
+        if (step < 2 ? !(to.count > 0.0) : step < 4 ? !(to.mass > 0.0) : !to.draw) continue;
+        const bool by_key = step == 0 || step == 2, draw = step == 4;
+        const int bits = by_key ? 32 - __clz(depth | 1) : 32 - __clz(r.n), shift0 = (bits - 1) / kDigit * kDigit;
+        uint32_t value = 0;
+        uint64_t goal = 0, before = 0, sum = 0;
+#pragma unroll 1
+        for (int shift = shift0; shift >= 0; shift -= kDigit) {
+            g.sync();
+#pragma unroll 1
+            for (int b = tid; b < static_cast<int>(kDigits); b += g.size()) sh.mass[b] = 0;
+            g.sync();
+#pragma unroll 1
+            for (int i = tid; i < n; i += g.size()) {
+                const uint64_t t = sh.list[i];
+                const uint32_t key = static_cast<uint32_t>(t >> 32), idx = static_cast<uint32_t>(t), v = by_key ? top - (key >> low_bits) : idx;
+                const double w = sh.w[i];
+                bool in = cut.keeps(key, static_cast<int>(idx)) && (shift == shift0 || v >> (shift + kDigit) == value);
+                if (!by_key) in = in && (draw ? w >= r.min_p : key >> low_bits == cut.key >> low_bits);
+                // w in units of 2^-50: the low bits of w + 4
+                const uint64_t amount = step < 2 ? 1 : static_cast<uint64_t>(__double_as_longlong(w + 4.0) - __double_as_longlong(4.0));
+                if (in) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[v >> shift & (kDigits - 1)]), static_cast<unsigned long long>(amount));
             }
+            g.sync();
+            if (tid < kWave) {
+                const uint64_t mine = eight(sh);
+                if (shift == shift0) {  // the goal, as of the sum
+                    sum = wave_total(mine);
+                    const double t = step == 0 ? to.count : to.share ? to.mass * static_cast<double>(sum) : to.mass * 0x1p50;
+                    goal = by_key ? t >= 1.0 ? static_cast<uint64_t>(ceil(t)) : 1
+                                  : draw ? static_cast<uint64_t>(u * static_cast<double>(sum)) + 1 : rest;
+                    goal = min(goal, sum);
+                    if (tid == 0) {
+                        sh.goal = goal;
+                        sh.sum = sum;
+                    }
+                }
+                find_digit(before, goal, mine, sh);
+            }
+            g.sync();
+            goal = sh.goal;
+            sum = sh.sum;
+            before = sh.before;
+            value = value << kDigit | static_cast<uint32_t>(sh.digit);
+        }
+        if (by_key) {
+            const uint32_t k = (top - value) << low_bits;  // a negative bf16 number's key ends in ones
+            cut = Cut{low_bits && !(k >> 31) ? k | 0xFFFFu : k, r.n};
+            rest = goal - before;
+        } else if (!draw) {
+            if (goal < sum) cut.last = static_cast<int>(value);  // else all of the equal ones
+        } else {
+#pragma unroll 1
+            for (int i = tid; i < n; i += g.size())
+                if (static_cast<uint32_t>(sh.list[i]) == value) {
+                    *token = static_cast<int32_t>(value);
+                    if (logprob) *logprob = static_cast<float>(log(sh.w[i] * 0x1p50 / static_cast<double>(sum)));
+                }
         }
     }
     return cut;
@@ -501,160 +505,57 @@ __device__ __forceinline__ Found find_bin(const Pieces<T>& p, const Row& r, cons
     return f;
 }
 
-// The token of a row whose kept tokens are those of `cut` with w >= min_p: the
-// pieces are cut into sixteen ranges, one a wave, the first is taken in which the
-// running sum passes u Z, and so on down to 64 pieces, one a lane.
-template <class T>
-__device__ __forceinline__ void draw_from_row(const Pieces<T>& p, const Row& r, const Cut& cut, double u, int32_t* token, float* logprob,
-                              Shared& sh) {
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const bool all = cut.key == 0, low = r.min_p > 0.0;
-    // in logits: equal values have one key, and -inf has no mass either way
-    const float cut_x = all ? -INFINITY : value_of(cut.key);
-    auto piece = [&](int v, double (&w)[8]) {
-        float x[8];
-        p.load(v, x);
-        if (r.at_inf)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = r.fix(x[e]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            w[e] = r.w(x[e]);  // 0 outside the row, where x is -inf
-            if (!(x[e] > cut_x || (x[e] == cut_x && 8 * v - p.shift + e <= cut.last))) w[e] = 0.0;
-            if (low && w[e] < r.min_p) w[e] = 0.0;
-        }
-    };
-    // Under a cut most tokens are out: a wave queues those that are in, in any order,
-    // and weighs 64 at a time.
-    float* queue = sh.queue[wave];
-    // well below what min_p keeps
-    const double low_t = low ? 16.0 * log2(r.min_p) - 0.01 : 0.0;
-    const double low_d = low ? static_cast<double>(r.M) + low_t / r.c16 : -INFINITY;
-    const float low_x = static_cast<float>(low_d - fabs(low_d) * 0x1p-20);
-    int a = 0, b = p.count;
-    double z = 0.0, before = 0.0, target = 0.0;
-    bool first = true;
-    __syncthreads();
-#pragma unroll 1
-    while (first || b - a > kWave) {
-        const int per = ((b - a + kWaves - 1) / kWaves + kWave - 1) / kWave * kWave;
-        const int from = a + wave * per, to = min(from + per, b);
-        double s = 0.0;
-        if (all && !low) {
-#pragma unroll 1
-            for (int v = from + lane; v < to; v += kWave) {
-                double w[8];
-                piece(v, w);
-                s += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-            }
-        } else {
-            int n = 0;
-#pragma unroll 1
-            for (int v0 = from; v0 < to; v0 += kWave) {
-                float x[8];
-                const int v = v0 + lane;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = -INFINITY;
-                if (v < to) {
-                    p.load(v, x);
-                    if (r.at_inf)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = r.fix(x[e]);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool in = (x[e] > cut_x || (x[e] == cut_x && 8 * v - p.shift + e <= cut.last)) && x[e] >= low_x;
-                    const uint64_t mask = __ballot(in);
-                    const int at = n + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), 0));
-                    if (in) queue[at] = x[e];
-                    n += __popcll(mask);
-                }
-                wave_fence();
-                while (n >= kWave) {
-                    n -= kWave;
-                    const double w = r.w(queue[n + lane]);
-                    s += w >= r.min_p ? w : 0.0;
-                }
-                wave_fence();
-            }
-            if (lane < n) {
-                const double w = r.w(queue[lane]);
-                s += w >= r.min_p ? w : 0.0;
-            }
-        }
-        s = wave_sum_d(s);
-        __syncthreads();
-        if (lane == 0) sh.red_d[wave] = s;
-        __syncthreads();
-        if (first) {
-            for (int i = 0; i < kWaves; ++i) z += sh.red_d[i];
-            target = u * z;
-            first = false;
-        }
-        // the first range that passes the target; the last with any mass where rounding leaves none
-        int at = 0;
-        double run = before, at_before = before;
-#pragma unroll 1
-        for (int i = 0; i < kWaves; ++i) {
-            if (sh.red_d[i] <= 0.0) continue;
-            at = i;
-            at_before = run;
-            run += sh.red_d[i];
-            if (run > target) break;
-        }
-        before = at_before;
-        a += at * per;
-        b = min(a + per, b);
+// What a row asks for.
+struct Wants {
+    double c16, min_p, prob, u;
+    int k;
+    bool greedy;
+    __device__ Wants(const SampleArgs& a, int row) {
+        const float t0 = a.temperature ? a.temperature[row] : 1.f, low0 = a.min_p ? a.min_p[row] : 0.f;
+        const float p0 = a.top_p ? a.top_p[row] : 1.f, x0 = a.u[row];
+        const int32_t k0 = a.top_k ? a.top_k[row] : 0;
+        const float t = uniform(t0), low = uniform(low0), p = uniform(p0), x = uniform(x0);
+        const int32_t top_k = uniform(k0);
+        greedy = !(t > 0.f);
+        c16 = uniform(16.0 * 1.4426950408889634074 / static_cast<double>(t));
+        min_p = uniform(low > 0.f ? fmin(static_cast<double>(low), 1.0) : 0.0);
+        k = top_k > 0 && top_k < a.vocab ? top_k : 0;
+        prob = uniform(p < 1.f ? fmax(static_cast<double>(p), 0.0) : 1.0);
+        u = uniform(x > 0.f ? fmin(static_cast<double>(x), 0x1.fffffffffffffp-1) : 0.0);
     }
-    if (wave > 0) return;
-    double w[8] = {}, sum = 0.0;
-    if (a + lane < b) piece(a + lane, w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum += w[e];
-    double upto = sum;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const double q = __shfl_up(upto, o, kWave);
-        if (lane >= o) upto += q;
-    }
-    const uint64_t here = __ballot(before + upto > target && sum > 0.0), some = __ballot(sum > 0.0);
-    const int l = here ? __ffsll(static_cast<unsigned long long>(here)) - 1 : 63 - __clzll(static_cast<long long>(some));
-    if (lane == l) {
-        double run = before + upto - sum, wb = 0.0;
-        int best = -1;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (w[e] <= 0.0 || (best >= 0 && run > target)) continue;
-            run += w[e];
-            best = 8 * (a + lane) - p.shift + e;
-            wb = w[e];
-        }
-        *token = best;
-        if (logprob) *logprob = static_cast<float>(log(wb / z));
-    }
+    __device__ bool free() const { return !greedy && k == 0 && prob >= 1.0 && min_p == 0.0; }
+    __device__ bool by_mass() const { return !greedy && k == 0 && prob < 1.0; }
+    __device__ bool by_count() const { return !greedy && k > 0 && k <= kThreads; }
+};
+
+// Pieces of slice s of a row, a whole number for every thread (the last ones may have fewer, or none).
+__device__ __forceinline__ int slice_pieces(int count, int slices) {
+    return ((count + slices - 1) / slices + kThreads - 1) / kThreads * kThreads;
 }
 
+// 1. What is known of a slice.
 template <class T>
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
-    __shared__ Shared sh;
-    const int row = blockIdx.x, tid = threadIdx.x;
+__global__ __launch_bounds__(kThreads, 8) void sample_slices_kernel(SampleArgs a) {
+    __shared__ double root[16];
+    __shared__ uint64_t bins[kBins];
+    __shared__ uint64_t red_u[kWaves];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const size_t slice = blockIdx.x;
+    const int row = static_cast<int>(slice / a.slices);
+    const Wants want(a, row);
     const Pieces<T> p(static_cast<const T*>(a.logits) + row * a.ld, a.vocab);
-    int32_t* token = a.tokens + row;
-    float* logprob = a.logprob ? a.logprob + row : nullptr;
-    if (tid < 16) sh.root[tid] = exp2(tid / 16.0);
-    // asked for before the row, so that they are there after it
-    const float temperature = a.temperature ? a.temperature[row] : 1.f, min_p = a.min_p ? a.min_p[row] : 0.f;
-    const float top_p = a.top_p ? a.top_p[row] : 1.f, u_in = a.u[row];
-    const int32_t top_k = a.top_k ? a.top_k[row] : 0;
+    const int per = slice_pieces(p.count, a.slices), from = static_cast<int>(slice % a.slices) * per, to = min(from + per, p.count);
+    if (tid < 16) root[tid] = exp2(tid / 16.0);
+    for (int b = tid; b < kBins; b += kThreads) bins[b] = 0;
 
     // the thread's largest logit and the first piece that has it (NaN is below everything)
     float mine = -INFINITY;
     int at = -1;
-#pragma unroll 2
-    for (int v = tid; v < p.count; v += kThreads) {
+#pragma unroll 4
+    for (int v = from + tid; v < to; v += kThreads) {
         float x[8];
         p.load(v, x);
-        const float m = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+        const float m = largest(x);
         if (m > mine) {
             mine = m;
             at = v;
@@ -670,85 +571,389 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
             if (x[e] == mine) i = 8 * at - p.shift + e;
         best = static_cast<uint64_t>(key_of(mine)) << 32 | (0xFFFFFFFFu - static_cast<uint32_t>(i));
     }
-    best = block_max(best, sh);
-    if (best == 0 || !(temperature > 0.f)) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) best = max(best, static_cast<uint64_t>(__shfl_xor(best, o, kWave)));
+    if (lane == 0) red_u[wave] = best;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) best = max(best, red_u[w]);
+    if (tid == 0) a.best[slice] = best;
+    if (want.by_count()) {  // of four threads together from sixteen slices on, of two from eight on
+        const int group = max(1, a.slices * kThreads / kMost);
+        if (group >= 2) mine = fmaxf(mine, __shfl_xor(mine, 1, kWave));
+        if (group >= 4) mine = fmaxf(mine, __shfl_xor(mine, 2, kWave));
+        if (tid % group == 0)
+            a.most[static_cast<size_t>(row) * kMost + (slice % a.slices) * (kThreads / group) + tid / group] = key_of(mine);
+    }
+    const float m = value_of(static_cast<uint32_t>(best >> 32));
+    const bool by_mass = want.by_mass() && best != 0 && m != INFINITY;
+    if (!by_mass && !want.free()) return;
+
+    double s = 0.0;
+    if (by_mass) {
+        // By bins of whole sixteenths of an octave, which all slices share; in units of
+        // 2^-42 of the bin's w, the low bits of a number near 2^10.
+        const int ref = uniform(static_cast<int>(rint(static_cast<double>(m) * want.c16)));
+        const double floor = static_cast<double>(ref) - kBins;  // -inf and NaN too
+#pragma unroll 1
+        for (int v = from + tid; v < to; v += kThreads) {
+            float x[8];
+            p.load(v, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                int n;
+                const double w = Row::of_sixteenth(fmax(static_cast<double>(x[e]) * want.c16, floor), n);
+                if (static_cast<uint32_t>(ref - n) < kBins - 1)
+                    atomicAdd(reinterpret_cast<unsigned long long*>(&bins[ref - n]),
+                              static_cast<unsigned long long>(__double_as_longlong(w + 0x1p10) - __double_as_longlong(0x1p10)));
+            }
+        }
+        __syncthreads();
+        for (int b = tid; b < kBins; b += kThreads) a.bins[slice * kBins + b] = bins[b];
+        if (tid == 0) a.ref[slice] = ref;
+        return;
+    }
+    // of a sixteenth of the slice each wave, from the slice's largest logit
+    Row r;
+    r.at_inf = m == INFINITY;
+    r.M = r.at_inf || best == 0 ? 0.f : m;
+    r.c16 = want.c16;
+    r.root = (const __attribute__((address_space(3))) double*)root;
+    const int each_wave = per / kWaves, v1 = min(from + (wave + 1) * each_wave, to);
+#pragma unroll 1
+    for (int v = from + wave * each_wave + lane; v < v1; v += kWave) {
+        float x[8];
+        p.load(v, x);
+        if (r.at_inf)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = r.fix(x[e]);
+        double w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = r.w(x[e]);
+        s += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+    }
+    s = wave_total(s);
+    if (lane == 0) a.sums[slice * kWaves + wave] = best ? s : 0.0;
+}
+
+// The bin of the slices' masses where the running sum reaches prob of all of it; masses
+// as of M = 1, bins counted from `ref` down.
+__device__ __forceinline__ Found find_bin_of_slices(const SampleArgs& a, int row, const Row& r, double prob, int ref, Shared& sh) {
+    const int tid = threadIdx.x;
+    const size_t s0 = static_cast<size_t>(row) * a.slices;
+    const bool has = tid < kBins - 1;
+    uint64_t mass = 0;
+#pragma unroll 8
+    for (int s = 0; s < a.slices; ++s) {
+        const int b = tid - (ref - sh.ref[s]);  // the slice's bin that is this thread's
+        mass += has && b >= 0 && sh.best[s] ? a.bins[(s0 + s) * kBins + b] : 0;
+    }
+    int n;
+    const double tokens = static_cast<double>(mass) * 0x1p-42;  // nearly
+    const double mine = tokens * r.weight_from(ref - tid - static_cast<double>(r.M) * r.c16, 0, n);
+    const double upto = block_scan(mine, sh);
+    if (tid == 0) sh.found = kBins;
+    if (tid == kBins - 2) sh.found_d = upto;
+    __syncthreads();
+    Found f;
+    f.z = sh.found_d;
+    if (has && upto >= prob * f.z) atomicMin(&sh.found, tid);
+    __syncthreads();
+    f.bin = sh.found;
+    if (tid == f.bin) sh.above_d = upto - mine;
+    f.about = block_sum(has && tid <= f.bin ? tokens : 0.0, sh);
+    f.above = sh.above_d;
+    return f;
+}
+
+// 2. The token of a row.
+template <class T>
+__global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
+    __shared__ Shared sh;
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const Wants want(a, row);
+    if (tid < a.slices) {
+        const size_t s = static_cast<size_t>(row) * a.slices + tid;
+        sh.best[tid] = a.best[s];
+        sh.ref[tid] = a.ref[s];
+    }
+    if (tid < 16) sh.root[tid] = exp2(tid / 16.0);
+    if (tid == 0) {
+        sh.found = kThreads;
+        sh.digit = 0;
+    }
+    __syncthreads();
+    uint64_t best = 0;
+#pragma unroll 1
+    for (int s = 0; s < a.slices; ++s) best = max(best, sh.best[s]);
+    best = uniform(best);
+    int32_t* token = a.tokens + row;
+    float* logprob = a.logprob ? a.logprob + row : nullptr;
+    if (best == 0 || want.greedy) {
         if (tid == 0) {
             *token = best == 0 ? -1 : static_cast<int32_t>(0xFFFFFFFFu - static_cast<uint32_t>(best));
             if (logprob) *logprob = best == 0 ? -INFINITY : 0.f;
         }
         return;
     }
+    const Pieces<T> p(static_cast<const T*>(a.logits) + row * a.ld, a.vocab);
     Row r;
     r.M = value_of(static_cast<uint32_t>(best >> 32));
     r.at_inf = r.M == INFINITY;
-    if (r.at_inf) {
-        r.M = 0.f;
-        mine = r.fix(mine);
-    }
-    r.c16 = 16.0 * 1.4426950408889634074 / static_cast<double>(temperature);
-    r.root = (const __attribute__((address_space(3))) double*)sh.root;
+    if (r.at_inf) r.M = 0.f;
+    r.c16 = want.c16;
+    r.min_p = want.min_p;
     r.n = a.vocab;
-    r.min_p = min_p > 0.f ? fmin(static_cast<double>(min_p), 1.0) : 0.0;
-    const int k = top_k > 0 && top_k < a.vocab ? top_k : 0;
-    const double prob = top_p < 1.f ? fmax(static_cast<double>(top_p), 0.0) : 1.0;
-    const double u = u_in > 0.f ? fmin(static_cast<double>(u_in), 0x1.fffffffffffffp-1) : 0.0;
+    r.root = (const __attribute__((address_space(3))) double*)sh.root;
+    const int k = want.k;
+    const double prob = want.prob;
+    double z = 0.0, before = 0.0, target = 0.0;
+    int from = 0, to = p.count;
+    bool summed = false;
+    Cut cut{0, a.vocab};
+
+    if (want.free()) {
+        // the slices' sixteenths count from the slice's own largest
+        double mine = 0.0;
+        if (tid < a.slices * kWaves) {
+            const int s = tid / kWaves;
+            const float m = value_of(static_cast<uint32_t>(sh.best[s] >> 32));
+            mine = a.sums[(static_cast<size_t>(row) * a.slices) * kWaves + tid];
+            mine *= !sh.best[s] ? 0.0 : r.at_inf ? (m == INFINITY ? 1.0 : 0.0) : r.w(m);
+        }
+        const double upto = block_scan(mine, sh);
+        if (tid == kThreads - 1) sh.found_d = upto;
+        __syncthreads();
+        z = uniform(sh.found_d);
+        target = want.u * z;
+        if (mine > 0.0) {
+            if (upto > target) atomicMin(&sh.found, tid);
+            atomicMax(&sh.digit, tid);  // the last with any mass, where rounding leaves none
+        }
+        __syncthreads();
+        const int range = uniform(sh.found < kThreads ? sh.found : sh.digit), width = slice_pieces(p.count, a.slices) / kWaves;
+        if (tid == range) sh.above_d = upto - mine;
+        __syncthreads();
+        before = uniform(sh.above_d);
+        from = range * width;
+        to = min(from + width, p.count);
+        summed = true;
+    }
 
     // 0: top_k by the threads' largest; 1: top_k by bins, where that is no help; 2: top_p
-    Cut cut{0, a.vocab};
 #pragma unroll 1
     for (int way = 0; way < 3; ++way) {
-        if (way == 0 ? k == 0 || k > kThreads : way == 1 ? k == 0 : prob >= 1.0) continue;
-        uint32_t lo, hi = 0xFFFFFFFFu;
-        double z = 0.0;
-        Targets to{};
+        if (way == 0 ? !want.by_count() : way == 1 ? k == 0 : prob >= 1.0) continue;
+        uint32_t lo;
+        float hi = INFINITY;
+        double mass = 0.0;
+        Targets goal{};
         if (way == 0) {
-            // the k-th largest of the threads' largest, in its upper 16 bits: wave 0 counts them all
-            uint32_t* keys = reinterpret_cast<uint32_t*>(sh.list);
-            keys[tid] = key_of(mine);
-            __syncthreads();
-            if (tid < kWave) {
-                uint32_t mine16[kWaves];
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) mine16[w] = keys[w * kWave + tid] >> 16;
-                uint32_t least = 0, most = key_of(r.M) >> 16;
+            // a bound of the k-th largest of the threads' largest: counts by the distance of
+            // their keys' upper 16 bits from M's, in steps of 1, 16, 256, ...
+            const uint32_t top = key_of(r.M) >> 16;
+            uint32_t down = 0;
 #pragma unroll 1
-                while (least < most) {
-                    const uint32_t mid = most - (most - least) / 2;
-                    int count = 0;
+            for (int step = 0; step < 16; step += 4) {
+                __syncthreads();
+                if (tid < 512) sh.mass[tid] = 0;
+                __syncthreads();
 #pragma unroll
-                    for (int w = 0; w < kWaves; ++w) count += __popcll(__ballot(mine16[w] >= mid));
-                    if (count >= k) least = mid;
-                    else most = mid - 1;
+                for (int s = 0; s < kMost / kThreads; ++s) {
+                    uint32_t key = s < a.slices ? a.most[static_cast<size_t>(row) * kMost + s * kThreads + tid] : 0;
+                    if (r.at_inf) key = key_of(r.fix(value_of(key)));
+                    const uint32_t far = (top - (key >> 16)) >> step;
+                    if (far < 512) atomicAdd(reinterpret_cast<unsigned int*>(&sh.mass[far]), 1u);
                 }
-                if (tid == 0) sh.found = static_cast<int>(least);
+                __syncthreads();
+                if (tid < kWave) find_digit(0, k, eight(sh), sh);
+                __syncthreads();
+                down = ((static_cast<uint32_t>(sh.digit) + 1) << step) - 1;
+                if (sh.digit < 512) break;
             }
-            __syncthreads();
-            lo = static_cast<uint32_t>(sh.found) << 16;
-            if (lo <= 0x007FFFFFu) continue;  // -inf
-            to = Targets{static_cast<double>(k), prob < 1.0 ? fmax(prob, 0x1p-1000) : 0.0, true, true};
+            if (down >= top - (0x007FFFFFu >> 16)) continue;  // as far as -inf
+            lo = (top - down) << 16;
+            goal = Targets{static_cast<double>(k), prob < 1.0 ? fmax(prob, 0x1p-1000) : 0.0, true, true};
         } else {
             const bool by_mass = way == 2;
-            const Found f = find_bin(p, r, cut, by_mass, by_mass ? prob : k, sh);
+            // the slices' bins, where sixteenths from 0 on are as good as from M on
+            const bool slices = want.by_mass() && !r.at_inf && fabs(static_cast<double>(r.M)) * r.c16 <= 0x1p17;
+            const int ref = slices ? static_cast<int>(rint(static_cast<double>(r.M) * r.c16)) : 0;
+            const Found f = slices ? find_bin_of_slices(a, row, r, prob, ref, sh)
+                                   : find_bin(p, r, cut, by_mass, by_mass ? prob : k, sh);
             if (f.bin == kBins) continue;
-            z = f.z;
-            lo = bin_edge(r, f.bin);
+            mass = f.z;
+            auto bin_of = [&](float x) {  // a whole number; far down beyond any int
+                return slices ? ref - rint(static_cast<double>(x) * r.c16) : static_cast<double>(r.bin_of(x));
+            };
             // the tokens down to the bin where LDS holds them, else the bin's alone
             const bool all = by_mass && f.about < 0.97 * kList;
-            if (!all && f.bin > 0) hi = bin_edge(r, f.bin - 1);
-            if (by_mass) to = Targets{0.0, fmax(prob * z - (all ? 0.0 : f.above), 0x1p-1000), false, all};
-            else to = Targets{k - f.above, 0.0, false, false};
+            lo = 0;
+#pragma unroll 1
+            for (int i = 0; i < (all || f.bin == 0 ? 1 : 2); ++i) {
+                const uint32_t e = edge(r, [&](float x) { return bin_of(x) <= f.bin - i; });
+                if (i == 0) lo = e;
+                else hi = value_of(e);
+            }
+            if (by_mass) goal = Targets{0.0, fmax(prob * mass - (all ? 0.0 : f.above), 0x1p-1000), false, all};
+            else goal = Targets{k - f.above, 0.0, false, false};
         }
-        const int n = collect(p, r, lo, hi, cut, sh);
+        const int n = collect(p, r, value_of(lo), hi, cut, sh);
         if (n <= kList) {
-            const Cut c = cut_list(r, n, to, u, token, logprob, sh);
-            if (to.draw) return;
+            const Cut c = cut_list(r, n, lo, sizeof(T) == 2 ? 16 : 0, goal, want.u, token, logprob, sh);
+            if (goal.draw) return;
             cut = c;
-            if (way == 1) continue;
-            break;
+            if (way == 2) break;
+        } else if (way > 0) {
+            cut = bisect(p, r, cut, way == 2, way == 2 ? fmax(prob * mass, 0x1p-1000) : k, sh);
         }
-        if (way > 0) cut = bisect(p, r, cut, way == 2, way == 2 ? fmax(prob * z, 0x1p-1000) : k, sh);
     }
-    draw_from_row(p, r, cut, u, token, logprob, sh);
+
+    // The kept tokens' mass in sixteenths of the range, a wave each.  Under a cut most
+    // tokens are out: a wave queues those that are in, in any order, and weighs 64 at a time.
+    if (cut.key == 0 && r.min_p > 0.0) cut.key = edge(r, [&](float x) { return r.w(x) >= r.min_p; });
+    const float cut_x = cut.key == 0 ? -INFINITY : value_of(cut.key);
+    float* queue = sh.queue[wave];
+    auto load = [&](int v, float (&x)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = -INFINITY;
+        if (v < to) p.load(v, x);
+        if (r.at_inf)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = r.fix(x[e]);
+    };
+    auto kept = [&](float x, int i) { return x > cut_x || (x == cut_x && i <= cut.last); };
+    __syncthreads();
+#pragma unroll 1
+    while (!summed || to - from > kWave) {
+        const int per = ((to - from + kWaves - 1) / kWaves + kWave - 1) / kWave * kWave;
+        const int v1 = min(from + (wave + 1) * per, to);
+        double s = 0.0;
+        int n = 0;
+        float y[8];
+        load(from + wave * per + lane < v1 ? from + wave * per + lane : to, y);
+#pragma unroll 1
+        for (int v0 = from + wave * per; v0 < v1 || n > 0; v0 += kWave) {
+            if (v0 < v1) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = y[e];
+                load(v0 + kWave + lane < v1 ? v0 + kWave + lane : to, y);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool in = kept(x[e], 8 * (v0 + lane) - p.shift + e) && x[e] > -INFINITY;
+                    const uint64_t mask = __ballot(in);
+                    const int at = n + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32),
+                                                                 __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), 0));
+                    if (in) queue[at] = x[e];
+                    n += __popcll(mask);
+                }
+                wave_fence();
+            }
+            // 64 at a time, and the rest once there are no more pieces
+#pragma unroll 1
+            while (n >= kWave || (n > 0 && v0 + kWave >= v1)) {
+                const int m = min(n, kWave);
+                n -= m;
+                const double w = lane < m ? r.w(queue[n + lane]) : 0.0;
+                s += w >= r.min_p ? w : 0.0;
+            }
+            wave_fence();
+        }
+        s = wave_total(s);
+        __syncthreads();
+        if (lane == 0) sh.red_d[wave] = s;
+        __syncthreads();
+        if (!summed) {
+#pragma unroll 1
+            for (int i = 0; i < kWaves; ++i) z += sh.red_d[i];
+            target = want.u * z;
+            summed = true;
+        }
+        // the first in which the sum passes the target; the last with any mass, where rounding leaves none
+        int at = 0;
+        double run = before, at_before = before;
+#pragma unroll 1
+        for (int i = 0; i < kWaves; ++i) {
+            if (sh.red_d[i] <= 0.0) continue;
+            at = i;
+            at_before = run;
+            run += sh.red_d[i];
+            if (run > target) break;
+        }
+        before = at_before;
+        from += at * per;
+        to = min(from + per, to);
+    }
+    if (wave > 0) return;
+    // one wave: 64 pieces, whose lanes' eight weights go through LDS
+    {
+        float x[8];
+        load(from + lane, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) queue[8 * lane + e] = x[e];
+    }
+    wave_fence();
+    const int i0 = 8 * (from + lane) - p.shift;
+    auto weigh = [&](int e) {
+        const float x = queue[8 * lane + e];
+        const double w = kept(x, i0 + e) ? r.w(x) : 0.0;
+        return w >= r.min_p ? w : 0.0;
+    };
+    double sum = 0.0;
+#pragma unroll 1
+    for (int e = 0; e < 8; ++e) sum += weigh(e);
+    const double upto = before + wave_scan(sum);
+    const uint64_t here = __ballot(upto > target && sum > 0.0), some = __ballot(sum > 0.0);
+    const int l = here ? __ffsll(static_cast<unsigned long long>(here)) - 1 : 63 - __clzll(static_cast<long long>(some));
+    if (lane != l) return;
+    double run = upto - sum, wb = 0.0;
+    int chosen = -1;
+#pragma unroll 1
+    for (int e = 0; e < 8 && !(chosen >= 0 && run > target); ++e) {
+        const double w = weigh(e);
+        if (w <= 0.0) continue;
+        run += w;
+        chosen = i0 + e;
+        wb = w;
+    }
+    *token = chosen;
+    if (logprob) *logprob = static_cast<float>(log(wb / z));
+}
+
+// Slices of a row, a power of two: work-groups for two rounds of the chip, a piece a thread at least.
+int sample_slices(int rows, int vocab) {
+    int slices = 1;
+    while (slices < 16 && slices * static_cast<int64_t>(rows) < 1024 && slices * 8 * kThreads < vocab) slices *= 2;
+    return slices;
+}
+
+// Places of a call's workspace; the most slices of any call of up to `rows` rows.
+struct SampleLayout {
+    size_t best, ref, sums, bins, most, end;
+};
+SampleLayout sample_layout(size_t slices, size_t rows) {
+    SampleLayout l{};
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    l.best = take(slices * 8);
+    l.ref = take(slices * 4);
+    l.sums = take(slices * kWaves * 8);
+    l.bins = take(slices * kBins * 8);
+    l.most = take(rows * kMost * 4);
+    l.end = off;
+    return l;
+}
+
+template <class T>
+void launch_sample(const SampleArgs& a, hipStream_t s) {
+    const unsigned rows = static_cast<unsigned>(a.rows), slices = rows * static_cast<unsigned>(a.slices);
+    sample_slices_kernel<T><<<slices, kThreads, 0, s>>>(a);
+    sample_rows_kernel<T><<<rows, kThreads, 0, s>>>(a);
 }
 
 }  // namespace
@@ -762,7 +967,9 @@ extern "C" int slw_sample_workspace_size(int32_t max_rows, int32_t vocab, size_t
         if (max_rows < 0) return fail(SLW_EINVAL, "negative rows");
         if (vocab < 1 || vocab > SLW_SAMPLE_MAX_VOCAB)
             return fail(SLW_EUNSUPPORTED, "vocab must be in [1, %d] (got %d)", SLW_SAMPLE_MAX_VOCAB, vocab);
-        *bytes = 0;
+        // the slices of a call are fewer than twice 1024, or as many as its rows, and those of one row each at most
+        const size_t rows = static_cast<size_t>(max_rows);
+        *bytes = rows ? sample_layout(std::min(std::max<size_t>(rows, 2047), rows * sample_slices(1, vocab)), rows).end : 0;
         return SLW_OK;
     });
 }
@@ -782,10 +989,32 @@ extern "C" int slw_sample(const slw_sample_args* a, void* ws, size_t ws_bytes, v
         const void* words[] = {a->temperature, a->top_k, a->top_p, a->min_p, a->u, a->tokens, a->logprob};
         for (const void* p : words)
             if (reinterpret_cast<uintptr_t>(p) % 4) return fail(SLW_EINVAL, "parameters, tokens and logprob must be 4-byte aligned");
-        const SampleArgs g{a->logits, a->ld, a->temperature, a->top_k, a->top_p, a->min_p, a->u, a->tokens, a->logprob, a->vocab};
+        SampleArgs g{};
+        g.slices = sample_slices(a->rows, a->vocab);
+        const size_t slices = static_cast<size_t>(a->rows) * g.slices;
+        const SampleLayout l = sample_layout(slices, a->rows);
+        if (!ws || reinterpret_cast<uintptr_t>(ws) % 16) return fail(SLW_EINVAL, "the workspace must be 16-byte aligned device memory");
+        if (ws_bytes < l.end) return fail(SLW_ENOMEM, "the workspace holds %zu bytes, %d rows need %zu", ws_bytes, a->rows, l.end);
+        g.logits = a->logits;
+        g.ld = a->ld;
+        g.temperature = a->temperature;
+        g.top_k = a->top_k;
+        g.top_p = a->top_p;
+        g.min_p = a->min_p;
+        g.u = a->u;
+        g.tokens = a->tokens;
+        g.logprob = a->logprob;
+        g.vocab = a->vocab;
+        g.rows = a->rows;
+        char* w = static_cast<char*>(ws);
+        g.best = reinterpret_cast<uint64_t*>(w + l.best);
+        g.ref = reinterpret_cast<int32_t*>(w + l.ref);
+        g.sums = reinterpret_cast<double*>(w + l.sums);
+        g.bins = reinterpret_cast<uint64_t*>(w + l.bins);
+        g.most = reinterpret_cast<uint32_t*>(w + l.most);
         hipStream_t s = static_cast<hipStream_t>(stream);
-        if (a->logits_f32) sample_kernel<float><<<a->rows, kThreads, 0, s>>>(g);
-        else sample_kernel<bf16><<<a->rows, kThreads, 0, s>>>(g);
+        if (a->logits_f32) launch_sample<float>(g, s);
+        else launch_sample<bf16>(g, s);
         HIP_TRY(hipGetLastError());
         return SLW_OK;
     });
