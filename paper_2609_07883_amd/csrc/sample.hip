@@ -119,6 +119,7 @@ struct Shared {
         float queue[kWaves][kQueue];
     };
     uint64_t mass[kBins];
+    __attribute__((aligned(16))) float ends[16];
     double root[16];
     double red_d[kWaves];
     uint64_t best[16];  // of the slices
@@ -210,35 +211,79 @@ __device__ __forceinline__ double block_scan(double v, Shared& sh) {
 
 // The row in pieces of 8 tokens, aligned to 16 bytes as far as the row's start
 // allows: piece v holds tokens 8 v - shift .. + 7, those outside the row as -inf.
+// The first and the last piece, which may have such, wait in LDS.
+typedef const __attribute__((address_space(3))) f32x4* LdsVec;
 template <class T>
 struct Pieces {
     const T* row;
     int n, shift, count;
-    __device__ Pieces(const T* r, int n_) : row(r), n(n_) {
+    LdsVec ends;
+    // by every thread, before the work-group's next barrier
+    __device__ __forceinline__ Pieces(const T* r, int n_, float (&lds)[16]) : row(r), n(n_) {
         shift = static_cast<int>(reinterpret_cast<uintptr_t>(r) % 16 / sizeof(T));
         count = (n + shift + 7) / 8;
-    }
-    __device__ void load(int v, float (&x)[8]) const {
-        const int at = 8 * v - shift;
-        if (at >= 0 && at + 8 <= n) {
-            if (sizeof(T) == 2) {
-                const bf16x8 t = *reinterpret_cast<const bf16x8*>(row + at);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = static_cast<float>(t[e]);
-            } else {
-                const f32x4 a = *reinterpret_cast<const f32x4*>(row + at), b = *reinterpret_cast<const f32x4*>(row + at + 4);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = a[e];
-                    x[4 + e] = b[e];
-                }
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = at + e >= 0 && at + e < n ? static_cast<float>(row[at + e]) : -INFINITY;
+        ends = (LdsVec)lds;
+        if (threadIdx.x < 16) {
+            const int i = 8 * (threadIdx.x < 8 ? 0 : count - 1) - shift + static_cast<int>(threadIdx.x % 8);
+            lds[threadIdx.x] = i >= 0 && i < n ? static_cast<float>(row[i]) : -INFINITY;
         }
     }
+    struct Raw {
+        f32x4 w[sizeof(T) / 2];
+    };
+    // A piece inside the row (or the nearest such), for `spread`: nothing waits for it yet.
+    __device__ __forceinline__ Raw ask(int v) const {
+        Raw r;
+        const f32x4* at = reinterpret_cast<const f32x4*>(row + (8 * min(max(v, 1), count - 2) - shift));
+        if (count >= 3)
+#pragma unroll
+            for (size_t i = 0; i < sizeof(T) / 2; ++i) r.w[i] = at[i];
+        return r;
+    }
+    __device__ __forceinline__ void spread(const Raw& r, int v, float (&x)[8]) const {
+        if (v == 0 || v == count - 1) {
+            const f32x4 a = ends[v == 0 ? 0 : 2], b = ends[v == 0 ? 1 : 3];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[e] = a[e];
+                x[4 + e] = b[e];
+            }
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t w = __float_as_uint(r.w[sizeof(T) == 2 ? 0 : e / 4][sizeof(T) == 2 ? e / 2 : e % 4]);
+            x[e] = __uint_as_float(sizeof(T) == 4 ? w : e % 2 ? w & 0xFFFF0000u : w << 16);
+        }
+    }
+    __device__ __forceinline__ void load(int v, float (&x)[8]) const { spread(ask(v), v, x); }
 };
+
+// Pieces v, v + stride, ... below `end`, f(x, v).  N are asked for at a time, and
+// where that is one, it is asked for while f looks at the one before it.
+template <int N, class T, class F>
+__device__ __forceinline__ void each_piece(const Pieces<T>& p, int v, int end, int stride, F&& f) {
+    typename Pieces<T>::Raw raw[N];
+    if (N == 1) raw[0] = p.ask(v);
+#pragma unroll 1
+    for (; v < end; v += N * stride) {
+        float x[8];
+        if (N == 1) {
+            p.spread(raw[0], v, x);
+            raw[0] = p.ask(v + stride);
+            f(x, v);
+            continue;
+        }
+#pragma unroll
+        for (int q = 0; q < N; ++q) raw[q] = p.ask(v + q * stride);
+#pragma unroll
+        for (int q = 0; q < N; ++q)
+            if (v + q * stride < end) {
+                p.spread(raw[q], v + q * stride, x);
+                f(x, v + q * stride);
+            }
+    }
+}
 
 __device__ __forceinline__ float largest(const float (&x)[8]) {
     return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
@@ -301,31 +346,30 @@ __device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float l
     __syncthreads();
     if (threadIdx.x == 0) sh.n_list = 0;
     __syncthreads();
-    // a piece is loaded before the one ahead of it is looked at
-    float x[8], y[8];
-    if (static_cast<int>(threadIdx.x) < p.count) p.load(threadIdx.x, y);
-#pragma unroll 1
-    for (int v = threadIdx.x; v < p.count; v += kThreads) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = y[e];
-        if (v + kThreads < p.count) p.load(v + kThreads, y);
-        if (r.at_inf)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = r.fix(x[e]);
+    each_piece<1>(p, threadIdx.x, p.count, kThreads, [&](const float (&x)[8], int v) {
         uint32_t keeps = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) keeps |= x[e] >= lo && x[e] < hi ? 1u << e : 0u;
-#pragma unroll 1
-        for (; keeps; keeps &= keeps - 1) {
-            const int i = 8 * v - p.shift + __ffs(keeps) - 1;
-            float one = static_cast<float>(p.row[i]);
-            if (r.at_inf) one = r.fix(one);
-            const uint32_t k = key_of(one);
-            if (!in.keeps(k, i)) continue;
-            const int at = atomicAdd(&sh.n_list, 1);
-            if (at < kList) sh.list[at] = static_cast<uint64_t>(k) << 32 | static_cast<uint32_t>(i);
+        for (int e = 0; e < 8; ++e) {
+            const float y = r.at_inf ? r.fix(x[e]) : x[e];
+            keeps |= y >= lo && y < hi ? 1u << e : 0u;
         }
-    }
+        if (in.key != 0) {  // few rows come with a cut
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (!in.keeps(key_of(r.at_inf ? r.fix(x[e]) : x[e]), 8 * v - p.shift + e)) keeps &= ~(1u << e);
+        }
+        if (!keeps) return;
+        int at = atomicAdd(&sh.n_list, __popc(keeps));
+#pragma unroll 1
+        for (; keeps; keeps &= keeps - 1, ++at) {
+            const int e = __ffs(keeps) - 1;
+            float y = x[0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) y = e == j ? x[j] : y;
+            if (at < kList)
+                sh.list[at] = static_cast<uint64_t>(key_of(r.at_inf ? r.fix(y) : y)) << 32 | static_cast<uint32_t>(8 * v - p.shift + e);
+        }
+    });
     __syncthreads();
     const int n = sh.n_list;
     __syncthreads();
@@ -537,30 +581,29 @@ __device__ __forceinline__ int slice_pieces(int count, int slices) {
 template <class T>
 __global__ __launch_bounds__(kThreads, 8) void sample_slices_kernel(SampleArgs a) {
     __shared__ double root[16];
+    __shared__ __attribute__((aligned(16))) float ends[16];
     __shared__ uint64_t bins[kBins];
     __shared__ uint64_t red_u[kWaves];
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     const size_t slice = blockIdx.x;
     const int row = static_cast<int>(slice / a.slices);
     const Wants want(a, row);
-    const Pieces<T> p(static_cast<const T*>(a.logits) + row * a.ld, a.vocab);
+    const Pieces<T> p(static_cast<const T*>(a.logits) + row * a.ld, a.vocab, ends);
     const int per = slice_pieces(p.count, a.slices), from = static_cast<int>(slice % a.slices) * per, to = min(from + per, p.count);
     if (tid < 16) root[tid] = exp2(tid / 16.0);
     for (int b = tid; b < kBins; b += kThreads) bins[b] = 0;
+    __syncthreads();
 
     // the thread's largest logit and the first piece that has it (NaN is below everything)
     float mine = -INFINITY;
     int at = -1;
-#pragma unroll 4
-    for (int v = from + tid; v < to; v += kThreads) {
-        float x[8];
-        p.load(v, x);
+    each_piece<4>(p, from + tid, to, kThreads, [&](const float (&x)[8], int v) {
         const float m = largest(x);
         if (m > mine) {
             mine = m;
             at = v;
         }
-    }
+    });
     uint64_t best = 0;
     if (at >= 0) {
         float x[8];
@@ -671,12 +714,18 @@ template <class T>
 __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
     __shared__ Shared sh;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    // what only some rows need is asked for before it is known which: all of it is a microsecond away
+    const size_t slice0 = static_cast<size_t>(row) * a.slices;
+    double range_sum = tid < a.slices * kWaves ? a.sums[slice0 * kWaves + tid] : 0.0;
+    uint32_t most[kMost / kThreads];
+#pragma unroll
+    for (int s = 0; s < kMost / kThreads; ++s) most[s] = s < a.slices ? a.most[static_cast<size_t>(row) * kMost + s * kThreads + tid] : 0;
     const Wants want(a, row);
     if (tid < a.slices) {
-        const size_t s = static_cast<size_t>(row) * a.slices + tid;
-        sh.best[tid] = a.best[s];
-        sh.ref[tid] = a.ref[s];
+        sh.best[tid] = a.best[slice0 + tid];
+        sh.ref[tid] = a.ref[slice0 + tid];
     }
+    const Pieces<T> p(static_cast<const T*>(a.logits) + row * a.ld, a.vocab, sh.ends);
     if (tid < 16) sh.root[tid] = exp2(tid / 16.0);
     if (tid == 0) {
         sh.found = kThreads;
@@ -696,7 +745,6 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
         }
         return;
     }
-    const Pieces<T> p(static_cast<const T*>(a.logits) + row * a.ld, a.vocab);
     Row r;
     r.M = value_of(static_cast<uint32_t>(best >> 32));
     r.at_inf = r.M == INFINITY;
@@ -714,11 +762,10 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
 
     if (want.free()) {
         // the slices' sixteenths count from the slice's own largest
-        double mine = 0.0;
+        double mine = range_sum;
         if (tid < a.slices * kWaves) {
             const int s = tid / kWaves;
             const float m = value_of(static_cast<uint32_t>(sh.best[s] >> 32));
-            mine = a.sums[(static_cast<size_t>(row) * a.slices) * kWaves + tid];
             mine *= !sh.best[s] ? 0.0 : r.at_inf ? (m == INFINITY ? 1.0 : 0.0) : r.w(m);
         }
         const double upto = block_scan(mine, sh);
@@ -740,10 +787,18 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
         summed = true;
     }
 
-    // 0: top_k by the threads' largest; 1: top_k by bins, where that is no help; 2: top_p
+    // the slices' bins count, where sixteenths from 0 on are as good as from M on
+    const bool slices = want.by_mass() && !r.at_inf && fabs(static_cast<double>(r.M)) * r.c16 <= 0x1p17;
+    const int ref = slices ? static_cast<int>(rint(static_cast<double>(r.M) * r.c16)) : 0;
+    auto bin_of = [&](float x) {  // a whole number; far down beyond any int
+        return slices ? ref - rint(static_cast<double>(x) * r.c16) : static_cast<double>(r.bin_of(x));
+    };
+    int bin = -1, listed = 0;  // the bin of the cut, whose kept tokens are among those in LDS
+
+    // 0: top_k by the threads' largest; 1: top_k by bins, where that is no help; 2: top_p; 3: min_p alone
 #pragma unroll 1
-    for (int way = 0; way < 3; ++way) {
-        if (way == 0 ? !want.by_count() : way == 1 ? k == 0 : prob >= 1.0) continue;
+    for (int way = 0; way < 4; ++way) {
+        if (way == 0 ? !want.by_count() : way == 1 ? k == 0 : way == 2 ? prob >= 1.0 : r.min_p == 0.0) continue;
         uint32_t lo;
         float hi = INFINITY;
         double mass = 0.0;
@@ -760,7 +815,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
                 __syncthreads();
 #pragma unroll
                 for (int s = 0; s < kMost / kThreads; ++s) {
-                    uint32_t key = s < a.slices ? a.most[static_cast<size_t>(row) * kMost + s * kThreads + tid] : 0;
+                    uint32_t key = most[s];
                     if (r.at_inf) key = key_of(r.fix(value_of(key)));
                     const uint32_t far = (top - (key >> 16)) >> step;
                     if (far < 512) atomicAdd(reinterpret_cast<unsigned int*>(&sh.mass[far]), 1u);
@@ -775,53 +830,88 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
             lo = (top - down) << 16;
             goal = Targets{static_cast<double>(k), prob < 1.0 ? fmax(prob, 0x1p-1000) : 0.0, true, true};
         } else {
-            const bool by_mass = way == 2;
-            // the slices' bins, where sixteenths from 0 on are as good as from M on
-            const bool slices = want.by_mass() && !r.at_inf && fabs(static_cast<double>(r.M)) * r.c16 <= 0x1p17;
-            const int ref = slices ? static_cast<int>(rint(static_cast<double>(r.M) * r.c16)) : 0;
-            const Found f = slices ? find_bin_of_slices(a, row, r, prob, ref, sh)
-                                   : find_bin(p, r, cut, by_mass, by_mass ? prob : k, sh);
-            if (f.bin == kBins) continue;
-            mass = f.z;
-            auto bin_of = [&](float x) {  // a whole number; far down beyond any int
-                return slices ? ref - rint(static_cast<double>(x) * r.c16) : static_cast<double>(r.bin_of(x));
-            };
-            // the tokens down to the bin where LDS holds them, else the bin's alone
-            const bool all = by_mass && f.about < 0.97 * kList;
+            const bool by_mass = way == 2, low = way == 3;
+            if (!low) {
+                const Found f = by_mass && slices ? find_bin_of_slices(a, row, r, prob, ref, sh)
+                                                  : find_bin(p, r, cut, by_mass, by_mass ? prob : k, sh);
+                if (f.bin == kBins) continue;
+                bin = f.bin;
+                mass = f.z;
+                // the tokens down to the bin where LDS holds them, else the bin's alone
+                const bool all = by_mass && f.about < 0.97 * kList;
+                if (by_mass) goal = Targets{0.0, fmax(prob * mass - (all ? 0.0 : f.above), 0x1p-1000), false, all};
+                else goal = Targets{k - f.above, 0.0, false, false};
+            } else {
+                goal.draw = true;
+            }
+            // the edges of the tokens to collect
             lo = 0;
 #pragma unroll 1
-            for (int i = 0; i < (all || f.bin == 0 ? 1 : 2); ++i) {
-                const uint32_t e = edge(r, [&](float x) { return bin_of(x) <= f.bin - i; });
+            for (int i = 0; i < (goal.draw || bin == 0 ? 1 : 2); ++i) {
+                const uint32_t e = edge(r, [&](float x) { return low ? r.w(x) >= r.min_p : bin_of(x) <= bin - i; });
                 if (i == 0) lo = e;
                 else hi = value_of(e);
             }
-            if (by_mass) goal = Targets{0.0, fmax(prob * mass - (all ? 0.0 : f.above), 0x1p-1000), false, all};
-            else goal = Targets{k - f.above, 0.0, false, false};
+            if (low && lo <= cut.key) continue;  // the cut is above it
         }
         const int n = collect(p, r, value_of(lo), hi, cut, sh);
+        listed = n <= kList ? n : -1;
         if (n <= kList) {
             const Cut c = cut_list(r, n, lo, sizeof(T) == 2 ? 16 : 0, goal, want.u, token, logprob, sh);
             if (goal.draw) return;
             cut = c;
-            if (way == 2) break;
+        } else if (way == 3) {
+            cut = Cut{lo, a.vocab};
         } else if (way > 0) {
             cut = bisect(p, r, cut, way == 2, way == 2 ? fmax(prob * mass, 0x1p-1000) : k, sh);
         }
     }
 
+    if (slices && !summed && listed >= 0) {
+        // A slice's kept mass: its bins above the cut's, and the kept tokens of that bin.  A wave a slice.
+        double s = 0.0;
+        if (wave < a.slices && sh.best[wave]) {
+            const int down = ref - sh.ref[wave], width = slice_pieces(p.count, a.slices);
+            int n;
+#pragma unroll 4
+            for (int b = down + lane; b < min(bin, down + kBins - 1); b += kWave)
+                s += static_cast<double>(a.bins[(slice0 + wave) * kBins + b - down]) * 0x1p-42 *
+                     r.weight_from(ref - b - static_cast<double>(r.M) * r.c16, 0, n);
+#pragma unroll 1
+            for (int i = lane; i < listed; i += kWave) {
+                const uint64_t t = sh.list[i];
+                const int idx = static_cast<int>(static_cast<uint32_t>(t));
+                if ((idx + p.shift) / 8 / width == wave && cut.keeps(static_cast<uint32_t>(t >> 32), idx))
+                    s += r.w(value_of(static_cast<uint32_t>(t >> 32)));
+            }
+        }
+        s = wave_total(s);
+        __syncthreads();
+        if (lane == 0) sh.red_d[wave] = s;
+        __syncthreads();
+        int at = 0;
+        double run = 0.0;
+#pragma unroll 1
+        for (int i = 0; i < kWaves; ++i) z += sh.red_d[i];
+        z = uniform(z);
+        target = want.u * z;
+#pragma unroll 1
+        for (int i = 0; i < kWaves; ++i) {
+            if (sh.red_d[i] <= 0.0) continue;
+            at = i;
+            before = run;
+            run += sh.red_d[i];
+            if (run > target) break;
+        }
+        from = at * slice_pieces(p.count, a.slices);
+        to = min(from + slice_pieces(p.count, a.slices), p.count);
+        summed = true;
+    }
+
     // The kept tokens' mass in sixteenths of the range, a wave each.  Under a cut most
     // tokens are out: a wave queues those that are in, in any order, and weighs 64 at a time.
-    if (cut.key == 0 && r.min_p > 0.0) cut.key = edge(r, [&](float x) { return r.w(x) >= r.min_p; });
     const float cut_x = cut.key == 0 ? -INFINITY : value_of(cut.key);
     float* queue = sh.queue[wave];
-    auto load = [&](int v, float (&x)[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = -INFINITY;
-        if (v < to) p.load(v, x);
-        if (r.at_inf)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = r.fix(x[e]);
-    };
     auto kept = [&](float x, int i) { return x > cut_x || (x == cut_x && i <= cut.last); };
     __syncthreads();
 #pragma unroll 1
@@ -830,36 +920,33 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
         const int v1 = min(from + (wave + 1) * per, to);
         double s = 0.0;
         int n = 0;
-        float y[8];
-        load(from + wave * per + lane < v1 ? from + wave * per + lane : to, y);
+        auto weigh = [&](int least) {  // 64 at a time, while there are that many
 #pragma unroll 1
-        for (int v0 = from + wave * per; v0 < v1 || n > 0; v0 += kWave) {
-            if (v0 < v1) {
-                float x[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = y[e];
-                load(v0 + kWave + lane < v1 ? v0 + kWave + lane : to, y);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool in = kept(x[e], 8 * (v0 + lane) - p.shift + e) && x[e] > -INFINITY;
-                    const uint64_t mask = __ballot(in);
-                    const int at = n + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32),
-                                                                 __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), 0));
-                    if (in) queue[at] = x[e];
-                    n += __popcll(mask);
-                }
-                wave_fence();
-            }
-            // 64 at a time, and the rest once there are no more pieces
-#pragma unroll 1
-            while (n >= kWave || (n > 0 && v0 + kWave >= v1)) {
+            while (n >= least) {
                 const int m = min(n, kWave);
                 n -= m;
                 const double w = lane < m ? r.w(queue[n + lane]) : 0.0;
                 s += w >= r.min_p ? w : 0.0;
             }
             wave_fence();
-        }
+        };
+        // whole waves: pieces past the range count as -inf
+        each_piece<1>(p, from + wave * per + lane, (v1 - (from + wave * per) + kWave - 1) / kWave * kWave + from + wave * per, kWave,
+                   [&](const float (&x)[8], int v) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float y = r.at_inf ? r.fix(x[e]) : x[e];
+                const bool in = v < v1 && kept(y, 8 * v - p.shift + e) && y > -INFINITY;
+                const uint64_t mask = __ballot(in);
+                const int at = n + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32),
+                                                             __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), 0));
+                if (in) queue[at] = y;
+                n += __popcll(mask);
+            }
+            wave_fence();
+            weigh(kWave);
+        });
+        weigh(1);
         s = wave_total(s);
         __syncthreads();
         if (lane == 0) sh.red_d[wave] = s;
@@ -889,9 +976,9 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
     // one wave: 64 pieces, whose lanes' eight weights go through LDS
     {
         float x[8];
-        load(from + lane, x);
+        p.load(from + lane, x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) queue[8 * lane + e] = x[e];
+        for (int e = 0; e < 8; ++e) queue[8 * lane + e] = from + lane >= to ? -INFINITY : r.at_inf ? r.fix(x[e]) : x[e];
     }
     wave_fence();
     const int i0 = 8 * (from + lane) - p.shift;
