@@ -18,6 +18,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device.h"
 #include "hip_try.h"
@@ -259,28 +260,28 @@ __global__ __launch_bounds__(128 * WN, 2) void w4_tile_kernel(W4Args g, int nt_m
         off[x] = static_cast<uint32_t>(min(row, g.m - 1 - m0)) * static_cast<uint32_t>(g.lda * 2) + (((lane & 15) ^ (row & 15)) << 4);
     }
     auto load_row = [&](int x, int t) {
-        uint32_t o = off[x];
-        if (tail && t == g.steps - 1) {
-            const int row = (x * NW + wave) * 4 + (lane >> 4), c = (lane & 15) ^ (row & 15);
-            if (c >= tail) o -= c << 4;
-        }
-        load_lds16(base + static_cast<size_t>(t) * 256, o, lds0 + (t - t0 & 1) * BUF + (x * NW + wave) * 1024);
+        const int row = (x * NW + wave) * 4 + (lane >> 4), c = (lane & 15) ^ (row & 15);
+        const bool past = tail && t == g.steps - 1 && c >= tail;
+        load_lds16(base + static_cast<size_t>(t) * 256, off[x] - (past ? c << 4 : 0), lds0 + (t - t0 & 1) * BUF + (x * NW + wave) * 1024);
     };
-    const u32x4* codes[4];
-    const uint32_t* scales[4];
+    // wave-uniform bases, so that a load takes one lane offset for all tiles
+    const char* codes[4];
+    const char* scales[4];
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
         const size_t tile = min(tile0 + b, g.tiles - 1);
-        codes[b] = g.codes + tile * g.steps * 64 + lane;
-        scales[b] = g.scales + tile * g.words * 64 + col * 4;
+        codes[b] = reinterpret_cast<const char*>(g.codes) + tile * g.steps * 1024;
+        scales[b] = reinterpret_cast<const char*>(g.scales) + tile * g.words * 256;
     }
+    const uint32_t code_off = lane * 16, scale_off = col * 16;
     u32x4 next[4];
     uint32_t sc[4], sc_next[4];
     auto load_weights = [&](int t) {
+        const size_t at = static_cast<size_t>(t) * 1024, word = static_cast<size_t>(t / 4) * 256 + t % 4 * 4;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) next[b] = codes[b][static_cast<size_t>(t) * 64];
+        for (int b = 0; b < 4; ++b) next[b] = *reinterpret_cast<const u32x4*>(codes[b] + at + code_off);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) sc_next[b] = scales[b][t / 4 * 64 + t % 4];
+        for (int b = 0; b < 4; ++b) sc_next[b] = *reinterpret_cast<const uint32_t*>(scales[b] + word + scale_off);
     };
     const char* frag[4];
 #pragma unroll
@@ -327,35 +328,40 @@ __global__ __launch_bounds__(128 * WN, 2) void w4_tile_kernel(W4Args g, int nt_m
     barrier_only();
     read(0, 0);
     take_weights();
-    for (int t = t0; t < t1; ++t) {
-        const int at = (t - t0 & 1) * BUF;
+    // MORE: another step follows, so this one has all four groups.  Within such a step
+    // nothing branches: across a branch the compiler waits for every read.
+    auto step = [&](auto more_c, int t) {
+        constexpr bool MORE = decltype(more_c)::value;
         const int groups = tail && t == g.steps - 1 ? tail / 4 : 4;
-        const bool more = t + 1 < t1;
-        if (more) load_weights(t + 1);
+        const int at = (t - t0 & 1) * BUF;
+        if (MORE) load_weights(t + 1);
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
             const int j = u / PER, h = u % PER;
             if (u + 1 < UNITS) {
                 read(u + 1, at);
-            } else {
+            } else if (MORE) {
                 wait_lgkmcnt<0>();
                 wait_vmcnt<0>();
                 barrier_only();
-                if (more) read(0, BUF - at);
+                read(0, BUF - at);
             }
-            if (more)
+            if (MORE)
 #pragma unroll
                 for (int q = u * EACH; q < (u + 1) * EACH && q < LOADS; ++q) load_row(q, t + 1);
             if (h == PER - 1 && j < 3) widen_group(j + 1);
-            if (u + 1 == UNITS && more) take_weights();
-            if (j < groups)
+            if (u + 1 == UNITS && MORE) take_weights();
+            if (MORE || j < groups)
 #pragma unroll
                 for (int i = 0; i < (h ? H1 : H0); ++i)
 #pragma unroll
                     for (int b = 0; b < 4; ++b) acc[h * H0 + i][b] = mfma16(w[j & 1][b], x[u & 1][i], acc[h * H0 + i][b]);
             __builtin_amdgcn_sched_barrier(0);
         }
-    }
+    };
+#pragma unroll 1
+    for (int t = t0; t + 1 < t1; ++t) step(std::integral_constant<bool, true>{}, t);
+    step(std::integral_constant<bool, false>{}, t1 - 1);
     const int row0 = m0 + wm * 16 * HA + col;
 #pragma unroll
     for (int i = 0; i < HA; ++i) {
@@ -450,8 +456,8 @@ W4Plan plan_w4(const W4Shape& s, int m, bool gated) {
         return p;
     }
     // Rounds of the work-groups that run together (eight waves a CU) times their steps.  us a step, fitted at 512 .. 2080 rows of the 8B
-    // layer's products: 0.75 + 0.29 HA with WN 4 (3.09 at HA 8, 1.91 at 4), 0.40 +
-    // 0.33 HA with WN 2 (1.71 at HA 4), never below 1.05, the wait for a step;
+    // layer's products: 0.45 + 0.305 HA (2.89 at HA 8, 2.28 at 6, 1.64 at 4; WN 2
+    // 1.64 at HA 4, 1.35 at 3), never below 1.05, the wait for a step;
     // work-groups alone on their CU take 0.65 of that.  A split's sums are written
     // and read at 6 TB/s, by one launch more.
     p.kind = 1;
@@ -462,7 +468,7 @@ W4Plan plan_w4(const W4Shape& s, int m, bool gated) {
             const int64_t tiles = ceil_div(m, 32 * ha) * ceil_div(s.tiles, 4 * wn), slots = 256 * 4 / wn;
             for (int sp = 1; sp == 1 || (sp <= 8 && sp * 4 <= s.steps && m <= kMostSplitRows); sp *= 2) {
                 const int64_t per = ceil_div(s.steps, sp), groups = tiles * sp;
-                double step = std::max(1.05, wn == 4 ? 0.75 + 0.29 * ha : wn == 2 ? 0.40 + 0.33 * ha : 0.45 + 0.35 * ha);
+                double step = std::max(1.05, 0.45 + 0.305 * ha);
                 if (wn < 4 && groups <= 256) step *= 0.65;
                 const double t = ceil_div(groups, slots) * (per * step + 1.5) +
                                  (sp > 1 ? 2.0 + sp * static_cast<double>(m) * s.tiles * 16 * 4 * 2 / 6e6 : 0.0);
