@@ -27,7 +27,7 @@
 namespace slw {
 namespace {
 
-constexpr int64_t kMostTileStride = 1 << 22;  // the tile kernel's row offsets are 32 bits
+constexpr int64_t kMostTileStride = 1 << 22;  // the tile and ring kernels' row offsets are 32 bits
 constexpr int kMostSplitRows = 4096;  // k is split for fewer rows only
 constexpr int kStep = 128;   // k of a step: a lane's 16 bytes of four groups
 
@@ -371,6 +371,108 @@ __global__ __launch_bounds__(128 * WN, 2) void w4_tile_kernel(W4Args g, int nt_m
     }
 }
 
+// Direct global->LDS load of 4 bytes per lane, as load_lds16.
+__device__ __forceinline__ void load_lds4(const void* base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory");
+}
+
+// Ring kernel, for some rows: four waves with two tiles each share 16 MT rows.
+// Codes, scale words and rows all come through LDS, a ring of DEPTH steps filled by
+// direct loads, so that two work-groups' 140 KB a CU are under way at no cost in
+// registers; the rows are read from the caches once for 128 columns, where the
+// stream kernel's waves, each with 64 columns, spend most of their loads on rows.
+// (Four tiles a wave halve that again but leave half the work-groups: slower.)
+template <int MT, int DEPTH>
+__global__ __launch_bounds__(256, 2) void w4_ring_kernel(W4Args g, int steps_per_split) {
+    constexpr int NB = 2, WAVE = NB * 1024 + 256, ROWS = MT * 4096, STAGE = 4 * WAVE + ROWS, EACH = NB + 1 + MT;
+    static_assert((DEPTH - 2) * EACH < 64, "vmcnt range");
+    __shared__ __attribute__((aligned(1024))) char smem[DEPTH * STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    const int col = lane & 15, grp = lane >> 4;
+    const int tile0 = (blockIdx.x * 4 + wave) * NB;
+    const int t0 = blockIdx.z * steps_per_split, t1 = min(t0 + steps_per_split, g.steps);
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&smem[0])));
+
+    const char* codes[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+        codes[b] = reinterpret_cast<const char*>(g.codes) + static_cast<size_t>(min(tile0 + b, g.tiles - 1)) * g.steps * 1024;
+    // scale words: lane l brings those of tile l / 16, row l % 16
+    const size_t first = min(tile0, g.tiles - 1);
+    const char* scales = reinterpret_cast<const char*>(g.scales) + first * g.words * 256;
+    const uint32_t scale_off = static_cast<uint32_t>(min(tile0 + min(grp, NB - 1), g.tiles - 1) - first) * g.words * 256 + col * 16;
+    // rows as in the tile kernel
+    const char* base = reinterpret_cast<const char*>(g.a);
+    const int tail = g.k % kStep / 8;
+    uint32_t off[MT];
+#pragma unroll
+    for (int x = 0; x < MT; ++x) {
+        const int row = (x * 4 + wave) * 4 + grp;
+        off[x] = static_cast<uint32_t>(min(row, g.m - 1)) * static_cast<uint32_t>(g.lda * 2) + ((col ^ (row & 15)) << 4);
+    }
+    auto ask = [&](int t) {
+        const uint32_t stage = lds0 + (t - t0) % DEPTH * STAGE, mine = stage + wave * WAVE;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) load_lds16(codes[b] + static_cast<size_t>(t) * 1024, lane * 16, mine + b * 1024);
+        load_lds4(scales + static_cast<size_t>(t / 4) * 256 + t % 4 * 4, scale_off, mine + NB * 1024);
+#pragma unroll
+        for (int x = 0; x < MT; ++x) {
+            const int c = col ^ (((x * 4 + wave) * 4 + grp) & 15);
+            const bool past = tail && t == g.steps - 1 && c >= tail;
+            load_lds16(base + static_cast<size_t>(t) * 256, off[x] - (past ? c << 4 : 0), stage + 4 * WAVE + (x * 4 + wave) * 1024);
+        }
+    };
+    uint32_t frag[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) frag[j] = 4 * WAVE + col * 256 + (((4 * j + grp) ^ col) << 4);
+    f32x4 acc[MT][NB];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+#pragma unroll
+    for (int d = 0; d < DEPTH - 1; ++d)
+        if (t0 + d < t1) ask(t0 + d);
+#pragma unroll 1
+    for (int t = t0; t < t1; ++t) {
+        // this step's loads have landed, everyone's rows too; the step before it is read out of the ring
+        if (t + DEPTH - 1 <= t1) wait_vmcnt<(DEPTH - 2) * EACH>();
+        else wait_vmcnt<0>();
+        barrier_only();
+        if (t + DEPTH - 1 < t1) ask(t + DEPTH - 1);
+        const char* stage = smem + (t - t0) % DEPTH * STAGE;
+        const char* mine = stage + wave * WAVE;
+        u32x4 c[NB];
+        uint32_t s[NB];
+        bf16x8 x[4][MT];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            c[b] = *reinterpret_cast<const u32x4*>(mine + b * 1024 + lane * 16);
+            s[b] = *reinterpret_cast<const uint32_t*>(mine + NB * 1024 + (b * 16 + col) * 4);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) x[j][i] = *reinterpret_cast<const bf16x8*>(stage + frag[j] + i * 4096);
+        const int groups = tail && t == g.steps - 1 ? tail / 4 : 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j >= groups) break;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const bf16x8 w = widen(c[b][j], group_scale(s[b], j));
+#pragma unroll
+                for (int i = 0; i < MT; ++i) acc[i][b] = mfma16(w, x[j][i], acc[i][b]);
+            }
+        }
+        wait_lgkmcnt<0>();
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+        if (16 * i + col < g.m) store_sums<NB>(g, 16 * i + col, tile0, grp, acc[i]);
+}
+
 // Adds a split product's sums, four columns (or pairs) of a row a thread, and stores them.
 __global__ __launch_bounds__(256) void w4_join_kernel(W4Args g) {
     const int per = g.gated ? 2 : 1, quads = g.tiles / per * 4;
@@ -437,34 +539,50 @@ constexpr int kStreamWaves = 8;
 
 // Which kernel a product runs on.
 struct W4Plan {
-    int kind;    // 0: stream, 1: tile
-    int mt, nt;  // stream: row and column tiles of a work-group; tile: HA, WN
+    int kind;    // 0: stream, 1: tile, 2: ring
+    int mt, nt;  // stream: row and column tiles of a work-group; tile: HA, WN; ring: row tiles
     int waves;   // stream
     int splits;
 };
 
 W4Plan plan_w4(const W4Shape& s, int m, bool gated) {
     W4Plan p{};
-    if (m <= 32) {
-        p.mt = m <= 16 ? 1 : 2;
-        p.nt = m > 16 || s.tiles >= 1024 ? 4 : gated || s.tiles >= 384 ? 2 : 1;
-        // one work-group a CU at least, by splitting k
-        const int64_t groups = ceil_div(s.tiles, p.nt);
-        p.splits = 1;
-        while (m > 16 && groups * p.splits < 256 && p.splits * 2 * 8 <= s.steps) p.splits *= 2;
-        p.waves = std::min(p.nt == 4 && p.splits == 1 ? 4 : 8, s.words);
+    p.splits = 1;
+    // Some rows: the ring, where its 128 columns a work-group, with k split in parts of
+    // eight steps at least, make some 200 of them.  us with the ring / the stream kernel:
+    // 32 rows of 14336 -> 4096 16.0 / 18.5, of 4096 -> 28672 21.7 / 25.1, 23 of 4096 -> 100003
+    // 55.5 / 69.2, 16 of them 51.3 / 55.8; but 32 of 4096 -> 4096 11.2 / 10.1 and 16 of 4096 ->
+    // 28672 18.2 / 17.8.  64 rows against the tile kernel: 27.5 / 31.1, 19.6 / 22.8, 13.7 / 14.1.
+    if (m <= 64 && (m > 32 || (m > 16 && (s.tiles >= 512 || s.steps >= 64)) || (m > 8 && s.tiles >= 4096))) {
+        p.kind = 2;
+        p.mt = m <= 16 ? 1 : m <= 32 ? 2 : 4;
+        while (ceil_div(s.tiles, 8) * p.splits * 2 <= 256 && p.splits * 2 * 8 <= s.steps) p.splits *= 2;
+        p.splits = static_cast<int>(ceil_div(s.steps, ceil_div(s.steps, p.splits)));
         return p;
     }
-    // Rounds of the work-groups that run together (eight waves a CU) times their steps.  us a step, fitted at 512 .. 2080 rows of the 8B
-    // layer's products: 0.45 + 0.305 HA (2.89 at HA 8, 2.28 at 6, 1.64 at 4; WN 2
-    // 1.64 at HA 4, 1.35 at 3), never below 1.05, the wait for a step;
-    // work-groups alone on their CU take 0.65 of that.  A split's sums are written
-    // and read at 6 TB/s, by one launch more.
+    if (m <= 32) {
+        p.mt = m <= 16 ? 1 : 2;
+        // Waves of 64 columns read the rows least, narrow ones give more work-groups: 4096 ->
+        // 28672 15.4 / 16.8 (32 columns), 4096 -> 6144 at 1 row 7.6 (64) / 5.9 (32) / 6.3 (16), 4096 ->
+        // 4096 7.5 / 5.5 / 5.1.  Beyond 8 rows of a long k the rows cost most, and k is
+        // split for the wide waves instead: 16 rows of 14336 -> 4096 14.3 / 19.0, 8 13.3 / 13.4.
+        const bool wide = m > 16 || (m > 8 && s.steps >= 64);
+        p.nt = wide || s.tiles >= 1024 ? 4 : gated || s.tiles >= 384 ? 2 : 1;
+        while (wide && ceil_div(s.tiles, p.nt) * p.splits < 256 && p.splits * 2 * 8 <= s.steps) p.splits *= 2;
+        p.waves = std::min(p.nt == 4 && p.splits == 1 ? 4 : kStreamWaves, s.words);
+        return p;
+    }
+    // More rows: rounds of the work-groups that run together (eight waves a CU) times
+    // their steps.  us a step, fitted at 512 .. 2080 rows of products of 4096 and 14336:
+    // 0.45 + 0.305 HA (2.89 at HA 8, 2.28 at 6, 1.64 at 4; WN 2 1.64 at HA 4, 1.35 at 3),
+    // never below 1.05, the wait for a step; work-groups alone on their CU take
+    // 0.65 of that.  A split's sums are written and read at 6 TB/s, by one launch
+    // more.  (WN 1 as well would win up to 0.05 of the time, on few shapes.)
     p.kind = 1;
     double best = 0;
-    for (int wn = 4; wn >= 1; wn /= 2)
-        for (int ha = 1; ha <= (wn == 4 ? 8 : wn == 2 ? 4 : 2); ++ha) {
-            if (ha == 7 || 4 * ha % wn) continue;
+    for (int wn = 4; wn >= 2; wn /= 2)
+        for (int ha = wn / 2; ha <= 2 * wn; ++ha) {
+            if (ha == 7) continue;
             const int64_t tiles = ceil_div(m, 32 * ha) * ceil_div(s.tiles, 4 * wn), slots = 256 * 4 / wn;
             for (int sp = 1; sp == 1 || (sp <= 8 && sp * 4 <= s.steps && m <= kMostSplitRows); sp *= 2) {
                 const int64_t per = ceil_div(s.steps, sp), groups = tiles * sp;
@@ -494,10 +612,10 @@ void stream_launch(const W4Args& g, int waves, hipStream_t s) {
     w4_stream_kernel<MT, NT, kStreamWaves><<<grid, 64 * waves, static_cast<size_t>(waves) * MT * NT * 1024, s>>>(g);
 }
 
-template <int NT>
-void stream_by_rows(const W4Args& g, const W4Plan& p, hipStream_t s) {
-    if (p.mt == 1) stream_launch<1, NT>(g, p.waves, s);
-    else stream_launch<2, NT>(g, p.waves, s);
+template <int MT, int DEPTH>
+void ring_launch(const W4Args& g, hipStream_t s) {
+    w4_ring_kernel<MT, DEPTH><<<dim3(static_cast<unsigned>(ceil_div(g.tiles, 8)), 1, static_cast<unsigned>(g.splits)), 256, 0, s>>>(
+        g, static_cast<int>(ceil_div(g.steps, g.splits)));
 }
 
 template <int HA, int WN>
@@ -510,11 +628,15 @@ void tile_launch(const W4Args& g, hipStream_t s) {
 
 void launch_w4(const W4Args& g, const W4Plan& p, hipStream_t s) {
     if (p.kind == 0) {
-        if (p.nt == 1) stream_by_rows<1>(g, p, s);
-        else if (p.nt == 2) stream_by_rows<2>(g, p, s);
-        else stream_by_rows<4>(g, p, s);
+        if (p.mt == 2) stream_launch<2, 4>(g, p.waves, s);
+        else if (p.nt == 1) stream_launch<1, 1>(g, p.waves, s);
+        else if (p.nt == 2) stream_launch<1, 2>(g, p.waves, s);
+        else stream_launch<1, 4>(g, p.waves, s);
+    } else if (p.kind == 2) {
+        if (p.mt == 1) ring_launch<1, 5>(g, s);
+        else if (p.mt == 2) ring_launch<2, 4>(g, s);
+        else ring_launch<4, 3>(g, s);
     } else switch (p.nt * 16 + p.mt) {
-        case 64 + 1: tile_launch<1, 4>(g, s); break;
         case 64 + 2: tile_launch<2, 4>(g, s); break;
         case 64 + 3: tile_launch<3, 4>(g, s); break;
         case 64 + 4: tile_launch<4, 4>(g, s); break;
@@ -524,9 +646,7 @@ void launch_w4(const W4Args& g, const W4Plan& p, hipStream_t s) {
         case 32 + 1: tile_launch<1, 2>(g, s); break;
         case 32 + 2: tile_launch<2, 2>(g, s); break;
         case 32 + 3: tile_launch<3, 2>(g, s); break;
-        case 32 + 4: tile_launch<4, 2>(g, s); break;
-        case 16 + 1: tile_launch<1, 1>(g, s); break;
-        default: tile_launch<2, 1>(g, s); break;
+        default: tile_launch<4, 2>(g, s); break;
     }
     if (p.splits > 1) {
         const int quads = g.tiles / (g.gated ? 2 : 1) * 4;
@@ -626,8 +746,7 @@ extern "C" int slw_w4_product(const slw_w4* w, const void* a, int64_t lda, int32
         g.vec = ldo % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (out_f32 ? 16 : 8) == 0;
         g.gated = w->gated != 0;
         g.f32 = out_f32 != 0;
-        W4Plan plan = plan_w4(sh, lda > kMostTileStride ? std::min(m, 32) : m, g.gated);
-        if (lda > kMostTileStride) plan.splits = 1;
+        const W4Plan plan = lda > kMostTileStride ? W4Plan{0, m <= 16 ? 1 : 2, 4, std::min(4, sh.words), 1} : plan_w4(sh, m, g.gated);
         const size_t need = w4_partial_bytes(sh, plan, m);
         if (need) {
             if (!ws || !aligned16(ws)) return fail(SLW_EINVAL, "the workspace must be 16-byte aligned device memory");
