@@ -40,6 +40,7 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 constexpr int kBins = 768;          // 16 for an octave; the last one holds w < 2^-47 and is weighed nowhere
+constexpr int kHeld = 4096;         // 16 bytes each of a slice that wait in LDS to be weighed
 constexpr int kQueue = 8 * kWave + 64;  // logits a wave has queued: a piece of every lane beside 63 left over
 constexpr int kMost = 4096;         // most groups of threads of a row whose largest logits are kept
 constexpr int kList = 4096;         // tokens sorted in LDS
@@ -74,6 +75,11 @@ __device__ __forceinline__ float value_of(uint32_t key) {
     return __uint_as_float(key ^ (key & 0x80000000u ? 0x80000000u : 0xFFFFFFFFu));
 }
 
+// Sixteenths of an octave from logit 0, whole.  Never falls as x grows; where it is
+// within kNear, single precision moves few x to the next one, past a half by 2^-6 at most.
+constexpr double kNear = 0x1p17;
+__device__ __forceinline__ float sixteenth(float x, float c16) { return rintf(x * c16); }
+
 // How w depends on x.  In a row that has +inf those tokens alone have mass.
 struct Row {
     float M;          // the largest logit; 0 where that is +inf
@@ -98,10 +104,14 @@ struct Row {
     }
     // 2^((t - n) / 16), n the nearest whole number
     static __device__ __forceinline__ double of_sixteenth(double t, int& n) {
-        const double whole = rint(t), f = t - whole;
+        const double whole = rint(t);
         n = static_cast<int>(whole);
+        return power(t - whole, 1.0);
+    }
+    // one - 1 + 2^(f / 16)
+    static __device__ __forceinline__ double power(double f, double one) {
         return fma(f, fma(f, fma(f, fma(f, 0x1.3b2c4ac7eb38ap-23, 0x1.c6b3488226c3bp-17), 0x1.ebfbdff6988cep-11),
-                          0x1.62e42fee4615cp-5), 1.0);
+                          0x1.62e42fee4615cp-5), one);
     }
     __device__ __forceinline__ double w(float x) const {
         int n;
@@ -126,7 +136,8 @@ struct Shared {
     int32_t ref[16];
     uint64_t goal, sum, before;
     double found_d, above_d;
-    int n_list, found, digit;
+    int n_list, n_groups, found, digit;
+    uint16_t groups[kMost / 2];
 };
 
 // Inclusive sums over the lanes of a wave by data-parallel moves: within rows of 16
@@ -142,6 +153,17 @@ __device__ __forceinline__ V moved(V v) {
 #pragma unroll
     for (size_t i = 0; i < sizeof(V) / 4; ++i) to.w[i] = __builtin_amdgcn_update_dpp(0, from.w[i], CTRL, ROWS, 0xf, false);
     return to.v;
+}
+template <class V>
+__device__ __forceinline__ V of_lane(V v, int lane);
+__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+    v = max(v, moved<0x111, 0xf>(v));
+    v = max(v, moved<0x112, 0xf>(v));
+    v = max(v, moved<0x114, 0xf>(v));
+    v = max(v, moved<0x118, 0xf>(v));
+    v = max(v, moved<0x142, 0xa>(v));
+    v = max(v, moved<0x143, 0xc>(v));
+    return of_lane(v, kWave - 1);
 }
 template <class V>
 __device__ __forceinline__ V wave_scan(V v) {
@@ -259,7 +281,7 @@ struct Pieces {
     __device__ __forceinline__ void load(int v, float (&x)[8]) const { spread(ask(v), v, x); }
 };
 
-// Pieces v, v + stride, ... below `end`, f(x, v).  N are asked for at a time, and
+// Pieces v, v + stride, ... below `end`, f(x, v, as it was read).  N are asked for at a time, and
 // where that is one, it is asked for while f looks at the one before it.
 template <int N, class T, class F>
 __device__ __forceinline__ void each_piece(const Pieces<T>& p, int v, int end, int stride, F&& f) {
@@ -269,9 +291,10 @@ __device__ __forceinline__ void each_piece(const Pieces<T>& p, int v, int end, i
     for (; v < end; v += N * stride) {
         float x[8];
         if (N == 1) {
-            p.spread(raw[0], v, x);
+            const typename Pieces<T>::Raw was = raw[0];
+            p.spread(was, v, x);
             raw[0] = p.ask(v + stride);
-            f(x, v);
+            f(x, v, was);
             continue;
         }
 #pragma unroll
@@ -280,7 +303,7 @@ __device__ __forceinline__ void each_piece(const Pieces<T>& p, int v, int end, i
         for (int q = 0; q < N; ++q)
             if (v + q * stride < end) {
                 p.spread(raw[q], v + q * stride, x);
-                f(x, v + q * stride);
+                f(x, v + q * stride, raw[q]);
             }
     }
 }
@@ -339,24 +362,44 @@ __device__ __forceinline__ Cut bisect(const Pieces<T>& p, const Row& r, const Cu
     return Cut{lo, a};
 }
 
+// Pieces of slice s of a row, a whole number for every thread (the last ones may have fewer, or none).
+__device__ __forceinline__ int slice_pieces(int count, int slices) {
+    return ((count + slices - 1) / slices + kThreads - 1) / kThreads * kThreads;
+}
+
+// Threads of a slice whose largest logit is kept together.
+__device__ __forceinline__ int group_size(int slices) { return max(1, slices * kThreads / kMost); }
+
 // Tokens of `in` from `lo` up and below `hi` (none: +inf), in LDS (in any order); how many there are, of
-// which the first kList are there.
+// which the first kList are there.  Where at most half of the groups of threads have
+// such a token, only their pieces are read.
 template <class T>
-__device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float lo, float hi, const Cut& in, Shared& sh) {
+__device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float lo, float hi, const Cut& in,
+                                       const uint32_t (&most)[kMost / kThreads], int slices, Shared& sh) {
     __syncthreads();
-    if (threadIdx.x == 0) sh.n_list = 0;
+    if (threadIdx.x == 0) sh.n_list = sh.n_groups = 0;
     __syncthreads();
-    each_piece<1>(p, threadIdx.x, p.count, kThreads, [&](const float (&x)[8], int v) {
+    // in a row with +inf, where they count as 0 and all else as -inf, only they can be meant
+    const float from = r.at_inf ? INFINITY : lo, below = r.at_inf ? NAN : hi;
+    const uint32_t least = key_of(from);
+#pragma unroll
+    for (int s = 0; s < kMost / kThreads; ++s)
+        if (most[s] >= least) {
+            const int at = atomicAdd(&sh.n_groups, 1);
+            if (at < kMost / 2) sh.groups[at] = static_cast<uint16_t>(s * kThreads + threadIdx.x);
+        }
+    auto look = [&](const float (&x)[8], int v, const typename Pieces<T>::Raw& raw) {
         uint32_t keeps = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float y = r.at_inf ? r.fix(x[e]) : x[e];
-            keeps |= y >= lo && y < hi ? 1u << e : 0u;
-        }
+        for (int e = 0; e < 8; ++e) keeps |= x[e] >= from && !(x[e] >= below) ? 1u << e : 0u;
         if (in.key != 0) {  // few rows come with a cut
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) {
+                float y = x[0];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (!in.keeps(key_of(r.at_inf ? r.fix(x[e]) : x[e]), 8 * v - p.shift + e)) keeps &= ~(1u << e);
+                for (int j = 1; j < 8; ++j) y = e == j ? x[j] : y;
+                if (!in.keeps(key_of(r.at_inf ? r.fix(y) : y), 8 * v - p.shift + e)) keeps &= ~(1u << e);
+            }
         }
         if (!keeps) return;
         int at = atomicAdd(&sh.n_list, __popc(keeps));
@@ -369,7 +412,24 @@ __device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float l
             if (at < kList)
                 sh.list[at] = static_cast<uint64_t>(key_of(r.at_inf ? r.fix(y) : y)) << 32 | static_cast<uint32_t>(8 * v - p.shift + e);
         }
-    });
+    };
+    __syncthreads();
+    const int groups = uniform(sh.n_groups), size = group_size(slices), in_slice = kThreads / size;
+    if (2 * groups <= slices * in_slice) {
+        const int per = slice_pieces(p.count, slices), rounds = per / kThreads;
+#pragma unroll 1
+        for (int j = threadIdx.x; j < groups * rounds * size; j += kThreads) {
+            const int group = sh.groups[j / (rounds * size)], i = j % (rounds * size);
+            const int slice = group / in_slice, v = slice * per + group % in_slice * size + i % size + i / size * kThreads;
+            if (v >= p.count) continue;
+            float x[8];
+            const typename Pieces<T>::Raw raw = p.ask(v);
+            p.spread(raw, v, x);
+            look(x, v, raw);
+        }
+    } else {
+        each_piece<4>(p, threadIdx.x, p.count, kThreads, look);
+    }
     __syncthreads();
     const int n = sh.n_list;
     __syncthreads();
@@ -572,24 +632,25 @@ struct Wants {
     __device__ bool by_count() const { return !greedy && k > 0 && k <= kThreads; }
 };
 
-// Pieces of slice s of a row, a whole number for every thread (the last ones may have fewer, or none).
-__device__ __forceinline__ int slice_pieces(int count, int slices) {
-    return ((count + slices - 1) / slices + kThreads - 1) / kThreads * kThreads;
-}
-
 // 1. What is known of a slice.
 template <class T>
 __global__ __launch_bounds__(kThreads, 8) void sample_slices_kernel(SampleArgs a) {
     __shared__ double root[16];
     __shared__ __attribute__((aligned(16))) float ends[16];
     __shared__ uint64_t bins[kBins];
+    __shared__ f32x4 held[kHeld];
     __shared__ uint64_t red_u[kWaves];
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     const size_t slice = blockIdx.x;
     const int row = static_cast<int>(slice / a.slices);
-    const Wants want(a, row);
+    // the first pieces, which wait in LDS to be weighed, are asked for before all else
+    constexpr int kRegs = sizeof(T) / 2, kWait = kHeld / kRegs, kFirst = kWait / kThreads;
     const Pieces<T> p(static_cast<const T*>(a.logits) + row * a.ld, a.vocab, ends);
     const int per = slice_pieces(p.count, a.slices), from = static_cast<int>(slice % a.slices) * per, to = min(from + per, p.count);
+    typename Pieces<T>::Raw first[kFirst];
+#pragma unroll
+    for (int q = 0; q < kFirst; ++q) first[q] = p.ask(from + tid + q * kThreads);
+    const Wants want(a, row);
     if (tid < 16) root[tid] = exp2(tid / 16.0);
     for (int b = tid; b < kBins; b += kThreads) bins[b] = 0;
     __syncthreads();
@@ -597,32 +658,52 @@ __global__ __launch_bounds__(kThreads, 8) void sample_slices_kernel(SampleArgs a
     // the thread's largest logit and the first piece that has it (NaN is below everything)
     float mine = -INFINITY;
     int at = -1;
-    each_piece<4>(p, from + tid, to, kThreads, [&](const float (&x)[8], int v) {
+    auto look = [&](const float (&x)[8], int v, const typename Pieces<T>::Raw&) {
         const float m = largest(x);
         if (m > mine) {
             mine = m;
             at = v;
         }
-    });
+    };
+#pragma unroll
+    for (int q = 0; q < kFirst; ++q) {
+        const int v = from + tid + q * kThreads;
+#pragma unroll
+        for (int i = 0; i < kRegs; ++i) held[i * kWait + v - from] = first[q].w[i];
+        float x[8];
+        p.spread(first[q], v, x);
+        if (v < to) look(x, v, first[q]);
+    }
+    each_piece<4>(p, from + tid + kWait, to, kThreads, look);
+    // a piece once more
+    auto again = [&](int v, float (&x)[8]) {
+        typename Pieces<T>::Raw raw;
+        if (v - from < kWait) {
+#pragma unroll
+            for (int i = 0; i < kRegs; ++i) raw.w[i] = held[i * kWait + v - from];
+        } else {
+            raw = p.ask(v);
+        }
+        p.spread(raw, v, x);
+    };
     uint64_t best = 0;
     if (at >= 0) {
         float x[8];
-        p.load(at, x);
+        again(at, x);
         int i = 0;
 #pragma unroll
         for (int e = 7; e >= 0; --e)
             if (x[e] == mine) i = 8 * at - p.shift + e;
         best = static_cast<uint64_t>(key_of(mine)) << 32 | (0xFFFFFFFFu - static_cast<uint32_t>(i));
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) best = max(best, static_cast<uint64_t>(__shfl_xor(best, o, kWave)));
+    best = wave_max(best);
     if (lane == 0) red_u[wave] = best;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) best = max(best, red_u[w]);
     if (tid == 0) a.best[slice] = best;
-    if (want.by_count()) {  // of four threads together from sixteen slices on, of two from eight on
-        const int group = max(1, a.slices * kThreads / kMost);
+    if (!want.greedy && !want.free()) {  // of four threads together from sixteen slices on, of two from eight on
+        const int group = group_size(a.slices);
         if (group >= 2) mine = fmaxf(mine, __shfl_xor(mine, 1, kWave));
         if (group >= 4) mine = fmaxf(mine, __shfl_xor(mine, 2, kWave));
         if (tid % group == 0)
@@ -635,25 +716,30 @@ __global__ __launch_bounds__(kThreads, 8) void sample_slices_kernel(SampleArgs a
     double s = 0.0;
     if (by_mass) {
         // By bins of whole sixteenths of an octave, which all slices share; in units of
-        // 2^-42 of the bin's w, the low bits of a number near 2^10.
-        const int ref = uniform(static_cast<int>(rint(static_cast<double>(m) * want.c16)));
-        const double floor = static_cast<double>(ref) - kBins;  // -inf and NaN too
+        // 2^-42 of the bin's w, the low bits of a number near 2^10.  Far from logit 0 single
+        // precision knows no sixteenths: such a slice has no bins.
+        const bool near = fabs(static_cast<double>(m)) * want.c16 <= kNear;
+        const float c = static_cast<float>(want.c16), first = near ? sixteenth(m, c) : -0x1p30f, floor = first - kBins;
+        const int ref = uniform(static_cast<int>(first));
+        if (tid == 0) a.ref[slice] = ref;
+        if (!near) return;
 #pragma unroll 1
         for (int v = from + tid; v < to; v += kThreads) {
             float x[8];
-            p.load(v, x);
+            again(v, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                int n;
-                const double w = Row::of_sixteenth(fmax(static_cast<double>(x[e]) * want.c16, floor), n);
-                if (static_cast<uint32_t>(ref - n) < kBins - 1)
+                const float y = fmaxf(x[e], -0x1p100f), whole = fmaxf(sixteenth(y, c), floor);  // -inf and NaN as far down
+                const double f = fma(static_cast<double>(y), want.c16, -static_cast<double>(whole));
+                const int n = static_cast<int>(whole);
+                if (ref - n < kBins - 1)
                     atomicAdd(reinterpret_cast<unsigned long long*>(&bins[ref - n]),
-                              static_cast<unsigned long long>(__double_as_longlong(w + 0x1p10) - __double_as_longlong(0x1p10)));
+                              static_cast<unsigned long long>(__double_as_longlong(Row::power(f, 1.0 + 0x1p10)) -
+                                                              __double_as_longlong(0x1p10)));
             }
         }
         __syncthreads();
         for (int b = tid; b < kBins; b += kThreads) a.bins[slice * kBins + b] = bins[b];
-        if (tid == 0) a.ref[slice] = ref;
         return;
     }
     // of a sixteenth of the slice each wave, from the slice's largest logit
@@ -666,7 +752,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_slices_kernel(SampleArgs a
 #pragma unroll 1
     for (int v = from + wave * each_wave + lane; v < v1; v += kWave) {
         float x[8];
-        p.load(v, x);
+        again(v, x);
         if (r.at_inf)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = r.fix(x[e]);
@@ -788,10 +874,11 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
     }
 
     // the slices' bins count, where sixteenths from 0 on are as good as from M on
-    const bool slices = want.by_mass() && !r.at_inf && fabs(static_cast<double>(r.M)) * r.c16 <= 0x1p17;
-    const int ref = slices ? static_cast<int>(rint(static_cast<double>(r.M) * r.c16)) : 0;
+    const bool slices = want.by_mass() && !r.at_inf && fabs(static_cast<double>(r.M)) * r.c16 <= kNear;
+    const float c16 = static_cast<float>(r.c16);
+    const int ref = slices ? static_cast<int>(sixteenth(r.M, c16)) : 0;
     auto bin_of = [&](float x) {  // a whole number; far down beyond any int
-        return slices ? ref - rint(static_cast<double>(x) * r.c16) : static_cast<double>(r.bin_of(x));
+        return slices ? static_cast<float>(ref) - sixteenth(x, c16) : static_cast<float>(r.bin_of(x));
     };
     int bin = -1, listed = 0;  // the bin of the cut, whose kept tokens are among those in LDS
 
@@ -854,7 +941,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
             }
             if (low && lo <= cut.key) continue;  // the cut is above it
         }
-        const int n = collect(p, r, value_of(lo), hi, cut, sh);
+        const int n = collect(p, r, value_of(lo), hi, cut, most, a.slices, sh);
         listed = n <= kList ? n : -1;
         if (n <= kList) {
             const Cut c = cut_list(r, n, lo, sizeof(T) == 2 ? 16 : 0, goal, want.u, token, logprob, sh);
@@ -932,7 +1019,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
         };
         // whole waves: pieces past the range count as -inf
         each_piece<1>(p, from + wave * per + lane, (v1 - (from + wave * per) + kWave - 1) / kWave * kWave + from + wave * per, kWave,
-                   [&](const float (&x)[8], int v) {
+                   [&](const float (&x)[8], int v, const typename Pieces<T>::Raw&) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float y = r.at_inf ? r.fix(x[e]) : x[e];
