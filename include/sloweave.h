@@ -367,9 +367,10 @@ int slw_attn_rotate(slw_ctx* ctx, const slw_attn* plan, const slw_rope* rope, co
  *   resid_out  as resid, or NULL: r' is not written;  out  bf16 [rows][d], or NULL: only r'
  * resid_out may be resid, and out may be block, each with the same stride.  d is a
  * multiple of 8 up to SLW_NORM_MAX_D; rows and gains are 16-byte aligned, strides
- * multiples of 8.
+ * multiples of 8.  0 <= rows <= SLW_NORM_MAX_ROWS; 0 does nothing.
  */
 #define SLW_NORM_MAX_D 32768
+#define SLW_NORM_MAX_ROWS (1 << 20)
 typedef struct slw_norm_args {
     const void* resid;
     const void* block;
@@ -439,9 +440,10 @@ int slw_w4_product(const slw_w4* w, const void* a, int64_t lda, int32_t m, void*
  *   ws       device, 16-byte aligned, ws_bytes >= slw_sample_workspace_size for at
  *            least these rows and this vocab (NULL where that is 0); shared as
  *            slw_w4_product's
- * 1 <= vocab <= SLW_SAMPLE_MAX_VOCAB.
+ * 1 <= vocab <= SLW_SAMPLE_MAX_VOCAB, 0 <= rows <= SLW_SAMPLE_MAX_ROWS; 0 does nothing.
  */
 #define SLW_SAMPLE_MAX_VOCAB (1 << 20)
+#define SLW_SAMPLE_MAX_ROWS (1 << 20)
 typedef struct slw_sample_args {
     const void* logits;
     int64_t ld;

@@ -263,6 +263,7 @@ extern "C" int slw_residual_norm(const slw_norm_args* a, void* stream) {
     return guarded([&] {
         if (!a) return fail(SLW_EINVAL, "null argument");
         if (a->rows < 0) return fail(SLW_EINVAL, "negative rows");
+        if (a->rows > SLW_NORM_MAX_ROWS) return fail(SLW_EUNSUPPORTED, "more than %d rows", SLW_NORM_MAX_ROWS);
         if (a->d < 8 || a->d % 8 || a->d > SLW_NORM_MAX_D)
             return fail(SLW_EUNSUPPORTED, "d must be a multiple of 8 in [8, %d] (got %d)", SLW_NORM_MAX_D, a->d);
         if (!(a->eps >= 0.f) || !std::isfinite(a->eps) || !std::isfinite(a->scale))

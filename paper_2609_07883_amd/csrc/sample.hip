@@ -1139,6 +1139,7 @@ extern "C" int slw_sample_workspace_size(int32_t max_rows, int32_t vocab, size_t
     return guarded([&] {
         if (!bytes) return fail(SLW_EINVAL, "null argument");
         if (max_rows < 0) return fail(SLW_EINVAL, "negative rows");
+        if (max_rows > SLW_SAMPLE_MAX_ROWS) return fail(SLW_EUNSUPPORTED, "more than %d rows", SLW_SAMPLE_MAX_ROWS);
         if (vocab < 1 || vocab > SLW_SAMPLE_MAX_VOCAB)
             return fail(SLW_EUNSUPPORTED, "vocab must be in [1, %d] (got %d)", SLW_SAMPLE_MAX_VOCAB, vocab);
         // the slices of a call are fewer than twice 1024, or as many as its rows, and those of one row each at most
@@ -1152,6 +1153,7 @@ extern "C" int slw_sample(const slw_sample_args* a, void* ws, size_t ws_bytes, v
     return guarded([&] {
         if (!a) return fail(SLW_EINVAL, "null argument");
         if (a->rows < 0) return fail(SLW_EINVAL, "negative rows");
+        if (a->rows > SLW_SAMPLE_MAX_ROWS) return fail(SLW_EUNSUPPORTED, "more than %d rows", SLW_SAMPLE_MAX_ROWS);
         if (a->vocab < 1 || a->vocab > SLW_SAMPLE_MAX_VOCAB)
             return fail(SLW_EUNSUPPORTED, "vocab must be in [1, %d] (got %d)", SLW_SAMPLE_MAX_VOCAB, a->vocab);
         if (a->logits_f32 != 0 && a->logits_f32 != 1) return fail(SLW_EINVAL, "logits_f32 must be 0 or 1");

@@ -494,30 +494,32 @@ __global__ __launch_bounds__(256) void w4_join_kernel(W4Args g) {
     }
 }
 
-// One thread for each lane of each tile's step: four words of codes; the first 16
+// A thread for each lane of each tile's step: four words of codes; the first 16
 // lanes of every step make the row's scale word.
+constexpr size_t kPackGroups = 1 << 20;  // at most; they go on that far apart
 __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                       u32x4* __restrict__ to_codes, uint32_t* __restrict__ to_scales,
                                                       int rows, int k, int tiles, int steps, int words, bool gated) {
-    const size_t i = blockIdx.x * static_cast<size_t>(256) + threadIdx.x;
-    const int lane = i % 64, step = i / 64 % (4 * words);
-    const size_t tile = i / 64 / (4 * words);
-    if (tile >= static_cast<size_t>(tiles)) return;
-    const int r = (gated ? tile / 2 : tile) * 16 + (lane & 15);  // of the gate or up rows, or of all
-    const int groups = k / 32;
-    const size_t row = gated && tile % 2 ? static_cast<size_t>(rows) + r : r;
-    if (step < steps) {
-        u32x4 c = {0u, 0u, 0u, 0u};
+    for (size_t i = blockIdx.x * static_cast<size_t>(256) + threadIdx.x; i < static_cast<size_t>(tiles) * words * 256;
+         i += gridDim.x * static_cast<size_t>(256)) {
+        const int lane = i % 64, step = i / 64 % (4 * words);
+        const size_t tile = i / 64 / (4 * words);
+        const int r = (gated ? tile / 2 : tile) * 16 + (lane & 15);  // of the gate or up rows, or of all
+        const int groups = k / 32;
+        const size_t row = gated && tile % 2 ? static_cast<size_t>(rows) + r : r;
+        if (step < steps) {
+            u32x4 c = {0u, 0u, 0u, 0u};
+            for (int j = 0; j < 4; ++j)
+                if (r < rows && 4 * step + j < groups)
+                    c[j] = *reinterpret_cast<const uint32_t*>(codes + row * (k / 2) + (4 * step + j) * 16 + 4 * (lane / 16));
+            to_codes[(tile * steps + step) * 64 + lane] = c;
+        }
+        if (lane >= 16) continue;
+        uint32_t w = 0;
         for (int j = 0; j < 4; ++j)
-            if (r < rows && 4 * step + j < groups)
-                c[j] = *reinterpret_cast<const uint32_t*>(codes + row * (k / 2) + (4 * step + j) * 16 + 4 * (lane / 16));
-        to_codes[(tile * steps + step) * 64 + lane] = c;
+            if (r < rows && 4 * step + j < groups) w |= static_cast<uint32_t>(scales[row * groups + 4 * step + j]) << (8 * j);
+        to_scales[((tile * words + step / 4) * 16 + lane) * 4 + step % 4] = w;
     }
-    if (lane >= 16) return;
-    uint32_t w = 0;
-    for (int j = 0; j < 4; ++j)
-        if (r < rows && 4 * step + j < groups) w |= static_cast<uint32_t>(scales[row * groups + 4 * step + j]) << (8 * j);
-    to_scales[((tile * words + step / 4) * 16 + lane) * 4 + step % 4] = w;
 }
 
 struct W4Shape {
@@ -688,8 +690,8 @@ extern "C" int slw_w4_pack(const void* codes, const void* scales, int32_t n, int
         if (!codes || !scales || !packed) return fail(SLW_EINVAL, "null argument");
         if (!aligned16(codes) || !aligned16(packed)) return fail(SLW_EINVAL, "codes and packed weights must be 16-byte aligned");
         const W4Shape w = w4_shape(n, k, gated);
-        const size_t threads = static_cast<size_t>(w.tiles) * w.words * 256;
-        w4_pack_kernel<<<static_cast<unsigned>((threads + 255) / 256), 256, 0, static_cast<hipStream_t>(stream)>>>(
+        const size_t groups = std::min(static_cast<size_t>(w.tiles) * w.words, kPackGroups);
+        w4_pack_kernel<<<static_cast<unsigned>(groups), 256, 0, static_cast<hipStream_t>(stream)>>>(
             static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), static_cast<u32x4*>(packed),
             reinterpret_cast<uint32_t*>(static_cast<char*>(packed) + w.code_bytes), gated ? n / 2 : n, k, w.tiles, w.steps,
             w.words, gated != 0);

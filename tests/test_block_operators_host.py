@@ -161,6 +161,44 @@ def test_sample_refusals():
     call(rows=0)
 
 
+def test_sample_workspace_refusals():
+    call = lambda **k: api.sample(64, 4, 1000, 1000, 64, 64, **k)
+    size = api.sample_workspace_size(4, 1000)
+    assert size > 0 and api.sample_workspace_size(0, 1000) == 0
+    _refused(api.EINVAL, call, ws=0, ws_bytes=size)
+    _refused(api.EINVAL, call, ws=72, ws_bytes=size)
+    _refused(api.ENOMEM, call, ws=64, ws_bytes=0)
+    _refused(api.ENOMEM, lambda: api.sample(64, 4, 1 << 20, 1 << 20, 64, 64, ws=64, ws_bytes=size))
+
+
+@pytest.mark.parametrize("vocab", [1, 8192, 8193, 50000, 1 << 20])
+def test_sample_workspace_grows_with_the_rows(vocab):
+    """What fits some rows fits fewer, whatever slices those are cut into."""
+    sizes = [api.sample_workspace_size(r, vocab) for r in (1, 2, 63, 64, 65, 127, 128, 129, 500, 512, 513, 1023, 1024, 1025, 5000)]
+    assert sizes == sorted(sizes)
+
+
+def test_rows_beyond_the_most():
+    most = 1 << 20
+    _refused(api.EUNSUPPORTED, _norm, rows=most + 1)
+    _refused(api.EUNSUPPORTED, api.sample, 64, most + 1, 8, 8, 64, 64, ws=64, ws_bytes=1 << 50)
+    _refused(api.EUNSUPPORTED, api.sample_workspace_size, most + 1, 8)
+    _refused(api.EUNSUPPORTED, api.W4(64, 32, 64).product, 64, 64, most + 1, 64, 32, ws=64, ws_bytes=1 << 50)
+
+
+def test_w4_workspace_refusals():
+    """A k that is split needs its workspace; what fits some rows fits fewer."""
+    w = api.W4(64, 4096, 14336)
+    sizes = [w.workspace_size(m) for m in range(0, 5000, 7)]
+    assert sizes[0] == 0 and sizes == sorted(sizes)
+    m = 48
+    need = w.workspace_size(m)
+    assert need > 0
+    _refused(api.EINVAL, w.product, 64, 14336, m, 64, 4096)
+    _refused(api.EINVAL, w.product, 64, 14336, m, 64, 4096, ws=72, ws_bytes=need)
+    _refused(api.ENOMEM, w.product, 64, 14336, m, 64, 4096, ws=64, ws_bytes=16)
+
+
 def test_sample_model_by_hand():
     x = np.log([0.5, 0.125, 0.25, 0.125])
     assert [O.sample(x, u=u)[0] for u in (0.0, 0.49, 0.51, 0.63, 0.7, 0.9)] == [0, 0, 1, 2, 2, 3]

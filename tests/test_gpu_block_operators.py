@@ -167,6 +167,23 @@ def test_product_of_whole_numbers_is_exact(m, n, k):
     assert torch.equal(w.product(t, m, k, True), want)
 
 
+@pytest.mark.parametrize("m,n,k", [(12, 70001, 288), (20, 64, 8448), (16, 300, 10016), (32, 9000, 160), (50, 100, 8224), (68, 17, 928),
+                                   (1038, 16, 4192), (196, 10918, 96), (102, 2108, 4000), (132, 10962, 32), (2056, 16, 4064),
+                                   (265, 13112, 160), (65, 8578, 1952), (4673, 1549, 32), (2210, 277, 7904), (392, 13064, 64),
+                                   (3129, 131, 5920), (514, 13223, 32), (129, 6451, 5792), (661, 13249, 160), (2732, 260, 10240),
+                                   (770, 13149, 288)])
+def test_product_of_every_shape_of_work_group_is_exact(m, n, k):
+    """The same where the rows, columns and k ask for each size of tile, with k whole and split."""
+    test_product_of_whole_numbers_is_exact(m, n, k)
+
+
+@pytest.mark.parametrize("m,n,k", [(11, 131074, 64), (23, 66, 8224), (64, 514, 4128), (131, 272, 9472), (263, 13124, 32), (648, 1082, 288)])
+def test_gated_product_of_more_shapes(m, n, k):
+    w = Weights(n, k, True)
+    a, av = _bf16(np.random.default_rng([m, n, k]).standard_normal((m, k)))
+    _within(_f64(w.product(a, m, k, True)), *O.product(av, w.values, True), "f32")
+
+
 def test_product_columns_do_not_mix():
     """Row i of a picks column i of W: every code of every lane comes back, once a group of scales."""
     n, k = 112, 384
@@ -406,6 +423,77 @@ def test_sample_of_the_largest_vocabulary():
     x[2] = 0
     for par in (dict(), dict(top_p=0.9), dict(top_k=50)):
         _check(x, False, u=[0.1, 0.6, 0.9], **par)
+
+
+@pytest.mark.parametrize("rows,vocab", [(1, 131072), (3, 100003), (70, 40000), (130, 20011), (300, 12001), (600, 9000), (1100, 4100)])
+def test_sample_of_many_rows(rows, vocab):
+    """Batches whose rows are cut into sixteen slices down to one."""
+    rng = np.random.default_rng([rows, vocab])
+    x = rng.standard_normal((rows, vocab)) * rng.choice([0.5, 2.0, 6.0], (rows, 1))
+    k = np.where(rng.random(rows) < 0.4, rng.integers(1, 3000, rows), 0)
+    p = np.where(rng.random(rows) < 0.5, rng.uniform(0.1, 0.99, rows), 1.0)
+    low = np.where(rng.random(rows) < 0.3, rng.uniform(0.001, 0.3, rows), 0.0)
+    for f32 in (False, True):
+        _check(x, f32, temperature=rng.uniform(0.5, 1.5, rows), top_k=k, top_p=p, min_p=low, u=rng.random(rows))
+
+
+@pytest.mark.parametrize("f32", [False, True])
+def test_sample_of_slices_that_hold_nothing(f32):
+    """Long rows with +inf in one part, with only -inf or NaN in others, and with the mass at either end."""
+    rng = np.random.default_rng(12)
+    n = 140001
+    x = rng.standard_normal((6, n)) * 2
+    x[0, [70000, 139999]] = np.inf
+    x[1, 20000:] = -np.inf
+    x[2, :130000] = np.nan
+    x[3, : n - 3] = -1e30
+    x[4, 9000:100000] = -np.inf
+    x[4, 5] = 30.0
+    x[5] = -np.inf
+    x[5, n - 1] = np.inf
+    for par in (dict(), dict(top_k=2), dict(top_k=1500, top_p=0.8), dict(top_p=0.6), dict(top_p=0.999, min_p=0.001), dict(min_p=0.05)):
+        _check(x, f32, u=rng.random(6), **par)
+
+
+@pytest.mark.parametrize("scale,shift,temperature", [(0.1, 1000.0, 0.05), (0.1, -1000.0, 0.05), (1.0, 3e4, 0.5), (1e-3, 0.0, 1e-4), (40.0, 0.0, 0.7)])
+def test_sample_far_from_zero(scale, shift, temperature):
+    """Large logits over small temperatures: their sixteenths of an octave are beyond what single precision tells apart."""
+    rng = np.random.default_rng(13)
+    x = shift + scale * rng.standard_normal((4, 50000))
+    for par in (dict(top_p=0.9), dict(top_p=0.3), dict(top_k=40, top_p=0.9), dict(top_p=0.95, min_p=0.01), dict()):
+        _check(x, True, temperature=temperature, u=rng.random(4), **par)
+
+
+def test_two_streams_at_once():
+    """A product and a draw on each of two streams, every call with a workspace of its own: as one after the other."""
+    rng = np.random.default_rng(14)
+    w = Weights(2048, 4096, lo=121, hi=123)
+    rows, vocab = 24, 30000
+    a, _ = _bf16(rng.standard_normal((rows, 4096)))
+    x = torch.from_numpy(rng.standard_normal((2, rows, vocab)) * 3).to(torch.bfloat16).cuda()
+    u = torch.from_numpy(rng.random(rows).astype(np.float32)).cuda()
+    p = torch.full((rows,), 0.9, device="cuda")
+    wsize, ssize = max(16, w.w.workspace_size(rows)), api.sample_workspace_size(rows, vocab)
+
+    def both(st, i):
+        out = torch.empty(rows, 2048, dtype=torch.float32, device="cuda")
+        tokens = torch.empty(rows, dtype=torch.int32, device="cuda")
+        ws, ws2 = (torch.empty(n, dtype=torch.uint8, device="cuda") for n in (wsize, ssize))
+        torch.cuda.synchronize()
+        yield
+        for _ in range(20):
+            w.w.product(a.data_ptr(), 4096, rows, out.data_ptr(), 2048, out_f32=True, ws=ws.data_ptr(), ws_bytes=wsize, stream=st)
+            api.sample(x[i].data_ptr(), rows, vocab, vocab, u.data_ptr(), tokens.data_ptr(), top_p=p.data_ptr(), ws=ws2.data_ptr(),
+                       ws_bytes=ssize, stream=st)
+            yield
+        torch.cuda.synchronize()
+        yield out, tokens
+
+    alone = [list(both(_stream(), i))[-1] for i in (0, 1)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    together = list(zip(*(both(s.cuda_stream, i) for i, s in enumerate(streams))))[-1]
+    for (o, t), (o2, t2) in zip(alone, together):
+        assert torch.equal(o, o2) and torch.equal(t, t2)
 
 
 def test_sample_is_the_same_every_time_and_in_every_batch():
