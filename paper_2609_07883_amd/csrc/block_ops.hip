@@ -40,6 +40,18 @@ __device__ __forceinline__ void store8(float* p, const F8& x) {
     *reinterpret_cast<f32x4*>(p + 4) = f32x4{x.v[4], x.v[5], x.v[6], x.v[7]};
 }
 
+// Past the caches, for what is read a whole block later.
+__device__ __forceinline__ void stream8(bf16* p, const F8& x) {
+    bf16x8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = f2bf(x.v[e]);
+    __builtin_nontemporal_store(o, reinterpret_cast<bf16x8*>(p));
+}
+__device__ __forceinline__ void stream8(float* p, const F8& x) {
+    __builtin_nontemporal_store(f32x4{x.v[0], x.v[1], x.v[2], x.v[3]}, reinterpret_cast<f32x4*>(p));
+    __builtin_nontemporal_store(f32x4{x.v[4], x.v[5], x.v[6], x.v[7]}, reinterpret_cast<f32x4*>(p + 4));
+}
+
 // Sum over the threads of a row: a wave, or the W waves of the work-group.
 template <int W>
 __device__ __forceinline__ float row_sum(float v, float* red) {
@@ -56,7 +68,12 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
 // r' = r + scale * gate * P(o), y = r' / sqrt(mean(r'^2) + eps) * gain, all in
 // fp32 between the loads and the one rounding of each output; y is taken of r'
 // before that rounding.  A row stays in the registers of W waves, NV vectors of
-// 8 values a thread, between the loads, the one or two sums and the stores.
+// 8 values a thread, between the loads, the one or two sums and the stores: one
+// pass, whose bytes bound it.  One vector a thread up to 8192 values, as the sums
+// then wait for one load: 1 row of 4096 2.4 us, with two 3.1.  4104 rows of 4096 (fp32
+// stream, post-norm and gate, 202 MB) take 43 us, 4.7 TB/s, where a copy reaches 5.1; with
+// two vectors 47.  r' goes past the caches, as the next block's end reads it: 2080 rows of
+// a bf16 stream 11.7 us, 13.5 through them.
 template <int W, int NV, class R>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void residual_norm_kernel(NormRows a) {
     constexpr int kThreads = 64 * W;
@@ -109,7 +126,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void residual_norm_kernel(No
     for (int j = 0; j < NV; ++j) {
         const int i = t + j * kThreads;
         if (i >= nvec) continue;
-        if (a.resid_out) store8(static_cast<R*>(a.resid_out) + static_cast<size_t>(row) * a.ld_resid_out + 8 * i, r[j]);
+        if (a.resid_out) stream8(static_cast<R*>(a.resid_out) + static_cast<size_t>(row) * a.ld_resid_out + 8 * i, r[j]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss += r[j].v[e] * r[j].v[e];
     }
@@ -131,8 +148,8 @@ void residual_norm_by_width(const NormRows& a, hipStream_t s) {
     const unsigned rows = static_cast<unsigned>(a.rows);
     if (a.d <= 512) residual_norm_kernel<1, 1, R><<<(rows + 3) / 4, 256, 0, s>>>(a);
     else if (a.d <= 2048) residual_norm_kernel<4, 1, R><<<rows, 256, 0, s>>>(a);
-    else if (a.d <= 4096) residual_norm_kernel<4, 2, R><<<rows, 256, 0, s>>>(a);
-    else if (a.d <= 8192) residual_norm_kernel<8, 2, R><<<rows, 512, 0, s>>>(a);
+    else if (a.d <= 4096) residual_norm_kernel<8, 1, R><<<rows, 512, 0, s>>>(a);
+    else if (a.d <= 8192) residual_norm_kernel<16, 1, R><<<rows, 1024, 0, s>>>(a);
     else residual_norm_kernel<16, 4, R><<<rows, 1024, 0, s>>>(a);
 }
 
@@ -154,7 +171,10 @@ __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_A
 // pair i, all lanes share them through LDS, and each takes the same 16 values of
 // a head for every head that falls to it: the values (8 u .. 8 u + 7) and their
 // partners rot / 2 further, or 16 u .. 16 u + 15 interleaved; units past rot
-// are copied.  Waves do not wait for each other.
+// are copied.  Waves do not wait for each other.  The bytes bound it: 4104 rows of
+// 32 + 8 heads of 128 (84 MB) take 17.6 us, 4.8 TB/s; 18.7 with a head's values asked
+// for when it is their turn.  fp64 keeps an angle's fraction of a turn at any position
+// (fp32 would be 0.01 off at 131072), and costs one lane a pair.
 template <int HD, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateRows a, RopeArgs rope) {
     constexpr int kUnits = HD / 16, kHeadLanes = kWave / kUnits;
@@ -166,7 +186,19 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateRows a, RopeArgs rope
     const int hi = u >= turning || INTERLEAVED ? lo + 8 : lo + half;
     const double turns = lane < half ? rope_turns(rope, lane) : 0.0;
     const int heads = a.hq + a.hkv, first = a.q ? 0 : a.hq, last = a.k ? heads : a.hq;
+    const bool copies = u >= turning && a.in_place;  // nothing to do
     for (int row = blockIdx.x * 4 + wave; row < a.rows; row += gridDim.x * 4) {
+        // a head's values are asked for before those of the head before it are dealt with, the first before the angles
+        F8 x, y;
+        auto place = [&](int h, int64_t ld) {
+            return static_cast<size_t>(row) * ld + static_cast<size_t>(h < a.hq ? h : h - a.hq) * HD;
+        };
+        auto ask = [&](int h, F8& p, F8& q) {
+            const bf16* in = static_cast<const bf16*>(h < a.hq ? a.q : a.k) + place(h, a.ld);
+            p = load8(in + lo);
+            q = load8(in + hi);
+        };
+        if (!copies && first + h0 < last) ask(first + h0, x, y);
         int pos;
         if (row < a.chunk) {
             int i = 0;
@@ -192,15 +224,10 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateRows a, RopeArgs rope
             }
         }
         wave_fence();  // the next row's values come after these reads
-        if (u >= turning && a.in_place) continue;
+        if (copies) continue;
         for (int h = first + h0; h < last; h += kHeadLanes) {
-            const bool is_q = h < a.hq;
-            const size_t at = static_cast<size_t>(row) * a.ld + static_cast<size_t>(is_q ? h : h - a.hq) * HD;
-            const size_t to = static_cast<size_t>(row) * a.ld_out + static_cast<size_t>(is_q ? h : h - a.hq) * HD;
-            const bf16* in = static_cast<const bf16*>(is_q ? a.q : a.k) + at;
-            bf16* out = static_cast<bf16*>(is_q ? a.q_out : a.k_out) + to;
-            const F8 x = load8(in + lo), y = load8(in + hi);
-            F8 p = x, q = y;
+            F8 p = x, q = y, x_next, y_next;
+            if (h + kHeadLanes < last) ask(h + kHeadLanes, x_next, y_next);
             if (u < turning) {
                 if (INTERLEAVED) {
 #pragma unroll
@@ -218,8 +245,11 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateRows a, RopeArgs rope
                     }
                 }
             }
+            bf16* out = static_cast<bf16*>(h < a.hq ? a.q_out : a.k_out) + place(h, a.ld_out);
             store8(out + lo, p);
             store8(out + hi, q);
+            x = x_next;
+            y = y_next;
         }
     }
 }
