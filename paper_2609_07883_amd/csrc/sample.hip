@@ -195,16 +195,12 @@ __device__ __forceinline__ V wave_total(V v) { return of_lane(wave_scan(v), kWav
 // LDS accesses of the lanes of one wave keep their order across it.
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-// Threads that deal with a list together: the work-group, or one wave of it alone,
-// which needs no barriers.
-struct Group {
-    bool solo;
-    __device__ __forceinline__ int size() const { return solo ? kWave : kThreads; }
-    __device__ __forceinline__ void sync() const {
-        wave_fence();
-        if (!solo) __syncthreads();
-    }
-};
+// *at becomes the first thread for which `is` holds, where that is below it; of a
+// wave one lane tells, as LDS would take the lanes one after the other.
+__device__ __forceinline__ void first_thread(bool is, int* at) {
+    const uint64_t mask = __ballot(is);
+    if (mask && threadIdx.x % kWave == 0) atomicMin(at, static_cast<int>(threadIdx.x) + __ffsll(static_cast<unsigned long long>(mask)) - 1);
+}
 
 // Sum over the work-group, in a fixed order, on every thread.
 __device__ __forceinline__ double block_sum(double v, Shared& sh) {
@@ -457,7 +453,6 @@ __device__ __forceinline__ uint32_t edge(const Row& r, F&& holds) {
     return hi;
 }
 
-constexpr int kSolo = 256;  // tokens that one wave deals with alone
 constexpr int kDigit = 9;
 
 // By wave 0: the first of 512 amounts up to which they add up to the goal (with
@@ -490,16 +485,100 @@ struct Targets {
     double count, mass;
     bool share, draw;
 };
+// w in units of 2^-50: the low bits of w + 4.
+__device__ __forceinline__ uint64_t amount_of(double w) {
+    return static_cast<uint64_t>(__double_as_longlong(w + 4.0) - __double_as_longlong(4.0));
+}
+// The running sum that a mass to keep, and the one that a draw, has to reach.
+__device__ __forceinline__ uint64_t goal_of(double t, uint64_t sum) { return min(t >= 1.0 ? static_cast<uint64_t>(ceil(t)) : 1, sum); }
+__device__ __forceinline__ uint64_t goal_of_draw(double u, uint64_t sum) { return min(static_cast<uint64_t>(u * static_cast<double>(sum)) + 1, sum); }
+
+// The draw from a few tokens: four threads compare each with a quarter of all, which
+// gives their ranks; their amounts, put in that order, are summed up over a wave's lanes.
+constexpr int kFew = 256;
+constexpr int kFewParts = kThreads / kFew, kPlaces = kFew / kWave;
+// How many of others[n] come above this thread's (nothing, 0, is above none), to rank[].
+template <class V, class F>
+__device__ __forceinline__ void rank_of(V mine, int n, int* rank, F&& other) {
+    const int part = threadIdx.x / kFew, per = (n + kFewParts - 1) / kFewParts;
+    int above = 0;
+#pragma unroll 4
+    for (int i = part * per; i < min((part + 1) * per, n); ++i) above += other(i) > mine;
+    if (mine && above) atomicAdd(rank + threadIdx.x % kFew, above);
+    __syncthreads();
+}
+struct Few {
+    uint64_t upto[kPlaces], total;  // of this lane's places, of all
+    // by one or more whole waves alike: the first n places
+    __device__ __forceinline__ Few(const uint64_t* place, int n) {
+        const int at = kPlaces * (threadIdx.x % kWave);
+        uint64_t mine = 0;
+#pragma unroll
+        for (int e = 0; e < kPlaces; ++e) upto[e] = mine += at + e < n ? place[at + e] : 0;
+        const uint64_t before = wave_scan(mine) - mine;
+#pragma unroll
+        for (int e = 0; e < kPlaces; ++e) upto[e] += before;
+        total = of_lane(upto[kPlaces - 1], kWave - 1);
+    }
+    // the first place where they reach the goal, which is not above the total
+    __device__ __forceinline__ int reach(uint64_t goal) const {
+        int short_of = 0;
+#pragma unroll
+        for (int e = 0; e < kPlaces; ++e) short_of += __popcll(__ballot(upto[e] < goal));
+        return short_of;
+    }
+};
+__device__ __forceinline__ void draw_of_few(const Row& r, int n, const Targets& to, double u, int32_t* token, float* logprob, Shared& sh) {
+    const int tid = threadIdx.x, at = tid % kFew;
+    int* rank = reinterpret_cast<int*>(sh.mass);              // [2][kFew]: by logit, by index
+    uint64_t* place = reinterpret_cast<uint64_t*>(sh.w);      // [2][kFew]
+    uint32_t* index = reinterpret_cast<uint32_t*>(place + 2 * kFew);  // [kFew] of the kept, ~: larger is earlier
+    if (tid < 2 * kFew) {
+        rank[tid] = 0;
+        place[tid] = 0;
+    }
+    // larger keys first, then smaller indices
+    const uint64_t order = at < n ? sh.list[at] ^ 0xFFFFFFFFu : 0;
+    const bool mine = tid < kFew && at < n;
+    const double w = mine ? r.w(value_of(static_cast<uint32_t>(order >> 32))) : 0.0;
+    const uint64_t amount = amount_of(w);
+    __syncthreads();
+    rank_of(order, n, rank, [&](int i) { return sh.list[i] ^ 0xFFFFFFFFu; });
+    if (mine) place[rank[at]] = amount;
+    __syncthreads();
+    if (tid < kFew) {
+        int keeps = to.count > 0.0 ? min(n, static_cast<int>(to.count)) : n;
+        if (to.mass > 0.0) {
+            const Few f(place, keeps);
+            keeps = min(keeps, f.reach(goal_of(to.mass * (to.share ? static_cast<double>(f.total) : 0x1p50), f.total)) + 1);
+        }
+        index[tid] = mine && rank[at] < keeps && w >= r.min_p ? static_cast<uint32_t>(order) : 0;
+    }
+    __syncthreads();
+    rank_of(index[at], n, rank + kFew, [&](int i) { return index[i]; });
+    if (mine && index[at]) place[kFew + rank[kFew + at]] = amount;
+    __syncthreads();
+    if (tid >= kFew) return;
+    const Few f(place + kFew, kFew);
+    const int drawn = f.reach(goal_of_draw(u, f.total));
+    if (mine && index[at] && rank[kFew + at] == drawn) {
+        *token = static_cast<int32_t>(~index[at]);
+        if (logprob) *logprob = static_cast<float>(log(w * 0x1p50 / static_cast<double>(f.total)));
+    }
+}
+
 // Of bf16 logits the keys' upper 16 bits say which (low_bits 16).
 __device__ __forceinline__ Cut cut_list(const Row& r, int n, uint32_t least, int low_bits, const Targets& to, double u,
                                         int32_t* token, float* logprob, Shared& sh) {
     constexpr uint32_t kDigits = 1u << kDigit;
-    const Group g{to.draw && n <= kSolo};
     const int tid = threadIdx.x;
     Cut cut{0, r.n};
-    if (g.solo && tid >= kWave) return cut;
+    if (to.draw && n <= kFew) {
+        draw_of_few(r, n, to, u, token, logprob, sh);
+        return cut;
+    }
 #pragma unroll 1
-    for (int i = tid; i < n; i += g.size()) sh.w[i] = r.w(value_of(static_cast<uint32_t>(sh.list[i] >> 32)));
+    for (int i = tid; i < n; i += kThreads) sh.w[i] = r.w(value_of(static_cast<uint32_t>(sh.list[i] >> 32)));
     const uint32_t top = key_of(r.M) >> low_bits, depth = top - (least >> low_bits);
     uint64_t rest = 0;  // of the goal, for the ones that equal the last by key
     // 0, 1: count by key, by index; 2, 3: mass; 4: the draw
@@ -512,30 +591,27 @@ __device__ __forceinline__ Cut cut_list(const Row& r, int n, uint32_t least, int
         uint64_t goal = 0, before = 0, sum = 0;
 #pragma unroll 1
         for (int shift = shift0; shift >= 0; shift -= kDigit) {
-            g.sync();
+            __syncthreads();
 #pragma unroll 1
-            for (int b = tid; b < static_cast<int>(kDigits); b += g.size()) sh.mass[b] = 0;
-            g.sync();
+            for (int b = tid; b < static_cast<int>(kDigits); b += kThreads) sh.mass[b] = 0;
+            __syncthreads();
 #pragma unroll 1
-            for (int i = tid; i < n; i += g.size()) {
+            for (int i = tid; i < n; i += kThreads) {
                 const uint64_t t = sh.list[i];
                 const uint32_t key = static_cast<uint32_t>(t >> 32), idx = static_cast<uint32_t>(t), v = by_key ? top - (key >> low_bits) : idx;
                 const double w = sh.w[i];
                 bool in = cut.keeps(key, static_cast<int>(idx)) && (shift == shift0 || v >> (shift + kDigit) == value);
                 if (!by_key) in = in && (draw ? w >= r.min_p : key >> low_bits == cut.key >> low_bits);
-                // w in units of 2^-50: the low bits of w + 4
-                const uint64_t amount = step < 2 ? 1 : static_cast<uint64_t>(__double_as_longlong(w + 4.0) - __double_as_longlong(4.0));
+                const uint64_t amount = step < 2 ? 1 : amount_of(w);
                 if (in) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[v >> shift & (kDigits - 1)]), static_cast<unsigned long long>(amount));
             }
-            g.sync();
+            __syncthreads();
             if (tid < kWave) {
                 const uint64_t mine = eight(sh);
                 if (shift == shift0) {  // the goal, as of the sum
                     sum = wave_total(mine);
                     const double t = step == 0 ? to.count : to.share ? to.mass * static_cast<double>(sum) : to.mass * 0x1p50;
-                    goal = by_key ? t >= 1.0 ? static_cast<uint64_t>(ceil(t)) : 1
-                                  : draw ? static_cast<uint64_t>(u * static_cast<double>(sum)) + 1 : rest;
-                    goal = min(goal, sum);
+                    goal = by_key ? goal_of(t, sum) : draw ? goal_of_draw(u, sum) : min(rest, sum);
                     if (tid == 0) {
                         sh.goal = goal;
                         sh.sum = sum;
@@ -543,7 +619,7 @@ __device__ __forceinline__ Cut cut_list(const Row& r, int n, uint32_t least, int
                 }
                 find_digit(before, goal, mine, sh);
             }
-            g.sync();
+            __syncthreads();
             goal = sh.goal;
             sum = sh.sum;
             before = sh.before;
@@ -557,7 +633,7 @@ __device__ __forceinline__ Cut cut_list(const Row& r, int n, uint32_t least, int
             if (goal < sum) cut.last = static_cast<int>(value);  // else all of the equal ones
         } else {
 #pragma unroll 1
-            for (int i = tid; i < n; i += g.size())
+            for (int i = tid; i < n; i += kThreads)
                 if (static_cast<uint32_t>(sh.list[i]) == value) {
                     *token = static_cast<int32_t>(value);
                     if (logprob) *logprob = static_cast<float>(log(sh.w[i] * 0x1p50 / static_cast<double>(sum)));
@@ -600,7 +676,7 @@ __device__ __forceinline__ Found find_bin(const Pieces<T>& p, const Row& r, cons
     if (tid == kBins - 2) sh.found_d = upto;
     __syncthreads();
     const double aim = by_mass ? target * sh.found_d : target;
-    if (has && upto >= aim) atomicMin(&sh.found, tid);
+    first_thread(has && upto >= aim, &sh.found);
     __syncthreads();
     f.bin = sh.found;
     if (tid == f.bin) sh.above_d = upto - mine;
@@ -786,7 +862,7 @@ __device__ __forceinline__ Found find_bin_of_slices(const SampleArgs& a, int row
     __syncthreads();
     Found f;
     f.z = sh.found_d;
-    if (has && upto >= prob * f.z) atomicMin(&sh.found, tid);
+    first_thread(has && upto >= prob * f.z, &sh.found);
     __syncthreads();
     f.bin = sh.found;
     if (tid == f.bin) sh.above_d = upto - mine;
@@ -859,10 +935,9 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
         __syncthreads();
         z = uniform(sh.found_d);
         target = want.u * z;
-        if (mine > 0.0) {
-            if (upto > target) atomicMin(&sh.found, tid);
-            atomicMax(&sh.digit, tid);  // the last with any mass, where rounding leaves none
-        }
+        first_thread(mine > 0.0 && upto > target, &sh.found);
+        const uint64_t any = __ballot(mine > 0.0);  // the last with any mass, where rounding leaves none
+        if (any && lane == 0) atomicMax(&sh.digit, tid + 63 - __clzll(static_cast<long long>(any)));
         __syncthreads();
         const int range = uniform(sh.found < kThreads ? sh.found : sh.digit), width = slice_pieces(p.count, a.slices) / kWaves;
         if (tid == range) sh.above_d = upto - mine;
