@@ -43,6 +43,7 @@ constexpr int kBins = 768;          // 16 for an octave; the last one holds w < 
 constexpr int kHeld = 4096;         // 16 bytes each of a slice that wait in LDS to be weighed
 constexpr int kQueue = 8 * kWave + 64;  // logits a wave has queued: a piece of every lane beside 63 left over
 constexpr int kMost = 4096;         // most groups of threads of a row whose largest logits are kept
+constexpr int kMostSlices = 16;     // of a row
 constexpr int kList = 4096;         // tokens sorted in LDS
 
 struct SampleArgs {
@@ -132,8 +133,8 @@ struct Shared {
     __attribute__((aligned(16))) float ends[16];
     double root[16];
     double red_d[kWaves];
-    uint64_t best[16];  // of the slices
-    int32_t ref[16];
+    uint64_t best[kMostSlices];
+    int32_t ref[kMostSlices];
     uint64_t goal, sum, before;
     double found_d, above_d;
     int n_list, n_groups, found, digit;
@@ -212,6 +213,23 @@ __device__ __forceinline__ double block_sum(double v, Shared& sh) {
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) v += sh.red_d[w];
     return v;
+}
+
+// Of the waves' sums in sh.red_d, which follow `before`: the first at which the running
+// sum passes u of all (or, once that is known, `target`), else the last with any mass.
+struct Part {
+    int at;
+    double before, total;
+};
+__device__ __forceinline__ Part find_part(double before, double u, double target, Shared& sh) {
+    const int lane = threadIdx.x % kWave;
+    const double mine = lane < kWaves ? sh.red_d[lane] : 0.0, upto = before + wave_scan(mine);
+    Part p;
+    p.total = of_lane(upto, kWave - 1);
+    const uint64_t some = __ballot(mine > 0.0), here = __ballot(mine > 0.0 && upto > (u >= 0.0 ? u * p.total : target));
+    p.at = here ? __ffsll(static_cast<unsigned long long>(here)) - 1 : max(63 - __clzll(static_cast<long long>(some)), 0);
+    p.before = p.at > 0 ? of_lane(upto, p.at - 1) : before;
+    return p;
 }
 
 // Inclusive sums over the work-group's threads, in thread order.
@@ -367,7 +385,7 @@ __device__ __forceinline__ int slice_pieces(int count, int slices) {
 __device__ __forceinline__ int group_size(int slices) { return max(1, slices * kThreads / kMost); }
 
 // Tokens of `in` from `lo` up and below `hi` (none: +inf), in LDS (in any order); how many there are, of
-// which the first kList are there.  Where at most half of the groups of threads have
+// which the first kList are there, or any number above kList.  Where at most half of the groups of threads have
 // such a token, only their pieces are read.
 template <class T>
 __device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float lo, float hi, const Cut& in,
@@ -384,7 +402,7 @@ __device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float l
             const int at = atomicAdd(&sh.n_groups, 1);
             if (at < kMost / 2) sh.groups[at] = static_cast<uint16_t>(s * kThreads + threadIdx.x);
         }
-    auto look = [&](const float (&x)[8], int v, const typename Pieces<T>::Raw& raw) {
+    auto look = [&](const float (&x)[8], int v) {
         uint32_t keeps = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) keeps |= x[e] >= from && !(x[e] >= below) ? 1u << e : 0u;
@@ -419,12 +437,29 @@ __device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float l
             const int slice = group / in_slice, v = slice * per + group % in_slice * size + i % size + i / size * kThreads;
             if (v >= p.count) continue;
             float x[8];
-            const typename Pieces<T>::Raw raw = p.ask(v);
-            p.spread(raw, v, x);
-            look(x, v, raw);
+            p.load(v, x);
+            look(x, v);
         }
     } else {
-        each_piece<4>(p, threadIdx.x, p.count, kThreads, look);
+        // first which pieces have any, 32 of a thread at a time; a wave has one in most of its
+        // rounds, and would go through all of `look` in each
+#pragma unroll 1
+        for (int v0 = threadIdx.x; v0 < p.count; v0 += 32 * kThreads) {
+            uint32_t pending = 0;
+            each_piece<4>(p, v0, min(v0 + 32 * kThreads, p.count), kThreads, [&](const float (&x)[8], int v, const typename Pieces<T>::Raw&) {
+                bool any = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) any |= x[e] >= from && !(x[e] >= below);
+                pending |= any ? 1u << (v - v0) / kThreads : 0u;
+            });
+#pragma unroll 1
+            for (; pending && *static_cast<volatile int*>(&sh.n_list) <= kList; pending &= pending - 1) {
+                const int v = v0 + (__ffs(pending) - 1) * kThreads;
+                float x[8];
+                p.load(v, x);
+                look(x, v);
+            }
+        }
     }
     __syncthreads();
     const int n = sh.n_list;
@@ -1034,16 +1069,18 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
         double s = 0.0;
         if (wave < a.slices && sh.best[wave]) {
             const int down = ref - sh.ref[wave], width = slice_pieces(p.count, a.slices);
-            int n;
+            // bins 64 apart are four octaves apart
+            const uint64_t* bins = a.bins + (slice0 + wave) * kBins;
 #pragma unroll 4
-            for (int b = down + lane; b < min(bin, down + kBins - 1); b += kWave)
-                s += static_cast<double>(a.bins[(slice0 + wave) * kBins + b - down]) * 0x1p-42 *
-                     r.weight_from(ref - b - static_cast<double>(r.M) * r.c16, 0, n);
+            for (int b = (min(bin - down, kBins - 1) - 1 - lane) / kWave * kWave + lane; b >= 0; b -= kWave)
+                s = s * 0x1p-4 + (b < bin - down ? static_cast<double>(bins[b]) : 0.0);
+            int n;
+            s *= 0x1p-42 * r.weight_from(ref - down - lane - static_cast<double>(r.M) * r.c16, 0, n);
 #pragma unroll 1
             for (int i = lane; i < listed; i += kWave) {
                 const uint64_t t = sh.list[i];
                 const int idx = static_cast<int>(static_cast<uint32_t>(t));
-                if ((idx + p.shift) / 8 / width == wave && cut.keeps(static_cast<uint32_t>(t >> 32), idx))
+                if (idx + p.shift - 8 * width * wave >= 0 && idx + p.shift - 8 * width * (wave + 1) < 0 && cut.keeps(static_cast<uint32_t>(t >> 32), idx))
                     s += r.w(value_of(static_cast<uint32_t>(t >> 32)));
             }
         }
@@ -1051,21 +1088,11 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
         __syncthreads();
         if (lane == 0) sh.red_d[wave] = s;
         __syncthreads();
-        int at = 0;
-        double run = 0.0;
-#pragma unroll 1
-        for (int i = 0; i < kWaves; ++i) z += sh.red_d[i];
-        z = uniform(z);
+        const Part part = find_part(0.0, want.u, 0.0, sh);
+        z = part.total;
         target = want.u * z;
-#pragma unroll 1
-        for (int i = 0; i < kWaves; ++i) {
-            if (sh.red_d[i] <= 0.0) continue;
-            at = i;
-            before = run;
-            run += sh.red_d[i];
-            if (run > target) break;
-        }
-        from = at * slice_pieces(p.count, a.slices);
+        before = part.before;
+        from = part.at * slice_pieces(p.count, a.slices);
         to = min(from + slice_pieces(p.count, a.slices), p.count);
         summed = true;
     }
@@ -1113,25 +1140,14 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
         __syncthreads();
         if (lane == 0) sh.red_d[wave] = s;
         __syncthreads();
+        const Part part = find_part(before, summed ? -1.0 : want.u, target, sh);
         if (!summed) {
-#pragma unroll 1
-            for (int i = 0; i < kWaves; ++i) z += sh.red_d[i];
+            z = part.total;
             target = want.u * z;
             summed = true;
         }
-        // the first in which the sum passes the target; the last with any mass, where rounding leaves none
-        int at = 0;
-        double run = before, at_before = before;
-#pragma unroll 1
-        for (int i = 0; i < kWaves; ++i) {
-            if (sh.red_d[i] <= 0.0) continue;
-            at = i;
-            at_before = run;
-            run += sh.red_d[i];
-            if (run > target) break;
-        }
-        before = at_before;
-        from += at * per;
+        before = part.before;
+        from += part.at * per;
         to = min(from + per, to);
     }
     if (wave > 0) return;
@@ -1173,7 +1189,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
 // Slices of a row, a power of two: work-groups for two rounds of the chip, a piece a thread at least.
 int sample_slices(int rows, int vocab) {
     int slices = 1;
-    while (slices < 16 && slices * static_cast<int64_t>(rows) < 1024 && slices * 8 * kThreads < vocab) slices *= 2;
+    while (slices < kMostSlices && slices * static_cast<int64_t>(rows) < 1024 && slices * 8 * kThreads < vocab) slices *= 2;
     return slices;
 }
 
