@@ -7,26 +7,34 @@
 // token kept, and no row is ever sorted.  A row is cut into slices, so that a few
 // rows fill the chip, and dealt with by two kernels:
 //   1. a slice's largest logit and, as the row needs them, the largest of every
-//      thread (top_k), the mass of the tokens in bins of 1/16 octave of w (top_p),
+//      thread (any filter), the mass of the tokens in bins of 1/16 octave of w (top_p),
 //      or the mass of sixteenths of the slice (no filter);
 //   2. a row's token.  top_k up to the number of threads: the k-th largest of the
 //      threads' largest bounds the k-th largest logit from below, and what is not
-//      below it, a little more than k tokens, is collected in LDS.  top_p: the running sum
-//      over bins says in which one the cut is; the tokens down to that bin are
-//      collected, or where they are too many those of the bin alone.  Cuts and the
-//      draw are one thing there, the first value of an order at which a running sum
-//      reaches a target, found digit by digit with a histogram: by logit and count
-//      for top_k, by logit and mass for top_p, by index and mass for the draw.  Where
-//      more tokens are kept than were collected, or all, sums over ranges of the row
-//      say in which the running sum passes u Z, then over sixteenths of that range,
-//      and so on.
-// The second kernel is a chain of short steps that meet their code cold, so it is
-// written in loops of few instructions rather than unrolled.
+//      below it, a little more than k tokens, is collected in LDS, from those threads'
+//      pieces alone.  top_p: the running sum over bins says in which one the cut is; the
+//      tokens down to that bin are collected, or where they are too many those of the
+//      bin alone.  A short list is drawn from by ranks.  In a longer one cuts and the draw
+//      are one thing, the first value of an order at which a running sum reaches a
+//      target, found digit by digit with a histogram: by logit and count for top_k, by
+//      logit and mass for top_p, by index and mass for the draw.  Where more tokens are
+//      kept than were collected, or all, sums over ranges of the row say in which the
+//      running sum passes u Z, then over sixteenths of that range, and so on.
 //
-// Every mass is held in 64 bits: w from an exponential good to 2^-37, bins and
+// Every mass is held in 64 bits: w from an exponential good to 2^-36, bins and
 // lists in fixed point (integer sums: the order of the atomics does not matter),
 // all else in doubles summed in a fixed order.  With fp32 sums one draw in a few
 // hundred would be another token.
+//
+// What bounds it.  A few rows: latency.  One row of 32768 with top_k and top_p takes 16.4 us:
+// 5 for the first kernel, 2.5 between the two, 9 for a chain of some 25 steps with a
+// barrier each, which meet their code cold and so are loops of few instructions rather
+// than unrolled.  256 rows of 131072 bf16 logits (67 MB, 13 us at a copy's rate): greedy 18.6 us;
+// top_k 42 (18 + 19 us of kernels); no filter 51 and top_p 92, where the first kernel's
+// fp64 instructions take 36 and 40 us (some 12 a token at 8 clocks a wave), and a nucleus
+// beyond the list takes the second kernel 50: a pass for the bin's tokens, then sums over
+// its slice and over the slice's sixteenths.  Slices: two rounds of work-groups; with four
+// the first kernel takes 50 us rather than 40, with one the second 68 rather than 60.
 #include <math.h>
 
 #include <algorithm>
@@ -40,7 +48,7 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 constexpr int kBins = 768;          // 16 for an octave; the last one holds w < 2^-47 and is weighed nowhere
-constexpr int kHeld = 4096;         // 16 bytes each of a slice that wait in LDS to be weighed
+constexpr int kHeld = 4096;         // 16 bytes each of a slice that wait in LDS to be weighed (256 rows top_p 43 us; read again 44)
 constexpr int kQueue = 8 * kWave + 64;  // logits a wave has queued: a piece of every lane beside 63 left over
 constexpr int kMost = 4096;         // most groups of threads of a row whose largest logits are kept
 constexpr int kMostSlices = 16;     // of a row
@@ -530,6 +538,7 @@ __device__ __forceinline__ uint64_t goal_of_draw(double u, uint64_t sum) { retur
 
 // The draw from a few tokens: four threads compare each with a quarter of all, which
 // gives their ranks; their amounts, put in that order, are summed up over a wave's lanes.
+// 3.2 us for 20 tokens and 5 for 120, where digits take some eight rounds of 1.1.
 constexpr int kFew = 256;
 constexpr int kFewParts = kThreads / kFew, kPlaces = kFew / kWave;
 // How many of others[n] come above this thread's (nothing, 0, is above none), to rank[].
