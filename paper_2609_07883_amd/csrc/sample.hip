@@ -33,8 +33,7 @@
 // top_k 42 (18 + 19 us of kernels); no filter 51 and top_p 92, where the first kernel's
 // fp64 instructions take 36 and 40 us (some 12 a token at 8 clocks a wave), and a nucleus
 // beyond the list takes the second kernel 50: a pass for the bin's tokens, then sums over
-// its slice and over the slice's sixteenths.  Slices: two rounds of work-groups; with four
-// the first kernel takes 50 us rather than 40, with one the second 68 rather than 60.
+// its slice and over the slice's sixteenths.
 #include <math.h>
 
 #include <algorithm>
@@ -1195,10 +1194,16 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
     if (logprob) *logprob = static_cast<float>(log(wb / z));
 }
 
-// Slices of a row, a power of two: work-groups for two rounds of the chip, a piece a thread at least.
-int sample_slices(int rows, int vocab) {
+// Slices of a row, a power of two: a work-group for every CU, of a piece a thread at
+// least, and of four at most.  us with slices of 8192 / 16384 / 32768 / 65536 tokens: 64
+// rows of 131072 with top_p 72 / 65 / 62 / -, with no filter 33 / 28 / 26 / -; 256 rows - / - / 91 / 99;
+// 256 rows of 32768 62 / 57 / 53 and with top_k 36 / 31 / 36; 8 rows with no filter 18 / 21.
+constexpr int kLongSlice = 4 * 8 * kThreads;
+int sample_slices(int64_t rows, int vocab) {
     int slices = 1;
-    while (slices < kMostSlices && slices * static_cast<int64_t>(rows) < 1024 && slices * 8 * kThreads < vocab) slices *= 2;
+    while (slices < kMostSlices && slices * 8 * kThreads < vocab && (slices * rows < 256 || slices * kLongSlice < vocab) &&
+           2 * slices * rows < 1 << 22)  // what a grid can have of 1024 threads
+        slices *= 2;
     return slices;
 }
 
@@ -1242,9 +1247,9 @@ extern "C" int slw_sample_workspace_size(int32_t max_rows, int32_t vocab, size_t
         if (max_rows > SLW_SAMPLE_MAX_ROWS) return fail(SLW_EUNSUPPORTED, "more than %d rows", SLW_SAMPLE_MAX_ROWS);
         if (vocab < 1 || vocab > SLW_SAMPLE_MAX_VOCAB)
             return fail(SLW_EUNSUPPORTED, "vocab must be in [1, %d] (got %d)", SLW_SAMPLE_MAX_VOCAB, vocab);
-        // the slices of a call are fewer than twice 1024, or as many as its rows, and those of one row each at most
-        const size_t rows = static_cast<size_t>(max_rows);
-        *bytes = rows ? sample_layout(std::min(std::max<size_t>(rows, 2047), rows * sample_slices(1, vocab)), rows).end : 0;
+        // the slices of a call are fewer than twice 256, or those that the vocabulary asks for, and those of one row each at most
+        const size_t rows = static_cast<size_t>(max_rows), of_any = sample_slices(1, vocab), of_many = sample_slices(256, vocab);
+        *bytes = rows ? sample_layout(std::min(std::max<size_t>(rows * of_many, 511), rows * of_any), rows).end : 0;
         return SLW_OK;
     });
 }
