@@ -83,9 +83,9 @@ __device__ __forceinline__ float value_of(uint32_t key) {
     return __uint_as_float(key ^ (key & 0x80000000u ? 0x80000000u : 0xFFFFFFFFu));
 }
 
-// Sixteenths of an octave from logit 0, whole.  Never falls as x grows; where it is
-// within kNear, single precision moves few x to the next one, past a half by 2^-6 at most.
-constexpr double kNear = 0x1p17;
+// Sixteenths of an octave from logit 0, whole.  Never falls as x grows; near enough to
+// 0, single precision moves few x to the next one, past a half by 2^-6 at most.
+__device__ __forceinline__ bool near_zero(float x, double c16) { return fabs(static_cast<double>(x)) * c16 <= 0x1p17 && c16 <= 0x1p100; }
 __device__ __forceinline__ float sixteenth(float x, float c16) { return rintf(x * c16); }
 
 // How w depends on x.  In a row that has +inf those tokens alone have mass.
@@ -837,7 +837,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_slices_kernel(SampleArgs a
         // By bins of whole sixteenths of an octave, which all slices share; in units of
         // 2^-42 of the bin's w, the low bits of a number near 2^10.  Far from logit 0 single
         // precision knows no sixteenths: such a slice has no bins.
-        const bool near = fabs(static_cast<double>(m)) * want.c16 <= kNear;
+        const bool near = near_zero(m, want.c16);
         const float c = static_cast<float>(want.c16), first = near ? sixteenth(m, c) : -0x1p30f, floor = first - kBins;
         const int ref = uniform(static_cast<int>(first));
         if (tid == 0) a.ref[slice] = ref;
@@ -992,7 +992,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
     }
 
     // the slices' bins count, where sixteenths from 0 on are as good as from M on
-    const bool slices = want.by_mass() && !r.at_inf && fabs(static_cast<double>(r.M)) * r.c16 <= kNear;
+    const bool slices = want.by_mass() && !r.at_inf && near_zero(r.M, r.c16);
     const float c16 = static_cast<float>(r.c16);
     const int ref = slices ? static_cast<int>(sixteenth(r.M, c16)) : 0;
     auto bin_of = [&](float x) {  // a whole number; far down beyond any int

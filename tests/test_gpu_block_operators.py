@@ -417,6 +417,19 @@ def test_sample_of_odd_parameters():
             _check(x, u=u, **par)
 
 
+@pytest.mark.parametrize("temperature", [1e-44, 1e-38, 7e-38, 1e-30, 1e-20])
+def test_sample_of_tiny_temperatures_with_0_on_top(temperature):
+    """The largest logit 0 is no sixteenth of an octave from itself at any temperature, and all others are beyond any count."""
+    rng = np.random.default_rng(15)
+    x = -np.abs(rng.standard_normal((4, 20000)))
+    x[0, 7] = x[0, 19000] = 0
+    x[1, :4] = -0.0
+    x[2] = 0
+    x[3] = np.where(rng.random(20000) < 0.5, 0.0, -1e-38)
+    for par in (dict(top_p=0.9), dict(top_p=0.5, min_p=0.1), dict(top_k=3, top_p=0.9), dict()):
+        _check(x, True, temperature=temperature, u=rng.random(4), **par)
+
+
 def test_sample_of_the_largest_vocabulary():
     rng = np.random.default_rng(10)
     x = rng.standard_normal((3, 1 << 20)) * 2
