@@ -31,8 +31,7 @@
 // barrier each, which meet their code cold and so are loops of few instructions rather
 // than unrolled.  256 rows of 131072 bf16 logits (67 MB, 13 us at a copy's rate): greedy 18.6 us;
 // top_k 42 (18 + 19 us of kernels); no filter 51 and top_p 92, where the first kernel's
-// fp64 instructions take 36 and 40 us (some 12 a token at 8 clocks a wave), and a nucleus
-// beyond the list takes the second kernel 50: a pass for the bin's tokens, then sums over
+// instructions take 36 and 40 us (24 a token, half of them fp64), and a nucleus beyond the list takes the second kernel 50: a pass for the bin's tokens, then sums over
 // its slice and over the slice's sixteenths.
 #include <math.h>
 
