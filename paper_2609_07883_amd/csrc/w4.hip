@@ -559,14 +559,16 @@ W4Plan plan_w4(const W4Shape& s, int m, bool gated) {
     W4Plan p{};
     p.splits = 1;
     // Some rows: the ring, where its 128 columns a work-group, with k split in parts of
-    // eight steps at least, make some 200 of them.  us with the ring / the stream kernel:
-    // 32 rows of 14336 -> 4096 16.0 / 18.5, of 4096 -> 28672 21.7 / 25.1, 23 of 4096 -> 100003
-    // 55.5 / 69.2, 16 of them 51.3 / 55.8; but 32 of 4096 -> 4096 11.2 / 10.1 and 16 of 4096 ->
-    // 28672 18.2 / 17.8.  64 rows against the tile kernel: 27.5 / 31.1, 19.6 / 22.8, 13.7 / 14.1.
-    if (m <= 64 && (m > 32 || (m > 16 && (s.tiles >= 512 || s.steps >= 64)) || (m > 8 && s.tiles >= 4096))) {
+    // four steps at least, make some 200 of them.  us with the ring / the stream kernel:
+    // 32 rows of 14336 -> 4096 16.0 / 18.5, of 4096 -> 28672 21.7 / 25.1, of 4096 -> 6144 11.7 / 14.2,
+    // 23 of 4096 -> 100003 55.5 / 69.2, 16 of them 51.3 / 55.8; but 32 of 4096 -> 4096 11.2 / 10.1
+    // and 16 of 4096 -> 28672 18.2 / 17.8.  64 rows against the tile kernel: 27.5 / 31.1, 19.6 /
+    // 22.8, 13.7 / 14.1.  Parts of eight steps: 64 rows of 14336 -> 2048 17.8, of seven 16.4.
+    // (One work-group a CU with nine steps in its ring rather than four: 12.4 / 10.9, 19.1 / 16.0.)
+    if (m <= 64 && (m > 32 || (m > 16 && (s.tiles >= 384 || s.steps >= 64)) || (m > 8 && s.tiles >= 4096))) {
         p.kind = 2;
         p.mt = m <= 16 ? 1 : m <= 32 ? 2 : 4;
-        while (ceil_div(s.tiles, 8) * p.splits * 2 <= 256 && p.splits * 2 * 8 <= s.steps) p.splits *= 2;
+        while (ceil_div(s.tiles, 8) * p.splits * 2 <= 256 && p.splits * 2 * 4 <= s.steps) p.splits *= 2;
         p.splits = static_cast<int>(ceil_div(s.steps, ceil_div(s.steps, p.splits)));
         return p;
     }
