@@ -544,6 +544,7 @@ W4Shape w4_shape(int n, int k, bool gated) {
     return s;
 }
 
+constexpr int kMostSplits = 32;  // the join reads them one after the other: 23 rows of 65536 -> 64 take 20 us, with 128 36
 // Most waves of a stream work-group.
 constexpr int kStreamWaves = 8;
 
@@ -568,7 +569,7 @@ W4Plan plan_w4(const W4Shape& s, int m, bool gated) {
     if (m <= 64 && (m > 32 || (m > 16 && (s.tiles >= 384 || s.steps >= 64)) || (m > 8 && s.tiles >= 4096))) {
         p.kind = 2;
         p.mt = m <= 16 ? 1 : m <= 32 ? 2 : 4;
-        while (ceil_div(s.tiles, 8) * p.splits * 2 <= 256 && p.splits * 2 * 4 <= s.steps) p.splits *= 2;
+        while (ceil_div(s.tiles, 8) * p.splits * 2 <= 256 && p.splits * 2 * 4 <= s.steps && p.splits < kMostSplits) p.splits *= 2;
         p.splits = static_cast<int>(ceil_div(s.steps, ceil_div(s.steps, p.splits)));
         return p;
     }
@@ -580,7 +581,7 @@ W4Plan plan_w4(const W4Shape& s, int m, bool gated) {
         // split for the wide waves instead: 16 rows of 14336 -> 4096 14.3 / 19.0, 8 13.3 / 13.4.
         const bool wide = m > 16 || (m > 8 && s.steps >= 64);
         p.nt = wide || s.tiles >= 1024 ? 4 : gated || s.tiles >= 384 ? 2 : 1;
-        while (wide && ceil_div(s.tiles, p.nt) * p.splits < 256 && p.splits * 2 * 8 <= s.steps) p.splits *= 2;
+        while (wide && ceil_div(s.tiles, p.nt) * p.splits < 256 && p.splits * 2 * 8 <= s.steps && p.splits < kMostSplits) p.splits *= 2;
         p.waves = std::min(p.nt == 4 && p.splits == 1 ? 4 : kStreamWaves, s.words);
         return p;
     }
