@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import numpy as np
@@ -82,22 +83,15 @@ class RopeC(C.Structure):
                 ("high", C.c_double), ("freq", C.c_void_p), ("mscale", C.c_float)]
 
 
-class NormArgsC(C.Structure):
-    _fields_ = [("resid", C.c_void_p), ("block", C.c_void_p), ("post_gain", C.c_void_p), ("gate", C.c_void_p),
-                ("gain", C.c_void_p), ("resid_out", C.c_void_p), ("out", C.c_void_p), ("ld_resid", C.c_int64),
-                ("ld_block", C.c_int64), ("ld_gate", C.c_int64), ("ld_resid_out", C.c_int64), ("ld_out", C.c_int64),
-                ("rows", C.c_int32), ("d", C.c_int32), ("resid_f32", C.c_int32), ("scale", C.c_float),
-                ("eps", C.c_float)]
+# slw_norm_args and slw_sample_args, packed anew by each call (a ctypes structure takes four times as long to fill):
+# resid, block, post_gain, gate, gain, resid_out, out; their five strides; rows, d, resid_f32; scale, eps
+NORM_ARGS = struct.Struct("@7P5q3i2f4x")
+# logits; ld; rows, vocab, logits_f32; temperature, top_k, top_p, min_p, u, tokens, logprob
+SAMPLE_ARGS = struct.Struct("@Pq3i7P")
 
 
 class W4C(C.Structure):
     _fields_ = [("packed", C.c_void_p), ("n", C.c_int32), ("k", C.c_int32), ("gated", C.c_int32)]
-
-
-class SampleArgsC(C.Structure):
-    _fields_ = [("logits", C.c_void_p), ("ld", C.c_int64), ("rows", C.c_int32), ("vocab", C.c_int32),
-                ("logits_f32", C.c_int32), ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p),
-                ("min_p", C.c_void_p), ("u", C.c_void_p), ("tokens", C.c_void_p), ("logprob", C.c_void_p)]
 
 
 ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3, "table": 4}
@@ -172,13 +166,13 @@ def lib() -> C.CDLL:
         "slw_attn_attend": ([vp, vp, i32, vp, i64, vp, vp], C.c_int),
         "slw_attn_end": ([vp], C.c_int),
         "slw_attn_rotate": ([vp, vp, P(RopeC), vp, vp, i64, vp, vp, i64, vp], C.c_int),
-        "slw_residual_norm": ([P(NormArgsC), vp], C.c_int),
+        "slw_residual_norm": ([C.c_char_p, vp], C.c_int),
         "slw_w4_packed_bytes": ([i32, i32, i32, P(sz)], C.c_int),
         "slw_w4_pack": ([vp, vp, i32, i32, i32, vp, vp], C.c_int),
         "slw_w4_workspace_size": ([i32, i32, i32, i32, P(sz)], C.c_int),
         "slw_w4_product": ([P(W4C), vp, i64, i32, vp, i64, i32, vp, sz, vp], C.c_int),
         "slw_sample_workspace_size": ([i32, i32, P(sz)], C.c_int),
-        "slw_sample": ([P(SampleArgsC), vp, sz, vp], C.c_int),
+        "slw_sample": ([C.c_char_p, vp, sz, vp], C.c_int),
         "slw_kv_free_blocks": ([vp, P(i32)], C.c_int),
         "slw_seq_create": ([vp, i64], C.c_int),
         "slw_seq_free": ([vp, i64], C.c_int),
@@ -544,8 +538,7 @@ class AttnPlan:
 
     def rotate(self, rope: "Rope", q: int, k: int, ld: int, q_out: int, k_out: int, ld_out: int, stream: int = 0):
         """Enqueue the rotation of the batch's query and key rows to their positions (0: not these)."""
-        _check(lib().slw_attn_rotate(self._ctx._h, self._h, C.byref(rope.c), q or None, k or None, ld, q_out or None,
-                                     k_out or None, ld_out, stream or None))
+        _check(lib().slw_attn_rotate(self._ctx._h, self._h, rope._ref, q, k, ld, q_out, k_out, ld_out, stream))
 
     def attend(self, layer: int, q: int, ld: int, out: int, stream: int = 0):
         """Enqueue one layer's attention of the batch's query rows (row stride ld elements)."""
@@ -562,6 +555,7 @@ class Rope:
                  mscale: float = 1.0):
         self.c = RopeC(int(rot_dim), int(interleaved), ROPE_SCALINGS[scaling], int(original_len), float(theta),
                        float(factor), float(low), float(high), freq or None, float(mscale))
+        self._ref = C.byref(self.c)
 
 
 def residual_norm(rows: int, d: int, resid: int, block: int, resid_out: int, gain: int, out: int, *,
@@ -570,11 +564,10 @@ def residual_norm(rows: int, d: int, resid: int, block: int, resid_out: int, gai
                   ld_resid_out: int | None = None, ld_out: int | None = None, stream: int = 0) -> None:
     """Enqueue r' = r + scale * gate * P(o) and y = RMSNorm(r') * gain (slw_residual_norm); addresses that are 0 are
     left out, strides that are None are d."""
-    a = NormArgsC(resid or None, block or None, post_gain or None, gate or None, gain or None, resid_out or None,
-                  out or None, d if ld_resid is None else ld_resid, d if ld_block is None else ld_block, ld_gate,
-                  d if ld_resid_out is None else ld_resid_out, d if ld_out is None else ld_out, rows, d,
-                  int(resid_f32), scale, eps)
-    _check(lib().slw_residual_norm(C.byref(a), stream or None))
+    a = NORM_ARGS.pack(resid, block, post_gain, gate, gain, resid_out, out, d if ld_resid is None else ld_resid,
+                       d if ld_block is None else ld_block, ld_gate, d if ld_resid_out is None else ld_resid_out,
+                       d if ld_out is None else ld_out, rows, d, resid_f32, scale, eps)
+    _check(lib().slw_residual_norm(a, stream))
 
 
 def w4_packed_bytes(n: int, k: int, gated: bool = False) -> int:
@@ -603,8 +596,7 @@ class W4:
     def product(self, a: int, lda: int, m: int, out: int, ldo: int, *, out_f32: bool = False, ws: int = 0,
                 ws_bytes: int = 0, stream: int = 0) -> None:
         """Enqueue out = a W^T, or silu(a Wg^T) * (a Wu^T) for gated weights."""
-        _check(lib().slw_w4_product(self._ref, a or None, lda, m, out or None, ldo, int(out_f32), ws or None, ws_bytes,
-                                    stream or None))
+        _check(lib().slw_w4_product(self._ref, a, lda, m, out, ldo, out_f32, ws, ws_bytes, stream))
 
 
 def sample_workspace_size(max_rows: int, vocab: int) -> int:
@@ -617,9 +609,8 @@ def sample(logits: int, rows: int, vocab: int, ld: int, u: int, tokens: int, *, 
            temperature: int = 0, top_k: int = 0, top_p: int = 0, min_p: int = 0, logprob: int = 0, ws: int = 0,
            ws_bytes: int = 0, stream: int = 0) -> None:
     """Enqueue the draw of each row's next token (slw_sample); the parameters are addresses of [rows], 0: left out."""
-    a = SampleArgsC(logits or None, ld, rows, vocab, int(logits_f32), temperature or None, top_k or None, top_p or None,
-                    min_p or None, u or None, tokens or None, logprob or None)
-    _check(lib().slw_sample(C.byref(a), ws or None, ws_bytes, stream or None))
+    a = SAMPLE_ARGS.pack(logits, ld, rows, vocab, logits_f32, temperature, top_k, top_p, min_p, u, tokens, logprob)
+    _check(lib().slw_sample(a, ws, ws_bytes, stream))
 
 
 class Context:
