@@ -301,7 +301,7 @@ struct Pieces {
     __device__ __forceinline__ void load(int v, float (&x)[8]) const { spread(ask(v), v, x); }
 };
 
-// Pieces v, v + stride, ... below `end`, f(x, v, as it was read).  N are asked for at a time, and
+// Pieces v, v + stride, ... below `end`, f(x, v).  N are asked for at a time, and
 // where that is one, it is asked for while f looks at the one before it.
 template <int N, class T, class F>
 __device__ __forceinline__ void each_piece(const Pieces<T>& p, int v, int end, int stride, F&& f) {
@@ -311,10 +311,9 @@ __device__ __forceinline__ void each_piece(const Pieces<T>& p, int v, int end, i
     for (; v < end; v += N * stride) {
         float x[8];
         if (N == 1) {
-            const typename Pieces<T>::Raw was = raw[0];
-            p.spread(was, v, x);
+            p.spread(raw[0], v, x);
             raw[0] = p.ask(v + stride);
-            f(x, v, was);
+            f(x, v);
             continue;
         }
 #pragma unroll
@@ -323,7 +322,7 @@ __device__ __forceinline__ void each_piece(const Pieces<T>& p, int v, int end, i
         for (int q = 0; q < N; ++q)
             if (v + q * stride < end) {
                 p.spread(raw[q], v + q * stride, x);
-                f(x, v + q * stride, raw[q]);
+                f(x, v + q * stride);
             }
     }
 }
@@ -452,7 +451,7 @@ __device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float l
 #pragma unroll 1
         for (int v0 = threadIdx.x; v0 < p.count; v0 += 32 * kThreads) {
             uint32_t pending = 0;
-            each_piece<4>(p, v0, min(v0 + 32 * kThreads, p.count), kThreads, [&](const float (&x)[8], int v, const typename Pieces<T>::Raw&) {
+            each_piece<4>(p, v0, min(v0 + 32 * kThreads, p.count), kThreads, [&](const float (&x)[8], int v) {
                 bool any = false;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) any |= x[e] >= from && !(x[e] >= below);
@@ -776,7 +775,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_slices_kernel(SampleArgs a
     // the thread's largest logit and the first piece that has it (NaN is below everything)
     float mine = -INFINITY;
     int at = -1;
-    auto look = [&](const float (&x)[8], int v, const typename Pieces<T>::Raw&) {
+    auto look = [&](const float (&x)[8], int v) {
         const float m = largest(x);
         if (m > mine) {
             mine = m;
@@ -790,7 +789,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_slices_kernel(SampleArgs a
         for (int i = 0; i < kRegs; ++i) held[i * kWait + v - from] = first[q].w[i];
         float x[8];
         p.spread(first[q], v, x);
-        if (v < to) look(x, v, first[q]);
+        if (v < to) look(x, v);
     }
     each_piece<4>(p, from + tid + kWait, to, kThreads, look);
     // a piece once more
@@ -926,8 +925,10 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
     for (int s = 0; s < kMost / kThreads; ++s) most[s] = s < a.slices ? a.most[static_cast<size_t>(row) * kMost + s * kThreads + tid] : 0;
     const Wants want(a, row);
     if (tid < a.slices) {
-        sh.best[tid] = a.best[slice0 + tid];
-        sh.ref[tid] = a.ref[slice0 + tid];
+        const uint64_t key = a.best[slice0 + tid];
+        const int32_t ref = a.ref[slice0 + tid];
+        sh.best[tid] = key;
+        sh.ref[tid] = key ? ref : 0;  // a slice of nothing has none
     }
     const Pieces<T> p(static_cast<const T*>(a.logits) + row * a.ld, a.vocab, sh.ends);
     if (tid < 16) sh.root[tid] = exp2(tid / 16.0);
@@ -1128,7 +1129,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
         };
         // whole waves: pieces past the range count as -inf
         each_piece<1>(p, from + wave * per + lane, (v1 - (from + wave * per) + kWave - 1) / kWave * kWave + from + wave * per, kWave,
-                   [&](const float (&x)[8], int v, const typename Pieces<T>::Raw&) {
+                   [&](const float (&x)[8], int v) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float y = r.at_inf ? r.fix(x[e]) : x[e];
