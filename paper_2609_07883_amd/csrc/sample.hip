@@ -26,8 +26,8 @@
 // all else in doubles summed in a fixed order.  With fp32 sums one draw in a few
 // hundred would be another token.
 //
-// What bounds it.  A few rows: latency.  One row of 32768 with top_k and top_p takes 16.4 us:
-// 5 for the first kernel, 2.5 between the two, 9 for a chain of some 25 steps with a
+// What bounds it.  A few rows: latency.  One row of 32768 with top_k and top_p takes 15.3 us:
+// 5 for the first kernel, 1 between the two, 9 for a chain of some 25 steps with a
 // barrier each, which meet their code cold and so are loops of few instructions rather
 // than unrolled.  256 rows of 131072 bf16 logits (67 MB, 13 us at a copy's rate): greedy 18.6 us;
 // top_k 42 (18 + 19 us of kernels); no filter 51 and top_p 92, where the first kernel's
@@ -198,6 +198,15 @@ template <class V>
 __device__ __forceinline__ V uniform(V v) { return of_lane(v, 0); }
 template <class V>
 __device__ __forceinline__ V wave_total(V v) { return of_lane(wave_scan(v), kWave - 1); }
+
+// threadIdx.x, of which the compiler does not know that it is the same each time: what
+// the steps of a row compute from it would be kept in registers over all of them, and
+// spilled (one row of 32768 with top_k and top_p 15.3 us; with threadIdx.x 16.3).
+__device__ __forceinline__ int thread_id() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
 
 // LDS accesses of the lanes of one wave keep their order across it.
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
@@ -395,8 +404,9 @@ __device__ __forceinline__ int group_size(int slices) { return max(1, slices * k
 template <class T>
 __device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float lo, float hi, const Cut& in,
                                        const uint32_t (&most)[kMost / kThreads], int slices, Shared& sh) {
+    const int tid = threadIdx.x;
     __syncthreads();
-    if (threadIdx.x == 0) sh.n_list = sh.n_groups = 0;
+    if (tid == 0) sh.n_list = sh.n_groups = 0;
     __syncthreads();
     // in a row with +inf, where they count as 0 and all else as -inf, only they can be meant
     const float from = r.at_inf ? INFINITY : lo, below = r.at_inf ? NAN : hi;
@@ -405,7 +415,7 @@ __device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float l
     for (int s = 0; s < kMost / kThreads; ++s)
         if (most[s] >= least) {
             const int at = atomicAdd(&sh.n_groups, 1);
-            if (at < kMost / 2) sh.groups[at] = static_cast<uint16_t>(s * kThreads + threadIdx.x);
+            if (at < kMost / 2) sh.groups[at] = static_cast<uint16_t>(s * kThreads + tid);
         }
     auto look = [&](const float (&x)[8], int v) {
         uint32_t keeps = 0;
@@ -437,7 +447,7 @@ __device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float l
     if (2 * groups <= slices * in_slice) {
         const int per = slice_pieces(p.count, slices), rounds = per / kThreads;
 #pragma unroll 1
-        for (int j = threadIdx.x; j < groups * rounds * size; j += kThreads) {
+        for (int j = tid; j < groups * rounds * size; j += kThreads) {
             const int group = sh.groups[j / (rounds * size)], i = j % (rounds * size);
             const int slice = group / in_slice, v = slice * per + group % in_slice * size + i % size + i / size * kThreads;
             if (v >= p.count) continue;
@@ -449,7 +459,7 @@ __device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float l
         // first which pieces have any, 32 of a thread at a time; a wave has one in most of its
         // rounds, and would go through all of `look` in each
 #pragma unroll 1
-        for (int v0 = threadIdx.x; v0 < p.count; v0 += 32 * kThreads) {
+        for (int v0 = tid; v0 < p.count; v0 += 32 * kThreads) {
             uint32_t pending = 0;
             each_piece<4>(p, v0, min(v0 + 32 * kThreads, p.count), kThreads, [&](const float (&x)[8], int v) {
                 bool any = false;
@@ -477,7 +487,7 @@ __device__ __forceinline__ int collect(const Pieces<T>& p, const Row& r, float l
 template <class F>
 __device__ __forceinline__ uint32_t edge(const Row& r, F&& holds) {
     uint32_t lo = 0x00800000u, hi = key_of(r.M);  // lo: the lowest finite key; hi holds
-    const uint32_t lane = threadIdx.x % kWave;
+    const uint32_t lane = thread_id() % kWave;
 #pragma unroll 1
     while (lo < hi) {
         const uint32_t step = max((hi - lo) / kWave, 1u), key = lo + lane * step;
@@ -498,7 +508,7 @@ constexpr int kDigit = 9;
 // By wave 0: the first of 512 amounts up to which they add up to the goal (with
 // what lies before them; 512: none), and what lies before that one.
 __device__ __forceinline__ void find_digit(uint64_t before, uint64_t goal, uint64_t sum8, Shared& sh) {
-    const int lane = threadIdx.x;
+    const int lane = thread_id();
     const uint64_t upto = before + wave_scan(sum8);
     const uint64_t reach = __ballot(upto >= goal);
     const int l = reach ? __ffsll(static_cast<unsigned long long>(reach)) - 1 : kWave - 1;
@@ -511,9 +521,10 @@ __device__ __forceinline__ void find_digit(uint64_t before, uint64_t goal, uint6
 }
 // The lane's eight amounts of those.
 __device__ __forceinline__ uint64_t eight(const Shared& sh) {
+    const int tid = thread_id();
     uint64_t s = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += sh.mass[8 * threadIdx.x + i];
+    for (int i = 0; i < 8; ++i) s += sh.mass[8 * tid + i];
     return s;
 }
 
@@ -541,18 +552,18 @@ constexpr int kFewParts = kThreads / kFew, kPlaces = kFew / kWave;
 // How many of others[n] come above this thread's (nothing, 0, is above none), to rank[].
 template <class V, class F>
 __device__ __forceinline__ void rank_of(V mine, int n, int* rank, F&& other) {
-    const int part = threadIdx.x / kFew, per = (n + kFewParts - 1) / kFewParts;
+    const int tid = thread_id(), part = tid / kFew, per = (n + kFewParts - 1) / kFewParts;
     int above = 0;
 #pragma unroll 4
     for (int i = part * per; i < min((part + 1) * per, n); ++i) above += other(i) > mine;
-    if (mine && above) atomicAdd(rank + threadIdx.x % kFew, above);
+    if (mine && above) atomicAdd(rank + tid % kFew, above);
     __syncthreads();
 }
 struct Few {
     uint64_t upto[kPlaces], total;  // of this lane's places, of all
     // by one or more whole waves alike: the first n places
     __device__ __forceinline__ Few(const uint64_t* place, int n) {
-        const int at = kPlaces * (threadIdx.x % kWave);
+        const int at = kPlaces * (thread_id() % kWave);
         uint64_t mine = 0;
 #pragma unroll
         for (int e = 0; e < kPlaces; ++e) upto[e] = mine += at + e < n ? place[at + e] : 0;
@@ -570,7 +581,7 @@ struct Few {
     }
 };
 __device__ __forceinline__ void draw_of_few(const Row& r, int n, const Targets& to, double u, int32_t* token, float* logprob, Shared& sh) {
-    const int tid = threadIdx.x, at = tid % kFew;
+    const int tid = thread_id(), at = tid % kFew;
     int* rank = reinterpret_cast<int*>(sh.mass);              // [2][kFew]: by logit, by index
     uint64_t* place = reinterpret_cast<uint64_t*>(sh.w);      // [2][kFew]
     uint32_t* index = reinterpret_cast<uint32_t*>(place + 2 * kFew);  // [kFew] of the kept, ~: larger is earlier
@@ -612,7 +623,7 @@ __device__ __forceinline__ void draw_of_few(const Row& r, int n, const Targets& 
 __device__ __forceinline__ Cut cut_list(const Row& r, int n, uint32_t least, int low_bits, const Targets& to, double u,
                                         int32_t* token, float* logprob, Shared& sh) {
     constexpr uint32_t kDigits = 1u << kDigit;
-    const int tid = threadIdx.x;
+    const int tid = thread_id();
     Cut cut{0, r.n};
     if (to.draw && n <= kFew) {
         draw_of_few(r, n, to, u, token, logprob, sh);
