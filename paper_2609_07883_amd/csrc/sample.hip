@@ -1042,8 +1042,11 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
                 down = ((static_cast<uint32_t>(sh.digit) + 1) << step) - 1;
                 if (sh.digit < 512) break;
             }
-            if (down >= top - (0x007FFFFFu >> 16)) continue;  // as far as -inf
-            lo = (top - down) << 16;
+            // as far as -inf, fewer threads than k have any: all tokens, where LDS holds them (256
+            // rows of 1000 with top_k and top_p 35 us, by bins 47)
+            const bool none = down >= top - (0x007FFFFFu >> 16);
+            if (none && r.n > kList) continue;
+            lo = none ? 0x00800000u : (top - down) << 16;
             goal = Targets{static_cast<double>(k), prob < 1.0 ? fmax(prob, 0x1p-1000) : 0.0, true, true};
         } else {
             const bool by_mass = way == 2, low = way == 3;
