@@ -33,6 +33,7 @@
 // top_k 42 (18 + 19 us of kernels); no filter 51 and top_p 92, where the first kernel's
 // instructions take 36 and 40 us (24 a token, half of them fp64), and a nucleus beyond the list takes the second kernel 50: a pass for the bin's tokens, then sums over
 // its slice and over the slice's sixteenths.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -857,7 +858,8 @@ __global__ __launch_bounds__(kThreads, 8) void sample_slices_kernel(SampleArgs a
             again(v, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float y = fmaxf(x[e], -0x1p100f), whole = fmaxf(sixteenth(y, c), floor);  // -inf and NaN as far down
+                // -inf and NaN as the lowest number, so that nothing lies above the slice's largest: no bin is below 0
+                const float y = fmaxf(x[e], -FLT_MAX), whole = fmaxf(sixteenth(y, c), floor);
                 const double f = fma(static_cast<double>(y), want.c16, -static_cast<double>(whole));
                 const int n = static_cast<int>(whole);
                 if (ref - n < kBins - 1)
