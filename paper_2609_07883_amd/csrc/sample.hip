@@ -33,7 +33,6 @@
 // top_k 42 (18 + 19 us of kernels); no filter 51 and top_p 92, where the first kernel's
 // instructions take 36 and 40 us (24 a token, half of them fp64), and a nucleus beyond the list takes the second kernel 50: a pass for the bin's tokens, then sums over
 // its slice and over the slice's sixteenths.
-#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -858,9 +857,10 @@ __global__ __launch_bounds__(kThreads, 8) void sample_slices_kernel(SampleArgs a
             again(v, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                // -inf and NaN as the lowest number, so that nothing lies above the slice's largest: no bin is below 0
-                const float y = fmaxf(x[e], -FLT_MAX), whole = fmaxf(sixteenth(y, c), floor);
-                const double f = fma(static_cast<double>(y), want.c16, -static_cast<double>(whole));
+                // Nothing that has a mass lies above the slice's largest, and what has none (-inf, NaN, places beside
+                // the row) comes to -inf or NaN in sixteenths, also where c is 0: `floor`, which is in no bin.
+                const float whole = fmaxf(sixteenth(x[e], c), floor);
+                const double f = fma(static_cast<double>(x[e]), want.c16, -static_cast<double>(whole));
                 const int n = static_cast<int>(whole);
                 if (ref - n < kBins - 1)
                     atomicAdd(reinterpret_cast<unsigned long long*>(&bins[ref - n]),

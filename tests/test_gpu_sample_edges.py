@@ -51,3 +51,33 @@ def test_top_p_over_slices_of_the_lowest_value(temperature, f32):
     x[4, ::2] = low
     for p in (0.3, 0.9, 0.9999):
         _check(x, f32, temperature=temperature, top_p=p, u=rng.random(5))
+
+
+HOT = [1e28, 3.8e28, 1e29, 1e30, 1e37, FLT_MAX, math.inf]
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("temperature", HOT)
+def test_top_p_leaves_out_what_has_no_mass_at_any_temperature(temperature, f32):
+    """-inf, NaN and the places beside the row in its first and last piece: never part of the mass, however flat w is."""
+    rng = np.random.default_rng([HOT.index(temperature), f32])
+    for n, shift in ((100, 0), (1001, 3), (1001, 5), (8191, 1), (30011, 7), (140001, 2)):
+        x = np.round(rng.standard_normal((6, n)) * 4) / 4
+        x[0, n // 10:] = -np.inf
+        x[1, rng.random(n) < 0.5] = -np.inf
+        x[2, : n - n // 20] = np.nan
+        x[3, rng.random(n) < 0.3] = np.nan
+        x[4] = -np.inf
+        x[4, [0, n // 2, n - 1]] = 1.0, 2.0, 3.0
+        for p in (0.5, 0.9, 0.01):
+            _check(x, f32, ld=n + 3, shift=shift, temperature=temperature, top_p=p, u=rng.random(6))
+        _check(x, f32, ld=n + 3, shift=shift, temperature=temperature, top_p=0.7, min_p=0.5, u=0.0)
+
+
+def test_top_p_of_masked_tokens_by_hand():
+    """1000 tokens of which 500 are masked, weights alike to 2^-80: a nucleus of a half keeps 250."""
+    x = np.full((1, 1000), -np.inf)
+    x[0, ::2] = np.linspace(1, 0, 500)
+    for t in (1e30, FLT_MAX):
+        got, lp, _ = _sample(x, temperature=t, top_p=0.5, u=0.9999999)
+        assert got[0] == 498 and lp[0] == np.float32(-math.log(250))
