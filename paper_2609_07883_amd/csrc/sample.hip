@@ -120,6 +120,10 @@ struct Row {
         return fma(f, fma(f, fma(f, fma(f, 0x1.3b2c4ac7eb38ap-23, 0x1.c6b3488226c3bp-17), 0x1.ebfbdff6988cep-11),
                           0x1.62e42fee4615cp-5), one);
     }
+    // 2^(f / 16) in units of 2^-42: the low bits of a number near 2^10
+    static __device__ __forceinline__ uint64_t units(double f) {
+        return static_cast<uint64_t>(__double_as_longlong(power(f, 1.0 + 0x1p10)) - __double_as_longlong(0x1p10));
+    }
     __device__ __forceinline__ double w(float x) const {
         int n;
         return weight(depth(x), n);
@@ -844,8 +848,8 @@ __global__ __launch_bounds__(kThreads, 8) void sample_slices_kernel(SampleArgs a
     double s = 0.0;
     if (by_mass) {
         // By bins of whole sixteenths of an octave, which all slices share; in units of
-        // 2^-42 of the bin's w, the low bits of a number near 2^10.  Far from logit 0 single
-        // precision knows no sixteenths: such a slice has no bins.
+        // 2^-42 of the bin's w.  Far from logit 0 single precision knows no sixteenths: such a
+        // slice has no bins.
         const bool near = near_zero(m, want.c16);
         const float c = static_cast<float>(want.c16), first = near ? sixteenth(m, c) : -0x1p30f, floor = first - kBins;
         const int ref = uniform(static_cast<int>(first));
@@ -863,9 +867,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_slices_kernel(SampleArgs a
                 const double f = fma(static_cast<double>(x[e]), want.c16, -static_cast<double>(whole));
                 const int n = static_cast<int>(whole);
                 if (ref - n < kBins - 1)
-                    atomicAdd(reinterpret_cast<unsigned long long*>(&bins[ref - n]),
-                              static_cast<unsigned long long>(__double_as_longlong(Row::power(f, 1.0 + 0x1p10)) -
-                                                              __double_as_longlong(0x1p10)));
+                    atomicAdd(reinterpret_cast<unsigned long long*>(&bins[ref - n]), static_cast<unsigned long long>(Row::units(f)));
             }
         }
         __syncthreads();
@@ -909,7 +911,15 @@ __device__ __forceinline__ Found find_bin_of_slices(const SampleArgs& a, int row
     }
     int n;
     const double tokens = static_cast<double>(mass) * 0x1p-42;  // nearly
-    const double mine = tokens * r.weight_from(ref - tid - static_cast<double>(r.M) * r.c16, 0, n);
+    double mine = tokens * r.weight_from(ref - tid - static_cast<double>(r.M) * r.c16, 0, n);
+    if (tid == 0) {
+        // In M's bin by what one M adds to it, so that M weighs 1 here as in the lists.  Only among equal
+        // logits does prob of the mass end with a token exactly; m of them come to m, where the factor
+        // above, the product of two approximations, makes it m (1 + 1e-14) and one token more.
+        const uint64_t one = Row::units(fma(static_cast<double>(r.M), r.c16, -static_cast<double>(ref)));
+        const double whole = floor(static_cast<double>(mass) / static_cast<double>(one));  // or one off: the rest makes up for it
+        mine = whole + static_cast<double>(static_cast<int64_t>(mass - static_cast<uint64_t>(whole) * one)) / static_cast<double>(one);
+    }
     const double upto = block_scan(mine, sh);
     if (tid == 0) sh.found = kBins;
     if (tid == kBins - 2) sh.found_d = upto;

@@ -81,3 +81,37 @@ def test_top_p_of_masked_tokens_by_hand():
     for t in (1e30, FLT_MAX):
         got, lp, _ = _sample(x, temperature=t, top_p=0.5, u=0.9999999)
         assert got[0] == 498 and lp[0] == np.float32(-math.log(250))
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("value", [0.0, 1.0, 3.0, -1.0, -19.625, 7.25, 100.5, -1000.0])
+def test_top_p_at_exact_ties(value, f32):
+    """Equal logits alone have mass: the share that top_p asks for ends with a token exactly, which is the last one kept.
+    In one slice and several, in lists, in a bin of its own (4000) and in more tokens than a list holds."""
+    u = np.array([0.0, 0.25, 0.5, 0.75, 1 - 2.0**-24])
+    for n, kept in ((20, 2), (20, 4), (1000, 100), (30000, 2), (30000, 100), (5000, 4000), (30000, 4000), (30000, 4096), (40000, 20000)):
+        x = np.full((5, n), -np.inf)
+        x[:, :: n // kept][:, :kept] = value
+        assert (x[0] > -np.inf).sum() == kept
+        for p in (0.25, 0.5, 0.75, np.float32(0.1)):
+            for temperature in (1.0, 0.7):
+                got, lp, _ = _sample(x, f32, temperature=temperature, top_p=p, u=u)
+                count = math.ceil(float(np.float32(p)) * kept)
+                assert got.tolist() == [n // kept * int(math.floor(a * count)) for a in u.astype(np.float32).astype(float)], (n, kept, p)
+                assert (lp == np.float32(-math.log(count))).all(), (n, kept, p)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+def test_top_p_does_not_change_with_the_rows_level(f32):
+    """The same row some eighths higher or lower: the same draws, ties among its largest logits too."""
+    rng = np.random.default_rng([16, f32])
+    x = np.round(rng.standard_normal((8, 3000)) * 4) / 8
+    x[:, rng.permutation(3000)[:40]] = 4.0
+    x[4:] = np.where(x[4:] == 4.0, 4.0, -np.inf)
+    u = rng.random(8)
+    for p in (0.5, 0.8):
+        want = None
+        for level in (0.0, 0.125, -1.5, 3.0, 11.375, -8.0):
+            got, lp, _ = _sample(x + level, f32, temperature=0.9, top_p=p, u=u)
+            want = want if want is not None else (got, lp)
+            assert np.array_equal(got, want[0]) and np.allclose(lp, want[1], rtol=2.0**-22, atol=0)
