@@ -544,6 +544,8 @@ struct Targets {
 __device__ __forceinline__ uint64_t amount_of(double w) {
     return static_cast<uint64_t>(__double_as_longlong(w + 4.0) - __double_as_longlong(4.0));
 }
+// The same in a draw, where the least mass counts as a unit: u = 0 draws the first token that has any.
+__device__ __forceinline__ uint64_t amount_to_draw(double w) { return max(amount_of(w), w > 0.0 ? uint64_t{1} : uint64_t{0}); }
 // The running sum that a mass to keep, and the one that a draw, has to reach.
 __device__ __forceinline__ uint64_t goal_of(double t, uint64_t sum) { return min(t >= 1.0 ? static_cast<uint64_t>(ceil(t)) : 1, sum); }
 __device__ __forceinline__ uint64_t goal_of_draw(double u, uint64_t sum) { return min(static_cast<uint64_t>(u * static_cast<double>(sum)) + 1, sum); }
@@ -612,7 +614,7 @@ __device__ __forceinline__ void draw_of_few(const Row& r, int n, const Targets& 
     }
     __syncthreads();
     rank_of(index[at], n, rank + kFew, [&](int i) { return index[i]; });
-    if (mine && index[at]) place[kFew + rank[kFew + at]] = amount;
+    if (mine && index[at]) place[kFew + rank[kFew + at]] = amount_to_draw(w);
     __syncthreads();
     if (tid >= kFew) return;
     const Few f(place + kFew, kFew);
@@ -658,7 +660,7 @@ __device__ __forceinline__ Cut cut_list(const Row& r, int n, uint32_t least, int
                 const double w = sh.w[i];
                 bool in = cut.keeps(key, static_cast<int>(idx)) && (shift == shift0 || v >> (shift + kDigit) == value);
                 if (!by_key) in = in && (draw ? w >= r.min_p : key >> low_bits == cut.key >> low_bits);
-                const uint64_t amount = step < 2 ? 1 : amount_of(w);
+                const uint64_t amount = step < 2 ? 1 : draw ? amount_to_draw(w) : amount_of(w);
                 if (in) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[v >> shift & (kDigits - 1)]), static_cast<unsigned long long>(amount));
             }
             __syncthreads();

@@ -115,3 +115,17 @@ def test_top_p_does_not_change_with_the_rows_level(f32):
             got, lp, _ = _sample(x + level, f32, temperature=0.9, top_p=p, u=u)
             want = want if want is not None else (got, lp)
             assert np.array_equal(got, want[0]) and np.allclose(lp, want[1], rtol=2.0**-22, atol=0)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+def test_u_of_zero_draws_the_first_token_with_any_mass(f32):
+    """The running sum passes 0 with the first kept token whose w is not 0, however small: down to 2^-1000 here."""
+    rng = np.random.default_rng([17, f32])
+    for n in (60, 3000, 30000):
+        x = rng.standard_normal((6, n)) * np.array([1, 3, 20, 50, 100, 2])[:, None]
+        x[5] = np.round(x[5] * 2) / 2
+        for t in (1.0, 0.3, 0.02):
+            x4 = np.maximum(x, x.max(1, keepdims=True) - 650 * t)      # no w in the numbers below 2^-1022
+            for par in (dict(top_k=5), dict(top_k=50), dict(top_k=300), dict(top_k=1024), dict(top_k=50, min_p=1e-30), dict(min_p=1e-30),
+                        dict(top_k=40, top_p=0.9), dict(top_p=0.999), dict()):
+                _check(x4, f32, temperature=t, u=0.0, **par)
