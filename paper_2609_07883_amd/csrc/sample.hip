@@ -548,7 +548,10 @@ __device__ __forceinline__ uint64_t amount_of(double w) {
 __device__ __forceinline__ uint64_t amount_to_draw(double w) { return max(amount_of(w), w > 0.0 ? uint64_t{1} : uint64_t{0}); }
 // The running sum that a mass to keep, and the one that a draw, has to reach.
 __device__ __forceinline__ uint64_t goal_of(double t, uint64_t sum) { return min(t >= 1.0 ? static_cast<uint64_t>(ceil(t)) : 1, sum); }
-__device__ __forceinline__ uint64_t goal_of_draw(double u, uint64_t sum) { return min(static_cast<uint64_t>(u * static_cast<double>(sum)) + 1, sum); }
+// u sum exactly, as a sum may have more bits than a double: u = 1/2 of a row of two like halves draws from the second.
+__device__ __forceinline__ uint64_t goal_of_draw(double u, uint64_t sum) {
+    return min(static_cast<uint64_t>(__umul64hi(static_cast<uint64_t>(u * 0x1p64), sum)) + 1, sum);
+}
 
 // The draw from a few tokens: four threads compare each with a quarter of all, which
 // gives their ranks; their amounts, put in that order, are summed up over a wave's lanes.

@@ -129,3 +129,23 @@ def test_u_of_zero_draws_the_first_token_with_any_mass(f32):
             for par in (dict(top_k=5), dict(top_k=50), dict(top_k=300), dict(top_k=1024), dict(top_k=50, min_p=1e-30), dict(min_p=1e-30),
                         dict(top_k=40, top_p=0.9), dict(top_p=0.999), dict()):
                 _check(x4, f32, temperature=t, u=0.0, **par)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+def test_draws_at_exact_ties(f32):
+    """A row whose first quarter, half and three quarters hold that share of the mass exactly: u at the share draws the
+    token behind it, as the running sum has to exceed u of the whole; u just below it the token before."""
+    for n in (4, 8, 24, 48, 96, 240):
+        for levels in ((1.5, -2.25), (0.0, 1.0), (7.0, 7.0), (3.0, 2.75)):
+            x = np.tile(np.where(np.arange(n // 4) % 2, *levels), 4)[None, :]
+            for u, at in ((0.25, n // 4), (0.5, n // 2), (0.75, 3 * n // 4)):
+                for par in (dict(top_k=n - 1, min_p=1e-30), dict(min_p=1e-30), dict(top_p=1 - 2.0**-24, min_p=1e-30)):
+                    if "top_k" in par:
+                        x1 = np.concatenate([x, np.full((1, 1), -np.inf)], 1)
+                        par["top_k"] = n
+                    else:
+                        x1 = x
+                    got, _, _ = _sample(x1, f32, temperature=0.7, u=np.float32(u), **par)
+                    assert got[0] == at, (n, levels, u, par)
+                    got, _, _ = _sample(x1, f32, temperature=0.7, u=np.nextafter(np.float32(u), np.float32(0)), **par)
+                    assert got[0] == at - 1, (n, levels, u, par)
