@@ -1000,6 +1000,9 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
             const int s = tid / kWaves;
             const float m = value_of(static_cast<uint32_t>(sh.best[s] >> 32));
             mine *= !sh.best[s] ? 0.0 : r.at_inf ? (m == INFINITY ? 1.0 : 0.0) : r.w(m);
+            // A sixteenth to draw from needs a token whose own w is not 0: of its 2^16 tokens at most
+            // one has 2^-1066 then.
+            if (mine < 0x1p-1050) mine = 0.0;
         }
         const double upto = block_scan(mine, sh);
         if (tid == kThreads - 1) sh.found_d = upto;

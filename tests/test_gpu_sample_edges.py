@@ -149,3 +149,20 @@ def test_draws_at_exact_ties(f32):
                     assert got[0] == at, (n, levels, u, par)
                     got, _, _ = _sample(x1, f32, temperature=0.7, u=np.nextafter(np.float32(u), np.float32(0)), **par)
                     assert got[0] == at - 1, (n, levels, u, par)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+def test_every_row_gets_a_token_where_masses_leave_the_numbers(f32):
+    """Parts of a row whose mass is a number while their tokens' alone are not (below 2^-1074 of the largest): masses
+    below 2^-1050 may count as none, but a token is drawn."""
+    n = 20000
+    x = np.full((4, n), -np.inf)
+    x[:, :500] = -746.0                      # e^-746 = 2^-1076.3, 500 of them 2^-1067
+    x[:, 600] = -740.0
+    x[:, n - 1] = 0.0
+    x[1, 600:9000] = -np.inf
+    x[2, 10000:11000] = -745.0
+    x[3, :600] = -np.inf
+    for par in (dict(), dict(temperature=1.0, top_p=1.0)):
+        got, lp, _ = _sample(x, f32, u=0.0, **par)
+        assert got.tolist() == [n - 1] * 4 and (lp == 0).all()
