@@ -45,7 +45,7 @@ namespace slw {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
-constexpr int kBins = 768;          // 16 for an octave; the last one holds w < 2^-47 and is weighed nowhere
+constexpr int kBins = 768;          // 16 for an octave; of a mass the last one holds w < 2^-47 and is weighed nowhere
 constexpr int kHeld = 4096;         // 16 bytes each of a slice that wait in LDS to be weighed (256 rows top_p 43 us; read again 44)
 constexpr int kQueue = 8 * kWave + 64;  // logits a wave has queued: a piece of every lane beside 63 left over
 constexpr int kMost = 4096;         // most groups of threads of a row whose largest logits are kept
@@ -129,6 +129,10 @@ struct Row {
         return weight(depth(x), n);
     }
     __device__ __forceinline__ int bin_of(float x) const { return min(-static_cast<int>(rint(depth(x))), kBins - 1); }
+    // The same for a count, which is cut wherever a token has any mass: d sixteenths (at most
+    // 17600) below M, from 32 octaves on 67 of them in a bin.
+    static __device__ __forceinline__ int count_bin(int d) { return d < 512 ? d : 512 + (d - 512) / 67; }
+    __device__ __forceinline__ int count_bin_of(float x) const { return count_bin(-static_cast<int>(rint(depth(x)))); }
 };
 
 struct Shared {
@@ -708,7 +712,7 @@ __device__ __forceinline__ Cut cut_list(const Row& r, int n, uint32_t least, int
 // `target` (of them, or of all of their mass), what lies above that bin, and
 // their mass and the number of tokens down to it.
 struct Found {
-    int bin;  // kBins: beyond the weighed tokens, whose rest has no mass
+    int bin;  // kBins: fewer tokens than the target have any mass
     double above, z, about;
 };
 template <class T>
@@ -725,13 +729,14 @@ __device__ __forceinline__ Found find_bin(const Pieces<T>& p, const Row& r, cons
         const double w = r.weight(r.depth(x), n);
         f.z += w;
         // w in units of 2^-42: the low bits of w + 2^10
-        if (n > 1 - kBins)
-            atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[-n]),
+        const int b = by_mass ? -n : Row::count_bin(-n);
+        if (by_mass ? b < kBins - 1 : w > 0.0)
+            atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[b]),
                       static_cast<unsigned long long>(by_mass ? __double_as_longlong(w + 0x1p10) - __double_as_longlong(0x1p10) : 1));
     });
     f.z = block_sum(f.z, sh);
     // a bin's mass says how many tokens it has to 2.2% either way
-    const bool has = tid < kBins - 1;
+    const bool has = tid < (by_mass ? kBins - 1 : kBins);
     const double mine = has ? static_cast<double>(sh.mass[tid]) : 0.0, upto = block_scan(mine, sh);
     if (tid == 0) sh.found = kBins;
     if (tid == kBins - 2) sh.found_d = upto;
@@ -1087,7 +1092,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
             lo = 0;
 #pragma unroll 1
             for (int i = 0; i < (goal.draw || bin == 0 ? 1 : 2); ++i) {
-                const uint32_t e = edge(r, [&](float x) { return low ? r.w(x) >= r.min_p : bin_of(x) <= bin - i; });
+                const uint32_t e = edge(r, [&](float x) { return low ? r.w(x) >= r.min_p : (way == 1 ? r.count_bin_of(x) : bin_of(x)) <= bin - i; });
                 if (i == 0) lo = e;
                 else hi = value_of(e);
             }

@@ -166,3 +166,22 @@ def test_every_row_gets_a_token_where_masses_leave_the_numbers(f32):
     for par in (dict(), dict(temperature=1.0, top_p=1.0)):
         got, lp, _ = _sample(x, f32, u=0.0, **par)
         assert got.tolist() == [n - 1] * 4 and (lp == 0).all()
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("temperature", [1.0, 0.1, 0.02, 0.004])
+def test_top_k_cuts_among_the_smallest_masses(temperature, f32):
+    """A k-th largest logit at 2^-47 of the largest and far below: where k is more than the threads of a work-group, or
+    all tokens left are in a few threads' hands.  u = 0 shows a token that ought to be out."""
+    rng = np.random.default_rng([int(1000 * temperature), f32])
+    x = rng.standard_normal((6, 30000)) * 2
+    x[1] = np.round(x[1] * 4) / 4
+    x[2, 5000:] = -np.inf                                     # 5000 tokens, in 625 threads' pieces
+    x[3, 20000:] = float(_lowest(f32))
+    x[4] *= 4
+    x[5, 3000:] = -np.inf
+    for k in (700, 1025, 2000, 4097, 10000, 25000):
+        for u in (0.0, 0.5, 1 - 2.0**-24):
+            _check(x, f32, temperature=temperature, top_k=k, u=u)
+    _check(x, f32, temperature=temperature, top_k=3000, top_p=0.999, u=0.0)
+    _check(x, f32, temperature=temperature, top_k=3000, min_p=1e-30, u=0.0)
