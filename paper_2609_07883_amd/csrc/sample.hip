@@ -128,11 +128,10 @@ struct Row {
         int n;
         return weight(depth(x), n);
     }
-    __device__ __forceinline__ int bin_of(float x) const { return min(-static_cast<int>(rint(depth(x))), kBins - 1); }
-    // The same for a count, which is cut wherever a token has any mass: d sixteenths (at most
-    // 17600) below M, from 32 octaves on 67 of them in a bin.
-    static __device__ __forceinline__ int count_bin(int d) { return d < 512 ? d : 512 + (d - 512) / 67; }
-    __device__ __forceinline__ int count_bin_of(float x) const { return count_bin(-static_cast<int>(rint(depth(x)))); }
+    // The bin of what lies d sixteenths below M, up to where w is 0 (17600), as a count is cut there
+    // too: from 40 octaves on, of no weight in a mass, 256 sixteenths to one.
+    static __device__ __forceinline__ int bin_at(int d) { return d < 640 ? d : 640 + ((d - 640) >> 8); }
+    __device__ __forceinline__ int bin_of(float x) const { return bin_at(-static_cast<int>(rint(depth(x)))); }
 };
 
 struct Shared {
@@ -214,6 +213,13 @@ __device__ __forceinline__ int thread_id() {
     int t = threadIdx.x;
     asm volatile("" : "+v"(t));
     return t;
+}
+
+// The same for any value: what is computed from it is not kept over the steps of a row.
+template <class V>
+__device__ __forceinline__ V anew(V v) {
+    asm volatile("" : "+v"(v));
+    return v;
 }
 
 // LDS accesses of the lanes of one wave keep their order across it.
@@ -554,7 +560,7 @@ __device__ __forceinline__ uint64_t amount_to_draw(double w) { return max(amount
 __device__ __forceinline__ uint64_t goal_of(double t, uint64_t sum) { return min(t >= 1.0 ? static_cast<uint64_t>(ceil(t)) : 1, sum); }
 // u sum exactly, as a sum may have more bits than a double: u = 1/2 of a row of two like halves draws from the second.
 __device__ __forceinline__ uint64_t goal_of_draw(double u, uint64_t sum) {
-    return min(static_cast<uint64_t>(__umul64hi(static_cast<uint64_t>(u * 0x1p64), sum)) + 1, sum);
+    return min(static_cast<uint64_t>(__umul64hi(static_cast<uint64_t>(anew(u) * 0x1p64), sum)) + 1, sum);
 }
 
 // The draw from a few tokens: four threads compare each with a quarter of all, which
@@ -667,7 +673,7 @@ __device__ __forceinline__ Cut cut_list(const Row& r, int n, uint32_t least, int
                 const double w = sh.w[i];
                 bool in = cut.keeps(key, static_cast<int>(idx)) && (shift == shift0 || v >> (shift + kDigit) == value);
                 if (!by_key) in = in && (draw ? w >= r.min_p : key >> low_bits == cut.key >> low_bits);
-                const uint64_t amount = step < 2 ? 1 : draw ? amount_to_draw(w) : amount_of(w);
+                const uint64_t amount = step < 2 ? 1 : max(amount_of(w), draw && w > 0.0 ? uint64_t{1} : uint64_t{0});
                 if (in) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[v >> shift & (kDigits - 1)]), static_cast<unsigned long long>(amount));
             }
             __syncthreads();
@@ -729,14 +735,13 @@ __device__ __forceinline__ Found find_bin(const Pieces<T>& p, const Row& r, cons
         const double w = r.weight(r.depth(x), n);
         f.z += w;
         // w in units of 2^-42: the low bits of w + 2^10
-        const int b = by_mass ? -n : Row::count_bin(-n);
-        if (by_mass ? b < kBins - 1 : w > 0.0)
-            atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[b]),
+        if (w > 0.0)
+            atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[Row::bin_at(-n)]),
                       static_cast<unsigned long long>(by_mass ? __double_as_longlong(w + 0x1p10) - __double_as_longlong(0x1p10) : 1));
     });
     f.z = block_sum(f.z, sh);
     // a bin's mass says how many tokens it has to 2.2% either way
-    const bool has = tid < (by_mass ? kBins - 1 : kBins);
+    const bool has = tid < kBins - 1;
     const double mine = has ? static_cast<double>(sh.mass[tid]) : 0.0, upto = block_scan(mine, sh);
     if (tid == 0) sh.found = kBins;
     if (tid == kBins - 2) sh.found_d = upto;
@@ -921,14 +926,14 @@ __device__ __forceinline__ Found find_bin_of_slices(const SampleArgs& a, int row
     }
     int n;
     const double tokens = static_cast<double>(mass) * 0x1p-42;  // nearly
-    double mine = tokens * r.weight_from(ref - tid - static_cast<double>(r.M) * r.c16, 0, n);
+    double mine = tokens * r.weight_from(ref - tid - static_cast<double>(anew(r.M)) * r.c16, 0, n);
     if (tid == 0) {
         // In M's bin by what one M adds to it, so that M weighs 1 here as in the lists.  Only among equal
         // logits does prob of the mass end with a token exactly; m of them come to m, where the factor
         // above, the product of two approximations, makes it m (1 + 1e-14) and one token more.
-        const uint64_t one = Row::units(fma(static_cast<double>(r.M), r.c16, -static_cast<double>(ref)));
-        const double whole = floor(static_cast<double>(mass) / static_cast<double>(one));  // or one off: the rest makes up for it
-        mine = whole + static_cast<double>(static_cast<int64_t>(mass - static_cast<uint64_t>(whole) * one)) / static_cast<double>(one);
+        const uint64_t one = Row::units(fma(static_cast<double>(anew(r.M)), r.c16, -static_cast<double>(ref)));
+        const double inv = 1.0 / static_cast<double>(one), whole = rint(static_cast<double>(mass) * inv);
+        mine = whole + static_cast<double>(static_cast<int64_t>(mass - static_cast<uint64_t>(whole) * one)) * inv;
     }
     const double upto = block_scan(mine, sh);
     if (tid == 0) sh.found = kBins;
@@ -1092,7 +1097,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
             lo = 0;
 #pragma unroll 1
             for (int i = 0; i < (goal.draw || bin == 0 ? 1 : 2); ++i) {
-                const uint32_t e = edge(r, [&](float x) { return low ? r.w(x) >= r.min_p : (way == 1 ? r.count_bin_of(x) : bin_of(x)) <= bin - i; });
+                const uint32_t e = edge(r, [&](float x) { return low ? r.w(x) >= r.min_p : bin_of(x) <= bin - i; });
                 if (i == 0) lo = e;
                 else hi = value_of(e);
             }
@@ -1122,7 +1127,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
             for (int b = (min(bin - down, kBins - 1) - 1 - lane) / kWave * kWave + lane; b >= 0; b -= kWave)
                 s = s * 0x1p-4 + (b < bin - down ? static_cast<double>(bins[b]) : 0.0);
             int n;
-            s *= 0x1p-42 * r.weight_from(ref - down - lane - static_cast<double>(r.M) * r.c16, 0, n);
+            s *= 0x1p-42 * r.weight_from(ref - down - lane - static_cast<double>(anew(r.M)) * r.c16, 0, n);
 #pragma unroll 1
             for (int i = lane; i < listed; i += kWave) {
                 const uint64_t t = sh.list[i];
