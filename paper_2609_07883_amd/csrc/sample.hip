@@ -45,7 +45,7 @@ namespace slw {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
-constexpr int kBins = 768;          // 16 for an octave; of a mass the last one holds w < 2^-47 and is weighed nowhere
+constexpr int kBins = 896;          // 16 for an octave; of a mass the last one holds w < 2^-55, all together 2^-35, and is weighed nowhere
 constexpr int kHeld = 4096;         // 16 bytes each of a slice that wait in LDS to be weighed (256 rows top_p 43 us; read again 44)
 constexpr int kQueue = 8 * kWave + 64;  // logits a wave has queued: a piece of every lane beside 63 left over
 constexpr int kMost = 4096;         // most groups of threads of a row whose largest logits are kept

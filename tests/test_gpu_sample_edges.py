@@ -185,3 +185,18 @@ def test_top_k_cuts_among_the_smallest_masses(temperature, f32):
             _check(x, f32, temperature=temperature, top_k=k, u=u)
     _check(x, f32, temperature=temperature, top_k=3000, top_p=0.999, u=0.0)
     _check(x, f32, temperature=temperature, top_k=3000, min_p=1e-30, u=0.0)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+def test_top_p_weighs_the_far_tail(f32):
+    """Two equal logits on top and all others 2^-48 or less of them: half of the mass is more than the first alone, if
+    only by the tail, and so keeps both."""
+    for n in (1000, 30000, 140001):
+        for below in (33.5, 34.5, 35.0):
+            x = np.full((4, n), 2.0 - below)
+            x[:, [n // 7, n // 2]] = 2.0
+            _check(x, f32, temperature=1.0, top_p=0.5, u=[0.0, 0.4, 0.6, 0.99])
+    low = _lowest(f32)                                        # e^-34 = 2^-49 of the others at this temperature
+    x = np.full((4, 30000), low)
+    x[:, [100, 20000]] = 5.0
+    _check(x, f32, temperature=1e37, top_p=0.5, u=[0.0, 0.4, 0.6, 0.99])
