@@ -390,7 +390,7 @@ int slw_residual_norm(const slw_norm_args* args, void* stream);
  * Products with weights in 4 bits: out = a W^T, W[n][k] in the OCP MX format
  * (e2m1 codes: bit 3 the sign, then 0, 1/2, 1, 3/2, 2, 3, 4, 6; one e8m0 scale
  * byte b, 2^(b - 127), for 32 values of a row).  A weight is its value as a bf16
- * number: exact for 1 <= b <= 252, infinite where it exceeds bf16's range, NaN for
+ * number: exact for b <= 252, infinite where it exceeds bf16's range, NaN for
  * b = 255.  Products are exact, sums fp32.
  *   Gated weights hold n/2 gate rows, then n/2 up rows, and
  * out[m][n/2] = silu(a Wg^T) * (a Wu^T), silu(x) = x / (1 + e^-x).
