@@ -1148,7 +1148,11 @@ int rope_args(const slw_model_cfg& c, const slw_rope& r, RopeArgs* out) {
             break;
         default: return fail(SLW_EINVAL, "unknown scaling %d", r.scaling);
     }
-    if (!a.freq) a.step = -2.0 * std::log2(theta) / r.rot_dim;
+    if (!a.freq) {
+        a.step = -2.0 * std::log2(theta) / r.rot_dim;
+        if (!positive(theta) || !std::isfinite(a.first) || !std::isfinite(a.inv_factor) || (a.by_parts && a.inv_width == 0.0))
+            return fail(SLW_EINVAL, "theta, factor, low and high make frequencies that are not finite");
+    }
     *out = a;
     return SLW_OK;
 }
