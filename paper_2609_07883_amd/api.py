@@ -85,9 +85,9 @@ class RopeC(C.Structure):
 
 # slw_norm_args and slw_sample_args, packed anew by each call (a ctypes structure takes four times as long to fill):
 # resid, block, post_gain, gate, gain, resid_out, out; their five strides; rows, d, resid_f32; scale, eps
-NORM_ARGS = struct.Struct("@7P5q3i2f4x")
+NORM_ARGS = struct.Struct("@PPPPPPPqqqqqiiiff4x")
 # logits; ld; rows, vocab, logits_f32; temperature, top_k, top_p, min_p, u, tokens, logprob
-SAMPLE_ARGS = struct.Struct("@Pq3i7P")
+SAMPLE_ARGS = struct.Struct("@PqiiiPPPPPPP")
 
 
 class W4C(C.Structure):
@@ -558,15 +558,27 @@ class Rope:
         self._ref = C.byref(self.c)
 
 
+def _repack(form: struct.Struct, values: tuple) -> bytes:
+    """Arguments that do not pack as they are: addresses that are None are 0, the rest is refused."""
+    try:
+        return form.pack(*(0 if v is None and kind == "P" else v for kind, v in zip(form.format[1:], values)))
+    except (struct.error, OverflowError) as e:
+        raise SloweaveError(EINVAL, f"an argument does not fit its field: {e}") from None
+
+
 def residual_norm(rows: int, d: int, resid: int, block: int, resid_out: int, gain: int, out: int, *,
                   resid_f32: bool = False, eps: float = 1e-5, post_gain: int = 0, gate: int = 0, ld_gate: int = 0,
                   scale: float = 1.0, ld_resid: int | None = None, ld_block: int | None = None,
                   ld_resid_out: int | None = None, ld_out: int | None = None, stream: int = 0) -> None:
-    """Enqueue r' = r + scale * gate * P(o) and y = RMSNorm(r') * gain (slw_residual_norm); addresses that are 0 are
-    left out, strides that are None are d."""
-    a = NORM_ARGS.pack(resid, block, post_gain, gate, gain, resid_out, out, d if ld_resid is None else ld_resid,
-                       d if ld_block is None else ld_block, ld_gate, d if ld_resid_out is None else ld_resid_out,
-                       d if ld_out is None else ld_out, rows, d, resid_f32, scale, eps)
+    """Enqueue r' = r + scale * gate * P(o) and y = RMSNorm(r') * gain (slw_residual_norm); addresses that are 0 or
+    None are left out, strides that are None are d."""
+    v = (resid, block, post_gain, gate, gain, resid_out, out, d if ld_resid is None else ld_resid,
+         d if ld_block is None else ld_block, ld_gate, d if ld_resid_out is None else ld_resid_out,
+         d if ld_out is None else ld_out, rows, d, resid_f32, scale, eps)
+    try:
+        a = NORM_ARGS.pack(*v)
+    except (struct.error, OverflowError):
+        a = _repack(NORM_ARGS, v)
     _check(lib().slw_residual_norm(a, stream))
 
 
@@ -608,8 +620,13 @@ def sample_workspace_size(max_rows: int, vocab: int) -> int:
 def sample(logits: int, rows: int, vocab: int, ld: int, u: int, tokens: int, *, logits_f32: bool = False,
            temperature: int = 0, top_k: int = 0, top_p: int = 0, min_p: int = 0, logprob: int = 0, ws: int = 0,
            ws_bytes: int = 0, stream: int = 0) -> None:
-    """Enqueue the draw of each row's next token (slw_sample); the parameters are addresses of [rows], 0: left out."""
-    a = SAMPLE_ARGS.pack(logits, ld, rows, vocab, logits_f32, temperature, top_k, top_p, min_p, u, tokens, logprob)
+    """Enqueue the draw of each row's next token (slw_sample); the parameters are addresses of [rows], 0 or None:
+    left out."""
+    v = (logits, ld, rows, vocab, logits_f32, temperature, top_k, top_p, min_p, u, tokens, logprob)
+    try:
+        a = SAMPLE_ARGS.pack(*v)
+    except (struct.error, OverflowError):
+        a = _repack(SAMPLE_ARGS, v)
     _check(lib().slw_sample(a, ws, ws_bytes, stream))
 
 

@@ -23,3 +23,25 @@ def test_rotation_refuses_frequencies_that_are_no_numbers():
     _refused(api.EINVAL, call, 64, 1e4, scaling="linear", factor=5e-324)
     _refused(api.EINVAL, call, 64, 1e4, scaling="by_parts", factor=5e-324, original_len=8192)
     _refused(api.EINVAL, call, 64, 1e4, scaling="by_parts", factor=2.0, original_len=8192, low=-1.7e308, high=1.7e308)
+
+
+def test_calls_that_pack_their_arguments_refuse_as_the_others_do():
+    """Addresses that are None are left out; what does not fit its field is the library's error, not the packing's."""
+    norm = lambda rows=1, d=64, resid=64, block=64, resid_out=64, gain=64, out=64, **k: api.residual_norm(
+        rows, d, resid, block, resid_out, gain, out, **k)
+    norm(rows=0, block=None, resid_out=None, post_gain=None, gate=None)
+    _refused(api.EINVAL, norm, resid=None)
+    _refused(api.EINVAL, norm, gain=None)
+    _refused(api.EINVAL, norm, block=None, gate=64)
+    _refused(api.EINVAL, norm, out=None, resid_out=None)
+    for bad in (dict(rows=1 << 32), dict(rows=(1 << 32) + 1), dict(rows=None), dict(d=1 << 31), dict(out=1 << 64), dict(ld_out=1 << 63),
+                dict(scale=1e300), dict(eps=1e300)):
+        _refused(api.EINVAL, norm, **bad)
+    sample = lambda logits=64, rows=1, vocab=100, ld=100, u=64, tokens=64, **k: api.sample(
+        logits, rows, vocab, ld, u, tokens, **{"ws": 64, "ws_bytes": 1 << 40, **k})
+    sample(rows=0, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None)
+    for name in ("logits", "u", "tokens"):
+        _refused(api.EINVAL, sample, **{name: None})
+    _refused(api.EINVAL, sample, ws=None)
+    for bad in (dict(rows=1 << 31), dict(rows=1 << 32), dict(vocab=1 << 33), dict(vocab=None), dict(top_k=1 << 64), dict(ld=1 << 64)):
+        _refused(api.EINVAL, sample, **bad)
