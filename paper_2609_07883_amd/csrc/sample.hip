@@ -84,7 +84,9 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 
 // Sixteenths of an octave from logit 0, whole.  Never falls as x grows; near enough to
 // 0, single precision moves few x to the next one, past a half by 2^-6 at most.
-__device__ __forceinline__ bool near_zero(float x, double c16) { return fabs(static_cast<double>(x)) * c16 <= 0x1p17 && c16 <= 0x1p100; }
+__device__ __forceinline__ bool near_zero(float x, double c16, double margin = 0.0) {
+    return fabs(static_cast<double>(x)) * c16 <= 0x1p17 - margin && c16 <= 0x1p100;
+}
 __device__ __forceinline__ float sixteenth(float x, float c16) { return rintf(x * c16); }
 
 // How w depends on x.  In a row that has +inf those tokens alone have mass.
@@ -1033,7 +1035,8 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
     }
 
     // the slices' bins count, where sixteenths from 0 on are as good as from M on
-    const bool slices = want.by_mass() && !r.at_inf && near_zero(r.M, r.c16);
+    // (slices that have none, as they are further from it, are 2^-64 of M at most then)
+    const bool slices = want.by_mass() && !r.at_inf && near_zero(r.M, r.c16, 1024.0);
     const float c16 = static_cast<float>(r.c16);
     const int ref = slices ? static_cast<int>(sixteenth(r.M, c16)) : 0;
     auto bin_of = [&](float x) {  // a whole number; far down beyond any int

@@ -200,3 +200,21 @@ def test_top_p_weighs_the_far_tail(f32):
     x = np.full((4, 30000), low)
     x[:, [100, 20000]] = 5.0
     _check(x, f32, temperature=1e37, top_p=0.5, u=[0.0, 0.4, 0.6, 0.99])
+
+
+@pytest.mark.parametrize("temperature", [1.0, 0.01, 30.0])
+def test_top_p_where_bins_end_between_the_slices(temperature):
+    """Rows whose largest logit lies within the reach of single precision's sixteenths (5678 T from 0) and other parts'
+    largest just beyond it: those have the same mass to give."""
+    rng = np.random.default_rng(18)
+    edge = 2.0**17 / (16 * math.log2(math.e)) * temperature
+    for n in (20000, 40960, 140001):
+        x = rng.standard_normal((6, n)) * temperature
+        x = x - x.max(1, keepdims=True) - edge
+        x[0, 100] = -edge + 0.01 * temperature               # one token within
+        x[1, :5000] += 0.5 * temperature
+        x[2, n - 5000:] += 2.0 * temperature
+        x[3] += 30 * temperature
+        x[4] += 45 * temperature
+        for p in (0.3, 0.9, 0.999):
+            _check(x, True, temperature=temperature, top_p=p, u=rng.random(6))
