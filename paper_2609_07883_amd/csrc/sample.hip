@@ -48,6 +48,7 @@ constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 constexpr int kBins = 896;          // 16 for an octave; of a mass the last one holds w < 2^-55, all together 2^-35, and is weighed nowhere
 constexpr int kHeld = 4096;         // 16 bytes each of a slice that wait in LDS to be weighed (256 rows top_p 43 us; read again 44)
 constexpr int kQueue = 8 * kWave + 64;  // logits a wave has queued: a piece of every lane beside 63 left over
+constexpr int kRowBins = kThreads;  // of a row that goes by its own
 constexpr int kMost = 4096;         // most groups of threads of a row whose largest logits are kept
 constexpr int kMostSlices = 16;     // of a row
 constexpr int kList = 4096;         // tokens sorted in LDS
@@ -130,9 +131,17 @@ struct Row {
         int n;
         return weight(depth(x), n);
     }
-    // The bin of what lies d sixteenths below M, up to where w is 0 (17600), as a count is cut there
-    // too: from 40 octaves on, of no weight in a mass, 256 sixteenths to one.
-    static __device__ __forceinline__ int bin_at(int d) { return d < 640 ? d : 640 + ((d - 640) >> 8); }
+    // The bin, of kRowBins, of what lies d sixteenths below M: 16 octaves of one each, then 128
+    // bins for the next 16 octaves, for the 32 after them, and so on, so that a count is cut among
+    // few tokens at any temperature; d >= 16384 is beyond them, as no w below 2^-1022 is to be told from 0.
+    static __device__ __forceinline__ int bin_at(int d) {
+        const int s = max(24 - __clz(d | 1), 0);
+        return 128 * s + (d >> s);
+    }
+    static __device__ __forceinline__ int start_of(int bin) {
+        const int s = max(bin / 128 - 1, 0);
+        return (bin - 128 * s) << s;
+    }
     __device__ __forceinline__ int bin_of(float x) const { return bin_at(-static_cast<int>(rint(depth(x)))); }
 };
 
@@ -144,7 +153,7 @@ struct Shared {
         };
         float queue[kWaves][kQueue];
     };
-    uint64_t mass[kBins];
+    uint64_t mass[kRowBins];
     __attribute__((aligned(16))) float ends[16];
     double root[16];
     double red_d[kWaves];
@@ -720,14 +729,14 @@ __device__ __forceinline__ Cut cut_list(const Row& r, int n, uint32_t least, int
 // `target` (of them, or of all of their mass), what lies above that bin, and
 // their mass and the number of tokens down to it.
 struct Found {
-    int bin;  // kBins: fewer tokens than the target have any mass
+    int bin;  // kThreads: fewer tokens than the target have any mass
     double above, z, about;
 };
 template <class T>
 __device__ __forceinline__ Found find_bin(const Pieces<T>& p, const Row& r, const Cut& in, bool by_mass, double target, Shared& sh) {
     const int tid = threadIdx.x;
     __syncthreads();
-    for (int b = tid; b < kBins; b += kThreads) sh.mass[b] = 0;
+    sh.mass[tid] = 0;
     __syncthreads();
     Found f;
     f.z = 0.0;
@@ -737,23 +746,23 @@ __device__ __forceinline__ Found find_bin(const Pieces<T>& p, const Row& r, cons
         const double w = r.weight(r.depth(x), n);
         f.z += w;
         // w in units of 2^-42: the low bits of w + 2^10
-        if (w > 0.0)
-            atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[Row::bin_at(-n)]),
+        const int b = Row::bin_at(-n);
+        if (b < kRowBins)
+            atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[b]),
                       static_cast<unsigned long long>(by_mass ? __double_as_longlong(w + 0x1p10) - __double_as_longlong(0x1p10) : 1));
     });
     f.z = block_sum(f.z, sh);
     // a bin's mass says how many tokens it has to 2.2% either way
-    const bool has = tid < kBins - 1;
-    const double mine = has ? static_cast<double>(sh.mass[tid]) : 0.0, upto = block_scan(mine, sh);
-    if (tid == 0) sh.found = kBins;
-    if (tid == kBins - 2) sh.found_d = upto;
+    const double mine = static_cast<double>(sh.mass[tid]), upto = block_scan(mine, sh);
+    if (tid == 0) sh.found = kThreads;
+    if (tid == kThreads - 1) sh.found_d = upto;
     __syncthreads();
     const double aim = by_mass ? target * sh.found_d : target;
-    first_thread(has && upto >= aim, &sh.found);
+    first_thread(upto >= aim, &sh.found);
     __syncthreads();
     f.bin = sh.found;
     if (tid == f.bin) sh.above_d = upto - mine;
-    f.about = block_sum(has && tid <= f.bin ? by_mass ? mine * 0x1p-42 * exp2(tid * (1 / 16.0)) : mine : 0.0, sh);
+    f.about = block_sum(tid <= f.bin ? by_mass ? mine * 0x1p-42 * exp2(Row::start_of(tid) * (1 / 16.0)) : mine : 0.0, sh);
     f.above = by_mass ? sh.above_d * 0x1p-42 : sh.above_d;
     return f;
 }
@@ -938,7 +947,7 @@ __device__ __forceinline__ Found find_bin_of_slices(const SampleArgs& a, int row
         mine = whole + static_cast<double>(static_cast<int64_t>(mass - static_cast<uint64_t>(whole) * one)) * inv;
     }
     const double upto = block_scan(mine, sh);
-    if (tid == 0) sh.found = kBins;
+    if (tid == 0) sh.found = kThreads;
     if (tid == kBins - 2) sh.found_d = upto;
     __syncthreads();
     Found f;
@@ -1086,7 +1095,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
             if (!low) {
                 const Found f = by_mass && slices ? find_bin_of_slices(a, row, r, prob, ref, sh)
                                                   : find_bin(p, r, cut, by_mass, by_mass ? prob : k, sh);
-                if (f.bin == kBins) continue;
+                if (f.bin == kThreads) continue;
                 bin = f.bin;
                 mass = f.z;
                 // the tokens down to the bin where LDS holds them, else the bin's alone
