@@ -565,13 +565,13 @@ struct Targets {
 __device__ __forceinline__ uint64_t amount_of(double w) {
     return static_cast<uint64_t>(__double_as_longlong(w + 4.0) - __double_as_longlong(4.0));
 }
-// The same in a draw, where the least mass counts as a unit: u = 0 draws the first token that has any.
-__device__ __forceinline__ uint64_t amount_to_draw(double w) { return max(amount_of(w), w > 0.0 ? uint64_t{1} : uint64_t{0}); }
+// In a draw tokens without any mass are left out and the others have a unit at least: u = 0 draws the
+// first that has any, however little.
 // The running sum that a mass to keep, and the one that a draw, has to reach.
 __device__ __forceinline__ uint64_t goal_of(double t, uint64_t sum) { return min(t >= 1.0 ? static_cast<uint64_t>(ceil(t)) : 1, sum); }
 // u sum exactly, as a sum may have more bits than a double: u = 1/2 of a row of two like halves draws from the second.
 __device__ __forceinline__ uint64_t goal_of_draw(double u, uint64_t sum) {
-    return min(static_cast<uint64_t>(__umul64hi(static_cast<uint64_t>(anew(u) * 0x1p64), sum)) + 1, sum);
+    return min(static_cast<uint64_t>(static_cast<unsigned __int128>(static_cast<uint64_t>(u * 0x1p64)) * sum >> 64) + 1, sum);
 }
 
 // The draw from a few tokens: four threads compare each with a quarter of all, which
@@ -634,11 +634,11 @@ __device__ __forceinline__ void draw_of_few(const Row& r, int n, const Targets& 
             const Few f(place, keeps);
             keeps = min(keeps, f.reach(goal_of(to.mass * (to.share ? static_cast<double>(f.total) : 0x1p50), f.total)) + 1);
         }
-        index[tid] = mine && rank[at] < keeps && w >= r.min_p ? static_cast<uint32_t>(order) : 0;
+        index[tid] = mine && rank[at] < keeps && w >= r.min_p && w > 0.0 ? static_cast<uint32_t>(order) : 0;
     }
     __syncthreads();
     rank_of(index[at], n, rank + kFew, [&](int i) { return index[i]; });
-    if (mine && index[at]) place[kFew + rank[kFew + at]] = amount_to_draw(w);
+    if (mine && index[at]) place[kFew + rank[kFew + at]] = max(amount, uint64_t{1});
     __syncthreads();
     if (tid >= kFew) return;
     const Few f(place + kFew, kFew);
@@ -683,8 +683,9 @@ __device__ __forceinline__ Cut cut_list(const Row& r, int n, uint32_t least, int
                 const uint32_t key = static_cast<uint32_t>(t >> 32), idx = static_cast<uint32_t>(t), v = by_key ? top - (key >> low_bits) : idx;
                 const double w = sh.w[i];
                 bool in = cut.keeps(key, static_cast<int>(idx)) && (shift == shift0 || v >> (shift + kDigit) == value);
-                if (!by_key) in = in && (draw ? w >= r.min_p : key >> low_bits == cut.key >> low_bits);
-                const uint64_t amount = step < 2 ? 1 : max(amount_of(w), draw && w > 0.0 ? uint64_t{1} : uint64_t{0});
+                if (!by_key) in = in && (draw ? w >= r.min_p && w > 0.0 : key >> low_bits == cut.key >> low_bits);
+                uint64_t amount = step < 2 ? 1 : amount_of(w);
+                if (draw) amount = max(amount, uint64_t{1});
                 if (in) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[v >> shift & (kDigits - 1)]), static_cast<unsigned long long>(amount));
             }
             __syncthreads();
