@@ -7,7 +7,7 @@
 // token kept, and no row is ever sorted.  A row is cut into slices, so that a few
 // rows fill the chip, and dealt with by two kernels:
 //   1. a slice's largest logit and, as the row needs them, the largest of every
-//      thread (any filter), the mass of the tokens in bins of 1/16 octave of w (top_p),
+//      thread (any filter), the mass of the tokens in bins of 1/16 octave of w (top_p alone),
 //      or the mass of sixteenths of the slice (no filter);
 //   2. a row's token.  top_k up to the number of threads: the k-th largest of the
 //      threads' largest bounds the k-th largest logit from below, and what is not
@@ -23,16 +23,23 @@
 //
 // Every mass is held in 64 bits: w from an exponential good to 2^-36, bins and
 // lists in fixed point (integer sums: the order of the atomics does not matter),
-// all else in doubles summed in a fixed order.  With fp32 sums one draw in a few
-// hundred would be another token.
+// all else in doubles summed in a fixed order, of slices whose number depends on the
+// batch's rows.  So a cut or a draw is the definition's where its target is further than
+// some 2^-36 of the mass from a running sum; and at exact ties of equal logits with
+// nothing else in the row, where all of these are whole numbers.  With fp32 sums one draw
+// in a few hundred would be another token.
 //
-// What bounds it.  A few rows: latency.  One row of 32768 with top_k and top_p takes 15.3 us:
-// 5 for the first kernel, 1 between the two, 9 for a chain of some 25 steps with a
-// barrier each, which meet their code cold and so are loops of few instructions rather
-// than unrolled.  256 rows of 131072 bf16 logits (67 MB, 13 us at a copy's rate): greedy 18.6 us;
-// top_k 42 (18 + 19 us of kernels); no filter 51 and top_p 92, where the first kernel's
-// instructions take 36 and 40 us (24 a token, half of them fp64), and a nucleus beyond the list takes the second kernel 50: a pass for the bin's tokens, then sums over
-// its slice and over the slice's sixteenths.
+// What bounds it (times of calls back to back).  A few rows: latency.  One row of 32768 with
+// top_k and top_p takes 15.6 us where the list has up to 256 tokens: 5 for the first kernel, 1
+// between the two, 9 for a chain of some 25 steps with a barrier each, which meet their code
+// cold and so are loops of few instructions rather than unrolled; 26 us with top_k 650, by digits.
+// 256 rows of 131072 bf16 logits (67 MB, 13 us at a copy's rate): greedy 18.2 us; top_k 41 (18 +
+// 19 us of kernels); no filter 49 and top_p 90, where the first kernel's instructions take 36 and
+// 40 us (23 a token, half of them fp64), and a nucleus beyond the list takes the second kernel 50: a
+// pass for the bin's tokens, then sums over its slice and over the slice's sixteenths.
+// Slow are rows whose cut is among more tokens of one bin than a list holds: 50 passes of
+// bisection by one work-group.  131072 equal logits with top_p 2.4 ms; 262144 of standard deviation 2 at
+// T = 2 with top_p 0.9 4.8, 64 such rows 5.0 (fp32 6.4).
 #include <math.h>
 
 #include <algorithm>
@@ -51,7 +58,7 @@ constexpr int kQueue = 8 * kWave + 64;  // logits a wave has queued: a piece of 
 constexpr int kRowBins = kThreads;  // of a row that goes by its own
 constexpr int kMost = 4096;         // most groups of threads of a row whose largest logits are kept
 constexpr int kMostSlices = 16;     // of a row
-constexpr int kList = 4096;         // tokens sorted in LDS
+constexpr int kList = 4096;         // tokens of a row's list in LDS, in any order
 
 struct SampleArgs {
     const void* logits;
@@ -735,7 +742,7 @@ struct Found {
 };
 template <class T>
 __device__ __forceinline__ Found find_bin(const Pieces<T>& p, const Row& r, const Cut& in, bool by_mass, double target, Shared& sh) {
-    const int tid = threadIdx.x;
+    const int tid = thread_id();
     __syncthreads();
     sh.mass[tid] = 0;
     __syncthreads();
@@ -746,15 +753,17 @@ __device__ __forceinline__ Found find_bin(const Pieces<T>& p, const Row& r, cons
         int n;
         const double w = r.weight(r.depth(x), n);
         f.z += w;
-        // w in units of 2^-42: the low bits of w + 2^10
+        // w in units of 2^-42 of the bin's octave: the low bits of such a number + 2^10
         const int b = Row::bin_at(-n);
         if (b < kRowBins)
             atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[b]),
-                      static_cast<unsigned long long>(by_mass ? __double_as_longlong(w + 0x1p10) - __double_as_longlong(0x1p10) : 1));
+                      static_cast<unsigned long long>(by_mass ? __double_as_longlong(ldexp(w, Row::start_of(b) >> 4) + 0x1p10) -
+                                                                __double_as_longlong(0x1p10) : 1));
     });
     f.z = block_sum(f.z, sh);
-    // a bin's mass says how many tokens it has to 2.2% either way
-    const double mine = static_cast<double>(sh.mass[tid]), upto = block_scan(mine, sh);
+    const double amount = static_cast<double>(sh.mass[thread_id()]);
+    const int start = Row::start_of(thread_id());
+    const double mine = by_mass ? ldexp(amount, -42 - (start >> 4)) : amount, upto = block_scan(mine, sh);
     if (tid == 0) sh.found = kThreads;
     if (tid == kThreads - 1) sh.found_d = upto;
     __syncthreads();
@@ -763,8 +772,9 @@ __device__ __forceinline__ Found find_bin(const Pieces<T>& p, const Row& r, cons
     __syncthreads();
     f.bin = sh.found;
     if (tid == f.bin) sh.above_d = upto - mine;
-    f.about = block_sum(tid <= f.bin ? by_mass ? mine * 0x1p-42 * exp2(Row::start_of(tid) * (1 / 16.0)) : mine : 0.0, sh);
-    f.above = by_mass ? sh.above_d * 0x1p-42 : sh.above_d;
+    // a bin's mass says how many tokens it has, to 2.2% either way down to 16 octaves
+    f.about = block_sum(tid <= f.bin ? by_mass ? amount * 0x1p-42 * r.root[start & 15] : amount : 0.0, sh);
+    f.above = sh.above_d;
     return f;
 }
 

@@ -139,7 +139,7 @@ struct Words {
 // split over work-groups too.  A wave takes D steps at a time, 4 KB of codes,
 // which it loads a turn ahead; the rows' operands come straight from the caches.
 // The weights' bytes bound it: 1 row of 4096 -> 28672 (62 MB) takes 15.4 us from HBM, 12.8
-// where the last-level cache has them (12.2 at a copy's 5.1 TB/s); of 4096 -> 4096 5.1, which
+// where the last-level cache has them (12.2 at a copy's 5.1 TB/s); of 4096 -> 4096 4.0, which
 // is a launch, one load's latency and the join in LDS.
 template <int MT, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void w4_stream_kernel(W4Args g) {
@@ -239,9 +239,10 @@ __global__ __launch_bounds__(64 * WAVES) void w4_stream_kernel(W4Args g) {
 // serves 16 rows on distinct banks.  The weights never pass through LDS: a
 // wave's operands of a step are 4 KB of consecutive codes, loaded a step ahead
 // into registers and widened there.  The matrix cores bound it: 2080 rows of 4096 -> 28672
-// take 371 us, 1.32 PFLOP/s, where a large bf16 library product reaches 1.40; of 14336 ->
-// 4096 195, of 4096 -> 4096 62.  A step that waits for its loads in one place and branches
-// nowhere is what got it there (1.28 with a branch for a last step in each).
+// take 384 us back to back, 1.27 PFLOP/s at the power limit, where a large bf16 library product
+// reaches 1.40; of 14336 -> 4096 200, of 4096 -> 4096 70.  A step that waits for its loads in one
+// place and branches nowhere is what got it there (395 us with a branch for a last step in
+// each, in a session where it took 371).
 template <int HA, int WN>
 __global__ __launch_bounds__(128 * WN, 2) void w4_tile_kernel(W4Args g, int nt_m, int nt_n, int steps_per_split) {
     constexpr int BM = 32 * HA, NW = 2 * WN, BUF = BM * 256, LOADS = BM / 4 / NW;

@@ -218,3 +218,24 @@ def test_top_p_where_bins_end_between_the_slices(temperature):
         x[4] += 45 * temperature
         for p in (0.3, 0.9, 0.999):
             _check(x, True, temperature=temperature, top_p=p, u=rng.random(6))
+
+
+@pytest.mark.parametrize("par", [dict(), dict(top_k=1 << 20)])
+@pytest.mark.parametrize("depth", [13.9, 14.0, 14.1, 14.3])
+def test_top_p_behind_many_tokens_of_little_mass(depth, par):
+    """Half a million equal logits between the largest and those the nucleus ends among, in a row too far from 0 for the
+    slices' bins, or cut by top_k before: what they weigh together, to less than one of the last."""
+    rng = np.random.default_rng([19, int(10 * depth)])
+    n, many, last = 524288 + 4000, 524288, 3000
+    x = np.full((8, n), -np.inf)
+    level = 0.0 if par else -9000.0
+    x[:, 0] = level
+    x[:, 1:1 + many] = np.float32(level - depth)
+    x[:, n - last:] = np.float32(level - depth - 1.5)
+    w = np.exp(x[0] - level)
+    z, before = w.sum(), w[:1 + many].sum()
+    p = np.float32((before + rng.uniform(0.1, 0.9, 8) * (z - before)) / z)
+    if par:
+        par = dict(top_k=n - 500)                             # the first 2500 of the last ones, and what is -inf never
+        x[:, n - last - 600:n - last] = level - depth - 3.0
+    _check(x, True, temperature=1.0, top_p=p, u=1 - 2.0**-24, **par)
