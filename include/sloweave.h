@@ -327,7 +327,7 @@ int slw_attn_end(slw_attn* plan);
  *             t = original_len * g_i / 2 pi the turns within the original length
  *   TABLE     freq[i], device memory, radians a position
  * rot_dim is a multiple of 16 up to head_dim.  Fields a kind does not name are
- * ignored.
+ * ignored; scalings that are not finite are refused (SLW_EINVAL).
  */
 #define SLW_ROPE_NONE 0
 #define SLW_ROPE_LINEAR 1
@@ -358,8 +358,8 @@ int slw_attn_rotate(slw_ctx* ctx, const slw_attn* plan, const slw_rope* rope, co
  * The residual stream between two blocks:
  *   r' = r + scale * gate * P(o),  y = r' / sqrt(mean(r'^2) + eps) * gain
  * with o a block's output, P(o) = o, or with post_gain
- * o / sqrt(mean(o^2) + eps) * post_gain.  fp32 arithmetic; y is taken of r'
- * before r' is rounded to the stream's type.
+ * o / sqrt(mean(o^2) + eps) * post_gain.  fp32 arithmetic, squares too (for values
+ * up to 1e17 in magnitude); y is taken of r' before r' is rounded to the stream's type.
  *   resid      [rows][d], bf16, or fp32 with resid_f32 = 1
  *   block      bf16 [rows][d], or NULL: r' = r (then no post_gain and no gate)
  *   post_gain  bf16 [d], or NULL;  gate  bf16 [rows][d], or [d] with ld_gate = 0, or NULL
@@ -427,7 +427,10 @@ int slw_w4_product(const slw_w4* w, const void* a, int64_t lda, int32_t m, void*
  * less than top_p of those tokens' mass before them (the first one always); of
  * those, the ones with w >= min_p.  The token is the first, by index, at which the
  * running sum of the kept w exceeds u times their sum; logprob is ln(w / sum).
- * Masses are held in 64 bits, so that the result is the definition's.
+ * Masses are held in 64 bits and each w is right to 2^-36, so that the result is the
+ * definition's unless the share that top_p or u asks for ends within some 2^-36 of the
+ * mass of a token's end (there it may also depend on the number of rows).  Where equal
+ * logits alone have mass it may end with a token exactly.  A w below 2^-1020 may count as 0.
  *   logits   device bf16, or fp32 with logits_f32 = 1, [rows][vocab], row stride ld,
  *            aligned to their type; NaN counts as -inf
  *   temperature, top_k, top_p, min_p   device [rows], each may be NULL (1, off, off, off).

@@ -52,10 +52,10 @@ namespace slw {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
-constexpr int kBins = 896;          // 16 for an octave; of a mass the last one holds w < 2^-55, all together 2^-35, and is weighed nowhere
+constexpr int kBins = 896;          // of a slice: 16 for an octave; the last one holds w < 2^-55, 2^-35 in all, and is weighed nowhere
 constexpr int kHeld = 4096;         // 16 bytes each of a slice that wait in LDS to be weighed (256 rows top_p 43 us; read again 44)
 constexpr int kQueue = 8 * kWave + 64;  // logits a wave has queued: a piece of every lane beside 63 left over
-constexpr int kRowBins = kThreads;  // of a row that goes by its own
+constexpr int kRowBins = kThreads;  // of a row that goes by its own (Row::bin_at)
 constexpr int kMost = 4096;         // most groups of threads of a row whose largest logits are kept
 constexpr int kMostSlices = 16;     // of a row
 constexpr int kList = 4096;         // tokens of a row's list in LDS, in any order
@@ -568,12 +568,11 @@ struct Targets {
     double count, mass;
     bool share, draw;
 };
-// w in units of 2^-50: the low bits of w + 4.
+// w in units of 2^-50: the low bits of w + 4.  In a draw tokens without any mass are left out and the
+// others have a unit at least: u = 0 draws the first that has any, however little.
 __device__ __forceinline__ uint64_t amount_of(double w) {
     return static_cast<uint64_t>(__double_as_longlong(w + 4.0) - __double_as_longlong(4.0));
 }
-// In a draw tokens without any mass are left out and the others have a unit at least: u = 0 draws the
-// first that has any, however little.
 // The running sum that a mass to keep, and the one that a draw, has to reach.
 __device__ __forceinline__ uint64_t goal_of(double t, uint64_t sum) { return min(t >= 1.0 ? static_cast<uint64_t>(ceil(t)) : 1, sum); }
 // u sum exactly, as a sum may have more bits than a double: u = 1/2 of a row of two like halves draws from the second.
