@@ -1141,6 +1141,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
     if (slices && !summed && listed >= 0) {
         // A slice's kept mass: its bins above the cut's, and the kept tokens of that bin.  A wave a slice.
         double s = 0.0;
+        uint64_t listed_mass = 0;  // whole units, as the list's order is any
         if (wave < a.slices && sh.best[wave]) {
             const int down = ref - sh.ref[wave], width = slice_pieces(p.count, a.slices);
             // bins 64 apart are four octaves apart
@@ -1155,10 +1156,10 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
                 const uint64_t t = sh.list[i];
                 const int idx = static_cast<int>(static_cast<uint32_t>(t));
                 if (idx + p.shift - 8 * width * wave >= 0 && idx + p.shift - 8 * width * (wave + 1) < 0 && cut.keeps(static_cast<uint32_t>(t >> 32), idx))
-                    s += r.w(value_of(static_cast<uint32_t>(t >> 32)));
+                    listed_mass += amount_of(r.w(value_of(static_cast<uint32_t>(t >> 32))));
             }
         }
-        s = wave_total(s);
+        s = wave_total(s) + static_cast<double>(wave_total(listed_mass)) * 0x1p-50;
         __syncthreads();
         if (lane == 0) sh.red_d[wave] = s;
         __syncthreads();

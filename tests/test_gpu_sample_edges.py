@@ -239,3 +239,15 @@ def test_top_p_behind_many_tokens_of_little_mass(depth, par):
         par = dict(top_k=n - 500)                             # the first 2500 of the last ones, and what is -inf never
         x[:, n - last - 600:n - last] = level - depth - 3.0
     _check(x, True, temperature=1.0, top_p=p, u=1 - 2.0**-24, **par)
+
+
+def test_large_nuclei_draw_the_same_bits_every_time():
+    """Nuclei beyond a list: whatever order their last bin's tokens were collected in."""
+    rng = np.random.default_rng(20)
+    rows, n = 24, 140001
+    x = rng.standard_normal((rows, n)) * rng.choice([0.3, 0.8, 1.5], (rows, 1))
+    par = dict(temperature=1.0, top_p=rng.uniform(0.6, 0.99, rows), u=rng.random(rows))
+    want = _sample(x, True, **par)[:2]
+    for _ in range(20):
+        got = _sample(x, True, **par)[:2]
+        assert all(np.array_equal(a, b) for a, b in zip(got, want))
